@@ -22,6 +22,9 @@ enum StatIndex {
 // uses several devices sets it on each.  Thread-safe.
 cudaError_t set_dyn_smem_on_device(const void* func, int bytes);
 
+// A call without a handle failed with `why`: kept for moeca_last_error(NULL).
+void keep_call_error(const char* why) noexcept;
+
 constexpr int kMaxExperts = 64;
 constexpr int kMaxTopK = 8;
 constexpr int kRouterTokensPerBlock = 16;   // 8 warps x 2 tokens

@@ -60,11 +60,20 @@ cudaError_t set_dyn_smem_on_device(const void* func, int bytes) {
   return cudaSuccess;
 }
 
+thread_local std::string g_create_error;
+
+void keep_call_error(const char* why) noexcept {
+  try {
+    g_create_error = why;
+  } catch (...) {  // no memory for the message: the status alone tells
+  }
+}
+
 }  // namespace moeca
 
 namespace {
 
-thread_local std::string g_create_error;
+using moeca::g_create_error;
 
 struct LayerBuf {
   moeca_layer_weights w;

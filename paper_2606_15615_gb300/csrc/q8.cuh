@@ -1,0 +1,106 @@
+// 8-bit rows (include/moeca_q8.h): block scales, encoding and decoding.
+//
+// The scale of a block of 128 values is a power of two, so dividing by it is
+// exact and the only rounding is the one to the 8-bit format: any order of
+// evaluation, and the tensor core's own scaling, gives the same value.  A
+// power of two costs no precision against a free fp32 scale, since the values
+// themselves are floating point; at most one binade of range at the top stays
+// unused.
+#pragma once
+
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "moeca_q8.h"
+
+namespace moeca {
+
+constexpr int kQ8Block = 128;
+
+// What the launches of q8.cu and q8_matmul.cu take (checked by their C calls).
+struct Q8Rows {
+  uint8_t* q;
+  uint8_t* scale;
+  int64_t rows, q_stride, scale_stride;
+  int width;
+};
+
+// Bits of |x|; infinities and NaN are those from kNonFinite on.
+constexpr uint32_t kNonFinite = 0x7f800000u;
+__device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+
+// Scale byte of a block whose largest finite magnitude has the bits `a`.
+// MAX is 1.75 x 2^8 (e4m3) or 1.75 x 2^15 (e5m2): the scale's exponent is a's
+// less 8 or 15, one more where a's significand exceeds 1.75.
+template <bool E5>
+__device__ __forceinline__ int scale_byte(uint32_t a) {
+  const int e = static_cast<int>(a >> 23) - (E5 ? 15 : 8) + ((a & 0x7fffffu) > 0x600000u);
+  return a == 0 ? 127 : max(e, 0);
+}
+// 1 / scale: 2^(127 - byte), byte <= 247 as written by scale_byte.
+__device__ __forceinline__ float scale_inverse(int byte) { return __uint_as_float(static_cast<uint32_t>(254 - byte) << 23); }
+// The scale: 2^(byte - 127); 2^-127 is subnormal, 255 is NaN.
+__device__ __forceinline__ float scale_value(uint32_t byte) {
+  const uint32_t b = byte == 0 ? 0x400000u : byte << 23;
+  return __uint_as_float(byte == 255 ? 0x7fffffffu : b);
+}
+
+// Two values (already divided by the scale) in 8 bits, the first in the low byte.
+// Finite values that the scale brings in range; see encode_any for others.
+template <bool E5>
+__device__ __forceinline__ uint32_t encode2(float lo, float hi) {
+  return __nv_cvt_float2_to_fp8x2(make_float2(lo, hi), __NV_SATFINITE, E5 ? __NV_E5M2 : __NV_E4M3);
+}
+// One value that may be infinite or NaN.
+template <bool E5>
+__device__ __forceinline__ uint32_t encode_any(float v) {
+  const uint32_t sign = (__float_as_uint(v) >> 24) & 0x80u;
+  if (abs_bits(v) > kNonFinite) return 0x7fu;
+  if (abs_bits(v) == kNonFinite) return E5 ? (sign | 0x7cu) : 0x7fu;
+  return encode2<E5>(v, 0.f) & 0xffu;
+}
+
+// Two bytes as two floats (every e4m3 / e5m2 value is an fp16 value).
+template <bool E5>
+__device__ __forceinline__ float2 decode2(uint32_t pair) {
+  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(pair), E5 ? __NV_E5M2 : __NV_E4M3);
+  return __half22float2(*reinterpret_cast<const __half2*>(&h));
+}
+
+struct Q8WriteArgs {
+  Q8Rows c;
+  const void* x;
+  int64_t x_rows, x_stride;
+  int n;
+  const int32_t *src, *dst, *count;
+};
+cudaError_t launch_q8_write(const Q8WriteArgs& a, bool bf16, bool e5, cudaStream_t s);
+
+struct Q8CombineArgs {
+  Q8Rows c;
+  const int32_t* rows;   // null: slot row = token (one slot)
+  const float* weights;
+  const void* x;
+  int64_t x_stride;
+  const float* gate;
+  int64_t gate_stride;
+  void* out;
+  int64_t out_stride;
+  float* norms;
+  int T, k, seq;
+};
+cudaError_t launch_q8_combine(const Q8CombineArgs& a, bool bf16, bool e5, cudaStream_t s);
+
+struct Q8MatmulArgs {
+  Q8Rows a, b, out;
+  bool a_e5, b_e5;
+  int out_format, act, n_groups, n_cols;
+  const int32_t *offsets, *dst;
+  const float* bias;
+  int32_t* status;
+};
+cudaError_t launch_q8_matmul(const Q8MatmulArgs& a, cudaStream_t s);
+
+}  // namespace moeca

@@ -12,6 +12,7 @@ import ctypes as C
 import math
 import os
 import re
+from typing import NamedTuple
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(PKG, "libmoeca.so")
@@ -28,6 +29,8 @@ MOECA_FFN_AUTO, MOECA_FFN_SIMT = 0, 1
 KERNEL_KINDS = ["router", "select", "compact", "ffn1", "ffn2", "combine", "prep", "ffn",
                 "qkv", "attn", "oproj", "attn_aux", "adaln"]
 ATTN_SYNC, ATTN_STALE, ATTN_FULL = 0, 1, 2
+MOECA_E4M3, MOECA_E5M2 = 2, 3
+MOECA_ACT_NONE, MOECA_ACT_GELU, MOECA_ACT_GELU_TANH = 0, 1, 2
 
 
 class moeca_config(C.Structure):
@@ -103,6 +106,35 @@ class moeca_ddpm_args(C.Structure):
                 ("x_prev", C.c_void_p), ("x_next", C.c_void_p)]
 
 
+class moeca_q8_rows(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("scale", C.c_void_p), ("rows", C.c_int64), ("q_stride", C.c_int64),
+                ("scale_stride", C.c_int64), ("width", C.c_int32), ("format", C.c_int32)]
+
+
+class moeca_q8_write_args(C.Structure):
+    _fields_ = [("cache", moeca_q8_rows), ("x", C.c_void_p), ("x_rows", C.c_int64), ("x_stride", C.c_int64),
+                ("dtype", C.c_int32), ("n", C.c_int32), ("src", C.c_void_p), ("dst", C.c_void_p),
+                ("count", C.c_void_p)]
+
+
+class moeca_q8_read_args(C.Structure):
+    _fields_ = [("cache", moeca_q8_rows), ("out", C.c_void_p), ("out_stride", C.c_int64), ("dtype", C.c_int32),
+                ("n", C.c_int32), ("rows", C.c_void_p)]
+
+
+class moeca_q8_combine_args(C.Structure):
+    _fields_ = [("cache", moeca_q8_rows), ("rows", C.c_void_p), ("weights", C.c_void_p), ("x", C.c_void_p),
+                ("x_stride", C.c_int64), ("gate", C.c_void_p), ("gate_stride", C.c_int64), ("out", C.c_void_p),
+                ("out_stride", C.c_int64), ("norms", C.c_void_p), ("dtype", C.c_int32), ("n_tokens", C.c_int32),
+                ("n_slots", C.c_int32), ("seq", C.c_int32)]
+
+
+class moeca_q8_matmul_args(C.Structure):
+    _fields_ = [("a", moeca_q8_rows), ("b", moeca_q8_rows), ("out", moeca_q8_rows), ("offsets", C.c_void_p),
+                ("bias", C.c_void_p), ("dst", C.c_void_p), ("status", C.c_void_p), ("n_groups", C.c_int32),
+                ("n_cols", C.c_int32), ("act", C.c_int32)]
+
+
 class MoecaError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__(f"{STATUS_NAMES.get(status, status)}: {msg}")
@@ -143,6 +175,10 @@ def _load():
         "moeca_ddpm_schedule": (C.c_int, [C.c_int32, C.c_int32, C.c_double, C.c_double, C.POINTER(C.c_int32),
                                           C.POINTER(C.c_double), C.POINTER(C.c_double), C.POINTER(C.c_double)]),
         "moeca_ddpm_step": (C.c_int, [C.POINTER(moeca_ddpm_args), C.c_void_p]),
+        "moeca_q8_write": (C.c_int, [C.POINTER(moeca_q8_write_args), C.c_void_p]),
+        "moeca_q8_read": (C.c_int, [C.POINTER(moeca_q8_read_args), C.c_void_p]),
+        "moeca_q8_combine": (C.c_int, [C.POINTER(moeca_q8_combine_args), C.c_void_p]),
+        "moeca_q8_matmul": (C.c_int, [C.POINTER(moeca_q8_matmul_args), C.c_void_p]),
         "moeca_probe_ffma": (C.c_int32, [C.c_int32, C.c_int32, C.POINTER(C.c_double), C.POINTER(C.c_double)]),
         "moeca_probe_maps_encoded": (C.c_int64, []),
         "moeca_probe_prefetch_bytes": (C.c_int64, [C.c_int64, C.c_int32, C.c_int32]),
@@ -167,7 +203,7 @@ def header_functions() -> list:
         if fn.endswith(".h"):
             with open(os.path.join(INCLUDE, fn)) as f:
                 text = re.sub(r"/\*.*?\*/", "", f.read(), flags=re.S)
-            names |= set(re.findall(r"\b(moeca_[a-z_]+)\s*\(", text))
+            names |= set(re.findall(r"\b(moeca_[a-z0-9_]+)\s*\(", text))
     return sorted(names)
 
 
@@ -322,6 +358,26 @@ def moeca_ddpm_step(args: moeca_ddpm_args, stream: int = 0):
     st = LIB.moeca_ddpm_step(C.byref(args), stream or None)
     if st != MOECA_OK:
         _check(st, None)
+
+
+def moeca_q8_write(args: moeca_q8_write_args, stream: int = 0):
+    """Quantise rows into an 8-bit cache (see include/moeca_q8.h)."""
+    _check(LIB.moeca_q8_write(C.byref(args), stream or None))
+
+
+def moeca_q8_read(args: moeca_q8_read_args, stream: int = 0):
+    """Read rows of an 8-bit cache back (see include/moeca_q8.h)."""
+    _check(LIB.moeca_q8_read(C.byref(args), stream or None))
+
+
+def moeca_q8_combine(args: moeca_q8_combine_args, stream: int = 0):
+    """Eq. 8 over an 8-bit branch cache (see include/moeca_q8.h)."""
+    _check(LIB.moeca_q8_combine(C.byref(args), stream or None))
+
+
+def moeca_q8_matmul(args: moeca_q8_matmul_args, stream: int = 0):
+    """Grouped product of 8-bit rows (see include/moeca_q8.h)."""
+    _check(LIB.moeca_q8_matmul(C.byref(args), stream or None))
 
 
 def moeca_probe_ffma(device: int = 0, iterations: int = 1 << 16) -> tuple:
@@ -529,3 +585,200 @@ def ddpm_step(x_t, eps, alpha: float, alpha_bar: float, sigma: float, z=None, x_
         x_next.data_ptr() if x_next is not None else None)
     moeca_ddpm_step(args, stream or torch.cuda.current_stream(x_t.device).cuda_stream)
     return x_prev
+
+
+# ---------------------------------------------------------------------------
+# 8-bit rows (include/moeca_q8.h) on torch CUDA tensors
+# ---------------------------------------------------------------------------
+
+Q8_BLOCK = 128
+_ACTS = {"none": MOECA_ACT_NONE, "gelu": MOECA_ACT_GELU, "gelu_tanh": MOECA_ACT_GELU_TANH}
+
+
+class Q8(NamedTuple):
+    """Rows held in 8 bits: ``q`` [rows, width] float8_e4m3fn or float8_e5m2, its row stride a multiple
+    of 16 bytes; ``scale`` [rows, ceil(width / 128)] uint8, its row stride a multiple of 4, byte s for 2^(s - 127).
+    The storage under a row reaches to the next row's start."""
+    q: "torch.Tensor"  # noqa: F821
+    scale: "torch.Tensor"  # noqa: F821
+
+
+def q8_empty(rows: int, width: int, dtype=None, device="cuda") -> Q8:
+    """Room for ``rows`` 8-bit rows of ``width`` values (zeros; float8_e4m3fn by default)."""
+    import torch
+    nb = -(-width // Q8_BLOCK)
+    q = torch.zeros((rows, -(-width // 16) * 16), dtype=torch.uint8, device=device)
+    s = torch.full((rows, -(-nb // 4) * 4), 127, dtype=torch.uint8, device=device)
+    return Q8(q.view(dtype or torch.float8_e4m3fn)[:, :width], s[:, :nb])
+
+
+_TYPES = {}
+
+
+def _type_code(dtype) -> int:
+    """The C code of a torch dtype, -1 for one the library does not take."""
+    if not _TYPES:
+        import torch
+        _TYPES.update({torch.float32: MOECA_F32, torch.bfloat16: MOECA_BF16, torch.float8_e4m3fn: MOECA_E4M3,
+                       torch.float8_e5m2: MOECA_E5M2})
+    return _TYPES.get(dtype, -1)
+
+
+def _row_stride(t, unit: int = 1) -> int:
+    """Elements from row to row.  One row (or none) has no next one: its length, in units of ``unit``."""
+    return t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] // unit) * unit
+
+
+def _q8_rows(r, what: str, device) -> moeca_q8_rows:
+    q, s = r
+    code = _type_code(q.dtype)
+    if code < MOECA_E4M3 or q.dim() != 2 or (q.shape[1] > 1 and q.stride(1) != 1) or q.device != device:
+        raise ValueError(f"{what}.q must be a 2-D float8_e4m3fn or float8_e5m2 tensor on {device} with unit column stride")
+    if s.dim() != 2 or s.element_size() != 1 or s.shape[0] != q.shape[0] or s.shape[1] != -(-q.shape[1] // Q8_BLOCK) \
+            or (s.shape[1] > 1 and s.stride(1) != 1) or s.device != device:
+        raise ValueError(f"{what}.scale must be [rows, ceil(width / 128)] bytes on {device} with unit column stride")
+    return moeca_q8_rows(q.data_ptr(), s.data_ptr(), q.shape[0], _row_stride(q, 16), _row_stride(s, 4), q.shape[1], code)
+
+
+def _list(t, dtype, shape, what: str, device):
+    """The address of a contiguous device tensor of one shape (None: NULL)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor {list(shape)} on {device}")
+    return t.data_ptr()
+
+
+def _values(t, what: str, device) -> int:
+    """The C type code of a 2-D tensor of fp32 or bf16 rows."""
+    code = _type_code(t.dtype)
+    if code not in (MOECA_F32, MOECA_BF16) or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or t.device != device:
+        raise ValueError(f"{what} must be a 2-D float32 or bfloat16 tensor on {device} with unit column stride")
+    return code
+
+
+def _call(fn, args, device, stream):
+    """Run a C call with the tensors' device current, on ``stream`` or that device's current stream."""
+    import torch
+    if device.type != "cuda":
+        raise ValueError("8-bit rows live on a CUDA device")
+    if device.index == torch.cuda.current_device():
+        fn(args, stream or torch.cuda.current_stream().cuda_stream)
+    else:
+        with torch.cuda.device(device):
+            fn(args, stream or torch.cuda.current_stream().cuda_stream)
+
+
+def q8_write(x, cache: Q8, src=None, dst=None, count=None, stream: int = 0) -> Q8:
+    """Quantise rows of ``x`` (fp32 or bf16) into ``cache`` (float8 type and scales as allocated): cache row
+    dst[i] from x row src[i], int32 lists on the device (None: i), for all entries or the first ``count``
+    (an int32 device tensor of one value).  Entries out of range are skipped.  Returns ``cache``."""
+    import torch
+    dev = x.device
+    dtype = _values(x, "x", dev)
+    rows = _q8_rows(cache, "cache", dev)
+    if x.shape[1] != rows.width:
+        raise ValueError(f"x is {x.shape[1]} wide, the cache {rows.width}")
+    if src is not None and dst is not None and src.numel() != dst.numel():
+        raise ValueError("src and dst must have the same length")
+    n = dst.numel() if dst is not None else src.numel() if src is not None else x.shape[0]
+    args = moeca_q8_write_args(
+        rows, x.data_ptr(), x.shape[0], _row_stride(x), dtype, n, _list(src, torch.int32, (n,), "src", dev),
+        _list(dst, torch.int32, (n,), "dst", dev), _list(count, torch.int32, (1,), "count", dev))
+    _call(moeca_q8_write, args, dev, stream)
+    return cache
+
+
+def q8_read(cache: Q8, rows=None, dtype=None, out=None, stream: int = 0):
+    """Cache rows as bf16 (default) or fp32: all of them, or those of ``rows`` (int32, on the device); zeros
+    where an entry is out of range."""
+    import torch
+    dev = cache.q.device
+    c = _q8_rows(cache, "cache", dev)
+    n = c.rows if rows is None else rows.numel()
+    if out is None:
+        out = torch.empty((n, c.width), dtype=dtype or torch.bfloat16, device=dev)
+    code = _values(out, "out", dev)
+    if tuple(out.shape) != (n, c.width) or (dtype is not None and out.dtype != dtype):
+        raise ValueError(f"out must be [{n}, {c.width}] of the asked dtype")
+    args = moeca_q8_read_args(c, out.data_ptr(), _row_stride(out), code, n,
+                              _list(rows, torch.int32, (n,), "rows", dev))
+    _call(moeca_q8_read, args, dev, stream)
+    return out
+
+
+def q8_combine(cache: Q8, rows, weights=None, x=None, gate=None, norms=False, dtype=None, out=None, stream: int = 0):
+    """Eq. 8 over an 8-bit branch cache: x + gate * sum_p weights[:, p] cache[rows[:, p]].  ``rows`` [T, k]
+    int32 (out of range: an empty slot), ``weights`` [T, k] fp32 (None: 1), ``x`` [T, D] fp32 or bf16 (None: 0),
+    ``gate`` [B, D] fp32, one row for each T / B consecutive tokens.  ``norms``: True or a [T, k] fp32 tensor
+    also gives the rows' 2-norms.  The result has x's dtype (without x: ``dtype``, default bf16); ``out`` may be
+    x.  Returns out, or (out, norms)."""
+    import torch
+    dev = cache.q.device
+    c = _q8_rows(cache, "cache", dev)
+    if rows.dim() != 2:
+        raise ValueError("rows must be [tokens, slots]")
+    T, k = rows.shape
+    if out is None:
+        out = torch.empty((T, c.width), dtype=x.dtype if x is not None else dtype or torch.bfloat16, device=dev)
+    code = _values(out, "out", dev)
+    if tuple(out.shape) != (T, c.width):
+        raise ValueError(f"out must be [{T}, {c.width}]")
+    if x is not None and (_values(x, "x", dev) != code or x.shape != out.shape):
+        raise ValueError("x must have out's dtype and shape")
+    seq = 1
+    if gate is not None:
+        if _values(gate, "gate", dev) != MOECA_F32 or gate.shape[1] != c.width or (T and (not gate.shape[0] or T % gate.shape[0])):
+            raise ValueError("gate must be float32 rows, one for each T / rows consecutive tokens")
+        seq = T // gate.shape[0] if T else 1
+    if norms is True:
+        norms = torch.empty((T, k), dtype=torch.float32, device=dev)
+    elif norms is False:
+        norms = None
+    args = moeca_q8_combine_args(
+        c, _list(rows, torch.int32, (T, k), "rows", dev), _list(weights, torch.float32, (T, k), "weights", dev),
+        x.data_ptr() if x is not None else None, _row_stride(x) if x is not None else 0,
+        gate.data_ptr() if gate is not None else None, _row_stride(gate) if gate is not None else 0,
+        out.data_ptr(), _row_stride(out), _list(norms, torch.float32, (T, k), "norms", dev), code, T, k, seq)
+    _call(moeca_q8_combine, args, dev, stream)
+    return out if norms is None else (out, norms)
+
+
+def q8_matmul(a: Q8, b: Q8, offsets=None, bias=None, act: str = "none", dst=None, out=None, dtype=None, status=None,
+              stream: int = 0):
+    """Grouped product of 8-bit rows: for the rows offsets[g] <= m < offsets[g + 1] of ``a`` (one group of all
+    rows without offsets), act(a[m] b_g^T + bias_g), act "none", "gelu" or "gelu_tanh".  ``b`` holds the groups'
+    weight rows one group after another; ``offsets`` [groups + 1] and ``dst`` [rows of a] (the output row of
+    each; out of range: dropped) are int32 on the device, ``bias`` [groups, columns] fp32.  ``out``: a tensor of
+    fp32 / bf16 rows or a Q8 that takes the rows in 8 bits; without it a new tensor of ``dtype`` (bf16; float8
+    types give a Q8).  Returns out."""
+    import torch
+    dev = a.q.device
+    ra, rb = _q8_rows(a, "a", dev), _q8_rows(b, "b", dev)
+    groups = offsets.numel() - 1 if offsets is not None else 1
+    if groups < 1 or rb.rows % groups or rb.rows == 0:
+        raise ValueError("b must hold the same number of rows for each group, one at least")
+    cols = rb.rows // groups
+    if act not in _ACTS:
+        raise ValueError(f"act must be one of {sorted(_ACTS)}")
+    if out is None:
+        code = _type_code(dtype or torch.bfloat16)
+        if code < 0:
+            raise ValueError("dtype must be float32, bfloat16, float8_e4m3fn or float8_e5m2")
+        if code >= MOECA_E4M3:
+            out = q8_empty(ra.rows, cols, dtype, dev)
+        else:
+            out = torch.empty((ra.rows, cols), dtype=dtype or torch.bfloat16, device=dev)
+    if isinstance(out, Q8):
+        ro = _q8_rows(out, "out", dev)
+    else:
+        code, size = _values(out, "out", dev), out.element_size()
+        ro = moeca_q8_rows(out.data_ptr(), None, out.shape[0], _row_stride(out) * size, 0, out.shape[1], code)
+    if ro.width != cols:
+        raise ValueError(f"out must be {cols} wide")
+    args = moeca_q8_matmul_args(
+        ra, rb, ro, _list(offsets, torch.int32, (groups + 1,), "offsets", dev),
+        _list(bias, torch.float32, (groups, cols), "bias", dev), _list(dst, torch.int32, (ra.rows,), "dst", dev),
+        _list(status, torch.int32, (2,), "status", dev), groups, cols, _ACTS[act])
+    _call(moeca_q8_matmul, args, dev, stream)
+    return out
