@@ -35,6 +35,7 @@
 #include <cuda.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "common.cuh"
 #include "kernels.h"
@@ -46,29 +47,33 @@ namespace {
 
 constexpr int kBM = 128;                  // weight rows per CTA (half of the MMA's M)
 constexpr int kSub = 2;                   // K blocks of 128 per stage
-constexpr int kMaxN = 192;                // token rows per tile
-constexpr int kBoxes = kMaxN / 16;        // token boxes of 8, 16, .., 96 rows
+constexpr int kMaxN = 224;                // token rows per tile
+constexpr int kBoxes = kMaxN / 16;        // token boxes of 8, 16, .., 112 rows
 constexpr int kMaxStages = 5;
-constexpr int kRingBytes = 200 * 1024;    // weight slots first, then token slots
+constexpr int kRingBytes = 192 * 1024;    // weight slots first, then token slots
 constexpr int kWBytes = kBM * kQ8Block;   // 16 KB: one weight block
 constexpr int kWSlot = kSub * kWBytes;
 constexpr int kSfStages = 4;              // scale words of 4 K blocks each
 constexpr int kSfCols = 16;               // TMEM columns of one: 4 for the weights, from 8 on the tokens
 constexpr int kSfBase = 2 * kMaxN;
 constexpr int kEpiWarps = 8;              // warps 2-9
+constexpr int kParts = kEpiWarps / 4;     // warps per lane quadrant
+constexpr int kChunks = (kMaxN / 32 + kParts - 1) / kParts;  // chunks of 32 tokens a part has in a tile, at most
 constexpr int kSfWarp = 2 + kEpiWarps;    // warps 10-13
 constexpr int kTokWarp = kSfWarp + 4;
 constexpr int kThreads = 32 * (kTokWarp + 1);
 constexpr int kTmemCols = 512;
 constexpr int kMaxGroups = 1024;
 static_assert(kSfBase + kSfStages * kSfCols <= kTmemCols, "TMEM");
+static_assert(kMaxN <= 256, "eight scale columns");
 
 // Behind the ring: what the warps share.
 struct Shared {
   int units[kMaxGroups + 1];              // first unit of each group
   int lo[kMaxGroups], rows[kMaxGroups];   // first row, rows
-  uint32_t top[2][2][4][32];              // [part][buffer][quadrant][token]: largest |z| bits
-  alignas(16) float inv[kEpiWarps][32];   // 1 / scale of the chunk's tokens, read four at a time
+  uint32_t top[kParts][2][4][32];         // [part][buffer][quadrant][token]: largest |z| bits
+  alignas(16) uint32_t stage[kEpiWarps][512];  // a chunk on its way out: 32 tokens x 32 features of at most two bytes
+  float inv[kEpiWarps][32];   // 1 / scale of the chunk's tokens, read four at a time
   uint64_t full[kMaxStages], empty[kMaxStages], sf_full[kSfStages], sf_empty[kSfStages], tfull[2], tempty[2], drain;
   uint32_t tmem;
   int max_n;
@@ -79,7 +84,7 @@ static_assert(kSmem <= 227 * 1024, "shared memory");
 
 struct Maps {
   CUtensorMap w;             // weights, box 128 rows
-  CUtensorMap act[kBoxes];   // token rows, boxes of 8 .. 96 rows
+  CUtensorMap act[kBoxes];   // token rows, boxes of 8 .. 112 rows
 };
 
 // Token tiles of a group of `rows` rows, and their width.
@@ -122,36 +127,70 @@ __device__ __forceinline__ uint32_t mx_desc(int n, bool a_e5, bool b_e5) {
          (static_cast<uint32_t>(2 * kBM >> 4) << 24);
 }
 
-__device__ __forceinline__ void mma_mx_pair(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t idesc,
-                                            uint32_t sf_a, uint32_t sf_b, uint32_t acc) {
+// The four MMAs of one K block (128 values), issued by the lane whose `issue`
+// is set; all lanes of the warp run it, so that the operands stay in uniform
+// registers (one thread alone spent longer moving them there than the MMAs
+// take).  acc: 0 where the block is the tile's first.
+__device__ __forceinline__ void mma_mx_block(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t idesc,
+                                             uint32_t sf_a, uint32_t sf_b, uint32_t acc, uint32_t issue) {
   constexpr uint32_t kHi = (1024u >> 4) | (1u << 14) | (2u << 29);  // smem_desc's bits 32-63
   asm volatile(
-      "{\n .reg .pred p;\n .reg .b64 a, b;\n setp.ne.b32 p, %4, 0;\n"
+      "{\n .reg .pred p, e;\n .reg .b64 a, b;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 e, %8, 0;\n"
       " mov.b64 a, {%1, %5};\n mov.b64 b, {%2, %5};\n"
-      " tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], a, b, %3, [%6], [%7], p;\n}"
-      ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(acc), "r"(kHi), "r"(sf_a), "r"(sf_b)
+      " @e tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], a, b, %3, [%6], [%7], p;\n"
+      " add.s64 a, a, 2;\n add.s64 b, b, 2;\n setp.eq.b32 p, 0, 0;\n"
+      " @e tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], a, b, %3, [%6], [%7], p;\n"
+      " add.s64 a, a, 2;\n add.s64 b, b, 2;\n"
+      " @e tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], a, b, %3, [%6], [%7], p;\n"
+      " add.s64 a, a, 2;\n add.s64 b, b, 2;\n"
+      " @e tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], a, b, %3, [%6], [%7], p;\n}"
+      ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(acc), "r"(kHi), "r"(sf_a), "r"(sf_b), "r"(issue)
       : "memory");
 }
+__device__ __forceinline__ void commit_pair_if(uint32_t bar, uint32_t issue) {
+  asm volatile(
+      "{\n .reg .pred e;\n setp.ne.b32 e, %2, 0;\n"
+      " @e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n}" ::"r"(bar),
+      "h"(static_cast<uint16_t>(3)), "r"(issue)
+      : "memory");
+}
+// Every lane's bounded wait, the first try inline; the same answer in all lanes.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  if (__all_sync(0xffffffffu, mbar_try(bar, parity))) return true;
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
+}
 
+// 2^x and 1 / x of the special-function unit (about 2^-22 relative).
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float rcp(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 // GELU of an epilogue value (Eq. 5).  tanh form: z sigmoid(2 u), u = sqrt(2/pi) (z + 0.044715 z^3).
 // erf form: Phi(-|z|) = erfc(|z| / sqrt 2) / 2 by Abramowitz and Stegun's
 // formula 7.1.26, P(t) exp(-z^2 / 2) / 2 with t = 1 / (1 + p |z| / sqrt 2), within
 // 0.75e-7; z Phi(z) is z - z Phi(-z) or z Phi(-|z|), so that nothing cancels.
-// Both cost two special-function evaluations and about ten others; the library
+// Both cost two special-function evaluations and few others; the library
 // functions' longer forms would bound the products with short K.
 template <int ACT>
 __device__ __forceinline__ float act_f(float z) {
+  constexpr float kLog2e = 1.44269504f;
   if constexpr (ACT == MOECA_ACT_GELU_TANH) {
-    const float v = z * fmaf(0.0713548163f, z * z, 1.5957691216f);  // 2 u
-    return __fdividef(z, 1.f + __expf(-v));
+    const float v = z * fmaf(-0.0713548163f * kLog2e, z * z, -1.5957691216f * kLog2e);  // -2 u log2(e)
+    return z * rcp(1.f + ex2(v));
   } else if constexpr (ACT == MOECA_ACT_GELU) {
     const float x = fabsf(z);
-    const float t = __fdividef(1.f, fmaf(0.3275911f * 0.70710678f, x, 1.f));
-    float s = fmaf(1.061405429f, t, -1.453152027f);
-    s = fmaf(s, t, 1.421413741f);
-    s = fmaf(s, t, -0.284496736f);
-    s = fmaf(s, t, 0.254829592f);
-    const float tail = 0.5f * s * t * __expf(-0.5f * z * z) * x;  // |z| Phi(-|z|)
+    const float t = rcp(fmaf(0.3275911f * 0.70710678f, x, 1.f));
+    float s = fmaf(0.5f * 1.061405429f, t, 0.5f * -1.453152027f);
+    s = fmaf(s, t, 0.5f * 1.421413741f);
+    s = fmaf(s, t, 0.5f * -0.284496736f);
+    s = fmaf(s, t, 0.5f * 0.254829592f);
+    const float tail = s * t * ex2(-0.5f * kLog2e * z * z) * x;  // |z| Phi(-|z|)
     return fmaxf(z, 0.f) - tail;
   } else {
     return z;
@@ -189,44 +228,48 @@ struct MatmulParams {
   uint8_t* out;
   uint8_t* out_scale;
   int64_t out_rows, out_stride, os_stride;
-  bool w_e5, t_e5, wide;       // wide: 4-byte stores of bf16 pairs
+  bool w_e5, t_e5, wide;       // wide: 16-byte stores of bf16 rows
   int32_t* status;
 };
 
 // Epilogue of one chunk: 32 features (lanes) x 32 tokens (z), all four
 // quadrants of the part together.  row: lane t's output row of token t, or -1.
+// Rows go out through shared memory in 16-byte pieces; rows that are not
+// aligned for them, and fp32 rows, straight from the registers, a token's 32
+// features at a time.
 template <int OUT>
 __device__ __forceinline__ void store_chunk(const MatmulParams& p, Shared& sh, float (&z)[32], int row, int feat0,
                                             int block, int lane, int warp, int part, int quad, int buf) {
-  if constexpr (OUT == MOECA_F32) {
+  uint32_t* stage = sh.stage[warp - 2];
+  if constexpr (OUT == MOECA_F32 || OUT == MOECA_BF16) {
     if (feat0 >= p.N) return;
+    if (OUT == MOECA_BF16 && p.wide) {
+      __syncwarp();  // the last chunk has left the stage
+      stage_by_token(stage, lane, [&](int t) { return z[t]; });
+      __syncwarp();
+      const int f = feat0 + (lane & 3) * 8, left = p.N - f;
 #pragma unroll
-    for (int t = 0; t < 32; ++t) {
-      const int r = __shfl_sync(0xffffffffu, row, t);
-      if (r >= 0 && feat0 + lane < p.N) reinterpret_cast<float*>(p.out + r * p.out_stride)[feat0 + lane] = z[t];
-    }
-  } else if constexpr (OUT == MOECA_BF16) {
-    if (feat0 >= p.N) return;
-    if (p.wide) {
-      // Lanes 2i and 2i + 1 swap halves: each holds the feature pair of every other token.
-      const int odd = lane & 1, f = feat0 + (lane & ~1);
-#pragma unroll
-      for (int t = 0; t < 16; ++t) {
-        const uint32_t own = pack_bf16(z[2 * t], z[2 * t + 1]);
-        const uint32_t got = __shfl_xor_sync(0xffffffffu, own, 1);
-        const uint32_t word = odd ? __byte_perm(got, own, 0x7632) : __byte_perm(own, got, 0x5410);
-        const int r = __shfl_sync(0xffffffffu, row, 2 * t + odd);
-        if (r < 0 || f >= p.N) continue;
+      for (int i = 0; i < 4; ++i) {
+        const uint4 v = *reinterpret_cast<const uint4*>(stage + (i * 8 + (lane >> 2)) * 16 + (lane & 3) * 4);
+        const int r = __shfl_sync(0xffffffffu, row, i * 8 + (lane >> 2));
         uint8_t* at = p.out + r * p.out_stride + f * 2;
-        if (f + 1 < p.N) *reinterpret_cast<uint32_t*>(at) = word;
-        else *reinterpret_cast<uint16_t*>(at) = static_cast<uint16_t>(word);
+        if (r >= 0 && left >= 8) {
+          *reinterpret_cast<uint4*>(at) = v;
+        } else if (r >= 0 && left > 0) {
+          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int j = 0; j < 7; ++j)
+            if (j < left) reinterpret_cast<uint16_t*>(at)[j] = static_cast<uint16_t>(w[j >> 1] >> 16 * (j & 1));
+        }
       }
     } else {
+      using T = std::conditional_t<OUT == MOECA_F32, float, __nv_bfloat16>;
+      const bool live = feat0 + lane < p.N;
+      uint8_t* base = p.out + static_cast<int64_t>(feat0 + lane) * sizeof(T);
 #pragma unroll
       for (int t = 0; t < 32; ++t) {
         const int r = __shfl_sync(0xffffffffu, row, t);
-        if (r >= 0 && feat0 + lane < p.N)
-          reinterpret_cast<__nv_bfloat16*>(p.out + r * p.out_stride)[feat0 + lane] = __float2bfloat16_rn(z[t]);
+        if (r >= 0 && live) *reinterpret_cast<T*>(base + r * p.out_stride) = Elem<T>::from_f(z[t]);
       }
     }
   } else {
@@ -258,7 +301,6 @@ __device__ __forceinline__ void store_chunk(const MatmulParams& p, Shared& sh, f
     __syncwarp();
     if (quad == 0 && row >= 0) p.out_scale[row * p.os_stride + block] = static_cast<uint8_t>(byte);
     if (feat0 >= p.N) return;
-    const int f = feat0 + (lane >> 2) * 4, left = p.N - f;
 #pragma unroll
     for (int t = 0; t < 32; t += 4) {
       const float4 s = *reinterpret_cast<const float4*>(inv + t);
@@ -266,14 +308,22 @@ __device__ __forceinline__ void store_chunk(const MatmulParams& p, Shared& sh, f
       if (odd)
         word = encode_any<E5>(z[t] * s.x) | encode_any<E5>(z[t + 1] * s.y) << 8 | encode_any<E5>(z[t + 2] * s.z) << 16 |
                encode_any<E5>(z[t + 3] * s.w) << 24;
-      word = transpose4(word, lane);
-      const int r = __shfl_sync(0xffffffffu, row, t + (lane & 3));
-      if (r < 0 || left <= 0) continue;
+      stage[(t + (lane & 3)) * 8 + (lane >> 2)] = transpose4(word, lane);
+    }
+    __syncwarp();
+    const int f = feat0 + (lane & 1) * 16, left = p.N - f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint4 v = *reinterpret_cast<const uint4*>(stage + (i * 16 + (lane >> 1)) * 8 + (lane & 1) * 4);
+      const int r = __shfl_sync(0xffffffffu, row, i * 16 + (lane >> 1));
       uint8_t* at = p.out + r * p.out_stride + f;
-      if (left >= 4) {
-        *reinterpret_cast<uint32_t*>(at) = word;
-      } else {
-        for (int i = 0; i < left; ++i) at[i] = static_cast<uint8_t>(word >> 8 * i);
+      if (r >= 0 && left >= 16) {
+        *reinterpret_cast<uint4*>(at) = v;
+      } else if (r >= 0 && left > 0) {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int j = 0; j < 15; ++j)
+          if (j < left) at[j] = static_cast<uint8_t>(w[j >> 2] >> 8 * (j & 3));
       }
     }
   }
@@ -413,73 +463,66 @@ __global__ void __launch_bounds__(kThreads, 1) q8_matmul_kernel(const __grid_con
       }
     }
   } else if (warp == 1) {
-    if (lane == 0 && rank == 0) {
+    if (rank == 0) {
       // ---------------- MMA issuer (the leader, for both CTAs) ----------------
+      uint32_t issue;
+      asm volatile("{\n .reg .pred e;\n elect.sync _|e, 0xffffffff;\n selp.u32 %0, 1, 0, e;\n}" : "=r"(issue));
       const uint32_t w_lo0 = ((ring & 0x3FFFFu) >> 4) | (1u << 16), x_lo0 = ((ring_t & 0x3FFFFu) >> 4) | (1u << 16);
-      const uint32_t full0 = smem_u32(&sh.full[0]);
-      const uint32_t x_end = x_lo0 + nst * (static_cast<uint32_t>(t_slot) >> 4);
-      const int last_steps = (p.K - (kb - 1) * kQ8Block + 31) / 32;  // MMAs of the last K block
-      uint32_t w_lo = w_lo0, x_lo = x_lo0, fb = full0, eb = empty0, par = 0u, acc_phase = 0, sf_par = 0;
-      int acc = 0, sfs = 0, g = 0;
+      const uint32_t full0 = smem_u32(&sh.full[0]), sf_full0 = smem_u32(&sh.sf_full[0]), sf_empty0 = smem_u32(&sh.sf_empty[0]);
+      int slot = 0, acc = 0, sfs = 0, g = 0;
+      uint32_t par = 0u, acc_phase = 0, sf_par = 0;
       bool ok = true;
       for (int u = pair; u < units; u += n_pairs) {
         const Unit t = unit_at(sh, u, g, nw);
         g = t.g;
-        if (!(ok = mbar_wait_cluster(smem_u32(&sh.tempty[acc]), acc_phase ^ 1u, abort_flag))) break;
-        tc_fence_after();
+        if (!(ok = warp_wait(smem_u32(&sh.tempty[acc]), acc_phase ^ 1u, abort_flag))) break;
         const uint32_t d_tmem = tmem + static_cast<uint32_t>(acc * kMaxN);
         const uint32_t idesc = mx_desc(t.n, p.w_e5, p.t_e5), x_sub = static_cast<uint32_t>(t.n >> 1) * kQ8Block >> 4;
         for (int k = 0; k < ks; ++k) {
-          if ((k & 1) == 0 && !(ok = mbar_wait_cluster(smem_u32(&sh.sf_full[sfs]), sf_par, abort_flag))) break;
-          if (!(ok = mbar_wait_hot(fb, par, abort_flag))) break;
+          if (k % (4 / kSub) == 0 && !(ok = warp_wait(sf_full0 + sfs * 8, sf_par, abort_flag))) break;
+          if (!(ok = warp_wait(full0 + slot * 8, par, abort_flag))) break;
           tc_fence_after();
           const uint32_t sf = tmem + kSfBase + sfs * kSfCols;
+          const uint32_t w_lo = w_lo0 + slot * (kWSlot >> 4), x_lo = x_lo0 + slot * (t_slot >> 4);
+          // The values past K in the last block are zeros on both sides.
 #pragma unroll
           for (int q = 0; q < kSub; ++q) {
             const int b = k * kSub + q;
-            if (b >= kb) break;
-            const uint32_t wq = w_lo + q * (kWBytes >> 4), xq = x_lo + q * x_sub;
-            const uint32_t id = static_cast<uint32_t>(b & 3), desc = idesc | id << 4 | id << 29;
-            const int steps = b == kb - 1 ? last_steps : 4;
-#pragma unroll
-            for (int kk = 0; kk < 4; ++kk)
-              if (kk < steps) mma_mx_pair(d_tmem, wq + kk * 2, xq + kk * 2, desc, sf, sf + 8, b != 0 || kk != 0);
+            const uint32_t id = static_cast<uint32_t>(b & 3);
+            if (q == 0 || b < kb)
+              mma_mx_block(d_tmem, w_lo + q * (kWBytes >> 4), x_lo + q * x_sub, idesc | id << 4 | id << 29, sf, sf + 8,
+                           b != 0, issue);
           }
-          mma_commit_pair(eb);
-          if ((k & 1) || k == ks - 1) {
-            mma_commit_pair(smem_u32(&sh.sf_empty[sfs]));
+          commit_pair_if(empty0 + slot * 8, issue);
+          if (k % (4 / kSub) == 4 / kSub - 1 || k == ks - 1) {
+            commit_pair_if(sf_empty0 + sfs * 8, issue);
             if (++sfs == kSfStages) {
               sfs = 0;
               sf_par ^= 1u;
             }
           }
-          w_lo += kWSlot >> 4;
-          x_lo += static_cast<uint32_t>(t_slot) >> 4;
-          fb += 8;
-          eb += 8;
-          if (x_lo == x_end) {
-            w_lo = w_lo0;
-            x_lo = x_lo0;
-            fb = full0;
-            eb = empty0;
+          if (++slot == nst) {
+            slot = 0;
             par ^= 1u;
           }
         }
         if (!ok) break;
-        mma_commit_pair(smem_u32(&sh.tfull[acc]));
+        commit_pair_if(smem_u32(&sh.tfull[acc]), issue);
         if (++acc == 2) {
           acc = 0;
           acc_phase ^= 1u;
         }
       }
-      if (!ok) {
-        if (!sh.abort_flag) report_status(p.status, MOECA_ERR_TIMEOUT, 701);
-        sh.abort_flag = 1;
-      }
-      // Every MMA issued so far has completed once the drain barrier fires.
-      mma_commit_pair(smem_u32(&sh.drain), 1);
-      const unsigned long long t0 = globaltimer();
-      while (!mbar_try(smem_u32(&sh.drain), 0) && globaltimer() - t0 < kTcWaitNs) {
+      if (lane == 0) {
+        if (!ok) {
+          if (!sh.abort_flag) report_status(p.status, MOECA_ERR_TIMEOUT, 701);
+          sh.abort_flag = 1;
+        }
+        // Every MMA issued so far has completed once the drain barrier fires.
+        mma_commit_pair(smem_u32(&sh.drain), 1);
+        const unsigned long long t0 = globaltimer();
+        while (!mbar_try(smem_u32(&sh.drain), 0) && globaltimer() - t0 < kTcWaitNs) {
+        }
       }
     }
   } else if (warp >= kSfWarp) {
@@ -523,7 +566,10 @@ __global__ void __launch_bounds__(kThreads, 1) q8_matmul_kernel(const __grid_con
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(full0 + sfs * 8);
+        // Relaxed: what is handed over lies in TMEM and is ordered by the fences
+        // (a release would wait for the loads in flight).
+        if (lane == 0)
+          asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(full0 + sfs * 8) : "memory");
         if (++sfs == kSfStages) {
           sfs = 0;
           par ^= 1u;
@@ -545,14 +591,22 @@ __global__ void __launch_bounds__(kThreads, 1) q8_matmul_kernel(const __grid_con
       const Unit t = unit_at(sh, u, g, nw);
       g = t.g;
       const int block = t.w * 2 + static_cast<int>(rank), feat0 = block * kBM + quad * 32;
-      const float bias = p.bias && feat0 + lane < p.N ? __ldg(p.bias + static_cast<int64_t>(g) * p.N + feat0 + lane) : 0.f;
       const bool live = feat0 + lane < p.N;
+      const float bias = p.bias && live ? __ldg(p.bias + static_cast<int64_t>(g) * p.N + feat0 + lane) : 0.f;
+      // A CTA whose features lie past N has no block: it only keeps in step.
+      const int cols = block * kBM < p.N ? t.m_end - t.m0 : 0;
+      int rows[kChunks];  // this lane's output row in each of the part's chunks
+#pragma unroll
+      for (int j = 0; j < kChunks; ++j) {
+        const int m = t.m0 + (j * kParts + part) * 32 + lane;
+        rows[j] = -1;
+        if (m < t.m_end) rows[j] = p.dst ? __ldg(p.dst + m) : m;
+        if (rows[j] >= p.out_rows) rows[j] = -1;
+      }
       ok = mbar_wait(smem_u32(&sh.tfull[acc]), acc_phase, abort_flag);
       if (!(ok = part_sync(part, ok))) break;  // all warps of the part, or none: the chunks' exchanges need all
       tc_fence_after();
       const uint32_t tb = tmem + (static_cast<uint32_t>(quad * 32) << 16) + static_cast<uint32_t>(acc * kMaxN);
-      // A CTA whose features lie past N has no block: it only keeps in step.
-      const int cols = block * kBM < p.N ? t.m_end - t.m0 : 0;
       int c = part * 32;
       if (c >= cols) {
         tc_fence_before();
@@ -560,24 +614,25 @@ __global__ void __launch_bounds__(kThreads, 1) q8_matmul_kernel(const __grid_con
         if (lane == 0) mbar_arrive_cluster(tempty0 + acc * 8);
       }
 #pragma unroll 1
-      for (; c < cols; c += 64) {
-        const int m = t.m0 + c + lane;
-        int row = -1;
-        if (m < t.m_end) {
-          row = p.dst ? __ldg(p.dst + m) : m;
-          if (row >= p.out_rows) row = -1;
+      for (; c < cols; c += 32 * kParts) {
+        float z[32];
+        {
+          uint32_t v[32];
+          tmem_ld32_async(tb + c, v);
+          tmem_wait32(v);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) z[i] = __uint_as_float(v[i]);
         }
-        uint32_t v[32];
-        tmem_ld32_async(tb + c, v);
-        tmem_wait32(v);
-        if (c + 64 >= cols) {
+        if (c + 32 * kParts >= cols) {
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive_cluster(tempty0 + acc * 8);
         }
-        float z[32];
 #pragma unroll
-        for (int i = 0; i < 32; ++i) z[i] = live ? act_f<ACT>(__uint_as_float(v[i]) + bias) : 0.f;
+        for (int i = 0; i < 32; ++i) z[i] = live ? act_f<ACT>(z[i] + bias) : 0.f;
+        const int row = rows[0];
+#pragma unroll
+        for (int j = 0; j + 1 < kChunks; ++j) rows[j] = rows[j + 1];
         store_chunk<OUT>(p, sh, z, row, feat0, block, lane, warp, part, quad, buf);
         buf ^= 1;
       }
@@ -635,7 +690,7 @@ cudaError_t launch_q8_matmul(const Q8MatmulArgs& a, cudaStream_t s) {
   p.out = a.out.q; p.out_scale = a.out.scale;
   p.out_rows = a.out.rows; p.out_stride = a.out.q_stride; p.os_stride = a.out.scale_stride;
   p.w_e5 = a.b_e5; p.t_e5 = a.a_e5;
-  p.wide = reinterpret_cast<uintptr_t>(a.out.q) % 4 == 0 && a.out.q_stride % 4 == 0;
+  p.wide = reinterpret_cast<uintptr_t>(a.out.q) % 16 == 0 && a.out.q_stride % 16 == 0;
   p.status = a.status;
   // At most one pair per tile there can be.
   const int64_t nw = (a.n_cols + 2 * kBM - 1) / (2 * kBM);
