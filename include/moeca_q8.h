@@ -132,7 +132,7 @@ typedef struct {
   int32_t* status;         /* device int32 [2], or NULL: [0] becomes a negative
                               moeca_status if the kernel's bounded waits ran out
                               (the output is then incomplete), else stays as it is    */
-  int32_t n_groups;        /* 1 .. 1024 (1 where offsets is NULL)                     */
+  int32_t n_groups;        /* 1 .. 512 (1 where offsets is NULL)                     */
   int32_t n_cols;          /* N >= 1                                                  */
   int32_t act;             /* moeca_q8_act                                            */
 } moeca_q8_matmul_args;

@@ -312,7 +312,7 @@ cudaError_t launch_q8_combine(const Q8CombineArgs& a, bool bf16, bool e5, cudaSt
 namespace {
 
 constexpr int64_t kMaxRows = 0x7fffffff;
-constexpr int kMaxWidth = 1 << 20, kMaxSlots = 16, kMaxGroups = 1024;
+constexpr int kMaxWidth = 1 << 20, kMaxSlots = 16, kMaxGroups = 512;
 
 bool is_format(int f) { return f == MOECA_E4M3 || f == MOECA_E5M2; }
 bool is_dtype(int d) { return d == MOECA_F32 || d == MOECA_BF16; }
@@ -469,7 +469,7 @@ moeca_status moeca_q8_matmul(const moeca_q8_matmul_args* a, void* stream) {
   if (const char* why = bad_rows(a->a)) return refuse(why);
   if (const char* why = bad_rows(a->b)) return refuse(why);
   if (a->n_groups < 1 || a->n_groups > kMaxGroups || (!a->offsets && a->n_groups != 1))
-    return refuse("1 <= n_groups <= 1024, and offsets for more than one group");
+    return refuse("1 <= n_groups <= 512, and offsets for more than one group");
   if (a->n_cols < 1 || a->n_cols > kMaxWidth || a->b.rows != static_cast<int64_t>(a->n_groups) * a->n_cols)
     return refuse("b must have n_groups x n_cols rows, n_cols in 1 .. 2^20");
   if (a->a.width != a->b.width) return refuse("a and b must have the same width");

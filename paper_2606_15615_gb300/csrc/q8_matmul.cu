@@ -11,10 +11,10 @@
 //
 // Persistent CTA pairs (clusters of two, cta_group::2): a tile is 256 weight
 // rows (the MMA's M side, 128 per CTA) by n token rows (its N side, half per
-// CTA; n a multiple of 16 up to 192, chosen per group so that its tiles are as
+// CTA; n a multiple of 16 up to 224, chosen per group so that its tiles are as
 // even and as narrow as its rows allow), K in stages of two blocks of 128.
 // The weights take the wide side because a group's rows are few and ragged,
-// its weights neither.  Two accumulators of 192 TMEM columns, so that a tile's
+// its weights neither.  Two accumulators of 224 TMEM columns, so that a tile's
 // epilogue runs beside the next one's MMAs; the rest of TMEM holds the scales.
 // 15 warps per CTA:
 //   warp 0      TMA producer of the weight boxes (128 rows x 128 bytes);
@@ -63,7 +63,7 @@ constexpr int kSfWarp = 2 + kEpiWarps;    // warps 10-13
 constexpr int kTokWarp = kSfWarp + 4;
 constexpr int kThreads = 32 * (kTokWarp + 1);
 constexpr int kTmemCols = 512;
-constexpr int kMaxGroups = 1024;
+constexpr int kMaxGroups = 512;
 static_assert(kSfBase + kSfStages * kSfCols <= kTmemCols, "TMEM");
 static_assert(kMaxN <= 256, "eight scale columns");
 
@@ -71,8 +71,8 @@ static_assert(kMaxN <= 256, "eight scale columns");
 struct Shared {
   int units[kMaxGroups + 1];              // first unit of each group
   int lo[kMaxGroups], rows[kMaxGroups];   // first row, rows
-  uint32_t top[kParts][2][4][32];         // [part][buffer][quadrant][token]: largest |z| bits
-  alignas(16) uint32_t stage[kEpiWarps][512];  // a chunk on its way out: 32 tokens x 32 features of at most two bytes
+  alignas(16) uint32_t top[kParts][2][4][32];         // [part][buffer][quadrant][token]: largest |z| bits
+  alignas(16) uint32_t stage[kEpiWarps][256];  // a chunk on its way out: 32 x 32 bytes, or 16 x 32 bf16
   float inv[kEpiWarps][32];   // 1 / scale of the chunk's tokens, read four at a time
   uint64_t full[kMaxStages], empty[kMaxStages], sf_full[kSfStages], sf_empty[kSfStages], tfull[2], tempty[2], drain;
   uint32_t tmem;
@@ -154,6 +154,12 @@ __device__ __forceinline__ void commit_pair_if(uint32_t bar, uint32_t issue) {
       "h"(static_cast<uint16_t>(3)), "r"(issue)
       : "memory");
 }
+// Arrive on a barrier of either CTA without a release: what is handed over lies
+// in TMEM and is ordered by the tcgen05 fences; a release would wait for the
+// warp's global accesses in flight (16 us of 50 in products with short K).
+__device__ __forceinline__ void arrive_relaxed(uint32_t bar) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
 // Every lane's bounded wait, the first try inline; the same answer in all lanes.
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
   if (__all_sync(0xffffffffu, mbar_try(bar, parity))) return true;
@@ -171,42 +177,55 @@ __device__ __forceinline__ float rcp(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// GELU of an epilogue value (Eq. 5).  tanh form: z sigmoid(2 u), u = sqrt(2/pi) (z + 0.044715 z^3).
+// GELU of a chunk's values (Eq. 5).  tanh form: z sigmoid(2 u), u = sqrt(2/pi) (z + 0.044715 z^3).
 // erf form: Phi(-|z|) = erfc(|z| / sqrt 2) / 2 by Abramowitz and Stegun's
 // formula 7.1.26, P(t) exp(-z^2 / 2) / 2 with t = 1 / (1 + p |z| / sqrt 2), within
 // 0.75e-7; z Phi(z) is z - z Phi(-z) or z Phi(-|z|), so that nothing cancels.
-// Both cost two special-function evaluations and few others; the library
-// functions' longer forms would bound the products with short K.
+// Two values share one reciprocal, 1/a = b / (ab): the special-function unit
+// takes 8 clocks a warp for it, and the pairs' chains interleave (28 -> 11
+// clocks a value at two warps per scheduler).  The minima keep ab finite and
+// one value's NaN out of the other.
 template <int ACT>
-__device__ __forceinline__ float act_f(float z) {
+__device__ __forceinline__ void activate(float (&z)[32]) {
   constexpr float kLog2e = 1.44269504f;
-  if constexpr (ACT == MOECA_ACT_GELU_TANH) {
-    const float v = z * fmaf(-0.0713548163f * kLog2e, z * z, -1.5957691216f * kLog2e);  // -2 u log2(e)
-    return z * rcp(1.f + ex2(v));
-  } else if constexpr (ACT == MOECA_ACT_GELU) {
-    const float x = fabsf(z);
-    const float t = rcp(fmaf(0.3275911f * 0.70710678f, x, 1.f));
-    float s = fmaf(0.5f * 1.061405429f, t, 0.5f * -1.453152027f);
-    s = fmaf(s, t, 0.5f * 1.421413741f);
-    s = fmaf(s, t, 0.5f * -0.284496736f);
-    s = fmaf(s, t, 0.5f * 0.254829592f);
-    const float tail = s * t * ex2(-0.5f * kLog2e * z * z) * x;  // |z| Phi(-|z|)
-    return fmaxf(z, 0.f) - tail;
-  } else {
-    return z;
+  if constexpr (ACT != MOECA_ACT_NONE) {
+#pragma unroll
+    for (int i0 = 0; i0 < 32; i0 += 8) {
+      float d[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float v = z[i0 + i];
+        if constexpr (ACT == MOECA_ACT_GELU_TANH) {
+          const float w = v * fmaf(-0.0713548163f * kLog2e, v * v, -1.5957691216f * kLog2e);  // -2 u log2(e)
+          d[i] = 1.f + ex2(fminf(w, 60.f));
+        } else {
+          d[i] = fmaf(0.3275911f * 0.70710678f, fminf(fabsf(v), 1e18f), 1.f);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) {
+        const float r = rcp(d[i] * d[i + 1]), t = d[i + 1] * r;
+        d[i + 1] = d[i] * r;
+        d[i] = t;
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float v = z[i0 + i], t = d[i];
+        if constexpr (ACT == MOECA_ACT_GELU_TANH) {
+          z[i0 + i] = v * t;
+        } else {
+          float s = fmaf(0.5f * 1.061405429f, t, 0.5f * -1.453152027f);
+          s = fmaf(s, t, 0.5f * 1.421413741f);
+          s = fmaf(s, t, 0.5f * -0.284496736f);
+          s = fmaf(s, t, 0.5f * 0.254829592f);
+          z[i0 + i] = fmaxf(v, 0.f) - s * t * ex2(-0.5f * kLog2e * v * v) * fabsf(v);  // |z| Phi(-|z|)
+        }
+      }
+    }
   }
 }
 
-// Four features' bytes of one token per lane from four tokens' bytes of one
-// feature: lane j of each four lanes gets token j's.
-__device__ __forceinline__ uint32_t transpose4(uint32_t own, int lane) {
-  const uint32_t p1 = __shfl_xor_sync(0xffffffffu, own, 1);
-  const uint32_t a = lane & 1 ? __byte_perm(p1, own, 0x7351) : __byte_perm(own, p1, 0x6240);
-  const uint32_t p2 = __shfl_xor_sync(0xffffffffu, a, 2);
-  return lane & 2 ? __byte_perm(p2, a, 0x7632) : __byte_perm(a, p2, 0x5410);
-}
-
-// Barrier over the four epilogue warps of a part (ids 1 and 2); true if `ok` in all.
+// Barrier over the four epilogue warps of a part (ids 1 to kParts); true if `ok` in all.
 __device__ __forceinline__ bool part_sync(int part, bool ok) {
   uint32_t all;
   asm volatile(
@@ -244,13 +263,24 @@ __device__ __forceinline__ void store_chunk(const MatmulParams& p, Shared& sh, f
   if constexpr (OUT == MOECA_F32 || OUT == MOECA_BF16) {
     if (feat0 >= p.N) return;
     if (OUT == MOECA_BF16 && p.wide) {
-      __syncwarp();  // the last chunk has left the stage
-      stage_by_token(stage, lane, [&](int t) { return z[t]; });
-      __syncwarp();
-      const int f = feat0 + (lane & 3) * 8, left = p.N - f;
+      // 16 tokens at a time; lanes 2i and 2i + 1 swap halves, so that each holds
+      // the feature pair of every other token.
+      const int f = feat0 + (lane & 3) * 8, left = p.N - f, odd = lane & 1;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const uint4 v = *reinterpret_cast<const uint4*>(stage + (i * 8 + (lane >> 2)) * 16 + (lane & 3) * 4);
+        if (i % 2 == 0) {
+          __syncwarp();  // what was staged before has been read
+          uint32_t own[8], got[8];
+#pragma unroll
+          for (int t = 0; t < 8; ++t) own[t] = pack_bf16(z[8 * i + 2 * t], z[8 * i + 2 * t + 1]);
+#pragma unroll
+          for (int t = 0; t < 8; ++t) got[t] = __shfl_xor_sync(0xffffffffu, own[t], 1);
+#pragma unroll
+          for (int t = 0; t < 8; ++t)
+            stage[(2 * t + odd) * 16 + (lane >> 1)] = __byte_perm(own[t], got[t], odd ? 0x3276 : 0x5410);
+          __syncwarp();
+        }
+        const uint4 v = *reinterpret_cast<const uint4*>(stage + ((i & 1) * 8 + (lane >> 2)) * 16 + (lane & 3) * 4);
         const int r = __shfl_sync(0xffffffffu, row, i * 8 + (lane >> 2));
         uint8_t* at = p.out + r * p.out_stride + f * 2;
         if (r >= 0 && left >= 8) {
@@ -274,22 +304,29 @@ __device__ __forceinline__ void store_chunk(const MatmulParams& p, Shared& sh, f
     }
   } else {
     constexpr bool E5 = OUT == MOECA_E5M2;
-    uint32_t mine = 0;  // lane t: the largest |z| of token t over the warp's features
+    // The tokens' largest |z| over the warp's features, then over the block's.
+    uint32_t* mine = sh.top[part][buf][quad];
+    uint32_t all = 0;
 #pragma unroll
-    for (int t = 0; t < 32; ++t) {
-      const uint32_t top = __reduce_max_sync(0xffffffffu, abs_bits(z[t]));
-      if (lane == t) mine = top;
+    for (int t = 0; t < 32; t += 4) {
+      uint4 m;
+      m.x = __reduce_max_sync(0xffffffffu, abs_bits(z[t]));
+      m.y = __reduce_max_sync(0xffffffffu, abs_bits(z[t + 1]));
+      m.z = __reduce_max_sync(0xffffffffu, abs_bits(z[t + 2]));
+      m.w = __reduce_max_sync(0xffffffffu, abs_bits(z[t + 3]));
+      if (lane == 0) *reinterpret_cast<uint4*>(mine + t) = m;
+      all = max(max(max(m.x, m.y), max(m.z, m.w)), all);
     }
-    const bool odd = __any_sync(0xffffffffu, row >= 0 && mine >= kNonFinite);
+    const bool odd = all >= kNonFinite;  // the same in all lanes
     if (odd) {
-      mine = 0;
-#pragma unroll
       for (int t = 0; t < 32; ++t) {
-        const uint32_t b = abs_bits(z[t]), top = __reduce_max_sync(0xffffffffu, b < kNonFinite ? b : 0u);
-        if (lane == t) mine = top;
+        uint32_t b = 0;
+#pragma unroll
+        for (int j = 0; j < 32; ++j) b = j == t ? abs_bits(z[j]) : b;
+        b = __reduce_max_sync(0xffffffffu, b < kNonFinite ? b : 0u);
+        if (lane == 0) mine[t] = b;
       }
     }
-    sh.top[part][buf][quad][lane] = mine;
     part_sync(part, true);
     uint32_t top = 0;
 #pragma unroll
@@ -301,15 +338,34 @@ __device__ __forceinline__ void store_chunk(const MatmulParams& p, Shared& sh, f
     __syncwarp();
     if (quad == 0 && row >= 0) p.out_scale[row * p.os_stride + block] = static_cast<uint8_t>(byte);
     if (feat0 >= p.N) return;
+    // Step by step over all eight words, so that their chains interleave.
+    uint32_t word[8], got[8];
 #pragma unroll
-    for (int t = 0; t < 32; t += 4) {
-      const float4 s = *reinterpret_cast<const float4*>(inv + t);
-      uint32_t word = encode2<E5>(z[t] * s.x, z[t + 1] * s.y) | encode2<E5>(z[t + 2] * s.z, z[t + 3] * s.w) << 16;
-      if (odd)
-        word = encode_any<E5>(z[t] * s.x) | encode_any<E5>(z[t + 1] * s.y) << 8 | encode_any<E5>(z[t + 2] * s.z) << 16 |
-               encode_any<E5>(z[t + 3] * s.w) << 24;
-      stage[(t + (lane & 3)) * 8 + (lane >> 2)] = transpose4(word, lane);
+    for (int t = 0; t < 8; ++t) {
+      const float4 s = *reinterpret_cast<const float4*>(inv + 4 * t);
+      z[4 * t] *= s.x;
+      z[4 * t + 1] *= s.y;
+      z[4 * t + 2] *= s.z;
+      z[4 * t + 3] *= s.w;
+      word[t] = encode2<E5>(z[4 * t], z[4 * t + 1]) | encode2<E5>(z[4 * t + 2], z[4 * t + 3]) << 16;
     }
+    if (odd) {
+#pragma unroll
+      for (int t = 0; t < 8; ++t)
+        word[t] = encode_any<E5>(z[4 * t]) | encode_any<E5>(z[4 * t + 1]) << 8 | encode_any<E5>(z[4 * t + 2]) << 16 |
+                  encode_any<E5>(z[4 * t + 3]) << 24;
+    }
+    // Four features' bytes of one token per lane from four tokens' bytes of one
+    // feature: lane j of each four lanes gets token j's.
+    const uint32_t sel1 = lane & 1 ? 0x3715 : 0x6240, sel2 = lane & 2 ? 0x3276 : 0x5410;
+#pragma unroll
+    for (int t = 0; t < 8; ++t) got[t] = __shfl_xor_sync(0xffffffffu, word[t], 1);
+#pragma unroll
+    for (int t = 0; t < 8; ++t) word[t] = __byte_perm(word[t], got[t], sel1);
+#pragma unroll
+    for (int t = 0; t < 8; ++t) got[t] = __shfl_xor_sync(0xffffffffu, word[t], 2);
+#pragma unroll
+    for (int t = 0; t < 8; ++t) stage[(4 * t + (lane & 3)) * 8 + (lane >> 2)] = __byte_perm(word[t], got[t], sel2);
     __syncwarp();
     const int f = feat0 + (lane & 1) * 16, left = p.N - f;
 #pragma unroll
@@ -566,10 +622,7 @@ __global__ void __launch_bounds__(kThreads, 1) q8_matmul_kernel(const __grid_con
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         tc_fence_before();
         __syncwarp();
-        // Relaxed: what is handed over lies in TMEM and is ordered by the fences
-        // (a release would wait for the loads in flight).
-        if (lane == 0)
-          asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(full0 + sfs * 8) : "memory");
+        if (lane == 0) arrive_relaxed(full0 + sfs * 8);
         if (++sfs == kSfStages) {
           sfs = 0;
           par ^= 1u;
@@ -584,7 +637,7 @@ __global__ void __launch_bounds__(kThreads, 1) q8_matmul_kernel(const __grid_con
     // ---------------- Epilogue ----------------
     const int quad = warp & 3, part = (warp - 2) >> 2;
     const uint32_t tempty0 = cluster_addr(smem_u32(&sh.tempty[0]), 0);
-    int acc = 0, g = 0, buf = 0;
+    int acc = 0, g = 0, buf = 0, first = part;  // the part's first chunk turns, so that the parts' shares even out
     uint32_t acc_phase = 0;
     bool ok = true;
     for (int u = pair; u < units; u += n_pairs) {
@@ -598,7 +651,7 @@ __global__ void __launch_bounds__(kThreads, 1) q8_matmul_kernel(const __grid_con
       int rows[kChunks];  // this lane's output row in each of the part's chunks
 #pragma unroll
       for (int j = 0; j < kChunks; ++j) {
-        const int m = t.m0 + (j * kParts + part) * 32 + lane;
+        const int m = t.m0 + (j * kParts + first) * 32 + lane;
         rows[j] = -1;
         if (m < t.m_end) rows[j] = p.dst ? __ldg(p.dst + m) : m;
         if (rows[j] >= p.out_rows) rows[j] = -1;
@@ -607,11 +660,12 @@ __global__ void __launch_bounds__(kThreads, 1) q8_matmul_kernel(const __grid_con
       if (!(ok = part_sync(part, ok))) break;  // all warps of the part, or none: the chunks' exchanges need all
       tc_fence_after();
       const uint32_t tb = tmem + (static_cast<uint32_t>(quad * 32) << 16) + static_cast<uint32_t>(acc * kMaxN);
-      int c = part * 32;
+      int c = first * 32;
+      first = (first + 2) % kParts;
       if (c >= cols) {
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(tempty0 + acc * 8);
+        if (lane == 0) arrive_relaxed(tempty0 + acc * 8);
       }
 #pragma unroll 1
       for (; c < cols; c += 32 * kParts) {
@@ -626,10 +680,11 @@ __global__ void __launch_bounds__(kThreads, 1) q8_matmul_kernel(const __grid_con
         if (c + 32 * kParts >= cols) {
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive_cluster(tempty0 + acc * 8);
+          if (lane == 0) arrive_relaxed(tempty0 + acc * 8);
         }
 #pragma unroll
-        for (int i = 0; i < 32; ++i) z[i] = live ? act_f<ACT>(z[i] + bias) : 0.f;
+        for (int i = 0; i < 32; ++i) z[i] = live ? z[i] + bias : 0.f;
+        activate<ACT>(z);
         const int row = rows[0];
 #pragma unroll
         for (int j = 0; j + 1 < kChunks; ++j) rows[j] = rows[j + 1];
