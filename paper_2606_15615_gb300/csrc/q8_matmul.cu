@@ -225,6 +225,13 @@ __device__ __forceinline__ void activate(float (&z)[32]) {
   }
 }
 
+// Bits of the largest |v| over the warp's lanes; at least kNonFinite where one is NaN.
+__device__ __forceinline__ uint32_t warp_top(float v) {
+  float r;
+  asm volatile("redux.sync.max.abs.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+  return abs_bits(r);
+}
+
 // Barrier over the four epilogue warps of a part (ids 1 to kParts); true if `ok` in all.
 __device__ __forceinline__ bool part_sync(int part, bool ok) {
   uint32_t all;
@@ -304,33 +311,34 @@ __device__ __forceinline__ void store_chunk(const MatmulParams& p, Shared& sh, f
     }
   } else {
     constexpr bool E5 = OUT == MOECA_E5M2;
+    if (feat0 + 32 > p.N && feat0 + lane >= p.N) {  // not a feature: another group's weights, or none
+#pragma unroll
+      for (int t = 0; t < 32; ++t) z[t] = 0.f;
+    }
     // The tokens' largest |z| over the warp's features, then over the block's.
-    uint32_t* mine = sh.top[part][buf][quad];
-    uint32_t all = 0;
+    const auto exchange = [&](auto magnitude) {
+      uint32_t* mine = sh.top[part][buf][quad];
 #pragma unroll
-    for (int t = 0; t < 32; t += 4) {
-      uint4 m;
-      m.x = __reduce_max_sync(0xffffffffu, abs_bits(z[t]));
-      m.y = __reduce_max_sync(0xffffffffu, abs_bits(z[t + 1]));
-      m.z = __reduce_max_sync(0xffffffffu, abs_bits(z[t + 2]));
-      m.w = __reduce_max_sync(0xffffffffu, abs_bits(z[t + 3]));
-      if (lane == 0) *reinterpret_cast<uint4*>(mine + t) = m;
-      all = max(max(max(m.x, m.y), max(m.z, m.w)), all);
-    }
-    const bool odd = all >= kNonFinite;  // the same in all lanes
-    if (odd) {
-      for (int t = 0; t < 32; ++t) {
-        uint32_t b = 0;
-#pragma unroll
-        for (int j = 0; j < 32; ++j) b = j == t ? abs_bits(z[j]) : b;
-        b = __reduce_max_sync(0xffffffffu, b < kNonFinite ? b : 0u);
-        if (lane == 0) mine[t] = b;
+      for (int t = 0; t < 32; t += 4) {
+        uint4 m;
+        m.x = warp_top(magnitude(z[t]));
+        m.y = warp_top(magnitude(z[t + 1]));
+        m.z = warp_top(magnitude(z[t + 2]));
+        m.w = warp_top(magnitude(z[t + 3]));
+        if (lane == 0) *reinterpret_cast<uint4*>(mine + t) = m;
       }
-    }
-    part_sync(part, true);
-    uint32_t top = 0;
+      part_sync(part, true);
+      uint32_t top = 0;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) top = max(top, sh.top[part][buf][q][lane]);
+      for (int q = 0; q < 4; ++q) top = max(top, sh.top[part][buf][q][lane]);
+      return top;
+    };
+    uint32_t top = exchange([](float v) { return v; });
+    const bool odd = __any_sync(0xffffffffu, row >= 0 && top >= kNonFinite);  // the same in the part's four warps
+    if (odd) {
+      part_sync(part, true);  // all have read the first maxima
+      top = exchange([](float v) { return abs_bits(v) < kNonFinite ? v : 0.f; });
+    }
     const int byte = scale_byte<E5>(top);
     float* inv = sh.inv[warp - 2];
     __syncwarp();
@@ -350,10 +358,10 @@ __device__ __forceinline__ void store_chunk(const MatmulParams& p, Shared& sh, f
       word[t] = encode2<E5>(z[4 * t], z[4 * t + 1]) | encode2<E5>(z[4 * t + 2], z[4 * t + 3]) << 16;
     }
     if (odd) {
+      // The conversion takes infinities for the largest value, 0x7b in e5m2 (one
+      // below infinity) and 0x7e in e4m3 (one below NaN): one more is right in both.
 #pragma unroll
-      for (int t = 0; t < 8; ++t)
-        word[t] = encode_any<E5>(z[4 * t]) | encode_any<E5>(z[4 * t + 1]) << 8 | encode_any<E5>(z[4 * t + 2]) << 16 |
-                  encode_any<E5>(z[4 * t + 3]) << 24;
+      for (int t = 0; t < 32; ++t) word[t >> 2] += abs_bits(z[t]) == kNonFinite ? 1u << 8 * (t & 3) : 0u;
     }
     // Four features' bytes of one token per lane from four tokens' bytes of one
     // feature: lane j of each four lanes gets token j's.
@@ -683,7 +691,7 @@ __global__ void __launch_bounds__(kThreads, 1) q8_matmul_kernel(const __grid_con
           if (lane == 0) arrive_relaxed(tempty0 + acc * 8);
         }
 #pragma unroll
-        for (int i = 0; i < 32; ++i) z[i] = live ? z[i] + bias : 0.f;
+        for (int i = 0; i < 32; ++i) z[i] += bias;
         activate<ACT>(z);
         const int row = rows[0];
 #pragma unroll

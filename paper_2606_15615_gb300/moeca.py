@@ -12,6 +12,7 @@ import ctypes as C
 import math
 import os
 import re
+import struct
 from typing import NamedTuple
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -612,6 +613,21 @@ def q8_empty(rows: int, width: int, dtype=None, device="cuda") -> Q8:
     return Q8(q.view(dtype or torch.float8_e4m3fn)[:, :width], s[:, :nb])
 
 
+# The calls below pass their argument structs as packed bytes: filling a ctypes
+# structure field by field took longer than the launch itself.  The formats
+# are those of the moeca_q8_*_args structures.
+_ROWS = "QQqqqii"
+_PACK_WRITE = struct.Struct("@" + _ROWS + "QqqiiQQQ")
+_PACK_READ = struct.Struct("@" + _ROWS + "QqiiQ")
+_PACK_COMBINE = struct.Struct("@" + _ROWS + "QQQqQqQqQiiii")
+_PACK_MATMUL = struct.Struct("@" + 3 * _ROWS + "QQQQiii4x")
+for _s, _t in ((_PACK_WRITE, moeca_q8_write_args), (_PACK_READ, moeca_q8_read_args),
+               (_PACK_COMBINE, moeca_q8_combine_args), (_PACK_MATMUL, moeca_q8_matmul_args)):
+    assert _s.size == C.sizeof(_t)
+_q8_packed = [C.CFUNCTYPE(C.c_int, C.c_char_p, C.c_void_p)(C.cast(getattr(LIB, _n), C.c_void_p).value) for _n in (
+    "moeca_q8_write", "moeca_q8_read", "moeca_q8_combine", "moeca_q8_matmul")]
+
+
 _TYPES = {}
 
 
@@ -620,90 +636,93 @@ def _type_code(dtype) -> int:
     if not _TYPES:
         import torch
         _TYPES.update({torch.float32: MOECA_F32, torch.bfloat16: MOECA_BF16, torch.float8_e4m3fn: MOECA_E4M3,
-                       torch.float8_e5m2: MOECA_E5M2})
+                       torch.float8_e5m2: MOECA_E5M2, "i32": torch.int32, "f32": torch.float32})
     return _TYPES.get(dtype, -1)
 
 
-def _row_stride(t, unit: int = 1) -> int:
-    """Elements from row to row.  One row (or none) has no next one: its length, in units of ``unit``."""
-    return t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] // unit) * unit
-
-
-def _q8_rows(r, what: str, device) -> moeca_q8_rows:
+def _q8_fields(r, what: str, device: int) -> tuple:
+    """The fields of moeca_q8_rows.  One row (or none) has no next one: its strides are not looked at."""
     q, s = r
-    code = _type_code(q.dtype)
-    if code < MOECA_E4M3 or q.dim() != 2 or (q.shape[1] > 1 and q.stride(1) != 1) or q.device != device:
-        raise ValueError(f"{what}.q must be a 2-D float8_e4m3fn or float8_e5m2 tensor on {device} with unit column stride")
-    if s.dim() != 2 or s.element_size() != 1 or s.shape[0] != q.shape[0] or s.shape[1] != -(-q.shape[1] // Q8_BLOCK) \
-            or (s.shape[1] > 1 and s.stride(1) != 1) or s.device != device:
-        raise ValueError(f"{what}.scale must be [rows, ceil(width / 128)] bytes on {device} with unit column stride")
-    return moeca_q8_rows(q.data_ptr(), s.data_ptr(), q.shape[0], _row_stride(q, 16), _row_stride(s, 4), q.shape[1], code)
+    if q.dim() != 2 or s.dim() != 2:
+        raise ValueError(f"{what}: q and scale must be 2-D")
+    (n, width), (q_stride, unit), code = q.shape, q.stride(), _type_code(q.dtype)
+    if code < MOECA_E4M3 or (unit != 1 and width > 1) or q.get_device() != device:
+        raise ValueError(f"{what}.q must be float8_e4m3fn or float8_e5m2 on the call's device with unit column stride")
+    (sn, nb), (s_stride, unit) = s.shape, s.stride()
+    if sn != n or nb != (width + 127) // Q8_BLOCK or (unit != 1 and nb > 1) or s.element_size() != 1 or s.get_device() != device:
+        raise ValueError(f"{what}.scale must be [rows, ceil(width / 128)] bytes on the call's device with unit column stride")
+    if n <= 1:
+        q_stride, s_stride = (width + 15) // 16 * 16, (nb + 3) // 4 * 4
+    return q.data_ptr(), s.data_ptr(), n, q_stride, s_stride, width, code
 
 
-def _list(t, dtype, shape, what: str, device):
-    """The address of a contiguous device tensor of one shape (None: NULL)."""
+def _value_fields(t, what: str, device: int) -> tuple:
+    """(address, rows, row stride in elements, width, type code) of a tensor of fp32 or bf16 rows."""
+    code = _type_code(t.dtype)
+    if code not in (MOECA_F32, MOECA_BF16) or t.dim() != 2 or t.get_device() != device:
+        raise ValueError(f"{what} must be a 2-D float32 or bfloat16 tensor on the call's device")
+    (n, width), (stride, unit) = t.shape, t.stride()
+    if unit != 1 and width > 1:
+        raise ValueError(f"{what} must have unit column stride")
+    return t.data_ptr(), n, stride if n > 1 else width, width, code
+
+
+def _list(t, kind: str, shape: tuple, what: str, device: int) -> int:
+    """The address of a contiguous device tensor of int32 ("i32") or float32 ("f32") and one shape (None: NULL)."""
     if t is None:
-        return None
-    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous() or t.device != device:
-        raise ValueError(f"{what} must be a contiguous {dtype} tensor {list(shape)} on {device}")
+        return 0
+    if t.dtype != _TYPES[kind] or tuple(t.shape) != shape or not t.is_contiguous() or t.get_device() != device:
+        raise ValueError(f"{what} must be a contiguous {_TYPES[kind]} tensor {list(shape)} on the call's device")
     return t.data_ptr()
 
 
-def _values(t, what: str, device) -> int:
-    """The C type code of a 2-D tensor of fp32 or bf16 rows."""
-    code = _type_code(t.dtype)
-    if code not in (MOECA_F32, MOECA_BF16) or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or t.device != device:
-        raise ValueError(f"{what} must be a 2-D float32 or bfloat16 tensor on {device} with unit column stride")
-    return code
-
-
-def _call(fn, args, device, stream):
+def _call(fn, args: bytes, device: int, stream: int):
     """Run a C call with the tensors' device current, on ``stream`` or that device's current stream."""
     import torch
-    if device.type != "cuda":
+    if device < 0:
         raise ValueError("8-bit rows live on a CUDA device")
-    if device.index == torch.cuda.current_device():
-        fn(args, stream or torch.cuda.current_stream().cuda_stream)
+    stream = stream or torch._C._cuda_getCurrentRawStream(device)
+    if device == torch._C._cuda_getDevice():
+        status = fn(args, stream or None)
     else:
         with torch.cuda.device(device):
-            fn(args, stream or torch.cuda.current_stream().cuda_stream)
+            status = fn(args, stream or None)
+    if status != MOECA_OK:
+        _check(status)
 
 
 def q8_write(x, cache: Q8, src=None, dst=None, count=None, stream: int = 0) -> Q8:
     """Quantise rows of ``x`` (fp32 or bf16) into ``cache`` (float8 type and scales as allocated): cache row
     dst[i] from x row src[i], int32 lists on the device (None: i), for all entries or the first ``count``
     (an int32 device tensor of one value).  Entries out of range are skipped.  Returns ``cache``."""
-    import torch
-    dev = x.device
-    dtype = _values(x, "x", dev)
-    rows = _q8_rows(cache, "cache", dev)
-    if x.shape[1] != rows.width:
-        raise ValueError(f"x is {x.shape[1]} wide, the cache {rows.width}")
+    dev = x.get_device()
+    address, n_x, x_stride, width, dtype = _value_fields(x, "x", dev)
+    rows = _q8_fields(cache, "cache", dev)
+    if width != rows[5]:
+        raise ValueError(f"x is {width} wide, the cache {rows[5]}")
     if src is not None and dst is not None and src.numel() != dst.numel():
         raise ValueError("src and dst must have the same length")
-    n = dst.numel() if dst is not None else src.numel() if src is not None else x.shape[0]
-    args = moeca_q8_write_args(
-        rows, x.data_ptr(), x.shape[0], _row_stride(x), dtype, n, _list(src, torch.int32, (n,), "src", dev),
-        _list(dst, torch.int32, (n,), "dst", dev), _list(count, torch.int32, (1,), "count", dev))
-    _call(moeca_q8_write, args, dev, stream)
+    n = dst.numel() if dst is not None else src.numel() if src is not None else n_x
+    args = _PACK_WRITE.pack(*rows, address, n_x, x_stride, dtype, n, _list(src, "i32", (n,), "src", dev),
+                            _list(dst, "i32", (n,), "dst", dev), _list(count, "i32", (1,), "count", dev))
+    _call(_q8_packed[0], args, dev, stream)
     return cache
 
 
 def q8_read(cache: Q8, rows=None, dtype=None, out=None, stream: int = 0):
     """Cache rows as bf16 (default) or fp32: all of them, or those of ``rows`` (int32, on the device); zeros
     where an entry is out of range."""
-    import torch
-    dev = cache.q.device
-    c = _q8_rows(cache, "cache", dev)
-    n = c.rows if rows is None else rows.numel()
+    dev = cache[0].get_device()
+    c = _q8_fields(cache, "cache", dev)
+    n = c[2] if rows is None else rows.numel()
     if out is None:
-        out = torch.empty((n, c.width), dtype=dtype or torch.bfloat16, device=dev)
-    code = _values(out, "out", dev)
-    if tuple(out.shape) != (n, c.width) or (dtype is not None and out.dtype != dtype):
-        raise ValueError(f"out must be [{n}, {c.width}] of the asked dtype")
-    args = moeca_q8_read_args(c, out.data_ptr(), _row_stride(out), code, n,
-                              _list(rows, torch.int32, (n,), "rows", dev))
-    _call(moeca_q8_read, args, dev, stream)
+        import torch
+        out = torch.empty((n, c[5]), dtype=dtype or torch.bfloat16, device=cache[0].device)
+    address, n_out, stride, width, code = _value_fields(out, "out", dev)
+    if n_out != n or width != c[5] or (dtype is not None and out.dtype != dtype):
+        raise ValueError(f"out must be [{n}, {c[5]}] of the asked dtype")
+    args = _PACK_READ.pack(*c, address, stride, code, n, _list(rows, "i32", (n,), "rows", dev))
+    _call(_q8_packed[1], args, dev, stream)
     return out
 
 
@@ -714,33 +733,35 @@ def q8_combine(cache: Q8, rows, weights=None, x=None, gate=None, norms=False, dt
     also gives the rows' 2-norms.  The result has x's dtype (without x: ``dtype``, default bf16); ``out`` may be
     x.  Returns out, or (out, norms)."""
     import torch
-    dev = cache.q.device
-    c = _q8_rows(cache, "cache", dev)
+    dev = cache[0].get_device()
+    c = _q8_fields(cache, "cache", dev)
     if rows.dim() != 2:
         raise ValueError("rows must be [tokens, slots]")
-    T, k = rows.shape
+    T, k = shape = tuple(rows.shape)
     if out is None:
-        out = torch.empty((T, c.width), dtype=x.dtype if x is not None else dtype or torch.bfloat16, device=dev)
-    code = _values(out, "out", dev)
-    if tuple(out.shape) != (T, c.width):
-        raise ValueError(f"out must be [{T}, {c.width}]")
-    if x is not None and (_values(x, "x", dev) != code or x.shape != out.shape):
-        raise ValueError("x must have out's dtype and shape")
+        out = torch.empty((T, c[5]), dtype=x.dtype if x is not None else dtype or torch.bfloat16, device=rows.device)
+    address, n_out, stride, width, code = _value_fields(out, "out", dev)
+    if n_out != T or width != c[5]:
+        raise ValueError(f"out must be [{T}, {c[5]}]")
+    x_address = x_stride = gate_address = gate_stride = 0
     seq = 1
+    if x is not None:
+        x_address, n_x, x_stride, x_width, x_code = _value_fields(x, "x", dev)
+        if x_code != code or n_x != T or x_width != width:
+            raise ValueError("x must have out's dtype and shape")
     if gate is not None:
-        if _values(gate, "gate", dev) != MOECA_F32 or gate.shape[1] != c.width or (T and (not gate.shape[0] or T % gate.shape[0])):
+        gate_address, n_g, gate_stride, g_width, g_code = _value_fields(gate, "gate", dev)
+        if g_code != MOECA_F32 or g_width != width or (T and (not n_g or T % n_g)):
             raise ValueError("gate must be float32 rows, one for each T / rows consecutive tokens")
-        seq = T // gate.shape[0] if T else 1
+        seq = T // n_g if T else 1
     if norms is True:
-        norms = torch.empty((T, k), dtype=torch.float32, device=dev)
+        norms = torch.empty(shape, dtype=torch.float32, device=rows.device)
     elif norms is False:
         norms = None
-    args = moeca_q8_combine_args(
-        c, _list(rows, torch.int32, (T, k), "rows", dev), _list(weights, torch.float32, (T, k), "weights", dev),
-        x.data_ptr() if x is not None else None, _row_stride(x) if x is not None else 0,
-        gate.data_ptr() if gate is not None else None, _row_stride(gate) if gate is not None else 0,
-        out.data_ptr(), _row_stride(out), _list(norms, torch.float32, (T, k), "norms", dev), code, T, k, seq)
-    _call(moeca_q8_combine, args, dev, stream)
+    args = _PACK_COMBINE.pack(
+        *c, _list(rows, "i32", shape, "rows", dev), _list(weights, "f32", shape, "weights", dev), x_address, x_stride,
+        gate_address, gate_stride, address, stride, _list(norms, "f32", shape, "norms", dev), code, T, k, seq)
+    _call(_q8_packed[2], args, dev, stream)
     return out if norms is None else (out, norms)
 
 
@@ -751,34 +772,31 @@ def q8_matmul(a: Q8, b: Q8, offsets=None, bias=None, act: str = "none", dst=None
     weight rows one group after another; ``offsets`` [groups + 1] and ``dst`` [rows of a] (the output row of
     each; out of range: dropped) are int32 on the device, ``bias`` [groups, columns] fp32.  ``out``: a tensor of
     fp32 / bf16 rows or a Q8 that takes the rows in 8 bits; without it a new tensor of ``dtype`` (bf16; float8
-    types give a Q8).  Returns out."""
-    import torch
-    dev = a.q.device
-    ra, rb = _q8_rows(a, "a", dev), _q8_rows(b, "b", dev)
+    types give a Q8).  ``status`` [2] int32 on the device tells of a wait that ran out.  Returns out."""
+    dev = a[0].get_device()
+    ra, rb = _q8_fields(a, "a", dev), _q8_fields(b, "b", dev)
     groups = offsets.numel() - 1 if offsets is not None else 1
-    if groups < 1 or rb.rows % groups or rb.rows == 0:
+    if groups < 1 or rb[2] % groups or rb[2] == 0:
         raise ValueError("b must hold the same number of rows for each group, one at least")
-    cols = rb.rows // groups
+    cols = rb[2] // groups
     if act not in _ACTS:
         raise ValueError(f"act must be one of {sorted(_ACTS)}")
     if out is None:
+        import torch
         code = _type_code(dtype or torch.bfloat16)
         if code < 0:
             raise ValueError("dtype must be float32, bfloat16, float8_e4m3fn or float8_e5m2")
-        if code >= MOECA_E4M3:
-            out = q8_empty(ra.rows, cols, dtype, dev)
-        else:
-            out = torch.empty((ra.rows, cols), dtype=dtype or torch.bfloat16, device=dev)
+        out = q8_empty(ra[2], cols, dtype, a[0].device) if code >= MOECA_E4M3 else \
+            torch.empty((ra[2], cols), dtype=dtype or torch.bfloat16, device=a[0].device)
     if isinstance(out, Q8):
-        ro = _q8_rows(out, "out", dev)
+        ro = _q8_fields(out, "out", dev)
     else:
-        code, size = _values(out, "out", dev), out.element_size()
-        ro = moeca_q8_rows(out.data_ptr(), None, out.shape[0], _row_stride(out) * size, 0, out.shape[1], code)
-    if ro.width != cols:
+        address, n_out, stride, width, code = _value_fields(out, "out", dev)
+        ro = (address, 0, n_out, stride * out.element_size(), 0, width, code)
+    if ro[5] != cols:
         raise ValueError(f"out must be {cols} wide")
-    args = moeca_q8_matmul_args(
-        ra, rb, ro, _list(offsets, torch.int32, (groups + 1,), "offsets", dev),
-        _list(bias, torch.float32, (groups, cols), "bias", dev), _list(dst, torch.int32, (ra.rows,), "dst", dev),
-        _list(status, torch.int32, (2,), "status", dev), groups, cols, _ACTS[act])
-    _call(moeca_q8_matmul, args, dev, stream)
+    args = _PACK_MATMUL.pack(
+        *ra, *rb, *ro, _list(offsets, "i32", (groups + 1,), "offsets", dev), _list(bias, "f32", (groups, cols), "bias", dev),
+        _list(dst, "i32", (ra[2],), "dst", dev), _list(status, "i32", (2,), "status", dev), groups, cols, _ACTS[act])
+    _call(_q8_packed[3], args, dev, stream)
     return out
