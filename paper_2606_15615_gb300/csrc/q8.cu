@@ -10,25 +10,46 @@ namespace moeca {
 namespace {
 
 // ---------------------------------------------------------------------------
-// Write.  A block of 128 values is the work of 8 lanes: each loads 16 values in
-// 16-byte pieces (piece l + 8 j of the block, so that 8 lanes cover 128
-// contiguous bytes), the block's largest magnitude is an integer maximum of
-// |x|'s bits over the 8 lanes, and one byte per value goes out the same way.
-// One pass: b + 1 bytes a value (b = 2 or 4), nothing is read twice.  Blocks
-// are numbered over all rows, so that no lane idles at a row's end; kUnits of
-// them are in flight per 8 lanes.
+// Write.  A block of 128 values (a unit) is the work of 8 lanes: each takes 16
+// values in pieces of 16 bytes (piece l + 8 j of the block, so that 8 lanes
+// cover 128 contiguous bytes), the block's largest magnitude is an integer
+// maximum of |x|'s bits over the 8 lanes, and one byte per value goes out the
+// same way.  One pass: b + 1 bytes a value (b = 2 or 4), nothing is read twice.
+// Units are numbered over all rows, so that no lane idles at a row's end, and
+// the next unit's loads are in flight while one is worked on.  Rows that do
+// not start at 16 bytes are read in the aligned pieces that hold their values,
+// shifted into place in registers.
 // ---------------------------------------------------------------------------
 constexpr int kWriteThreads = 256;
-constexpr int kUnits = 2;
+constexpr int kWriteBlocks = 3;  // per SM: 45.7 us for 60000 bf16 rows of 1152; 4 with fewer registers each: the same, but 164 us for 134 in fp32
 
-// Where entry `u` (row, block) reads and writes; false: nothing to do.
+
+// The 16 bytes from byte `m` (a multiple of the type's size, below 16) of two
+// consecutive pieces.
+template <typename TI>
+__device__ __forceinline__ uint4 shifted(const uint4& a, const uint4& b, uint32_t m) {
+  uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+  for (int i = 0; i < 6; ++i) w[i] = m & 8 ? w[i + 2] : w[i];
+#pragma unroll
+  for (int i = 0; i < 5; ++i) w[i] = m & 4 ? w[i + 1] : w[i];
+  if (sizeof(TI) == 2) {
+    const uint32_t sel = m & 2 ? 0x5432 : 0x3210;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __byte_perm(w[i], w[i + 1], sel);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// One unit on its way: where it goes and its raw values.
+template <int J>
 struct WriteUnit {
-  int64_t from, to;  // element of x, byte of q
-  int row_to, block;
+  uint4 raw[J];
+  int row, block, left;  // cache row (< 0: nothing to write), block, values from the block's start to the row's end
 };
 
-template <typename TI, bool E5, bool VEC>
-__global__ void __launch_bounds__(kWriteThreads) q8_write_kernel(const Q8WriteArgs a) {
+template <typename TI, bool E5, bool ALIGNED>
+__global__ void __launch_bounds__(kWriteThreads, kWriteBlocks) q8_write_kernel(const Q8WriteArgs a) {
   constexpr int V = Elem<TI>::kVec, J = 16 / V;
   pdl_entry();
   const int n = a.count ? min(max(*a.count, 0), a.n) : a.n;
@@ -38,90 +59,93 @@ __global__ void __launch_bounds__(kWriteThreads) q8_write_kernel(const Q8WriteAr
   const int64_t step = static_cast<int64_t>(gridDim.x) * (kWriteThreads / 8);
   const int64_t first = static_cast<int64_t>(blockIdx.x) * (kWriteThreads / 8) + (threadIdx.x >> 5) * 4;
   const TI* x = static_cast<const TI*>(a.x);
-  for (int64_t base = first; base < total; base += step * kUnits) {  // base: the warp's first unit
-    float v[kUnits][16];
-    int block[kUnits], row[kUnits];  // row < 0: nothing to write
-    bool whole[kUnits];
+  const auto fetch = [&](int64_t u) {
+    WriteUnit<J> w;
+    w.row = -1;
+    w.block = w.left = 0;
 #pragma unroll
-    for (int q = 0; q < kUnits; ++q) {
-      const int64_t u = base + q * step + (lane >> 3);
-      row[q] = -1;
-      block[q] = 0;
-      int64_t from = 0;
-      if (u < total) {
-        const int i = total <= 0xffffffffll ? static_cast<int>(static_cast<uint32_t>(u) / static_cast<uint32_t>(nb))
-                                            : static_cast<int>(u / nb);
-        block[q] = static_cast<int>(u - static_cast<int64_t>(i) * nb);
-        const int r = a.src ? __ldg(a.src + i) : i, d = a.dst ? __ldg(a.dst + i) : i;
-        if (r >= 0 && r < a.x_rows && d >= 0 && d < a.c.rows) {
-          row[q] = d;
-          from = r * a.x_stride + block[q] * kQ8Block;
-        }
-      }
-      whole[q] = VEC && (block[q] + 1) * kQ8Block <= width;
+    for (int j = 0; j < J; ++j) w.raw[j] = make_uint4(0u, 0u, 0u, 0u);
+    if (u >= total) return w;
+    const int i = total <= 0xffffffffll ? static_cast<int>(static_cast<uint32_t>(u) / static_cast<uint32_t>(nb))
+                                        : static_cast<int>(u / nb);
+    w.block = static_cast<int>(u - static_cast<int64_t>(i) * nb);
+    w.left = width - w.block * kQ8Block;
+    const int r = a.src ? __ldg(a.src + i) : i, d = a.dst ? __ldg(a.dst + i) : i;
+    if (r < 0 || r >= a.x_rows || d < 0 || d >= a.c.rows) return w;
+    w.row = d;
+    const TI* from = x + r * a.x_stride + w.block * kQ8Block;
+    if constexpr (ALIGNED) {
 #pragma unroll
-      for (int t = 0; t < 16; ++t) v[q][t] = 0.f;
-      if (row[q] < 0) continue;
-      if (whole[q]) {
+      for (int j = 0; j < J; ++j)
+        if (V * (l + 8 * j) < w.left) w.raw[j] = __ldg(reinterpret_cast<const uint4*>(from) + l + 8 * j);
+    } else {
+      const uint32_t m = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(from)) & 15u;
+      const uint4* base = reinterpret_cast<const uint4*>(reinterpret_cast<uintptr_t>(from) - m);
 #pragma unroll
-        for (int j = 0; j < J; ++j) {
-          const uint4 raw = __ldg(reinterpret_cast<const uint4*>(x + from) + l + 8 * j);
-          unpack_vec(raw, &v[q][V * j], static_cast<TI*>(nullptr));
-        }
-      } else {
-        // The row's last block, or rows that 16-byte loads cannot take.
-        const int left = width - block[q] * kQ8Block;
-#pragma unroll
-        for (int t = 0; t < 16; ++t)
-          if (l + 8 * t < left) v[q][t] = Elem<TI>::to_f(x[from + l + 8 * t]);
+      for (int j = 0; j < J; ++j) {
+        const int e = V * (l + 8 * j), head = V - static_cast<int>(m / sizeof(TI));  // values in the first piece
+        uint4 p = make_uint4(0u, 0u, 0u, 0u), q = p;
+        if (e < w.left) p = __ldg(base + l + 8 * j);
+        if (m && e + head < w.left) q = __ldg(base + l + 8 * j + 1);
+        w.raw[j] = shifted<TI>(p, q, m);
       }
     }
+    return w;
+  };
+  const auto store = [&](const WriteUnit<J>& u) {
+    float v[16];
 #pragma unroll
-    for (int q = 0; q < kUnits; ++q) {
-      uint32_t top = 0;
+    for (int j = 0; j < J; ++j) unpack_vec(u.raw[j], &v[V * j], static_cast<TI*>(nullptr));
+    if (u.left < kQ8Block) {  // what lies past the row's end counts for nothing
 #pragma unroll
-      for (int t = 0; t < 16; ++t) top = max(top, abs_bits(v[q][t]));
+      for (int t = 0; t < 16; ++t)
+        if (V * (l + 8 * (t / V)) + t % V >= u.left) v[t] = 0.f;
+    }
+    uint32_t top = 0;
 #pragma unroll
-      for (int o = 4; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-      const bool odd = top >= kNonFinite;  // the same for the block's 8 lanes
-      if (__any_sync(0xffffffffu, odd)) {
-        uint32_t fin = 0;
+    for (int t = 0; t < 16; ++t) top = max(top, abs_bits(v[t]));
 #pragma unroll
-        for (int t = 0; t < 16; ++t) fin = max(fin, abs_bits(v[q][t]) < kNonFinite ? abs_bits(v[q][t]) : 0u);
+    for (int o = 4; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const bool odd = top >= kNonFinite;  // the same for the block's 8 lanes
+    if (__any_sync(0xffffffffu, odd)) {
+      uint32_t fin = 0;
 #pragma unroll
-        for (int o = 4; o > 0; o >>= 1) fin = max(fin, __shfl_xor_sync(0xffffffffu, fin, o));
-        top = fin;
-      }
-      if (row[q] < 0) continue;
-      const int byte = scale_byte<E5>(top);
-      const float inv = scale_inverse(byte);
-      if (l == 0) a.c.scale[row[q] * a.c.scale_stride + block[q]] = static_cast<uint8_t>(byte);
-      uint8_t* out = a.c.q + row[q] * a.c.q_stride + block[q] * kQ8Block;
-      uint32_t w[4];
+      for (int t = 0; t < 16; ++t) fin = max(fin, abs_bits(v[t]) < kNonFinite ? abs_bits(v[t]) : 0u);
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
-        w[t] = encode2<E5>(v[q][4 * t] * inv, v[q][4 * t + 1] * inv) |
-               encode2<E5>(v[q][4 * t + 2] * inv, v[q][4 * t + 3] * inv) << 16;
-      if (odd) {
+      for (int o = 4; o > 0; o >>= 1) fin = max(fin, __shfl_xor_sync(0xffffffffu, fin, o));
+      top = fin;
+    }
+    if (u.row < 0) return;
+    const int byte = scale_byte<E5>(top);
+    const float inv = scale_inverse(byte);
+    if (l == 0) a.c.scale[u.row * a.c.scale_stride + u.block] = static_cast<uint8_t>(byte);
+    uint8_t* out = a.c.q + u.row * a.c.q_stride + u.block * kQ8Block;
+    uint32_t w[4];
 #pragma unroll
-        for (int t = 0; t < 16; ++t)
-          w[t >> 2] = (w[t >> 2] & ~(0xffu << 8 * (t & 3))) | encode_any<E5>(v[q][t] * inv) << 8 * (t & 3);
-      }
-      if (whole[q]) {
+    for (int t = 0; t < 4; ++t)
+      w[t] = encode2<E5>(v[4 * t] * inv, v[4 * t + 1] * inv) | encode2<E5>(v[4 * t + 2] * inv, v[4 * t + 3] * inv) << 16;
+    if (odd) {
 #pragma unroll
-        for (int j = 0; j < J; ++j) {
-          if constexpr (V == 8)
-            *reinterpret_cast<uint2*>(out + 8 * (l + 8 * j)) = make_uint2(w[2 * j], w[2 * j + 1]);
-          else
-            *reinterpret_cast<uint32_t*>(out + 4 * (l + 8 * j)) = w[j];
-        }
+      for (int t = 0; t < 16; ++t) w[t >> 2] += abs_bits(v[t]) == kNonFinite ? 1u << 8 * (t & 3) : 0u;
+    }
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const int e = V * (l + 8 * j);
+      if (e + V <= u.left) {
+        if constexpr (V == 8) *reinterpret_cast<uint2*>(out + e) = make_uint2(w[2 * j], w[2 * j + 1]);
+        else *reinterpret_cast<uint32_t*>(out + e) = w[j];
       } else {
-        const int left = width - block[q] * kQ8Block;
 #pragma unroll
-        for (int t = 0; t < 16; ++t)
-          if (l + 8 * t < left) out[l + 8 * t] = static_cast<uint8_t>(w[t >> 2] >> 8 * (t & 3));
+        for (int t = 0; t < V; ++t)
+          if (e + t < u.left) out[e + t] = static_cast<uint8_t>(w[(V * j + t) >> 2] >> 8 * (t & 3));
       }
     }
+  };
+  WriteUnit<J> next = fetch(first + (lane >> 3));
+  for (int64_t base = first; base < total; base += step) {  // base: the warp's first unit
+    const WriteUnit<J> now = next;
+    next = fetch(base + step + (lane >> 3));
+    store(now);
   }
 }
 
@@ -130,105 +154,142 @@ __global__ void __launch_bounds__(kWriteThreads) q8_write_kernel(const Q8WriteAr
 //   out_i = x_i + g * sum_p w_p h_p,   norm_p = ||h_p||
 // A warp per token, 8 values a lane and step: 8 cache bytes of each slot and
 // their scale byte, all slots' loads in flight before any arithmetic.  Where
-// the tokens are few, a block of 8 warps shares one token (SPLIT).
+// the tokens are few, the 8 warps of a block share one token.  The scale is a
+// power of two, so w x scale is exact and one multiply-add per value does for
+// both; squares are summed over a lane's 8 values before their scale.
 // ---------------------------------------------------------------------------
 constexpr int kCombineWarps = 8;
+constexpr int kLaneValues = 8;
 
-template <typename TI, bool E5, int KMAX, int CG, bool VEC, bool SPLIT>
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;"
+      : "=l"(reinterpret_cast<uint64_t&>(r))
+      : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)));
+  return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;"
+      : "=l"(reinterpret_cast<uint64_t&>(r))
+      : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)), "l"(reinterpret_cast<uint64_t&>(c)));
+  return r;
+}
+
+template <typename TI, bool E5, int KMAX, int CG>
 __global__ void __launch_bounds__(kCombineWarps * 32) q8_combine_kernel(const Q8CombineArgs a) {
-  constexpr int W = 8;  // values per lane and step
-  __shared__ float part[SPLIT ? kCombineWarps : 1][KMAX];
+  constexpr int W = kLaneValues, NV = W / Elem<TI>::kVec;
+  __shared__ float part[kCombineWarps][KMAX];
   pdl_entry();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int i = SPLIT ? blockIdx.x : blockIdx.x * kCombineWarps + warp;
-  if (i >= a.T) return;  // whole warps; a split block has one token
+  const int64_t i = a.split ? blockIdx.x : static_cast<int64_t>(blockIdx.x) * kCombineWarps + warp;
+  if (i >= a.T) return;  // whole warps; a shared token's block has all its warps
   const int k = a.k, width = a.c.width, chunks = (width + W - 1) / W;
   float w[KMAX], ss[KMAX];
-  const uint8_t *qp[KMAX], *sp[KMAX];  // null: the slot holds nothing
+  int row[KMAX];  // < 0: the slot holds nothing
 #pragma unroll
   for (int p = 0; p < KMAX; ++p) {
     w[p] = ss[p] = 0.f;
-    qp[p] = sp[p] = nullptr;
+    row[p] = -1;
     if (p < k) {
-      const int64_t at = static_cast<int64_t>(i) * k + p;
-      const int r = a.rows ? __ldg(a.rows + at) : i;
+      const int64_t at = i * k + p;
+      const int r = a.rows ? __ldg(a.rows + at) : static_cast<int>(i);
       if (r >= 0 && r < a.c.rows) {
+        row[p] = r;
         w[p] = a.weights ? __ldg(a.weights + at) : 1.f;
-        qp[p] = a.c.q + r * a.c.q_stride;
-        sp[p] = a.c.scale + r * a.c.scale_stride;
       }
     }
   }
   const TI* x = a.x ? static_cast<const TI*>(a.x) + i * a.x_stride : nullptr;
   TI* out = static_cast<TI*>(a.out) + i * a.out_stride;
   const float* gate = a.gate ? a.gate + (i / a.seq) * a.gate_stride : nullptr;
-  const int c_first = SPLIT ? warp * 32 * CG : 0, c_step = (SPLIT ? kCombineWarps : 1) * 32 * CG;
-  for (int c0 = c_first; c0 < chunks; c0 += c_step) {
+  const int c_step = (a.split ? kCombineWarps : 1) * 32 * CG;
+  for (int c0 = (a.split ? warp * 32 * CG : 0) + lane; c0 < chunks; c0 += c_step) {
     uint2 h[CG][KMAX];
     uint8_t sc[CG][KMAX];
-    float xv[CG][W];
+    uint4 xr[CG][NV];
+    float xs[CG][W];
 #pragma unroll
     for (int g = 0; g < CG; ++g) {
-      const int c = c0 + g * 32 + lane;
-      if (c >= chunks) continue;
+      const int c = c0 + g * 32;
 #pragma unroll
       for (int p = 0; p < KMAX; ++p) {
         h[g][p] = make_uint2(0u, 0u);
         sc[g][p] = 127;
-        if (qp[p]) {
-          h[g][p] = *reinterpret_cast<const uint2*>(qp[p] + c * W);
-          sc[g][p] = sp[p][c >> 4];
+        if (c < chunks && row[p] >= 0) {
+          h[g][p] = __ldg(reinterpret_cast<const uint2*>(a.c.q + row[p] * a.c.q_stride + c * W));
+          sc[g][p] = __ldg(a.c.scale + row[p] * a.c.scale_stride + (c >> 4));
         }
       }
-      if (x) {
-        if (VEC && (c + 1) * W <= width) {
+      if (x && c < chunks) {
+        if (a.vec && (c + 1) * W <= width) {
 #pragma unroll
-          for (int j = 0; j < W / Elem<TI>::kVec; ++j) load_vec(x + c * W + j * Elem<TI>::kVec, &xv[g][j * Elem<TI>::kVec]);
+          for (int j = 0; j < NV; ++j) xr[g][j] = *(reinterpret_cast<const uint4*>(x + c * W) + j);
+#pragma unroll
+          for (int j = 0; j < NV; ++j) unpack_vec(xr[g][j], &xs[g][j * Elem<TI>::kVec], static_cast<TI*>(nullptr));
         } else {
 #pragma unroll
-          for (int t = 0; t < W; ++t) xv[g][t] = c * W + t < width ? Elem<TI>::to_f(x[c * W + t]) : 0.f;
+          for (int t = 0; t < W; ++t) xs[g][t] = c * W + t < width ? Elem<TI>::to_f(x[c * W + t]) : 0.f;
         }
       }
     }
 #pragma unroll
     for (int g = 0; g < CG; ++g) {
-      const int c = c0 + g * 32 + lane;
+      const int c = c0 + g * 32, live = width - c * W;
       if (c >= chunks) continue;
-      const int live = min(W, width - c * W);
-      float y[W];
+      if (live < W) {  // the bytes past the row's width are anything
+#pragma unroll
+        for (int p = 0; p < KMAX; ++p) {
+          h[g][p].x &= live >= 4 ? 0xffffffffu : (1u << 8 * live) - 1;
+          h[g][p].y &= live <= 4 ? 0u : (1u << 8 * (live - 4)) - 1;
+        }
+      }
+      float2 y[W / 2];
 #pragma unroll
       for (int p = 0; p < KMAX; ++p) {
         if (p >= k) continue;
-        const float f = scale_value(sc[g][p]);
-        float hv[W];
+        const float f = scale_value(sc[g][p]), wf = w[p] * f;
+        float2 d[W / 2], sq;
 #pragma unroll
-        for (int t = 0; t < W; t += 2) {
-          const float2 d = decode2<E5>(((t < 4 ? h[g][p].x : h[g][p].y) >> (t & 2 ? 16 : 0)) & 0xffffu);
-          hv[t] = t < live ? d.x * f : 0.f;
-          hv[t + 1] = t + 1 < live ? d.y * f : 0.f;
-        }
+        for (int t = 0; t < W / 2; ++t) d[t] = decode2<E5>((t < 2 ? h[g][p].x : h[g][p].y) >> (t & 1 ? 16 : 0) & 0xffffu);
+        const float2 wf2 = make_float2(wf, wf);
 #pragma unroll
-        for (int t = 0; t < W; ++t) {
-          y[t] = p == 0 ? w[0] * hv[t] : fmaf(w[p], hv[t], y[t]);
-          ss[p] = fmaf(hv[t], hv[t], ss[p]);
+        for (int t = 0; t < W / 2; ++t) y[t] = p == 0 ? mul2(wf2, d[t]) : fma2(wf2, d[t], y[t]);
+        if (a.norms) {
+          sq = mul2(d[0], d[0]);
+#pragma unroll
+          for (int t = 1; t < W / 2; ++t) sq = fma2(d[t], d[t], sq);
+          ss[p] = fmaf(f * (sq.x + sq.y), f, ss[p]);
         }
+      }
+      float o[W];
+#pragma unroll
+      for (int t = 0; t < W / 2; ++t) {
+        o[2 * t] = y[t].x;
+        o[2 * t + 1] = y[t].y;
       }
       if (gate) {
         const float* gp = gate + c * W;
+        if (a.gate_vec && live >= W) {
+          const float4 g0 = __ldg(reinterpret_cast<const float4*>(gp)), g1 = __ldg(reinterpret_cast<const float4*>(gp) + 1);
+          o[0] *= g0.x; o[1] *= g0.y; o[2] *= g0.z; o[3] *= g0.w;
+          o[4] *= g1.x; o[5] *= g1.y; o[6] *= g1.z; o[7] *= g1.w;
+        } else {
 #pragma unroll
-        for (int t = 0; t < W; ++t) y[t] *= t < live ? __ldg(gp + t) : 0.f;
+          for (int t = 0; t < W; ++t) o[t] *= t < live ? __ldg(gp + t) : 0.f;
+        }
       }
       if (x) {
 #pragma unroll
-        for (int t = 0; t < W; ++t) y[t] += xv[g][t];
+        for (int t = 0; t < W; ++t) o[t] += xs[g][t];
       }
-      if (VEC && live == W) {
+      if (a.vec && live >= W) {
 #pragma unroll
-        for (int j = 0; j < W / Elem<TI>::kVec; ++j) store_vec(out + c * W + j * Elem<TI>::kVec, &y[j * Elem<TI>::kVec]);
+        for (int j = 0; j < NV; ++j) store_vec(out + c * W + j * Elem<TI>::kVec, &o[j * Elem<TI>::kVec]);
       } else {
 #pragma unroll
         for (int t = 0; t < W; ++t)
-          if (t < live) out[c * W + t] = Elem<TI>::from_f(y[t]);
+          if (t < live) out[c * W + t] = Elem<TI>::from_f(o[t]);
       }
     }
   }
@@ -237,18 +298,199 @@ __global__ void __launch_bounds__(kCombineWarps * 32) q8_combine_kernel(const Q8
   for (int p = 0; p < KMAX; ++p) {
     if (p >= k) continue;
     const float s = warp_sum(ss[p]);
-    if constexpr (SPLIT) {
-      if (lane == 0) part[warp][p] = s;
-    } else if (lane == 0) {
-      a.norms[static_cast<int64_t>(i) * k + p] = sqrtf(s);
+    if (lane == 0) {
+      if (a.split) part[warp][p] = s;
+      else a.norms[i * k + p] = sqrtf(s);
     }
   }
-  if constexpr (SPLIT) {
+  if (a.split) {
     __syncthreads();
     if (threadIdx.x < k) {
       float s = 0.f;
       for (int q = 0; q < kCombineWarps; ++q) s += part[q][threadIdx.x];
-      a.norms[static_cast<int64_t>(i) * k + threadIdx.x] = sqrtf(s);
+      a.norms[i * k + threadIdx.x] = sqrtf(s);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// The same for many tokens, staged: a warp walks its tokens i = w, w + W, ...
+// (W the grid's warps), each brought into its buffer in shared memory by
+// asynchronous copies (16 bytes at a time for the live cache rows and x, 4 for
+// the scales), so that the bytes in flight do not hang on registers, and the
+// next token's copies start as soon as the last one's values are used.  Its
+// row list was loaded a token before.  One buffer per warp: twice the warps
+// hide more of the arithmetic's latency than a second buffer (decoding costs
+// 3.5 clocks a value and warp, as much as HBM takes for 8 slots).
+// ---------------------------------------------------------------------------
+constexpr int kStageWarps = 4;
+constexpr int kStageBlocks = 8;            // per SM at most
+constexpr int kStageSm = 227 * 1024, kStageMax = 112 * 1024;  // shared memory of an SM, and the most a block takes
+
+// Bytes of a token's buffer: slots' rows, x, slots' scales, slots' weights.
+struct StageLayout {
+  int row, x, scale_words, x_at, scale_at, weight_at, bytes;
+};
+__host__ __device__ inline StageLayout stage_layout(int k, int width, int x_size) {
+  StageLayout s;
+  s.row = (width + 15) / 16 * 16;
+  s.x = (width * x_size + 15) / 16 * 16;
+  s.scale_words = ((width + kQ8Block - 1) / kQ8Block + 3) / 4;
+  s.x_at = k * s.row;
+  s.scale_at = s.x_at + s.x;
+  s.weight_at = s.scale_at + k * s.scale_words * 4;
+  s.bytes = (s.weight_at + k * 4 + 15) / 16 * 16;
+  return s;
+}
+
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+
+template <typename TI, bool E5, int KMAX>
+__global__ void __launch_bounds__(kStageWarps * 32) q8_combine_staged_kernel(const Q8CombineArgs a) {
+  constexpr int W = kLaneValues, NV = W / Elem<TI>::kVec;
+  extern __shared__ __align__(16) uint8_t dyn[];
+  pdl_entry();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int k = a.k, width = a.c.width, chunks = (width + W - 1) / W;
+  const StageLayout L = stage_layout(k, width, a.x ? sizeof(TI) : 0);
+  uint8_t* const buf = dyn + static_cast<size_t>(warp) * L.bytes;
+  const int64_t w0 = static_cast<int64_t>(blockIdx.x) * kStageWarps + warp, step = static_cast<int64_t>(gridDim.x) * kStageWarps;
+  const TI* x = static_cast<const TI*>(a.x);
+
+  // Lane p holds slot p's row (-1: nothing) and weight of the next token to fetch.
+  int row = -1;
+  float weight = 0.f;
+  const auto look_up = [&](int64_t i) {
+    row = -1;
+    weight = 0.f;
+    if (i < a.T && lane < k) {
+      const int r = a.rows ? __ldg(a.rows + i * k + lane) : static_cast<int>(i);
+      if (r >= 0 && r < a.c.rows) {
+        row = r;
+        weight = a.weights ? __ldg(a.weights + i * k + lane) : 1.f;
+      }
+    }
+  };
+  // Start token i's copies.  A slot that holds nothing copies nothing.
+  const auto fetch = [&](int64_t i) {
+    const uint32_t to = smem_u32(buf);
+    if (i < a.T) {
+      for (int p = 0; p < k; ++p) {
+        const int r = __shfl_sync(0xffffffffu, row, p);
+        if (r < 0) continue;
+        const uint8_t* q = a.c.q + r * a.c.q_stride;
+        for (int c = lane * 16; c < L.row; c += 512) copy16(to + p * L.row + c, q + c);
+        const uint8_t* sc = a.c.scale + r * a.c.scale_stride;
+        for (int c = lane; c < L.scale_words; c += 32) copy4(to + L.scale_at + (p * L.scale_words + c) * 4, sc + c * 4);
+      }
+      if (x) {
+        const uint8_t* xr = reinterpret_cast<const uint8_t*>(x + i * a.x_stride);
+        for (int c = lane * 16; c < L.x; c += 512) copy16(to + L.x_at + c, xr + c);
+      }
+      if (lane < k) *reinterpret_cast<float*>(buf + L.weight_at + lane * 4) = weight;
+    }
+  };
+
+  look_up(w0);
+  uint32_t slots = __ballot_sync(0xffffffffu, row >= 0);  // bit p: slot p of the token in the buffer holds a row
+  fetch(w0);
+  look_up(w0 + step);
+  for (int64_t i = w0; i < a.T; i += step) {
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncwarp();
+    TI* out = static_cast<TI*>(a.out) + i * a.out_stride;
+    const float* gate = a.gate ? a.gate + (i / a.seq) * a.gate_stride : nullptr;
+    float ss[KMAX], w[KMAX];
+#pragma unroll
+    for (int p = 0; p < KMAX; ++p) {
+      ss[p] = 0.f;
+      w[p] = p < k ? *reinterpret_cast<const float*>(buf + L.weight_at + p * 4) : 0.f;
+    }
+    for (int c = lane; c < chunks; c += 32) {
+      const int left = width - c * W;
+      // Without branches, so that the slots' chains interleave: a slot that
+      // holds nothing (or is not there) counts as zeros of scale 1.
+      uint2 h[KMAX];
+      float f[KMAX];
+#pragma unroll
+      for (int p = 0; p < KMAX; ++p) {
+        const bool on = slots >> p & 1;
+        const uint2 raw = *reinterpret_cast<const uint2*>(buf + (p < k ? p : 0) * L.row + c * W);
+        const uint32_t byte = buf[L.scale_at + (p < k ? p : 0) * L.scale_words * 4 + (c >> 4)];
+        h[p] = make_uint2(on ? raw.x : 0u, on ? raw.y : 0u);
+        f[p] = scale_value(on ? byte : 127u);
+      }
+      if (left < W) {  // the bytes past the row's width are anything
+#pragma unroll
+        for (int p = 0; p < KMAX; ++p) {
+          h[p].x &= left >= 4 ? 0xffffffffu : (1u << 8 * left) - 1;
+          h[p].y &= left <= 4 ? 0u : (1u << 8 * (left - 4)) - 1;
+        }
+      }
+      float2 y[W / 2];
+#pragma unroll
+      for (int p = 0; p < KMAX; ++p) {
+        float2 d[W / 2];
+#pragma unroll
+        for (int t = 0; t < W / 2; ++t) d[t] = decode2<E5>((t < 2 ? h[p].x : h[p].y) >> (t & 1 ? 16 : 0) & 0xffffu);
+        const float wf = w[p] * f[p];
+        const float2 wf2 = make_float2(wf, wf);
+#pragma unroll
+        for (int t = 0; t < W / 2; ++t) y[t] = p == 0 ? mul2(wf2, d[t]) : fma2(wf2, d[t], y[t]);
+        float2 sq = mul2(d[0], d[0]);
+#pragma unroll
+        for (int t = 1; t < W / 2; ++t) sq = fma2(d[t], d[t], sq);
+        ss[p] = fmaf(f[p] * (sq.x + sq.y), f[p], ss[p]);
+      }
+      float o[W];
+#pragma unroll
+      for (int t = 0; t < W / 2; ++t) {
+        o[2 * t] = y[t].x;
+        o[2 * t + 1] = y[t].y;
+      }
+      if (gate) {
+        const float* gp = gate + c * W;
+        if (a.gate_vec && left >= W) {
+          const float4 g0 = __ldg(reinterpret_cast<const float4*>(gp)), g1 = __ldg(reinterpret_cast<const float4*>(gp) + 1);
+          o[0] *= g0.x; o[1] *= g0.y; o[2] *= g0.z; o[3] *= g0.w;
+          o[4] *= g1.x; o[5] *= g1.y; o[6] *= g1.z; o[7] *= g1.w;
+        } else {
+#pragma unroll
+          for (int t = 0; t < W; ++t) o[t] *= t < left ? __ldg(gp + t) : 0.f;
+        }
+      }
+      if (x) {
+        float xs[W];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) load_vec(reinterpret_cast<const TI*>(buf + L.x_at) + c * W + j * Elem<TI>::kVec, &xs[j * Elem<TI>::kVec]);
+#pragma unroll
+        for (int t = 0; t < W; ++t) o[t] += xs[t];
+      }
+      if (left >= W) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) store_vec(out + c * W + j * Elem<TI>::kVec, &o[j * Elem<TI>::kVec]);
+      } else {
+#pragma unroll
+        for (int t = 0; t < W; ++t)
+          if (t < left) out[c * W + t] = Elem<TI>::from_f(o[t]);
+      }
+    }
+    __syncwarp();  // all have read the buffer
+    slots = __ballot_sync(0xffffffffu, row >= 0);
+    fetch(i + step);
+    look_up(i + 2 * step);
+    if (a.norms) {
+#pragma unroll
+      for (int p = 0; p < KMAX; ++p) {
+        if (p >= k) continue;
+        const float s = warp_sum(ss[p]);
+        if (lane == 0) a.norms[i * k + p] = sqrtf(s);
+      }
     }
   }
 }
@@ -263,8 +505,8 @@ cudaError_t launch_q8_write(const Q8WriteArgs& a, bool bf16, bool e5, cudaStream
   if (a.n <= 0) return cudaSuccess;
   const bool vec = aligned16(a.x, a.x_stride * (bf16 ? 2 : 4));
   const int64_t units = static_cast<int64_t>(a.n) * ((a.c.width + kQ8Block - 1) / kQ8Block);
-  constexpr int64_t per_block = kWriteThreads / 8 * kUnits;
-  const dim3 grid(static_cast<unsigned>(std::min<int64_t>((units + per_block - 1) / per_block, 152 * 8)));
+  constexpr int64_t per_block = kWriteThreads / 8;
+  const dim3 grid(static_cast<unsigned>(std::min<int64_t>((units + per_block - 1) / per_block, 152 * kWriteBlocks)));
   auto run = [&](auto kern) { return launch_pdl(kern, grid, dim3(kWriteThreads), 0, s, a); };
   auto pick = [&](auto t) {
     using TI = decltype(t);
@@ -276,26 +518,36 @@ cudaError_t launch_q8_write(const Q8WriteArgs& a, bool bf16, bool e5, cudaStream
 
 namespace {
 
-template <typename TI, bool E5, int KMAX, int CG>
-cudaError_t run_combine(const Q8CombineArgs& a, bool vec, bool split, cudaStream_t s) {
-  const dim3 grid(split ? a.T : (a.T + kCombineWarps - 1) / kCombineWarps), block(kCombineWarps * 32);
-  if (split)
-    return vec ? launch_pdl(q8_combine_kernel<TI, E5, KMAX, 1, true, true>, grid, block, 0, s, a)
-               : launch_pdl(q8_combine_kernel<TI, E5, KMAX, 1, false, true>, grid, block, 0, s, a);
-  return vec ? launch_pdl(q8_combine_kernel<TI, E5, KMAX, CG, true, false>, grid, block, 0, s, a)
-             : launch_pdl(q8_combine_kernel<TI, E5, KMAX, CG, false, false>, grid, block, 0, s, a);
-}
-
 template <typename TI, bool E5>
-cudaError_t combine_slots(const Q8CombineArgs& a, cudaStream_t s) {
+cudaError_t combine_slots(Q8CombineArgs a, cudaStream_t s) {
   constexpr int size = sizeof(TI);
-  const bool vec = aligned16(a.out, a.out_stride * size) && (!a.x || aligned16(a.x, a.x_stride * size));
-  const bool split = a.T < 152 * 2;
-  if (a.k == 1) return run_combine<TI, E5, 1, 4>(a, vec, split, s);
-  if (a.k == 2) return run_combine<TI, E5, 2, 3>(a, vec, split, s);
-  if (a.k <= 4) return run_combine<TI, E5, 4, 2>(a, vec, split, s);
-  if (a.k <= 8) return run_combine<TI, E5, 8, 1>(a, vec, split, s);
-  return run_combine<TI, E5, 16, 1>(a, vec, split, s);
+  a.vec = aligned16(a.out, a.out_stride * size) && (!a.x || aligned16(a.x, a.x_stride * size));
+  a.gate_vec = a.gate && aligned16(a.gate, a.gate_stride * 4);
+  a.split = a.T < 152 * 2;
+  // Staged from two tokens per warp slot of the GPU on, where 16-byte copies can take the rows and four warps'
+  // buffers fit a block.
+  const int smem = kStageWarps * stage_layout(a.k, a.c.width, a.x ? size : 0).bytes;
+  if (!a.split && a.vec && smem <= kStageMax) {
+    const auto staged = [&](auto kern) {
+      const cudaError_t e = set_dyn_smem_on_device(reinterpret_cast<const void*>(kern), kStageMax);
+      if (e != cudaSuccess) return e;
+      const int per_sm = std::max(1, std::min(kStageSm / (smem + 1024), kStageBlocks));
+      return launch_pdl(kern, dim3(std::min((a.T + kStageWarps - 1) / kStageWarps, 152 * per_sm)), dim3(kStageWarps * 32), smem, s, a);
+    };
+    if (a.k == 1) return staged(q8_combine_staged_kernel<TI, E5, 1>);
+    if (a.k == 2) return staged(q8_combine_staged_kernel<TI, E5, 2>);
+    if (a.k == 3) return staged(q8_combine_staged_kernel<TI, E5, 3>);
+    if (a.k == 4) return staged(q8_combine_staged_kernel<TI, E5, 4>);
+    if (a.k <= 6) return staged(q8_combine_staged_kernel<TI, E5, 6>);
+    if (a.k <= 9) return staged(q8_combine_staged_kernel<TI, E5, 9>);
+    return staged(q8_combine_staged_kernel<TI, E5, 16>);
+  }
+  const dim3 grid(a.split ? a.T : (a.T + kCombineWarps - 1) / kCombineWarps), block(kCombineWarps * 32);
+  if (a.k == 1) return launch_pdl(q8_combine_kernel<TI, E5, 1, 4>, grid, block, 0, s, a);
+  if (a.k == 2) return launch_pdl(q8_combine_kernel<TI, E5, 2, 2>, grid, block, 0, s, a);
+  if (a.k <= 4) return launch_pdl(q8_combine_kernel<TI, E5, 4, 2>, grid, block, 0, s, a);
+  if (a.k <= 8) return launch_pdl(q8_combine_kernel<TI, E5, 8, 1>, grid, block, 0, s, a);
+  return launch_pdl(q8_combine_kernel<TI, E5, 16, 1>, grid, block, 0, s, a);
 }
 
 }  // namespace

@@ -43,23 +43,16 @@ __device__ __forceinline__ int scale_byte(uint32_t a) {
 __device__ __forceinline__ float scale_inverse(int byte) { return __uint_as_float(static_cast<uint32_t>(254 - byte) << 23); }
 // The scale: 2^(byte - 127); 2^-127 is subnormal, 255 is NaN.
 __device__ __forceinline__ float scale_value(uint32_t byte) {
-  const uint32_t b = byte == 0 ? 0x400000u : byte << 23;
-  return __uint_as_float(byte == 255 ? 0x7fffffffu : b);
+  return __uint_as_float(max(byte << 23, 0x400000u) + (byte == 255));
 }
 
 // Two values (already divided by the scale) in 8 bits, the first in the low byte.
-// Finite values that the scale brings in range; see encode_any for others.
+// NaN becomes NaN.  An infinity is taken for the largest value, 0x7b in e5m2 (one
+// below infinity) and 0x7e in e4m3 (one below NaN): a caller that may have met
+// one adds 1 to its byte, which is right in both.
 template <bool E5>
 __device__ __forceinline__ uint32_t encode2(float lo, float hi) {
   return __nv_cvt_float2_to_fp8x2(make_float2(lo, hi), __NV_SATFINITE, E5 ? __NV_E5M2 : __NV_E4M3);
-}
-// One value that may be infinite or NaN.
-template <bool E5>
-__device__ __forceinline__ uint32_t encode_any(float v) {
-  const uint32_t sign = (__float_as_uint(v) >> 24) & 0x80u;
-  if (abs_bits(v) > kNonFinite) return 0x7fu;
-  if (abs_bits(v) == kNonFinite) return E5 ? (sign | 0x7cu) : 0x7fu;
-  return encode2<E5>(v, 0.f) & 0xffu;
 }
 
 // Two bytes as two floats (every e4m3 / e5m2 value is an fp16 value).
@@ -90,6 +83,7 @@ struct Q8CombineArgs {
   int64_t out_stride;
   float* norms;
   int T, k, seq;
+  bool vec, gate_vec, split;  // set at the launch: 16-byte accesses of x and out, of the gate; a block per token
 };
 cudaError_t launch_q8_combine(const Q8CombineArgs& a, bool bf16, bool e5, cudaStream_t s);
 

@@ -358,8 +358,7 @@ __device__ __forceinline__ void store_chunk(const MatmulParams& p, Shared& sh, f
       word[t] = encode2<E5>(z[4 * t], z[4 * t + 1]) | encode2<E5>(z[4 * t + 2], z[4 * t + 3]) << 16;
     }
     if (odd) {
-      // The conversion takes infinities for the largest value, 0x7b in e5m2 (one
-      // below infinity) and 0x7e in e4m3 (one below NaN): one more is right in both.
+      // Infinities (see encode2).
 #pragma unroll
       for (int t = 0; t < 32; ++t) word[t >> 2] += abs_bits(z[t]) == kNonFinite ? 1u << 8 * (t & 3) : 0u;
     }
