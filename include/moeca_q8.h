@@ -79,6 +79,7 @@ typedef struct {
   int32_t dtype;         /* moeca_dtype of out                                        */
   int32_t n;             /* rows of out, >= 0; without a list at most cache.rows      */
   const int32_t* rows;   /* [n] rows of the cache, or NULL: i                         */
+  int32_t* status;       /* as in moeca_q8_matmul_args                                */
 } moeca_q8_read_args;
 moeca_status moeca_q8_read(const moeca_q8_read_args* args, void* stream);
 
@@ -104,6 +105,7 @@ typedef struct {
   int32_t n_tokens;      /* >= 0                                                      */
   int32_t n_slots;       /* 1 .. 16                                                   */
   int32_t seq;           /* tokens per gate row, >= 1 (with a gate)                   */
+  int32_t* status;       /* as in moeca_q8_matmul_args                                */
 } moeca_q8_combine_args;
 moeca_status moeca_q8_combine(const moeca_q8_combine_args* args, void* stream);
 

@@ -21,7 +21,7 @@ LIB = os.path.join(PKG, "libmoeca.so")
 
 SOURCES = ["moeca_api.cu", "router.cu", "select.cu", "prep.cu", "ffn_simt.cu", "ffn_tc.cu", "combine.cu",
            "proj_tc.cu", "attention.cu", "attn_tc.cu", "prep_attn.cu", "prep_shard.cu", "adaln.cu", "q8.cu",
-           "q8_matmul.cu", "probe.cu"]
+           "q8_combine.cu", "q8_combine_f32.cu", "q8_matmul.cu", "probe.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-std=c++20", "-lineinfo", "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC]
 

@@ -62,6 +62,28 @@ __device__ __forceinline__ float2 decode2(uint32_t pair) {
   return __half22float2(*reinterpret_cast<const __half2*>(&h));
 }
 
+// The 16 bytes from byte `m` (a multiple of the type's size, below 16) of two
+// consecutive 16-byte pieces.
+template <typename TI>
+__device__ __forceinline__ uint4 shifted(const uint4& a, const uint4& b, uint32_t m) {
+  uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+  for (int i = 0; i < 6; ++i) w[i] = m & 8 ? w[i + 2] : w[i];
+#pragma unroll
+  for (int i = 0; i < 5; ++i) w[i] = m & 4 ? w[i + 1] : w[i];
+  if (sizeof(TI) == 2) {
+    const uint32_t sel = m & 2 ? 0x5432 : 0x3210;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __byte_perm(w[i], w[i + 1], sel);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Whether 16-byte accesses can take rows of this base and stride.
+inline bool q8_aligned16(const void* p, int64_t stride_bytes) {
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride_bytes % 16 == 0;
+}
+
 struct Q8WriteArgs {
   Q8Rows c;
   const void* x;
@@ -82,10 +104,12 @@ struct Q8CombineArgs {
   void* out;
   int64_t out_stride;
   float* norms;
+  int32_t* status;
   int T, k, seq;
   bool vec, gate_vec, split;  // set at the launch: 16-byte accesses of x and out, of the gate; a block per token
 };
-cudaError_t launch_q8_combine(const Q8CombineArgs& a, bool bf16, bool e5, cudaStream_t s);
+cudaError_t launch_q8_combine_bf16(const Q8CombineArgs& a, bool e5, cudaStream_t s);
+cudaError_t launch_q8_combine_f32(const Q8CombineArgs& a, bool e5, cudaStream_t s);
 
 struct Q8MatmulArgs {
   Q8Rows a, b, out;

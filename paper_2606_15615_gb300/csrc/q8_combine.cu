@@ -1,0 +1,463 @@
+// Eq. 8 over an 8-bit branch cache, and the cache read back as it is (one
+// slot, no weights, no residual) (include/moeca_q8.h):
+//   out_i = x_i + g * sum_p w_p h_p,   norm_p = ||h_p||
+// The scale of a block is a power of two, so w x scale is exact and one
+// multiply-add per value does for both; squares are summed over a lane's 8
+// values of a block before their scale.  Two values go through one packed
+// fp32 instruction.  Compiled twice: bf16 rows here, fp32 rows in
+// q8_combine_f32.cu.
+#include <algorithm>
+
+#include "common.cuh"
+#include "kernels.h"
+#include "q8.cuh"
+
+namespace moeca {
+namespace {
+
+#ifdef MOECA_Q8_COMBINE_F32
+using TI = float;
+#else
+using TI = __nv_bfloat16;
+#endif
+
+constexpr int W = 8;                      // values per lane and step
+constexpr int V = Elem<TI>::kVec, NV = W / V;
+
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;"
+      : "=l"(reinterpret_cast<uint64_t&>(r))
+      : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)));
+  return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;"
+      : "=l"(reinterpret_cast<uint64_t&>(r))
+      : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)), "l"(reinterpret_cast<uint64_t&>(c)));
+  return r;
+}
+
+// Eight cache bytes as floats, without their scale.  An e5m2 byte is the upper
+// byte of an fp16 value.
+template <bool E5>
+__device__ __forceinline__ void decode8(const uint2& h, float2 (&d)[4]) {
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    const uint32_t word = t < 2 ? h.x : h.y;
+    if constexpr (E5) {
+      const uint32_t two = __byte_perm(word, 0u, t & 1 ? 0x3424 : 0x1404);
+      d[t] = __half22float2(*reinterpret_cast<const __half2*>(&two));
+    } else {
+      d[t] = decode2<E5>(t & 1 ? word >> 16 : word & 0xffffu);
+    }
+  }
+}
+
+// y (+)= w f h and the square sum of the 8 values times f^2.
+template <bool FIRST>
+__device__ __forceinline__ float slot_values(const float2 (&d)[4], float f, float wf, float2 (&y)[4], float ss) {
+  const float2 wf2 = make_float2(wf, wf);
+#pragma unroll
+  for (int t = 0; t < 4; ++t) y[t] = FIRST ? mul2(wf2, d[t]) : fma2(wf2, d[t], y[t]);
+  float2 sq = mul2(d[0], d[0]);
+#pragma unroll
+  for (int t = 1; t < 4; ++t) sq = fma2(d[t], d[t], sq);
+  return fmaf(f * (sq.x + sq.y), f, ss);
+}
+
+// The sum of K values over the warp's lanes, value p in lane p's result: each
+// step hands over half of the values that a lane still holds.
+template <int K>
+__device__ __forceinline__ float warp_sums(const float (&s)[K], int lane) {
+  constexpr int P = K <= 1 ? 1 : K <= 2 ? 2 : K <= 4 ? 4 : K <= 8 ? 8 : 16;
+  float v[P];
+#pragma unroll
+  for (int p = 0; p < P; ++p) v[p] = p < K ? s[p] : 0.f;
+#pragma unroll
+  for (int n = P / 2; n > 0; n >>= 1) {  // lanes that differ in bit n of their number
+    const bool up = lane & n;
+#pragma unroll
+    for (int j = 0; j < n; ++j) {
+      const float keep = up ? v[j + n] : v[j], give = up ? v[j] : v[j + n];
+      v[j] = keep + __shfl_xor_sync(0xffffffffu, give, n);
+    }
+  }
+#pragma unroll
+  for (int o = P; o < 32; o <<= 1) v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+  return v[0];
+}
+
+__device__ __forceinline__ void apply_gate(const float* gp, bool vec, int left, float (&o)[W]) {
+  if (vec && left >= W) {
+    const float4 g0 = __ldg(reinterpret_cast<const float4*>(gp)), g1 = __ldg(reinterpret_cast<const float4*>(gp) + 1);
+    o[0] *= g0.x; o[1] *= g0.y; o[2] *= g0.z; o[3] *= g0.w;
+    o[4] *= g1.x; o[5] *= g1.y; o[6] *= g1.z; o[7] *= g1.w;
+  } else {
+#pragma unroll
+    for (int t = 0; t < W; ++t) o[t] *= t < left ? __ldg(gp + t) : 0.f;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Direct form: few tokens (the 8 warps of a block share one), and rows too wide
+// for the staged form (a warp per token).  All slots' loads are in flight
+// before any arithmetic.
+// ---------------------------------------------------------------------------
+constexpr int kDirectWarps = 8;
+
+template <bool E5, int KMAX>
+__global__ void __launch_bounds__(kDirectWarps * 32) q8_combine_kernel(const Q8CombineArgs a) {
+  __shared__ float part[kDirectWarps][KMAX];
+  pdl_entry();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t i = a.split ? blockIdx.x : static_cast<int64_t>(blockIdx.x) * kDirectWarps + warp;
+  if (i >= a.T) return;  // whole warps; a shared token's block has all its warps
+  const int k = a.k, width = a.c.width, chunks = (width + W - 1) / W;
+  float w[KMAX], ss[KMAX];
+  int row[KMAX];  // < 0: the slot holds nothing
+#pragma unroll
+  for (int p = 0; p < KMAX; ++p) {
+    w[p] = ss[p] = 0.f;
+    row[p] = -1;
+    if (p < k) {
+      const int64_t at = i * k + p;
+      const int r = a.rows ? __ldg(a.rows + at) : static_cast<int>(i);
+      if (r >= 0 && r < a.c.rows) {
+        row[p] = r;
+        w[p] = a.weights ? __ldg(a.weights + at) : 1.f;
+      }
+    }
+  }
+  const TI* x = a.x ? static_cast<const TI*>(a.x) + i * a.x_stride : nullptr;
+  TI* out = static_cast<TI*>(a.out) + i * a.out_stride;
+  const float* gate = a.gate ? a.gate + (i / a.seq) * a.gate_stride : nullptr;
+  for (int c = (a.split ? warp * 32 : 0) + lane; c < chunks; c += (a.split ? kDirectWarps : 1) * 32) {
+    const int left = width - c * W;
+    uint2 h[KMAX];
+    float f[KMAX], xs[W];
+#pragma unroll
+    for (int p = 0; p < KMAX; ++p) {
+      h[p] = make_uint2(0u, 0u);
+      f[p] = 1.f;
+      if (row[p] >= 0) {
+        h[p] = __ldg(reinterpret_cast<const uint2*>(a.c.q + row[p] * a.c.q_stride + c * W));
+        f[p] = scale_value(__ldg(a.c.scale + row[p] * a.c.scale_stride + (c >> 4)));
+      }
+    }
+    if (x) {
+      if (a.vec && left >= W) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) load_vec(x + c * W + j * V, &xs[j * V]);
+      } else {
+#pragma unroll
+        for (int t = 0; t < W; ++t) xs[t] = t < left ? Elem<TI>::to_f(x[c * W + t]) : 0.f;
+      }
+    }
+    if (left < W) {  // the bytes past the row's width are anything
+#pragma unroll
+      for (int p = 0; p < KMAX; ++p) {
+        h[p].x &= left >= 4 ? 0xffffffffu : (1u << 8 * left) - 1;
+        h[p].y &= left <= 4 ? 0u : (1u << 8 * (left - 4)) - 1;
+      }
+    }
+    float2 y[4];
+#pragma unroll
+    for (int p = 0; p < KMAX; ++p) {
+      float2 d[4];
+      decode8<E5>(h[p], d);
+      ss[p] = p == 0 ? slot_values<true>(d, f[p], w[p] * f[p], y, ss[p]) : slot_values<false>(d, f[p], w[p] * f[p], y, ss[p]);
+    }
+    float o[W] = {y[0].x, y[0].y, y[1].x, y[1].y, y[2].x, y[2].y, y[3].x, y[3].y};
+    if (gate) apply_gate(gate + c * W, a.gate_vec, left, o);
+    if (x) {
+#pragma unroll
+      for (int t = 0; t < W; ++t) o[t] += xs[t];
+    }
+    if (a.vec && left >= W) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j) store_vec(out + c * W + j * V, &o[j * V]);
+    } else {
+#pragma unroll
+      for (int t = 0; t < W; ++t)
+        if (t < left) out[c * W + t] = Elem<TI>::from_f(o[t]);
+    }
+  }
+  if (!a.norms) return;
+  const float s = warp_sums<KMAX>(ss, lane);
+  if (!a.split) {
+    if (lane < k) a.norms[i * k + lane] = sqrtf(s);
+    return;
+  }
+  if (lane < KMAX) part[warp][lane] = s;
+  __syncthreads();
+  if (threadIdx.x < k) {
+    float t = 0.f;
+    for (int q = 0; q < kDirectWarps; ++q) t += part[q][threadIdx.x];
+    a.norms[i * k + threadIdx.x] = sqrtf(t);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Staged form: a warp walks its tokens i = w, w + W, ... (W the grid's warps),
+// each brought into its buffer in shared memory by bulk copies, a lane per row
+// (x's row is one more), so that the bytes in flight hang neither on registers
+// nor on instructions, and the next token's copies start as soon as the last
+// one's values are used.  The next token's row list is loaded a token ahead.
+// One buffer per warp: twice the warps hide more of the arithmetic's latency
+// than a second buffer does.
+//
+// Decoding is what costs next to HBM here: a conversion of two e4m3 values
+// takes a scheduler 4 clocks, their widening 3; the loop over a token's values
+// holds no branch and no select, so that the slots' chains interleave.  For
+// that the buffer is prepared once per token: slots that hold nothing and the
+// bytes past the row's width are zeros, and the scales are turned into floats
+// by block.
+//
+// Rows of x and out that do not start at 16 bytes (VEC false): x is copied in
+// the aligned pieces that hold it and shifted as it is read; out is put
+// together in the buffer at its own offset and leaves it in aligned pieces.
+// ---------------------------------------------------------------------------
+constexpr int kStageWarps = 2;
+constexpr int kStageSm = 227 * 1024, kStageMax = 112 * 1024;  // shared memory of an SM, and the most a block takes
+constexpr unsigned long long kCopyWaitNs = 1000000000ull;
+
+// A warp's buffer: the slots' rows, x's, out's (VEC false), the scale words, the
+// scales as floats.
+struct StageLayout {
+  int row, value, words, blocks, x_at, out_at, word_at, scale_at, bytes;
+};
+template <bool VEC>
+__host__ __device__ inline StageLayout stage_layout(int k, int width, bool x) {
+  StageLayout s;
+  s.row = (width + 15) / 16 * 16;
+  s.value = (width * static_cast<int>(sizeof(TI)) + 15) / 16 * 16 + (VEC ? 0 : 16);
+  s.blocks = (width + kQ8Block - 1) / kQ8Block;
+  s.words = (s.blocks + 3) / 4;
+  s.x_at = k * s.row;
+  s.out_at = s.x_at + (x ? s.value + 16 : 0);  // a last piece may be read past the copied ones
+  s.word_at = s.out_at + (VEC ? 0 : s.value);
+  s.scale_at = (s.word_at + k * s.words * 4 + 15) / 16 * 16;
+  s.bytes = (s.scale_at + k * s.blocks * 4 + 15) / 16 * 16;
+  return s;
+}
+
+template <bool E5, int KMAX, bool VEC>
+__global__ void __launch_bounds__(kStageWarps * 32) q8_combine_staged_kernel(const Q8CombineArgs a) {
+  extern __shared__ __align__(16) uint8_t dyn[];
+  __shared__ __align__(8) uint64_t bars[kStageWarps];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t bar = smem_u32(&bars[warp]);
+  if (lane == 0) mbar_init(bar, 1);
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  __syncwarp();
+  pdl_entry();
+  const int k = a.k, width = a.c.width, chunks = (width + W - 1) / W;
+  const StageLayout L = stage_layout<VEC>(k, width, a.x != nullptr);
+  uint8_t* const buf = dyn + static_cast<size_t>(warp) * L.bytes;
+  const int64_t w0 = static_cast<int64_t>(blockIdx.x) * kStageWarps + warp, step = static_cast<int64_t>(gridDim.x) * kStageWarps;
+  const TI* x = static_cast<const TI*>(a.x);
+
+  // Lane p holds slot p's row (-1: nothing) and weight of the next token to fetch.
+  int row = -1;
+  float weight = 0.f;
+  const auto look_up = [&](int64_t i) {
+    row = -1;
+    weight = 0.f;
+    if (i < a.T && lane < k) {
+      const int r = a.rows ? __ldg(a.rows + i * k + lane) : static_cast<int>(i);
+      if (r >= 0 && r < a.c.rows) {
+        row = r;
+        weight = a.weights ? __ldg(a.weights + i * k + lane) : 1.f;
+      }
+    }
+  };
+  // Start token i's copies.  All lanes have left the buffer.
+  const auto fetch = [&](int64_t i) {
+    if (i >= a.T) return;
+    const uint32_t slots = __ballot_sync(0xffffffffu, row >= 0);
+    const uint8_t* xr = reinterpret_cast<const uint8_t*>(x + (x ? i * a.x_stride : 0));
+    const uint32_t m = VEC ? 0u : static_cast<uint32_t>(reinterpret_cast<uintptr_t>(xr)) & 15u;
+    const uint32_t x_bytes = x ? (m + static_cast<uint32_t>(width * sizeof(TI)) + 15) / 16 * 16 : 0u;
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // before the copies: the lanes' own uses of the buffer
+    if (lane == 0) mbar_expect_tx(bar, __popc(slots) * L.row + x_bytes);
+    __syncwarp();
+    if (row >= 0) bulk_g2s(smem_u32(buf + lane * L.row), a.c.q + row * a.c.q_stride, L.row, bar);
+    if (lane == 31 && x) bulk_g2s(smem_u32(buf + L.x_at), xr - m, x_bytes, bar);
+    for (int j = lane; j < k * L.words; j += 32) {  // the scales, four blocks at a time
+      const int p = j / L.words;
+      const int r = a.rows ? __ldg(a.rows + i * k + p) : static_cast<int>(i);
+      if (r >= 0 && r < a.c.rows)
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(buf + L.word_at + j * 4)),
+                     "l"(a.c.scale + r * a.c.scale_stride + (j - p * L.words) * 4)
+                     : "memory");
+    }
+  };
+
+  look_up(w0);
+  uint32_t parity = 0;
+  float w_now = weight;
+  uint32_t slots = __ballot_sync(0xffffffffu, row >= 0);
+  fetch(w0);
+  look_up(w0 + step);
+  for (int64_t i = w0; i < a.T; i += step) {
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    if (!__all_sync(0xffffffffu, mbar_wait_for(bar, parity, kCopyWaitNs))) {
+      if (lane == 0) report_status(a.status, MOECA_ERR_TIMEOUT, 710);
+      return;
+    }
+    parity ^= 1u;
+    __syncwarp();
+    // Prepare the buffer: zeros for what is not there, scales as floats.
+    float* scales = reinterpret_cast<float*>(buf + L.scale_at);
+    for (int j = lane; j < k * L.blocks; j += 32) {
+      const int p = j / L.blocks, b = j - p * L.blocks;
+      scales[j] = slots >> p & 1 ? scale_value(buf[L.word_at + p * L.words * 4 + b]) : 1.f;
+    }
+    if (lane < k && width < L.row) {
+      for (int t = width; t < L.row; ++t) buf[lane * L.row + t] = 0;
+    }
+    for (int p = 0; p < k; ++p)
+      if (!(slots >> p & 1))
+        for (int c = lane * 16; c < L.row; c += 512) *reinterpret_cast<uint4*>(buf + p * L.row + c) = make_uint4(0u, 0u, 0u, 0u);
+    float wp[KMAX];
+#pragma unroll
+    for (int p = 0; p < KMAX; ++p) wp[p] = __shfl_sync(0xffffffffu, w_now, p);
+    __syncwarp();
+
+    TI* out = static_cast<TI*>(a.out) + i * a.out_stride;
+    const float* gate = a.gate ? a.gate + (i / a.seq) * a.gate_stride : nullptr;
+    const uint32_t mx = VEC || !x ? 0u : static_cast<uint32_t>(reinterpret_cast<uintptr_t>(x + i * a.x_stride)) & 15u;
+    const uint32_t mo = VEC ? 0u : static_cast<uint32_t>(reinterpret_cast<uintptr_t>(out)) & 15u;
+    float ss[KMAX];
+#pragma unroll
+    for (int p = 0; p < KMAX; ++p) ss[p] = 0.f;
+    for (int c = lane; c < chunks; c += 32) {
+      const int left = width - c * W;
+      float2 y[4];
+#pragma unroll
+      for (int p = 0; p < KMAX; ++p) {
+        const int at = p < k ? p : 0;  // a slot past the last reads the first with a weight of 0; its norm is not kept
+        float2 d[4];
+        decode8<E5>(*reinterpret_cast<const uint2*>(buf + at * L.row + c * W), d);
+        const float f = scales[at * L.blocks + (c >> 4)];
+        ss[p] = p == 0 ? slot_values<true>(d, f, wp[p] * f, y, ss[p]) : slot_values<false>(d, f, wp[p] * f, y, ss[p]);
+      }
+      float o[W] = {y[0].x, y[0].y, y[1].x, y[1].y, y[2].x, y[2].y, y[3].x, y[3].y};
+      if (gate) apply_gate(gate + c * W, a.gate_vec, left, o);
+      if (x) {
+        float xs[W];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+          const uint4* piece = reinterpret_cast<const uint4*>(buf + L.x_at) + c * NV + j;
+          if constexpr (VEC) unpack_vec(*piece, &xs[j * V], static_cast<TI*>(nullptr));
+          else unpack_vec(shifted<TI>(piece[0], piece[1], mx), &xs[j * V], static_cast<TI*>(nullptr));
+        }
+#pragma unroll
+        for (int t = 0; t < W; ++t) o[t] += xs[t];
+      }
+      if constexpr (VEC) {
+        if (left >= W) {
+#pragma unroll
+          for (int j = 0; j < NV; ++j) store_vec(out + c * W + j * V, &o[j * V]);
+        } else {
+#pragma unroll
+          for (int t = 0; t < W; ++t)
+            if (t < left) out[c * W + t] = Elem<TI>::from_f(o[t]);
+        }
+      } else {
+        TI* to = reinterpret_cast<TI*>(buf + L.out_at + mo) + c * W;
+#pragma unroll
+        for (int t = 0; t < W; ++t)
+          if (t < left) to[t] = Elem<TI>::from_f(o[t]);
+      }
+    }
+    __syncwarp();  // all have read the slots and x
+    if constexpr (!VEC) {
+      // out's aligned pieces; its first and last values alone where a piece is another row's too.
+      const uint32_t end = mo + width * sizeof(TI);
+      uint8_t* base = reinterpret_cast<uint8_t*>(out) - mo;
+      for (uint32_t t = lane * 16; t < end; t += 512) {
+        const uint8_t* from = buf + L.out_at + t;
+        if (t >= mo && t + 16 <= end) {
+          *reinterpret_cast<uint4*>(base + t) = *reinterpret_cast<const uint4*>(from);
+        } else {
+#pragma unroll
+          for (uint32_t q = 0; q < 16; q += sizeof(TI))
+            if (t + q >= mo && t + q < end) *reinterpret_cast<TI*>(base + t + q) = *reinterpret_cast<const TI*>(from + q);
+        }
+      }
+      __syncwarp();
+    }
+    w_now = weight;
+    slots = __ballot_sync(0xffffffffu, row >= 0);
+    fetch(i + step);
+    look_up(i + 2 * step);
+    if (a.norms) {
+      const float s = warp_sums<KMAX>(ss, lane);
+      if (lane < k) a.norms[i * k + lane] = sqrtf(s);
+    }
+  }
+}
+
+template <bool E5, bool VEC, int KMAX>
+cudaError_t run_staged(const Q8CombineArgs& a, int smem, cudaStream_t s) {
+  const auto kern = q8_combine_staged_kernel<E5, KMAX, VEC>;
+  const cudaError_t e = set_dyn_smem_on_device(reinterpret_cast<const void*>(kern), kStageMax);
+  if (e != cudaSuccess) return e;
+  const int per_sm = std::max(1, std::min(kStageSm / (smem + 1088), 16));
+  const int64_t blocks = std::min<int64_t>((static_cast<int64_t>(a.T) + kStageWarps - 1) / kStageWarps, 152 * per_sm);
+  return launch_pdl(kern, dim3(static_cast<unsigned>(blocks)), dim3(kStageWarps * 32), smem, s, a);
+}
+
+template <bool E5, bool VEC>
+cudaError_t staged(const Q8CombineArgs& a, int smem, cudaStream_t s) {
+  switch (a.k) {
+    case 1: return run_staged<E5, VEC, 1>(a, smem, s);
+    case 2: return run_staged<E5, VEC, 2>(a, smem, s);
+    case 3: return run_staged<E5, VEC, 3>(a, smem, s);
+    case 4: return run_staged<E5, VEC, 4>(a, smem, s);
+    case 5:
+    case 6: return run_staged<E5, VEC, 6>(a, smem, s);
+    case 7:
+    case 8: return run_staged<E5, VEC, 8>(a, smem, s);
+    case 9: return run_staged<E5, VEC, 9>(a, smem, s);
+    default: return run_staged<E5, VEC, 16>(a, smem, s);
+  }
+}
+
+template <bool E5>
+cudaError_t combine(Q8CombineArgs a, cudaStream_t s) {
+  constexpr int size = sizeof(TI);
+  a.vec = q8_aligned16(a.out, a.out_stride * size) && (!a.x || q8_aligned16(a.x, a.x_stride * size));
+  a.gate_vec = a.gate && q8_aligned16(a.gate, a.gate_stride * 4);
+  // A block per token below two tokens per SM; staged above, where two blocks'
+  // buffers fit an SM.
+  a.split = a.T < 152 * 2;
+  const int64_t wide = static_cast<int64_t>(a.c.width) * (a.k + 2 * size);
+  if (!a.split && wide < kStageMax / kStageWarps) {
+    const StageLayout L = a.vec ? stage_layout<true>(a.k, a.c.width, a.x != nullptr) : stage_layout<false>(a.k, a.c.width, a.x != nullptr);
+    const int smem = kStageWarps * L.bytes;
+    if (smem <= kStageMax) return a.vec ? staged<E5, true>(a, smem, s) : staged<E5, false>(a, smem, s);
+  }
+  const dim3 grid(a.split ? a.T : (a.T + kDirectWarps - 1) / kDirectWarps), block(kDirectWarps * 32);
+  if (a.k == 1) return launch_pdl(q8_combine_kernel<E5, 1>, grid, block, 0, s, a);
+  if (a.k == 2) return launch_pdl(q8_combine_kernel<E5, 2>, grid, block, 0, s, a);
+  if (a.k <= 4) return launch_pdl(q8_combine_kernel<E5, 4>, grid, block, 0, s, a);
+  if (a.k <= 8) return launch_pdl(q8_combine_kernel<E5, 8>, grid, block, 0, s, a);
+  return launch_pdl(q8_combine_kernel<E5, 16>, grid, block, 0, s, a);
+}
+
+}  // namespace
+
+#ifdef MOECA_Q8_COMBINE_F32
+cudaError_t launch_q8_combine_f32(const Q8CombineArgs& a, bool e5, cudaStream_t s) {
+#else
+cudaError_t launch_q8_combine_bf16(const Q8CombineArgs& a, bool e5, cudaStream_t s) {
+#endif
+  if (a.T <= 0) return cudaSuccess;
+  return e5 ? combine<true>(a, s) : combine<false>(a, s);
+}
+
+}  // namespace moeca

@@ -120,14 +120,14 @@ class moeca_q8_write_args(C.Structure):
 
 class moeca_q8_read_args(C.Structure):
     _fields_ = [("cache", moeca_q8_rows), ("out", C.c_void_p), ("out_stride", C.c_int64), ("dtype", C.c_int32),
-                ("n", C.c_int32), ("rows", C.c_void_p)]
+                ("n", C.c_int32), ("rows", C.c_void_p), ("status", C.c_void_p)]
 
 
 class moeca_q8_combine_args(C.Structure):
     _fields_ = [("cache", moeca_q8_rows), ("rows", C.c_void_p), ("weights", C.c_void_p), ("x", C.c_void_p),
                 ("x_stride", C.c_int64), ("gate", C.c_void_p), ("gate_stride", C.c_int64), ("out", C.c_void_p),
                 ("out_stride", C.c_int64), ("norms", C.c_void_p), ("dtype", C.c_int32), ("n_tokens", C.c_int32),
-                ("n_slots", C.c_int32), ("seq", C.c_int32)]
+                ("n_slots", C.c_int32), ("seq", C.c_int32), ("status", C.c_void_p)]
 
 
 class moeca_q8_matmul_args(C.Structure):
@@ -618,8 +618,8 @@ def q8_empty(rows: int, width: int, dtype=None, device="cuda") -> Q8:
 # are those of the moeca_q8_*_args structures.
 _ROWS = "QQqqqii"
 _PACK_WRITE = struct.Struct("@" + _ROWS + "QqqiiQQQ")
-_PACK_READ = struct.Struct("@" + _ROWS + "QqiiQ")
-_PACK_COMBINE = struct.Struct("@" + _ROWS + "QQQqQqQqQiiii")
+_PACK_READ = struct.Struct("@" + _ROWS + "QqiiQQ")
+_PACK_COMBINE = struct.Struct("@" + _ROWS + "QQQqQqQqQiiiiQ")
 _PACK_MATMUL = struct.Struct("@" + 3 * _ROWS + "QQQQiii4x")
 for _s, _t in ((_PACK_WRITE, moeca_q8_write_args), (_PACK_READ, moeca_q8_read_args),
                (_PACK_COMBINE, moeca_q8_combine_args), (_PACK_MATMUL, moeca_q8_matmul_args)):
@@ -709,9 +709,9 @@ def q8_write(x, cache: Q8, src=None, dst=None, count=None, stream: int = 0) -> Q
     return cache
 
 
-def q8_read(cache: Q8, rows=None, dtype=None, out=None, stream: int = 0):
+def q8_read(cache: Q8, rows=None, dtype=None, out=None, status=None, stream: int = 0):
     """Cache rows as bf16 (default) or fp32: all of them, or those of ``rows`` (int32, on the device); zeros
-    where an entry is out of range."""
+    where an entry is out of range.  ``status``: as for q8_matmul."""
     dev = cache[0].get_device()
     c = _q8_fields(cache, "cache", dev)
     n = c[2] if rows is None else rows.numel()
@@ -721,12 +721,13 @@ def q8_read(cache: Q8, rows=None, dtype=None, out=None, stream: int = 0):
     address, n_out, stride, width, code = _value_fields(out, "out", dev)
     if n_out != n or width != c[5] or (dtype is not None and out.dtype != dtype):
         raise ValueError(f"out must be [{n}, {c[5]}] of the asked dtype")
-    args = _PACK_READ.pack(*c, address, stride, code, n, _list(rows, "i32", (n,), "rows", dev))
+    args = _PACK_READ.pack(*c, address, stride, code, n, _list(rows, "i32", (n,), "rows", dev), _list(status, "i32", (2,), "status", dev))
     _call(_q8_packed[1], args, dev, stream)
     return out
 
 
-def q8_combine(cache: Q8, rows, weights=None, x=None, gate=None, norms=False, dtype=None, out=None, stream: int = 0):
+def q8_combine(cache: Q8, rows, weights=None, x=None, gate=None, norms=False, dtype=None, out=None, status=None,
+               stream: int = 0):
     """Eq. 8 over an 8-bit branch cache: x + gate * sum_p weights[:, p] cache[rows[:, p]].  ``rows`` [T, k]
     int32 (out of range: an empty slot), ``weights`` [T, k] fp32 (None: 1), ``x`` [T, D] fp32 or bf16 (None: 0),
     ``gate`` [B, D] fp32, one row for each T / B consecutive tokens.  ``norms``: True or a [T, k] fp32 tensor
@@ -760,7 +761,8 @@ def q8_combine(cache: Q8, rows, weights=None, x=None, gate=None, norms=False, dt
         norms = None
     args = _PACK_COMBINE.pack(
         *c, _list(rows, "i32", shape, "rows", dev), _list(weights, "f32", shape, "weights", dev), x_address, x_stride,
-        gate_address, gate_stride, address, stride, _list(norms, "f32", shape, "norms", dev), code, T, k, seq)
+        gate_address, gate_stride, address, stride, _list(norms, "f32", shape, "norms", dev), code, T, k, seq,
+        _list(status, "i32", (2,), "status", dev))
     _call(_q8_packed[2], args, dev, stream)
     return out if norms is None else (out, norms)
 
