@@ -431,6 +431,9 @@ __global__ void __launch_bounds__(kThreads, 1) q8_matmul_kernel(const __grid_con
     const CUtensorMap* t = lane ? &maps.act[lane - 1] : &maps.w;
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(t)) : "memory");
   }
+  cluster_arrive();
+  cluster_wait();  // both CTAs' barriers are initialised, TMEM is allocated
+  tc_fence_after();
   pdl_entry();
   const int nw = (p.N + 2 * kBM - 1) / (2 * kBM);
   if (warp == 0) {
@@ -465,9 +468,6 @@ __global__ void __launch_bounds__(kThreads, 1) q8_matmul_kernel(const __grid_con
     }
   }
   __syncthreads();
-  cluster_arrive();
-  cluster_wait();  // both CTAs' barriers are initialised, TMEM is allocated
-  tc_fence_after();
   const uint32_t tmem = sh.tmem;
   const int units = sh.units[p.G];
   const int kb = (p.K + kQ8Block - 1) / kQ8Block, ks = (kb + kSub - 1) / kSub, kc = (kb + 3) / 4;
@@ -738,7 +738,12 @@ bool encode_rows(CUtensorMap* m, const Q8Rows& r, uint32_t box_rows) {
 cudaError_t launch_q8_matmul(const Q8MatmulArgs& a, cudaStream_t s) {
   Maps maps;
   bool ok = encode_rows(&maps.w, a.b, kBM);
-  for (int i = 0; i < kBoxes && ok; ++i) ok = encode_rows(&maps.act[i], a.a, 8 * (i + 1));
+  // No group has more than all rows: no wider boxes than theirs.
+  const int boxes = static_cast<int>(std::min<int64_t>(kBoxes, (a.a.rows + 15) / 16));
+  for (int i = 0; i < kBoxes && ok; ++i) {
+    if (i < boxes) ok = encode_rows(&maps.act[i], a.a, 8 * (i + 1));
+    else maps.act[i] = maps.act[0];
+  }
   if (!ok) return cudaErrorInvalidValue;
   int dev = 0, sms = 0;
   cudaError_t e = cudaGetDevice(&dev);
