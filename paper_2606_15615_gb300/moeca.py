@@ -628,59 +628,57 @@ _q8_packed = [C.CFUNCTYPE(C.c_int, C.c_char_p, C.c_void_p)(C.cast(getattr(LIB, _
     "moeca_q8_write", "moeca_q8_read", "moeca_q8_combine", "moeca_q8_matmul")]
 
 
-_TYPES = {}
+_TYPES = {}  # torch dtypes: the C codes; "i32", "f32", "torch": the dtypes and the module
 
 
-def _type_code(dtype) -> int:
-    """The C code of a torch dtype, -1 for one the library does not take."""
+def _types() -> dict:
     if not _TYPES:
         import torch
         _TYPES.update({torch.float32: MOECA_F32, torch.bfloat16: MOECA_BF16, torch.float8_e4m3fn: MOECA_E4M3,
-                       torch.float8_e5m2: MOECA_E5M2, "i32": torch.int32, "f32": torch.float32})
-    return _TYPES.get(dtype, -1)
+                       torch.float8_e5m2: MOECA_E5M2, "i32": torch.int32, "f32": torch.float32, "torch": torch})
+    return _TYPES
 
 
 def _q8_fields(r, what: str, device: int) -> tuple:
     """The fields of moeca_q8_rows.  One row (or none) has no next one: its strides are not looked at."""
     q, s = r
-    if q.dim() != 2 or s.dim() != 2:
-        raise ValueError(f"{what}: q and scale must be 2-D")
-    (n, width), (q_stride, unit), code = q.shape, q.stride(), _type_code(q.dtype)
-    if code < MOECA_E4M3 or (unit != 1 and width > 1) or q.get_device() != device:
-        raise ValueError(f"{what}.q must be float8_e4m3fn or float8_e5m2 on the call's device with unit column stride")
-    (sn, nb), (s_stride, unit) = s.shape, s.stride()
-    if sn != n or nb != (width + 127) // Q8_BLOCK or (unit != 1 and nb > 1) or s.element_size() != 1 or s.get_device() != device:
+    shape, stride, code = q.shape, q.stride(), (_TYPES or _types()).get(q.dtype, -1)
+    if code < MOECA_E4M3 or len(shape) != 2 or (stride[1] != 1 and shape[1] > 1) or q.get_device() != device:
+        raise ValueError(f"{what}.q must be a 2-D float8_e4m3fn or float8_e5m2 tensor on the call's device with unit "
+                         "column stride")
+    n, width = shape
+    nb = (width + 127) // Q8_BLOCK
+    s_stride = s.stride()
+    if s.shape != (n, nb) or (s_stride[1] != 1 and nb > 1) or s.element_size() != 1 or s.get_device() != device:
         raise ValueError(f"{what}.scale must be [rows, ceil(width / 128)] bytes on the call's device with unit column stride")
     if n <= 1:
-        q_stride, s_stride = (width + 15) // 16 * 16, (nb + 3) // 4 * 4
-    return q.data_ptr(), s.data_ptr(), n, q_stride, s_stride, width, code
+        return q.data_ptr(), s.data_ptr(), n, (width + 15) // 16 * 16, (nb + 3) // 4 * 4, width, code
+    return q.data_ptr(), s.data_ptr(), n, stride[0], s_stride[0], width, code
 
 
 def _value_fields(t, what: str, device: int) -> tuple:
     """(address, rows, row stride in elements, width, type code) of a tensor of fp32 or bf16 rows."""
-    code = _type_code(t.dtype)
-    if code not in (MOECA_F32, MOECA_BF16) or t.dim() != 2 or t.get_device() != device:
-        raise ValueError(f"{what} must be a 2-D float32 or bfloat16 tensor on the call's device")
-    (n, width), (stride, unit) = t.shape, t.stride()
-    if unit != 1 and width > 1:
-        raise ValueError(f"{what} must have unit column stride")
-    return t.data_ptr(), n, stride if n > 1 else width, width, code
+    shape, stride, code = t.shape, t.stride(), (_TYPES or _types()).get(t.dtype, -1)
+    if code not in (MOECA_F32, MOECA_BF16) or len(shape) != 2 or (stride[1] != 1 and shape[1] > 1) or t.get_device() != device:
+        raise ValueError(f"{what} must be a 2-D float32 or bfloat16 tensor on the call's device with unit column stride")
+    n, width = shape
+    return t.data_ptr(), n, stride[0] if n > 1 else width, width, code
 
 
 def _list(t, kind: str, shape: tuple, what: str, device: int) -> int:
     """The address of a contiguous device tensor of int32 ("i32") or float32 ("f32") and one shape (None: NULL)."""
     if t is None:
         return 0
-    if t.dtype != _TYPES[kind] or tuple(t.shape) != shape or not t.is_contiguous() or t.get_device() != device:
+    if t.dtype != _types()[kind] or t.shape != shape or not t.is_contiguous() or t.get_device() != device:
         raise ValueError(f"{what} must be a contiguous {_TYPES[kind]} tensor {list(shape)} on the call's device")
     return t.data_ptr()
 
 
 def _call(fn, args: bytes, device: int, stream: int):
     """Run a C call with the tensors' device current, on ``stream`` or that device's current stream."""
-    import torch
     if device < 0:
         raise ValueError("8-bit rows live on a CUDA device")
+    torch = _TYPES["torch"]
     stream = stream or torch._C._cuda_getCurrentRawStream(device)
     if device == torch._C._cuda_getDevice():
         status = fn(args, stream or None)
@@ -716,7 +714,7 @@ def q8_read(cache: Q8, rows=None, dtype=None, out=None, status=None, stream: int
     c = _q8_fields(cache, "cache", dev)
     n = c[2] if rows is None else rows.numel()
     if out is None:
-        import torch
+        torch = _TYPES["torch"]
         out = torch.empty((n, c[5]), dtype=dtype or torch.bfloat16, device=cache[0].device)
     address, n_out, stride, width, code = _value_fields(out, "out", dev)
     if n_out != n or width != c[5] or (dtype is not None and out.dtype != dtype):
@@ -733,23 +731,25 @@ def q8_combine(cache: Q8, rows, weights=None, x=None, gate=None, norms=False, dt
     ``gate`` [B, D] fp32, one row for each T / B consecutive tokens.  ``norms``: True or a [T, k] fp32 tensor
     also gives the rows' 2-norms.  The result has x's dtype (without x: ``dtype``, default bf16); ``out`` may be
     x.  Returns out, or (out, norms)."""
-    import torch
     dev = cache[0].get_device()
     c = _q8_fields(cache, "cache", dev)
-    if rows.dim() != 2:
+    shape = rows.shape
+    if len(shape) != 2:
         raise ValueError("rows must be [tokens, slots]")
-    T, k = shape = tuple(rows.shape)
-    if out is None:
-        out = torch.empty((T, c[5]), dtype=x.dtype if x is not None else dtype or torch.bfloat16, device=rows.device)
-    address, n_out, stride, width, code = _value_fields(out, "out", dev)
-    if n_out != T or width != c[5]:
-        raise ValueError(f"out must be [{T}, {c[5]}]")
+    T, k = shape
+    width = c[5]
+    torch = _TYPES["torch"]
     x_address = x_stride = gate_address = gate_stride = 0
     seq = 1
     if x is not None:
-        x_address, n_x, x_stride, x_width, x_code = _value_fields(x, "x", dev)
-        if x_code != code or n_x != T or x_width != width:
-            raise ValueError("x must have out's dtype and shape")
+        x_address, n_x, x_stride, x_width, code = _value_fields(x, "x", dev)
+        if n_x != T or x_width != width:
+            raise ValueError(f"x must be [{T}, {width}]")
+    if out is None:
+        out = torch.empty((T, width), dtype=x.dtype if x is not None else dtype or torch.bfloat16, device=rows.device)
+    address, n_out, stride, o_width, o_code = _value_fields(out, "out", dev)
+    if n_out != T or o_width != width or (x is not None and o_code != code):
+        raise ValueError(f"out must be [{T}, {width}] of x's dtype")
     if gate is not None:
         gate_address, n_g, gate_stride, g_width, g_code = _value_fields(gate, "gate", dev)
         if g_code != MOECA_F32 or g_width != width or (T and (not n_g or T % n_g)):
@@ -761,7 +761,7 @@ def q8_combine(cache: Q8, rows, weights=None, x=None, gate=None, norms=False, dt
         norms = None
     args = _PACK_COMBINE.pack(
         *c, _list(rows, "i32", shape, "rows", dev), _list(weights, "f32", shape, "weights", dev), x_address, x_stride,
-        gate_address, gate_stride, address, stride, _list(norms, "f32", shape, "norms", dev), code, T, k, seq,
+        gate_address, gate_stride, address, stride, _list(norms, "f32", shape, "norms", dev), o_code, T, k, seq,
         _list(status, "i32", (2,), "status", dev))
     _call(_q8_packed[2], args, dev, stream)
     return out if norms is None else (out, norms)
@@ -784,8 +784,8 @@ def q8_matmul(a: Q8, b: Q8, offsets=None, bias=None, act: str = "none", dst=None
     if act not in _ACTS:
         raise ValueError(f"act must be one of {sorted(_ACTS)}")
     if out is None:
-        import torch
-        code = _type_code(dtype or torch.bfloat16)
+        torch = _TYPES["torch"]
+        code = _TYPES.get(dtype or torch.bfloat16, -1)
         if code < 0:
             raise ValueError("dtype must be float32, bfloat16, float8_e4m3fn or float8_e5m2")
         out = q8_empty(ra[2], cols, dtype, a[0].device) if code >= MOECA_E4M3 else \
