@@ -258,6 +258,24 @@ struct MatmulParams {
   int32_t* status;
 };
 
+// Stores under a predicate, without a branch (a branch per store keeps the
+// stores' address arithmetic from overlapping).
+__device__ __forceinline__ void store_if(bool on, void* to, const uint4& v) {
+  asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %5, 0;\n @p st.global.v4.b32 [%0], {%1, %2, %3, %4};\n}" ::"l"(to), "r"(v.x),
+               "r"(v.y), "r"(v.z), "r"(v.w), "r"(static_cast<uint32_t>(on))
+               : "memory");
+}
+__device__ __forceinline__ void store_if(bool on, void* to, float v) {
+  asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %2, 0;\n @p st.global.f32 [%0], %1;\n}" ::"l"(to), "f"(v),
+               "r"(static_cast<uint32_t>(on))
+               : "memory");
+}
+__device__ __forceinline__ void store_if(bool on, void* to, __nv_bfloat16 v) {
+  asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %2, 0;\n @p st.global.b16 [%0], %1;\n}" ::"l"(to),
+               "h"(__bfloat16_as_ushort(v)), "r"(static_cast<uint32_t>(on))
+               : "memory");
+}
+
 // Epilogue of one chunk: 32 features (lanes) x 32 tokens (z), all four
 // quadrants of the part together.  row: lane t's output row of token t, or -1.
 // Rows go out through shared memory in 16-byte pieces; rows that are not
@@ -290,9 +308,8 @@ __device__ __forceinline__ void store_chunk(const MatmulParams& p, Shared& sh, f
         const uint4 v = *reinterpret_cast<const uint4*>(stage + ((i & 1) * 8 + (lane >> 2)) * 16 + (lane & 3) * 4);
         const int r = __shfl_sync(0xffffffffu, row, i * 8 + (lane >> 2));
         uint8_t* at = p.out + r * p.out_stride + f * 2;
-        if (r >= 0 && left >= 8) {
-          *reinterpret_cast<uint4*>(at) = v;
-        } else if (r >= 0 && left > 0) {
+        store_if(r >= 0 && left >= 8, at, v);
+        if (feat0 + 32 > p.N && r >= 0 && left > 0 && left < 8) {
           const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
           for (int j = 0; j < 7; ++j)
@@ -301,13 +318,11 @@ __device__ __forceinline__ void store_chunk(const MatmulParams& p, Shared& sh, f
       }
     } else {
       using T = std::conditional_t<OUT == MOECA_F32, float, __nv_bfloat16>;
-      const bool live = feat0 + lane < p.N;
+      const uint32_t rows = __ballot_sync(0xffffffffu, row >= 0), live = feat0 + lane < p.N ? rows : 0u;
       uint8_t* base = p.out + static_cast<int64_t>(feat0 + lane) * sizeof(T);
+      const int64_t mine = row * p.out_stride;
 #pragma unroll
-      for (int t = 0; t < 32; ++t) {
-        const int r = __shfl_sync(0xffffffffu, row, t);
-        if (r >= 0 && live) *reinterpret_cast<T*>(base + r * p.out_stride) = Elem<T>::from_f(z[t]);
-      }
+      for (int t = 0; t < 32; ++t) store_if(live >> t & 1, base + __shfl_sync(0xffffffffu, mine, t), Elem<T>::from_f(z[t]));
     }
   } else {
     constexpr bool E5 = OUT == MOECA_E5M2;
@@ -380,9 +395,8 @@ __device__ __forceinline__ void store_chunk(const MatmulParams& p, Shared& sh, f
       const uint4 v = *reinterpret_cast<const uint4*>(stage + (i * 16 + (lane >> 1)) * 8 + (lane & 1) * 4);
       const int r = __shfl_sync(0xffffffffu, row, i * 16 + (lane >> 1));
       uint8_t* at = p.out + r * p.out_stride + f;
-      if (r >= 0 && left >= 16) {
-        *reinterpret_cast<uint4*>(at) = v;
-      } else if (r >= 0 && left > 0) {
+      store_if(r >= 0 && left >= 16, at, v);
+      if (feat0 + 32 > p.N && r >= 0 && left > 0 && left < 16) {
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
         for (int j = 0; j < 15; ++j)
