@@ -89,15 +89,21 @@ __device__ __forceinline__ float warp_sums(const float (&s)[K], int lane) {
   return v[0];
 }
 
-__device__ __forceinline__ void apply_gate(const float* gp, bool vec, int left, float (&o)[W]) {
+// A lane's gate values (zeros past the row's end).
+struct Gate {
+  float v[W];
+};
+__device__ __forceinline__ Gate load_gate(const float* gp, bool vec, int left) {
+  Gate g;
   if (vec && left >= W) {
-    const float4 g0 = __ldg(reinterpret_cast<const float4*>(gp)), g1 = __ldg(reinterpret_cast<const float4*>(gp) + 1);
-    o[0] *= g0.x; o[1] *= g0.y; o[2] *= g0.z; o[3] *= g0.w;
-    o[4] *= g1.x; o[5] *= g1.y; o[6] *= g1.z; o[7] *= g1.w;
+    const float4 a = __ldg(reinterpret_cast<const float4*>(gp)), b = __ldg(reinterpret_cast<const float4*>(gp) + 1);
+    g.v[0] = a.x; g.v[1] = a.y; g.v[2] = a.z; g.v[3] = a.w;
+    g.v[4] = b.x; g.v[5] = b.y; g.v[6] = b.z; g.v[7] = b.w;
   } else {
 #pragma unroll
-    for (int t = 0; t < W; ++t) o[t] *= t < left ? __ldg(gp + t) : 0.f;
+    for (int t = 0; t < W; ++t) g.v[t] = t < left ? __ldg(gp + t) : 0.f;
   }
+  return g;
 }
 
 // ---------------------------------------------------------------------------
@@ -137,6 +143,8 @@ __global__ void __launch_bounds__(kDirectWarps * 32) q8_combine_kernel(const Q8C
     const int left = width - c * W;
     uint2 h[KMAX];
     float f[KMAX], xs[W];
+    Gate g{};
+    if (gate) g = load_gate(gate + c * W, a.gate_vec, left);
 #pragma unroll
     for (int p = 0; p < KMAX; ++p) {
       h[p] = make_uint2(0u, 0u);
@@ -170,7 +178,10 @@ __global__ void __launch_bounds__(kDirectWarps * 32) q8_combine_kernel(const Q8C
       ss[p] = p == 0 ? slot_values<true>(d, f[p], w[p] * f[p], y, ss[p]) : slot_values<false>(d, f[p], w[p] * f[p], y, ss[p]);
     }
     float o[W] = {y[0].x, y[0].y, y[1].x, y[1].y, y[2].x, y[2].y, y[3].x, y[3].y};
-    if (gate) apply_gate(gate + c * W, a.gate_vec, left, o);
+    if (gate) {
+#pragma unroll
+      for (int t = 0; t < W; ++t) o[t] *= g.v[t];
+    }
     if (x) {
 #pragma unroll
       for (int t = 0; t < W; ++t) o[t] += xs[t];
@@ -221,6 +232,8 @@ __global__ void __launch_bounds__(kDirectWarps * 32) q8_combine_kernel(const Q8C
 // ---------------------------------------------------------------------------
 constexpr int kStageWarps = 2;
 constexpr int kStageSm = 227 * 1024, kStageMax = 112 * 1024;  // shared memory of an SM, and the most a block takes
+// Blocks per SM that the registers allow (the grid is persistent: none may wait for another).
+constexpr int stage_blocks(int k) { return k <= 2 ? 16 : k <= 4 ? 12 : k <= 9 ? 8 : 6; }
 constexpr unsigned long long kCopyWaitNs = 1000000000ull;
 
 // A warp's buffer: the slots' rows, x's, out's (VEC false), the scale words, the
@@ -243,8 +256,8 @@ __host__ __device__ inline StageLayout stage_layout(int k, int width, bool x) {
   return s;
 }
 
-template <bool E5, int KMAX, bool VEC>
-__global__ void __launch_bounds__(kStageWarps * 32) q8_combine_staged_kernel(const Q8CombineArgs a) {
+template <bool E5, int KMAX, bool VEC, bool GATED>
+__global__ void __launch_bounds__(kStageWarps * 32, stage_blocks(KMAX)) q8_combine_staged_kernel(const Q8CombineArgs a) {
   extern __shared__ __align__(16) uint8_t dyn[];
   __shared__ __align__(8) uint64_t bars[kStageWarps];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -302,6 +315,10 @@ __global__ void __launch_bounds__(kStageWarps * 32) q8_combine_staged_kernel(con
   fetch(w0);
   look_up(w0 + step);
   for (int64_t i = w0; i < a.T; i += step) {
+    // The gate's values are loaded a step ahead of their use.
+    const float* gate = GATED ? a.gate + (i / a.seq) * a.gate_stride : nullptr;
+    Gate next{};
+    if (GATED && lane < chunks) next = load_gate(gate + lane * W, a.gate_vec, width - lane * W);
     asm volatile("cp.async.wait_all;" ::: "memory");
     if (!__all_sync(0xffffffffu, mbar_wait_for(bar, parity, kCopyWaitNs))) {
       if (lane == 0) report_status(a.status, MOECA_ERR_TIMEOUT, 710);
@@ -327,7 +344,6 @@ __global__ void __launch_bounds__(kStageWarps * 32) q8_combine_staged_kernel(con
     __syncwarp();
 
     TI* out = static_cast<TI*>(a.out) + i * a.out_stride;
-    const float* gate = a.gate ? a.gate + (i / a.seq) * a.gate_stride : nullptr;
     const uint32_t mx = VEC || !x ? 0u : static_cast<uint32_t>(reinterpret_cast<uintptr_t>(x + i * a.x_stride)) & 15u;
     const uint32_t mo = VEC ? 0u : static_cast<uint32_t>(reinterpret_cast<uintptr_t>(out)) & 15u;
     float ss[KMAX];
@@ -335,6 +351,8 @@ __global__ void __launch_bounds__(kStageWarps * 32) q8_combine_staged_kernel(con
     for (int p = 0; p < KMAX; ++p) ss[p] = 0.f;
     for (int c = lane; c < chunks; c += 32) {
       const int left = width - c * W;
+      const Gate now = next;
+      if (GATED && c + 32 < chunks) next = load_gate(gate + (c + 32) * W, a.gate_vec, left - 32 * W);
       float2 y[4];
 #pragma unroll
       for (int p = 0; p < KMAX; ++p) {
@@ -345,7 +363,10 @@ __global__ void __launch_bounds__(kStageWarps * 32) q8_combine_staged_kernel(con
         ss[p] = p == 0 ? slot_values<true>(d, f, wp[p] * f, y, ss[p]) : slot_values<false>(d, f, wp[p] * f, y, ss[p]);
       }
       float o[W] = {y[0].x, y[0].y, y[1].x, y[1].y, y[2].x, y[2].y, y[3].x, y[3].y};
-      if (gate) apply_gate(gate + c * W, a.gate_vec, left, o);
+      if constexpr (GATED) {
+#pragma unroll
+        for (int t = 0; t < W; ++t) o[t] *= now.v[t];
+      }
       if (x) {
         float xs[W];
 #pragma unroll
@@ -403,10 +424,10 @@ __global__ void __launch_bounds__(kStageWarps * 32) q8_combine_staged_kernel(con
 
 template <bool E5, bool VEC, int KMAX>
 cudaError_t run_staged(const Q8CombineArgs& a, int smem, cudaStream_t s) {
-  const auto kern = q8_combine_staged_kernel<E5, KMAX, VEC>;
+  const auto kern = a.gate ? q8_combine_staged_kernel<E5, KMAX, VEC, true> : q8_combine_staged_kernel<E5, KMAX, VEC, false>;
   const cudaError_t e = set_dyn_smem_on_device(reinterpret_cast<const void*>(kern), kStageMax);
   if (e != cudaSuccess) return e;
-  const int per_sm = std::max(1, std::min(kStageSm / (smem + 1088), 16));
+  const int per_sm = std::max(1, std::min(kStageSm / (smem + 1088), stage_blocks(KMAX)));
   const int64_t blocks = std::min<int64_t>((static_cast<int64_t>(a.T) + kStageWarps - 1) / kStageWarps, 152 * per_sm);
   return launch_pdl(kern, dim3(static_cast<unsigned>(blocks)), dim3(kStageWarps * 32), smem, s, a);
 }
