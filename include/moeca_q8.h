@@ -121,7 +121,9 @@ typedef enum { MOECA_ACT_NONE = 0, MOECA_ACT_GELU = 1, MOECA_ACT_GELU_TANH = 2 }
  * are clamped to [0, a.rows], a group that would end before it starts is
  * empty; rows that two groups claim hold either's result.  An entry of dst
  * out of [0, out.rows) drops its row; entries are distinct.  Rows of out that
- * no entry names, and bytes past a row's width, keep what they hold. */
+ * no entry names, and bytes past a row's width, keep what they hold.
+ * MOECA_ERR_UNSUPPORTED above 2^30 rows of a or b, or where (a.rows / 16 +
+ * n_groups) x ceil(n_cols / 256) passes 2^30. */
 typedef struct {
   moeca_q8_rows a;         /* activations                                             */
   moeca_q8_rows b;         /* weights: rows = n_groups x n_cols, width = a.width      */
@@ -131,9 +133,9 @@ typedef struct {
   const int32_t* offsets;  /* [n_groups + 1] device, or NULL: one group of all rows   */
   const float* bias;       /* [n_groups, n_cols] device, or NULL                      */
   const int32_t* dst;      /* [a.rows] device rows of out, or NULL: m                 */
-  int32_t* status;         /* device int32 [2], or NULL: [0] becomes a negative
-                              moeca_status if the kernel's bounded waits ran out
-                              (the output is then incomplete), else stays as it is    */
+  int32_t* status;         /* device int32 [2] of zeros, or NULL: [0] becomes
+                              MOECA_ERR_TIMEOUT if one of the kernel's bounded waits
+                              ran out (the output is then incomplete)                 */
   int32_t n_groups;        /* 1 .. 512 (1 where offsets is NULL)                     */
   int32_t n_cols;          /* N >= 1                                                  */
   int32_t act;             /* moeca_q8_act                                            */

@@ -155,6 +155,7 @@ cudaError_t launch_q8_write(const Q8WriteArgs& a, bool bf16, bool e5, cudaStream
 namespace {
 
 constexpr int64_t kMaxRows = 0x7fffffff;
+constexpr int64_t kMaxProductRows = 1 << 30;
 constexpr int kMaxWidth = 1 << 20, kMaxSlots = 16, kMaxGroups = 512;
 
 bool is_format(int f) { return f == MOECA_E4M3 || f == MOECA_E5M2; }
@@ -205,11 +206,19 @@ moeca_status refuse(const char* why) {
   keep_call_error(why);
   return MOECA_ERR_INVALID_ARG;
 }
-moeca_status launched(cudaError_t e) {
-  if (e == cudaSuccess) return MOECA_OK;
-  cudaGetLastError();
-  keep_call_error(cudaGetErrorString(e));
-  return MOECA_ERR_CUDA;
+// Runs a launch; nothing is thrown to the caller.
+template <typename F>
+moeca_status launched(F launch) {
+  try {
+    const cudaError_t e = launch();
+    if (e == cudaSuccess) return MOECA_OK;
+    cudaGetLastError();
+    keep_call_error(cudaGetErrorString(e));
+    return MOECA_ERR_CUDA;
+  } catch (...) {
+    keep_call_error("out of host memory");
+    return MOECA_ERR_OOM;
+  }
 }
 // Whether any buffer of `written` overlaps one of `read` or another one written.
 template <int NW, int NR>
@@ -245,7 +254,9 @@ moeca_status moeca_q8_write(const moeca_q8_write_args* a, void* stream) {
   if (any_overlap(written, read)) return refuse("the cache overlaps another buffer of the call");
   if (a->n == 0 || a->cache.rows == 0 || a->x_rows == 0) return MOECA_OK;
   const Q8WriteArgs d{device_rows(a->cache), a->x, a->x_rows, a->x_stride, a->n, a->src, a->dst, a->count};
-  return launched(launch_q8_write(d, a->dtype == MOECA_BF16, a->cache.format == MOECA_E5M2, static_cast<cudaStream_t>(stream)));
+  return launched([&] {
+    return launch_q8_write(d, a->dtype == MOECA_BF16, a->cache.format == MOECA_E5M2, static_cast<cudaStream_t>(stream));
+  });
 }
 
 moeca_status moeca_q8_read(const moeca_q8_read_args* a, void* stream) {
@@ -269,8 +280,10 @@ moeca_status moeca_q8_read(const moeca_q8_read_args* a, void* stream) {
   d.status = a->status;
   d.T = a->n;
   d.k = d.seq = 1;
-  return launched((a->dtype == MOECA_BF16 ? launch_q8_combine_bf16 : launch_q8_combine_f32)(d, a->cache.format == MOECA_E5M2,
-                                                                                            static_cast<cudaStream_t>(stream)));
+  return launched([&] {
+    return (a->dtype == MOECA_BF16 ? launch_q8_combine_bf16 : launch_q8_combine_f32)(d, a->cache.format == MOECA_E5M2,
+                                                                                     static_cast<cudaStream_t>(stream));
+  });
 }
 
 moeca_status moeca_q8_combine(const moeca_q8_combine_args* a, void* stream) {
@@ -307,8 +320,10 @@ moeca_status moeca_q8_combine(const moeca_q8_combine_args* a, void* stream) {
   d.norms = a->norms;
   d.status = a->status;
   d.T = T; d.k = a->n_slots; d.seq = a->gate ? a->seq : 1;
-  return launched((a->dtype == MOECA_BF16 ? launch_q8_combine_bf16 : launch_q8_combine_f32)(d, a->cache.format == MOECA_E5M2,
-                                                                                            static_cast<cudaStream_t>(stream)));
+  return launched([&] {
+    return (a->dtype == MOECA_BF16 ? launch_q8_combine_bf16 : launch_q8_combine_f32)(d, a->cache.format == MOECA_E5M2,
+                                                                                     static_cast<cudaStream_t>(stream));
+  });
 }
 
 moeca_status moeca_q8_matmul(const moeca_q8_matmul_args* a, void* stream) {
@@ -334,6 +349,12 @@ moeca_status moeca_q8_matmul(const moeca_q8_matmul_args* a, void* stream) {
       return refuse("out: base and row stride (bytes) aligned to the type, rows at least a row's bytes apart");
   }
   const int64_t M = a->a.rows;
+  // Rows and tiles are counted in 32 bits.
+  if (M > kMaxProductRows || a->b.rows > kMaxProductRows ||
+      (M / 16 + a->n_groups) * ((a->n_cols + 255ll) / 256) > kMaxProductRows) {
+    keep_call_error("a and b of at most 2^30 rows, (rows / 16 + n_groups) x ceil(n_cols / 256) at most 2^30");
+    return MOECA_ERR_UNSUPPORTED;
+  }
   if (!a->dst && o.rows < M) return refuse("out has fewer rows than a, and there is no dst");
   if (addr(a->offsets) % 4 || addr(a->dst) % 4 || addr(a->bias) % 4 || addr(a->status) % 4)
     return refuse("offsets, dst, bias or status is not 4-byte aligned");
@@ -348,7 +369,7 @@ moeca_status moeca_q8_matmul(const moeca_q8_matmul_args* a, void* stream) {
   d.a_e5 = a->a.format == MOECA_E5M2; d.b_e5 = a->b.format == MOECA_E5M2;
   d.out_format = o.format; d.act = a->act; d.n_groups = a->n_groups; d.n_cols = a->n_cols;
   d.offsets = a->offsets; d.dst = a->dst; d.bias = a->bias; d.status = a->status;
-  return launched(launch_q8_matmul(d, static_cast<cudaStream_t>(stream)));
+  return launched([&] { return launch_q8_matmul(d, static_cast<cudaStream_t>(stream)); });
 }
 
 }  // extern "C"

@@ -524,7 +524,9 @@ class Stack:
     def _empty(self, shape, dtype):
         return self.torch.empty(shape, dtype=dtype, device=self.device)
 
-    def get_state(self, layer: int) -> dict:
+    def get_state(self, layer: int, q8=None) -> dict:
+        """A layer's cached state.  ``q8``: a torch float8 type in which the cached branch outputs come back as
+        8-bit rows (a ``Q8`` of T k rows, about half of their bf16 bytes), for keeping many trajectories."""
         torch = self.torch
         c = self.cfg
         T = c.max_tokens
@@ -537,10 +539,18 @@ class Stack:
                  cache_y=self._empty((T, c.hidden), torch.float32) if c.token_reuse_policy else None)
         st = moeca_layer_state(**{k: (v.data_ptr() if v is not None else None) for k, v in t.items()})
         n = moeca_get_layer_state(self.handle, layer, st, self.stream_ptr())
-        return {k: (v[:n] if v is not None else None) for k, v in t.items()} | {"n_tokens": n}
+        state = {k: (v[:n] if v is not None else None) for k, v in t.items()} | {"n_tokens": n}
+        if q8 is not None:
+            rows = state["cache_h"].reshape(n * c.top_k, c.hidden)
+            state["cache_h"] = q8_write(rows, q8_empty(n * c.top_k, c.hidden, q8, self.device))
+        return state
 
     def set_state(self, layer: int, state: dict):
+        """Load a layer's cached state, as ``get_state`` gives it (branch outputs in 8 bits are read back)."""
         n = int(state["cache_e"].shape[0])
+        if isinstance(state["cache_h"], Q8):
+            rows = q8_read(state["cache_h"], dtype=self.dtype)
+            state = dict(state, cache_h=rows.view(n, self.cfg.top_k, self.cfg.hidden))
         keep = {k: v.contiguous() for k, v in state.items() if k != "n_tokens" and v is not None}
         st = moeca_layer_state(**{k: keep[k].data_ptr() if k in keep else None
                                   for k in ("cache_e", "cache_w", "cache_norm", "cache_h", "shared_h", "ema",

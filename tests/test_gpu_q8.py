@@ -503,3 +503,126 @@ def test_repeats_give_the_same_bits(M):
         part = M.Q8(a.q[:n], a.scale[:n])
         one = M.q8_matmul(part, M.Q8(b.q[:500], b.scale[:500]), dtype=torch.float32)
         assert torch.equal(one, M.q8_matmul(part, M.Q8(b.q[:500], b.scale[:500]), dtype=torch.float32))
+
+
+# --- sizes and paths at the edges --------------------------------------------
+
+@pytest.mark.parametrize("T,k,D", [(400, 9, 2600), (310, 16, 9000), (305, 2, 30001), (320, 3, 8), (5000, 2, 24)])
+@pytest.mark.parametrize("off", [0, 1])
+def test_combine_wide_and_narrow_rows(M, T, k, D, off):
+    """Rows that fit no shared-memory buffer, and many tokens of a few values; aligned and not."""
+    rng = np.random.default_rng(D)
+    c, h = filled(M, 5, 700, D, "e4m3")
+    rows = rng.integers(-2, 700, (T, k)).astype(np.int32)
+    w = rng.standard_normal((T, k)).astype(np.float32)
+    x = activations(3, T, D + off, "bf16")[:, off:]
+    out = torch.full((T, D + 3 * off), 9.0, dtype=torch.bfloat16, device="cuda")
+    got, norms = M.q8_combine(c, torch.from_numpy(rows).cuda(), torch.from_numpy(w).cuda(), x=x,
+                              out=out[:, 2 * off:2 * off + D], norms=True)
+    want, wn = O.combine(h, rows, w, f64(x))
+    big, _ = O.combine(np.abs(h), rows, np.abs(w), np.abs(f64(x)))
+    err = (k + 3) * 2.0 ** -23 * big
+    assert (np.abs(f64(got) - want) <= err + HALF["bf16"] * (np.abs(want) + err)).all()
+    assert (np.abs(f64(norms) - wn) <= (D + 4) * 2.0 ** -24 * wn).all()
+    assert bool((out[:, :2 * off] == 9).all()) and bool((out[:, 2 * off + D:] == 9).all())
+
+
+def test_offsets_past_32_bits(M):
+    """Rows whose bytes lie past 2^32: written, read back, combined, multiplied, scattered."""
+    rows, D = 4_200_000, 1024
+    c = M.Q8(torch.empty((rows, D), dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn),
+             torch.empty((rows, 8), dtype=torch.uint8, device="cuda"))
+    at = [rows - 1, 5, rows - 400, 4_194_304, 4_194_303, 17]
+    x = activations(1, 6, D, "bf16")
+    M.q8_write(x, c, dst=ints(at))
+    same(c, x, "e4m3", at)
+    q, e = O.quantise(f64(x), "e4m3")
+    h = O.dequantise(q, e)
+    np.testing.assert_array_equal(f64(M.q8_read(c, ints(at), dtype=torch.float32)), h)
+    for many in (1, 60):  # both forms of the kernel
+        got = M.q8_combine(c, ints([at] * many), dtype=torch.float32)
+        np.testing.assert_allclose(f64(got), np.repeat(h.sum(0)[None], many, 0), rtol=2 ** -20, atol=2 ** -18 * np.abs(h).max())
+    got = M.q8_read(c, ints(at * 60), dtype=torch.float32)
+    np.testing.assert_array_equal(f64(got), np.tile(h, (60, 1)))
+    b, bv = filled(M, 2, 1024, D, "e4m3")
+    small = M.q8_write(x, M.q8_empty(6, D))
+    z, _, big = O.matmul(h, bv, [0, 6], 1024)
+    check = lambda v: (np.abs(v - z) <= (D + 2) * 2.0 ** -23 * big + HALF["bf16"] * np.abs(z)).all()  # noqa: E731
+    tail = M.Q8(c.q[rows - 400:], c.scale[rows - 400:])  # a's own rows far into memory
+    a_all = M.q8_matmul(tail, b, dtype=torch.float32)
+    assert check(np.stack([f64(a_all[399]), f64(M.q8_matmul(small, b, dtype=torch.float32))[1], f64(a_all[0]),
+                           *[f64(M.q8_matmul(small, b, dtype=torch.float32))[i] for i in (3, 4, 5)]]))
+    out = c.q.view(torch.bfloat16)[:, :512]  # 8.6 GB seen as bf16 rows of half a width
+    b2 = M.Q8(b.q[:512], b.scale[:512])
+    M.q8_matmul(small, b2, dst=ints(at), out=out)
+    assert (np.abs(f64(out[torch.tensor(at)]) - z[:, :512]) <= (D + 2) * 2.0 ** -23 * big[:, :512]
+            + HALF["bf16"] * (np.abs(z[:, :512]) + 1e-30)).all()
+
+
+def test_matmul_many_groups_and_tiles(M):
+    """512 groups, most of a single row, one large; every tile width of a group's rows."""
+    rng = np.random.default_rng(0)
+    sizes = rng.integers(0, 3, 511).tolist() + [900]
+    run_matmul(M, sizes, 40, 96)
+    run_matmul(M, list(range(1, 60, 3)) + [100, 150, 223, 224, 225, 230, 448, 449], 130, 160, out="e4m3", bias=True)
+
+
+def test_first_call_of_a_process_may_be_captured(M):
+    """A captured call needs no eager one before it."""
+    import subprocess
+    import sys
+    from pathlib import Path
+    code = """
+import torch
+from paper_2606_15615_gb300 import moeca as M
+x = torch.randn(40, 256, device="cuda")
+rows8, out8, big = M.q8_empty(40, 256), M.q8_empty(40, 128), M.q8_empty(700, 256)
+w = M.q8_empty(128, 256)
+rows = torch.zeros(600, 2, dtype=torch.int32, device="cuda")
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    M.q8_write(x, rows8)
+    M.q8_write(torch.ones_like(x), w, src=torch.zeros(128, dtype=torch.int32, device="cuda"))
+    M.q8_matmul(rows8, w, out=out8)
+    y = M.q8_read(out8, dtype=torch.float32)
+    z = M.q8_combine(rows8, rows, dtype=torch.float32)
+g.replay()
+torch.cuda.synchronize()
+want = M.q8_read(rows8, dtype=torch.float32)
+assert torch.allclose(y, want.sum(1, keepdim=True).expand(-1, 128), rtol=0.07, atol=1e-3)
+assert torch.allclose(z, 2 * want[:1].expand(600, -1))
+"""
+    root = Path(__file__).resolve().parents[1]
+    subprocess.run([sys.executable, "-c", code], check=True, cwd=root, timeout=300)
+
+
+def test_stack_snapshot_in_8_bits(M):
+    """A stack's state with its branch outputs in 8 bits: half the bytes, and a resumed trajectory whose reused
+    branches are off by the format's rounding."""
+    from paper_2606_15615_gb300 import workloads as W
+    T, D, E, k, F = 256, 128, 8, 2, 256
+    w = W.tiny_layer(41, T, D, E, k, F, dtype="bf16", wscale=0.05)[0]
+    cfg = M.moeca_config_default(n_layers=1, hidden=D, ffn=F, n_experts=E, top_k=k, max_tokens=T, tau0=0.75)
+    x = torch.randn(T, D, device="cuda").bfloat16()
+    x2 = (x.float() + 0.05 * torch.randn_like(x.float())).bfloat16()
+    s = M.Stack(cfg, [w])
+    s.step(x, 1)
+    exact, small = s.get_state(0), s.get_state(0, q8=torch.float8_e4m3fn)
+    assert isinstance(small["cache_h"], M.Q8) and small["cache_h"].q.shape == (T * k, D)
+    same(small["cache_h"], exact["cache_h"].reshape(T * k, D), "e4m3")
+    assert torch.equal(small["cache_norm"], exact["cache_norm"]) and torch.equal(small["ema"], exact["ema"])
+    want = s.step(x2, 1)
+    s.set_state(0, small)
+    back = s.get_state(0)
+    h = M.q8_read(small["cache_h"]).view(T, k, D)
+    assert torch.equal(back["cache_h"], h) and torch.equal(back["cache_e"], exact["cache_e"])
+    got = s.step(x2, 1)
+    st = s.stats()
+    assert st["device_status"] == 0 and st["reused"] > 0
+    # Decisions read norms and weights, which are exact: only reused rows differ, by at most half a step of each.
+    tr = s.get_trace(0, T)
+    reused = (tr["recompute"] == 0).double()
+    bound = (reused * tr["route_w"].double()).sum(1, keepdim=True) * 2.0 ** -4 * exact["cache_h"].double().abs().amax((1, 2))[:, None]
+    assert bool(((got.double() - want.double()).abs() <= bound + 2.0 ** -7 * want.double().abs()).all())
+    s.close()

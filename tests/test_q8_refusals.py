@@ -119,6 +119,16 @@ def test_matmul_output_refusals(M):
     assert M.LIB.moeca_q8_write(None, None) == M.LIB.moeca_q8_read(None, None) == -1
 
 
+def test_products_too_large_to_count_are_unsupported(M):
+    far = 1 << 20  # 2^40 bytes
+    wide = rows(M, 2 * far, n=1 << 30, width=1 << 12, q_stride=1 << 12, scale_stride=32)
+    for args in (matmul_args(M, a=rows(M, far, n=(1 << 30) + 1)),
+                 matmul_args(M, a=rows(M, far, n=1 << 30), b=rows(M, 9, n=1 << 12), n_groups=1, n_cols=1 << 12, out=wide)):
+        with pytest.raises(M.MoecaError) as e:
+            M.moeca_q8_matmul(args)
+        assert e.value.status == M.MOECA_ERR_UNSUPPORTED
+
+
 def test_empty_calls_launch_nothing(M):
     """No rows: OK without a device."""
     M.moeca_q8_write(write_args(M, n=0))
