@@ -188,38 +188,40 @@ __device__ __forceinline__ float rcp(float x) {
 template <int ACT>
 __device__ __forceinline__ void activate(float (&z)[32]) {
   constexpr float kLog2e = 1.44269504f;
+  const auto both = [](float v) { return make_float2(v, v); };
   if constexpr (ACT != MOECA_ACT_NONE) {
 #pragma unroll
     for (int i0 = 0; i0 < 32; i0 += 8) {
-      float d[8];
+      float2 v[4], d[4];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float v = z[i0 + i];
+      for (int i = 0; i < 4; ++i) {
+        v[i] = make_float2(z[i0 + 2 * i], z[i0 + 2 * i + 1]);
         if constexpr (ACT == MOECA_ACT_GELU_TANH) {
-          const float w = v * fmaf(-0.0713548163f * kLog2e, v * v, -1.5957691216f * kLog2e);  // -2 u log2(e)
-          d[i] = 1.f + ex2(fminf(w, 60.f));
+          const float2 w = mul2(v[i], fma2(both(-0.0713548163f * kLog2e), mul2(v[i], v[i]), both(-1.5957691216f * kLog2e)));
+          d[i] = add2(both(1.f), make_float2(ex2(fminf(w.x, 60.f)), ex2(fminf(w.y, 60.f))));  // w = -2 u log2(e)
         } else {
-          d[i] = fmaf(0.3275911f * 0.70710678f, fminf(fabsf(v), 1e18f), 1.f);
+          d[i] = fma2(both(0.3275911f * 0.70710678f), make_float2(fminf(fabsf(v[i].x), 1e18f), fminf(fabsf(v[i].y), 1e18f)), both(1.f));
         }
       }
 #pragma unroll
-      for (int i = 0; i < 8; i += 2) {
-        const float r = rcp(d[i] * d[i + 1]), t = d[i + 1] * r;
-        d[i + 1] = d[i] * r;
-        d[i] = t;
-      }
+      for (int i = 0; i < 4; ++i) d[i] = mul2(both(rcp(d[i].x * d[i].y)), make_float2(d[i].y, d[i].x));
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float v = z[i0 + i], t = d[i];
+      for (int i = 0; i < 4; ++i) {
+        const float2 t = d[i];
+        float2 r;
         if constexpr (ACT == MOECA_ACT_GELU_TANH) {
-          z[i0 + i] = v * t;
+          r = mul2(v[i], t);
         } else {
-          float s = fmaf(0.5f * 1.061405429f, t, 0.5f * -1.453152027f);
-          s = fmaf(s, t, 0.5f * 1.421413741f);
-          s = fmaf(s, t, 0.5f * -0.284496736f);
-          s = fmaf(s, t, 0.5f * 0.254829592f);
-          z[i0 + i] = fmaxf(v, 0.f) - s * t * ex2(-0.5f * kLog2e * v * v) * fabsf(v);  // |z| Phi(-|z|)
+          float2 s = fma2(both(0.5f * 1.061405429f), t, both(0.5f * -1.453152027f));
+          s = fma2(s, t, both(0.5f * 1.421413741f));
+          s = fma2(s, t, both(0.5f * -0.284496736f));
+          s = fma2(s, t, both(0.5f * 0.254829592f));
+          const float2 w = mul2(v[i], mul2(v[i], both(-0.5f * kLog2e)));
+          const float2 tail = mul2(mul2(s, t), mul2(make_float2(ex2(w.x), ex2(w.y)), make_float2(fabsf(v[i].x), fabsf(v[i].y))));
+          r = make_float2(fmaxf(v[i].x, 0.f) - tail.x, fmaxf(v[i].y, 0.f) - tail.y);  // tail: |z| Phi(-|z|)
         }
+        z[i0 + 2 * i] = r.x;
+        z[i0 + 2 * i + 1] = r.y;
       }
     }
   }
@@ -366,10 +368,9 @@ __device__ __forceinline__ void store_chunk(const MatmulParams& p, Shared& sh, f
 #pragma unroll
     for (int t = 0; t < 8; ++t) {
       const float4 s = *reinterpret_cast<const float4*>(inv + 4 * t);
-      z[4 * t] *= s.x;
-      z[4 * t + 1] *= s.y;
-      z[4 * t + 2] *= s.z;
-      z[4 * t + 3] *= s.w;
+      const float2 lo = mul2(make_float2(z[4 * t], z[4 * t + 1]), make_float2(s.x, s.y));
+      const float2 hi = mul2(make_float2(z[4 * t + 2], z[4 * t + 3]), make_float2(s.z, s.w));
+      z[4 * t] = lo.x; z[4 * t + 1] = lo.y; z[4 * t + 2] = hi.x; z[4 * t + 3] = hi.y;
       word[t] = encode2<E5>(z[4 * t], z[4 * t + 1]) | encode2<E5>(z[4 * t + 2], z[4 * t + 3]) << 16;
     }
     if (odd) {
@@ -704,7 +705,11 @@ __global__ void __launch_bounds__(kThreads, 1) q8_matmul_kernel(const __grid_con
           if (lane == 0) arrive_relaxed(tempty0 + acc * 8);
         }
 #pragma unroll
-        for (int i = 0; i < 32; ++i) z[i] += bias;
+        for (int i = 0; i < 32; i += 2) {
+          const float2 v = add2(make_float2(z[i], z[i + 1]), make_float2(bias, bias));
+          z[i] = v.x;
+          z[i + 1] = v.y;
+        }
         activate<ACT>(z);
         const int row = rows[0];
 #pragma unroll
