@@ -213,7 +213,7 @@ __global__ void __launch_bounds__(kDirectWarps * 32) q8_combine_kernel(const Q8C
 //
 // Rows of x and out that do not start at 16 bytes (VEC false): x is copied in
 // the aligned pieces that hold it and shifted as it is read; out is put
-// together in the buffer at its own offset and leaves it in aligned pieces.
+// together in the buffer and leaves it in aligned pieces.
 // ---------------------------------------------------------------------------
 constexpr int kStageWarps = 2;
 constexpr int kStageSm = 227 * 1024, kStageMax = 112 * 1024;  // shared memory of an SM, and the most a block takes
@@ -235,7 +235,7 @@ __host__ __device__ inline StageLayout stage_layout(int k, int width, bool x) {
   s.words = (s.blocks + 3) / 4;
   s.x_at = k * s.row;
   s.out_at = s.x_at + (x ? s.value + 16 : 0);  // a last piece may be read past the copied ones
-  s.word_at = s.out_at + (VEC ? 0 : s.value);
+  s.word_at = s.out_at + (VEC ? 0 : s.value + 32);  // a piece before the first and one after the last may be read
   s.scale_at = (s.word_at + k * s.words * 4 + 15) / 16 * 16;
   s.bytes = (s.scale_at + k * s.blocks * 4 + 15) / 16 * 16;
   return s;
@@ -283,10 +283,9 @@ __global__ void __launch_bounds__(kStageWarps * 32, stage_blocks(KMAX)) q8_combi
     __syncwarp();
     if (row >= 0) bulk_g2s(smem_u32(buf + lane * L.row), a.c.q + row * a.c.q_stride, L.row, bar);
     if (lane == 31 && x) bulk_g2s(smem_u32(buf + L.x_at), xr - m, x_bytes, bar);
-    for (int j = lane; j < k * L.words; j += 32) {  // the scales, four blocks at a time
-      const int p = j / L.words;
-      const int r = a.rows ? __ldg(a.rows + i * k + p) : static_cast<int>(i);
-      if (r >= 0 && r < a.c.rows)
+    for (int j0 = 0; j0 < k * L.words; j0 += 32) {  // the scales, four blocks at a time
+      const int j = j0 + lane, p = min(j / L.words, k - 1), r = __shfl_sync(0xffffffffu, row, p);
+      if (j < k * L.words && r >= 0)
         asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(buf + L.word_at + j * 4)),
                      "l"(a.c.scale + r * a.c.scale_stride + (j - p * L.words) * 4)
                      : "memory");
@@ -373,25 +372,30 @@ __global__ void __launch_bounds__(kStageWarps * 32, stage_blocks(KMAX)) q8_combi
             if (t < left) out[c * W + t] = Elem<TI>::from_f(o[t]);
         }
       } else {
-        TI* to = reinterpret_cast<TI*>(buf + L.out_at + mo) + c * W;
 #pragma unroll
-        for (int t = 0; t < W; ++t)
-          if (t < left) to[t] = Elem<TI>::from_f(o[t]);
+        for (int j = 0; j < NV; ++j)
+          store_vec(reinterpret_cast<TI*>(buf + L.out_at + 16) + c * W + j * V, &o[j * V]);
       }
     }
     __syncwarp();  // all have read the slots and x
     if constexpr (!VEC) {
-      // out's aligned pieces; its first and last values alone where a piece is another row's too.
+      // out's aligned pieces, each from the two staged ones that it straddles; its
+      // first and last values alone where a piece is another row's too.
       const uint32_t end = mo + width * sizeof(TI);
       uint8_t* base = reinterpret_cast<uint8_t*>(out) - mo;
       for (uint32_t t = lane * 16; t < end; t += 512) {
-        const uint8_t* from = buf + L.out_at + t;
+        const uint4* staged = reinterpret_cast<const uint4*>(buf + L.out_at + t + (mo ? 0 : 16));
+        const uint4 v = shifted<TI>(staged[0], staged[1], mo ? 16 - mo : 0u);
         if (t >= mo && t + 16 <= end) {
-          *reinterpret_cast<uint4*>(base + t) = *reinterpret_cast<const uint4*>(from);
+          *reinterpret_cast<uint4*>(base + t) = v;
         } else {
+          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-          for (uint32_t q = 0; q < 16; q += sizeof(TI))
-            if (t + q >= mo && t + q < end) *reinterpret_cast<TI*>(base + t + q) = *reinterpret_cast<const TI*>(from + q);
+          for (uint32_t q = 0; q < 16; q += sizeof(TI)) {
+            if (t + q < mo || t + q >= end) continue;
+            if constexpr (sizeof(TI) == 2) *reinterpret_cast<uint16_t*>(base + t + q) = static_cast<uint16_t>(w[q / 4] >> 8 * (q & 3));
+            else *reinterpret_cast<uint32_t*>(base + t + q) = w[q / 4];
+          }
         }
       }
       __syncwarp();

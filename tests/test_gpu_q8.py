@@ -297,6 +297,10 @@ def run_matmul(M, sizes, N, K, a_fmt="e4m3", b_fmt="e4m3", out="bf16", act="none
     if out in TYPES:
         check_rows(f64(o.q)[at], exps(o.scale)[at], z, err, out)
         assert torch.equal(o.q.view(torch.uint8)[rest], before[0][rest]) and torch.equal(o.scale[rest], before[1][rest])
+        if out_rows > 1:  # the bytes past the rows' widths stay as they were
+            pad = o.q.view(torch.uint8).as_strided((out_rows, o.q.stride(0)), (o.q.stride(0), 1))[:, N:]
+            spad = o.scale.as_strided((out_rows, o.scale.stride(0)), (o.scale.stride(0), 1))[:, o.scale.shape[1]:]
+            assert bool((pad == 0x7f).all()) and bool((spad == 0xff).all())
     else:
         assert (np.abs(f64(o)[at] - z) <= err + HALF[out] * (np.abs(z) + err)).all()
         assert bool((o[rest] == 7).all())
@@ -307,6 +311,7 @@ SHAPES = [  # rows of each group, columns, inner
     ([33], 256, 64), ([64], 1000, 513), ([128], 384, 384), ([200], 129, 640), ([257], 513, 1024), ([700], 768, 256),
     ([1, 1], 200, 300), ([1, 0, 3, 0], 96, 130), ([0, 0, 0], 64, 64), ([31, 32, 33, 1, 64], 256, 1152),
     ([130, 0, 300, 7], 250, 700), ([3] * 40, 64, 200), ([193, 385, 96], 640, 2000),
+    ([3, 40], 20, 70001),
 ]
 
 
