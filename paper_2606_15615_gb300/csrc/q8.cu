@@ -42,16 +42,26 @@ __global__ void __launch_bounds__(kWriteThreads, kWriteBlocks) q8_write_kernel(c
   const int64_t step = static_cast<int64_t>(gridDim.x) * (kWriteThreads / 8);
   const int64_t first = static_cast<int64_t>(blockIdx.x) * (kWriteThreads / 8) + (threadIdx.x >> 5) * 4;
   const TI* x = static_cast<const TI*>(a.x);
-  const auto fetch = [&](int64_t u) {
+  // The entry and block of the next unit to fetch; a step further without a division.
+  int64_t entry = (first + (lane >> 3)) / nb;
+  int block = static_cast<int>(first + (lane >> 3) - entry * nb);
+  const int64_t step_entries = step / nb;
+  const int step_blocks = static_cast<int>(step - step_entries * nb);
+  const auto fetch = [&] {
     WriteUnit<J> w;
     w.row = -1;
-    w.block = w.left = 0;
+    w.block = block;
+    w.left = 0;
 #pragma unroll
     for (int j = 0; j < J; ++j) w.raw[j] = make_uint4(0u, 0u, 0u, 0u);
-    if (u >= total) return w;
-    const int i = total <= 0xffffffffll ? static_cast<int>(static_cast<uint32_t>(u) / static_cast<uint32_t>(nb))
-                                        : static_cast<int>(u / nb);
-    w.block = static_cast<int>(u - static_cast<int64_t>(i) * nb);
+    if (entry >= n) return w;
+    const int i = static_cast<int>(entry);
+    entry += step_entries;
+    block += step_blocks;
+    if (block >= nb) {
+      block -= nb;
+      ++entry;
+    }
     w.left = width - w.block * kQ8Block;
     const int r = a.src ? __ldg(a.src + i) : i, d = a.dst ? __ldg(a.dst + i) : i;
     if (r < 0 || r >= a.x_rows || d < 0 || d >= a.c.rows) return w;
@@ -76,17 +86,36 @@ __global__ void __launch_bounds__(kWriteThreads, kWriteBlocks) q8_write_kernel(c
     return w;
   };
   const auto store = [&](const WriteUnit<J>& u) {
-    float v[16];
+    uint32_t raw[4 * J];
 #pragma unroll
-    for (int j = 0; j < J; ++j) unpack_vec(u.raw[j], &v[V * j], static_cast<TI*>(nullptr));
+    for (int j = 0; j < J; ++j) {
+      raw[4 * j] = u.raw[j].x; raw[4 * j + 1] = u.raw[j].y; raw[4 * j + 2] = u.raw[j].z; raw[4 * j + 3] = u.raw[j].w;
+    }
     if (u.left < kQ8Block) {  // what lies past the row's end counts for nothing
 #pragma unroll
-      for (int t = 0; t < 16; ++t)
-        if (V * (l + 8 * (t / V)) + t % V >= u.left) v[t] = 0.f;
+      for (int t = 0; t < 4 * J; ++t) {
+        const int past = V * (l + 8 * (t / 4)) + t % 4 * (V / 4) - u.left;  // >= 0: all of the word
+        raw[t] &= past >= 0 ? 0u : V == 8 && past == -1 ? 0xffffu : 0xffffffffu;
+      }
     }
+    float v[16];
     uint32_t top = 0;
+    if constexpr (V == 8) {  // two bf16 magnitudes at a time
 #pragma unroll
-    for (int t = 0; t < 16; ++t) top = max(top, abs_bits(v[t]));
+      for (int t = 0; t < 4 * J; ++t) top = __vmaxu2(top, raw[t] & 0x7fff7fffu);
+      top = max(top << 16, top & 0xffff0000u);
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        v[2 * t] = __uint_as_float(raw[t] << 16);
+        v[2 * t + 1] = __uint_as_float(raw[t] & 0xffff0000u);
+      }
+    } else {
+#pragma unroll
+      for (int t = 0; t < 16; ++t) {
+        top = max(top, raw[t] & 0x7fffffffu);
+        v[t] = __uint_as_float(raw[t]);
+      }
+    }
 #pragma unroll
     for (int o = 4; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
     const bool odd = top >= kNonFinite;  // the same for the block's 8 lanes
@@ -105,8 +134,11 @@ __global__ void __launch_bounds__(kWriteThreads, kWriteBlocks) q8_write_kernel(c
     uint8_t* out = a.c.q + u.row * a.c.q_stride + u.block * kQ8Block;
     uint32_t w[4];
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
-      w[t] = encode2<E5>(v[4 * t] * inv, v[4 * t + 1] * inv) | encode2<E5>(v[4 * t + 2] * inv, v[4 * t + 3] * inv) << 16;
+    for (int t = 0; t < 4; ++t) {
+      const float2 lo = mul2(make_float2(v[4 * t], v[4 * t + 1]), make_float2(inv, inv));
+      const float2 hi = mul2(make_float2(v[4 * t + 2], v[4 * t + 3]), make_float2(inv, inv));
+      w[t] = __byte_perm(encode2<E5>(lo.x, lo.y), encode2<E5>(hi.x, hi.y), 0x5410);
+    }
     if (odd) {
 #pragma unroll
       for (int t = 0; t < 16; ++t) w[t >> 2] += abs_bits(v[t]) == kNonFinite ? 1u << 8 * (t & 3) : 0u;
@@ -124,10 +156,10 @@ __global__ void __launch_bounds__(kWriteThreads, kWriteBlocks) q8_write_kernel(c
       }
     }
   };
-  WriteUnit<J> next = fetch(first + (lane >> 3));
+  WriteUnit<J> next = fetch();
   for (int64_t base = first; base < total; base += step) {  // base: the warp's first unit
     const WriteUnit<J> now = next;
-    next = fetch(base + step + (lane >> 3));
+    next = fetch();
     store(now);
   }
 }
