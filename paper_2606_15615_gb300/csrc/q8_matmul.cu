@@ -690,7 +690,7 @@ __global__ void __launch_bounds__(kThreads, 1) q8_matmul_kernel(const __grid_con
       tc_fence_after();
       const uint32_t tb = tmem + (static_cast<uint32_t>(quad * 32) << 16) + static_cast<uint32_t>(acc * kMaxN);
       int c = first * 32;
-      first = (first + 2) % kParts;
+      first = (first + 1) % kParts;
       if (c >= cols) {
         tc_fence_before();
         __syncwarp();

@@ -726,9 +726,13 @@ def q8_read(cache: Q8, rows=None, dtype=None, out=None, status=None, stream: int
     if out is None:
         torch = _TYPES["torch"]
         out = torch.empty((n, c[5]), dtype=dtype or torch.bfloat16, device=cache[0].device)
-    address, n_out, stride, width, code = _value_fields(out, "out", dev)
-    if n_out != n or width != c[5] or (dtype is not None and out.dtype != dtype):
-        raise ValueError(f"out must be [{n}, {c[5]}] of the asked dtype")
+        address, stride, code = out.data_ptr(), c[5], _TYPES.get(out.dtype, -1)
+        if not MOECA_F32 <= code <= MOECA_BF16:
+            raise ValueError("dtype must be float32 or bfloat16")
+    else:
+        address, n_out, stride, width, code = _value_fields(out, "out", dev)
+        if n_out != n or width != c[5] or (dtype is not None and out.dtype != dtype):
+            raise ValueError(f"out must be [{n}, {c[5]}] of the asked dtype")
     args = _PACK_READ.pack(*c, address, stride, code, n, _list(rows, "i32", (n,), "rows", dev), _list(status, "i32", (2,), "status", dev))
     _call(_q8_packed[1], args, dev, stream)
     return out
@@ -741,7 +745,8 @@ def q8_combine(cache: Q8, rows, weights=None, x=None, gate=None, norms=False, dt
     ``gate`` [B, D] fp32, one row for each T / B consecutive tokens.  ``norms``: True or a [T, k] fp32 tensor
     also gives the rows' 2-norms.  The result has x's dtype (without x: ``dtype``, default bf16); ``out`` may be
     x.  Returns out, or (out, norms)."""
-    dev = cache[0].get_device()
+    q = cache[0]
+    dev = q.get_device()
     c = _q8_fields(cache, "cache", dev)
     shape = rows.shape
     if len(shape) != 2:
@@ -756,22 +761,28 @@ def q8_combine(cache: Q8, rows, weights=None, x=None, gate=None, norms=False, dt
         if n_x != T or x_width != width:
             raise ValueError(f"x must be [{T}, {width}]")
     if out is None:
-        out = torch.empty((T, width), dtype=x.dtype if x is not None else dtype or torch.bfloat16, device=rows.device)
-    address, n_out, stride, o_width, o_code = _value_fields(out, "out", dev)
-    if n_out != T or o_width != width or (x is not None and o_code != code):
-        raise ValueError(f"out must be [{T}, {width}] of x's dtype")
+        out = torch.empty((T, width), dtype=x.dtype if x is not None else dtype or torch.bfloat16, device=q.device)
+        address, stride, o_code = out.data_ptr(), width, _TYPES.get(out.dtype, -1)
+        if not MOECA_F32 <= o_code <= MOECA_BF16:
+            raise ValueError("dtype must be float32 or bfloat16")
+    else:
+        address, n_out, stride, o_width, o_code = _value_fields(out, "out", dev)
+        if n_out != T or o_width != width or (x is not None and o_code != code):
+            raise ValueError(f"out must be [{T}, {width}] of x's dtype")
     if gate is not None:
         gate_address, n_g, gate_stride, g_width, g_code = _value_fields(gate, "gate", dev)
         if g_code != MOECA_F32 or g_width != width or (T and (not n_g or T % n_g)):
             raise ValueError("gate must be float32 rows, one for each T / rows consecutive tokens")
         seq = T // n_g if T else 1
     if norms is True:
-        norms = torch.empty(shape, dtype=torch.float32, device=rows.device)
-    elif norms is False:
-        norms = None
+        norms = torch.empty(shape, dtype=torch.float32, device=q.device)
+        n_address = norms.data_ptr()
+    else:
+        norms = None if norms is False else norms
+        n_address = _list(norms, "f32", shape, "norms", dev)
     args = _PACK_COMBINE.pack(
         *c, _list(rows, "i32", shape, "rows", dev), _list(weights, "f32", shape, "weights", dev), x_address, x_stride,
-        gate_address, gate_stride, address, stride, _list(norms, "f32", shape, "norms", dev), o_code, T, k, seq,
+        gate_address, gate_stride, address, stride, n_address, o_code, T, k, seq,
         _list(status, "i32", (2,), "status", dev))
     _call(_q8_packed[2], args, dev, stream)
     return out if norms is None else (out, norms)

@@ -349,6 +349,29 @@ def test_matmul_scales_far_apart(M, rows):
 
 
 @pytest.mark.parametrize("rows", [3, 150])
+@pytest.mark.parametrize("ea,eb", [(-70, -62), (-70, -70), (61, 60), (62, 62)])
+def test_matmul_tiny_and_huge_results(M, rows, ea, eb):
+    """Results among fp32's subnormals keep their digits; past its largest value they are infinite, NaN in e4m3."""
+    a, _ = filled(M, 1, rows, 256, "e4m3")
+    b, _ = filled(M, 2, 96, 256, "e4m3")
+    for c, e in ((a, ea), (b, eb)):
+        c.scale.copy_(torch.full(c.scale.shape, 127 + e, dtype=torch.uint8))
+    z, _, big = O.matmul(O.dequantise(f64(a.q), exps(a.scale)), O.dequantise(f64(b.q), exps(b.scale)), [0, rows], 96)
+    err = 258 * 2.0 ** -23 * big + 2.0 ** -148  # and a few steps of the subnormals
+    got = f64(M.q8_matmul(a, b, dtype=torch.float32))
+    most = float(np.finfo(np.float32).max)
+    over = np.abs(z) > most * (1 + 2.0 ** -10)
+    fine = (np.abs(z) < most * (1 - 2.0 ** -10)) & (big < most)
+    assert np.isinf(got[over]).all() and (np.abs(got[fine] - z[fine]) <= err[fine]).all()
+    q = M.q8_matmul(a, b, dtype=torch.float8_e4m3fn)
+    if over.any():
+        assert np.isnan(f64(q.q)[over]).all()
+        assert not np.isnan(f64(q.q)[fine]).any()
+    else:
+        check_rows(f64(q.q), exps(q.scale), z, err, "e4m3")
+
+
+@pytest.mark.parametrize("rows", [3, 150])
 def test_matmul_non_finite_rows_stay_apart(M, rows):
     """A row of NaN, a NaN scale and an infinity reach their own results only."""
     a, av = filled(M, 1, rows, 260, "e5m2")
