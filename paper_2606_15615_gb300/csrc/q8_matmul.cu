@@ -31,7 +31,7 @@
 //               quadrants exchange them through shared memory, and 4 x 4 byte
 //               transposes among lanes make words of four features.
 // 16384 x 6912 x 2560 to bf16 takes 171 us (3.4 PFLOP/s, the tensor pipe 0.90
-// active under the power cap); 8192 x 4608 x 1152 in 16 groups 52 us to bf16 and 62
+// active under the power cap); 8192 x 4608 x 1152 in 16 groups 52 us to bf16 and 66
 // with GELU to e4m3, where the epilogue's issue slots bound it; 8192 x 1152 x 4608
 // 52 us (240 tiles are four rounds of 76 pairs); two rows of 16 experts' 4608 x 1152
 // 7 us.  224 tokens, not 192: a stage's fills and hand-overs cost the same for
@@ -184,10 +184,11 @@ __device__ __forceinline__ float rcp(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// GELU of a chunk's values (Eq. 5).  tanh form: z sigmoid(2 u), u = sqrt(2/pi) (z + 0.044715 z^3).
-// erf form: Phi(-|z|) = erfc(|z| / sqrt 2) / 2 by Abramowitz and Stegun's
-// formula 7.1.26, P(t) exp(-z^2 / 2) / 2 with t = 1 / (1 + p |z| / sqrt 2), within
-// 0.75e-7; z Phi(z) is z - z Phi(-z) or z Phi(-|z|), so that nothing cancels.
+// GELU of a chunk's values (Eq. 5), z (1 + h) / 2 with h in fp32 as gelu_f has it:
+// where h rounds to -1 the result is 0, so that an 8-bit block of nothing else
+// has the scale of zeros.  tanh form: h = 2 sigmoid(2 u) - 1, u = sqrt(2/pi) (z + 0.044715 z^3).
+// erf form: |h| = erf(|z| / sqrt 2) by Abramowitz and Stegun's formula 7.1.26,
+// 1 - P(t) exp(-z^2 / 2) with t = 1 / (1 + p |z| / sqrt 2), within 1.5e-7.
 // Two values share one reciprocal, 1/a = b / (ab): the special-function unit
 // takes 8 clocks a warp for it, and the pairs' chains interleave (28 -> 11
 // clocks a value at two warps per scheduler).  The minima keep ab finite and
@@ -216,16 +217,17 @@ __device__ __forceinline__ void activate(float (&z)[32]) {
       for (int i = 0; i < 4; ++i) {
         const float2 t = d[i];
         float2 r;
+        const float2 half = mul2(v[i], both(0.5f));
         if constexpr (ACT == MOECA_ACT_GELU_TANH) {
-          r = mul2(v[i], t);
+          r = fma2(half, fma2(both(2.f), t, both(-1.f)), half);
         } else {
-          float2 s = fma2(both(0.5f * 1.061405429f), t, both(0.5f * -1.453152027f));
-          s = fma2(s, t, both(0.5f * 1.421413741f));
-          s = fma2(s, t, both(0.5f * -0.284496736f));
-          s = fma2(s, t, both(0.5f * 0.254829592f));
-          const float2 w = mul2(v[i], mul2(v[i], both(-0.5f * kLog2e)));
-          const float2 tail = mul2(mul2(s, t), mul2(make_float2(ex2(w.x), ex2(w.y)), make_float2(fabsf(v[i].x), fabsf(v[i].y))));
-          r = make_float2(fmaxf(v[i].x, 0.f) - tail.x, fmaxf(v[i].y, 0.f) - tail.y);  // tail: |z| Phi(-|z|)
+          float2 s = fma2(both(1.061405429f), t, both(-1.453152027f));
+          s = fma2(s, t, both(1.421413741f));
+          s = fma2(s, t, both(-0.284496736f));
+          s = fma2(s, t, both(0.254829592f));
+          const float2 w = mul2(v[i], mul2(half, both(-kLog2e)));
+          const float2 rest = mul2(mul2(s, t), make_float2(-ex2(w.x), -ex2(w.y)));  // -erfc(|z| / sqrt 2)
+          r = fma2(make_float2(fabsf(half.x), fabsf(half.y)), add2(both(1.f), rest), half);
         }
         z[i0 + 2 * i] = r.x;
         z[i0 + 2 * i + 1] = r.y;

@@ -348,6 +348,23 @@ def test_matmul_scales_far_apart(M, rows):
     assert (np.abs(f64(out) - z) <= (K + 2) * 2.0 ** -23 * big + 2.0 ** -24 * np.abs(z)).all()
 
 
+@pytest.mark.parametrize("act", ["gelu", "gelu_tanh"])
+def test_matmul_activation_far_out(M, act):
+    """GELU from -40 to 40: within 8 x 2^-24 |z| of the function, zero where 1 + tanh and 1 + erf vanish in fp32; an
+    8-bit block of such values has the scale of zeros."""
+    z = torch.linspace(-40, 40, 641, device="cuda")
+    a = M.q8_write(torch.zeros(1, 1, device="cuda"), M.q8_empty(1, 1))
+    b = M.q8_empty(641, 1)
+    got = f64(M.q8_matmul(a, b, bias=z[None], act=act, dtype=torch.float32))[0]
+    z64 = f64(z)
+    assert (np.abs(got - O.gelu(z64, act == "gelu_tanh")) <= 2.0 ** -21 * np.abs(z64)).all()
+    assert (got[z64 < -6.5] == 0).all() and (got[z64 > 6.5] == z64[z64 > 6.5]).all()
+    low = torch.full((1, 130), -9.0, device="cuda")
+    low[0, 0] = 1.0
+    q = M.q8_matmul(a, M.q8_empty(130, 1), bias=low, act=act, dtype=torch.float8_e5m2)
+    assert exps(q.scale).tolist() == [[-16, 0]] and bool((q.q[:, 1:].float() == 0).all())
+
+
 @pytest.mark.parametrize("rows", [3, 150])
 @pytest.mark.parametrize("ea,eb", [(-70, -62), (-70, -70), (61, 60), (62, 62)])
 def test_matmul_tiny_and_huge_results(M, rows, ea, eb):
