@@ -129,7 +129,7 @@ struct Q8CombineArgs {
   float* norms;
   int32_t* status;
   int T, k, seq;
-  bool vec, gate_vec, split;  // set at the launch: 16-byte accesses of x and out, of the gate; a block per token
+  bool vec, gate_vec;  // set at the launch: 16-byte accesses of x and out, of the gate
 };
 cudaError_t launch_q8_combine_bf16(const Q8CombineArgs& a, bool e5, cudaStream_t s);
 cudaError_t launch_q8_combine_f32(const Q8CombineArgs& a, bool e5, cudaStream_t s);

@@ -92,19 +92,22 @@ __device__ __forceinline__ Gate load_gate(const float* gp, bool vec, int left) {
 }
 
 // ---------------------------------------------------------------------------
-// Direct form: few tokens (the 8 warps of a block share one), and rows too wide
-// for the staged form (a warp per token).  All slots' loads are in flight
-// before any arithmetic.  One token of two slots takes 3 us, launch to launch.
+// Direct form: a block per token, all slots' loads in flight before any
+// arithmetic.  For few tokens, as long as all blocks run at once, and for rows
+// too wide for the staged form.  Launch to launch, direct against staged: 2.2 and
+// 3.0 us for 8 tokens of two slots and 1152 values, 2.8 and 3.2 for 608, 4.8 and 3.5
+// for 1216; 3.8 and 4.3 for 304 tokens of eight slots, 6.7 and 4.3 for 608.
 // ---------------------------------------------------------------------------
 constexpr int kDirectWarps = 8;
+// Blocks per SM that the registers allow.
+constexpr int direct_blocks(int k) { return k <= 2 ? 4 : k <= 4 ? 3 : k <= 8 ? 2 : 1; }
 
 template <bool E5, int KMAX>
-__global__ void __launch_bounds__(kDirectWarps * 32) q8_combine_kernel(const Q8CombineArgs a) {
+__global__ void __launch_bounds__(kDirectWarps * 32, direct_blocks(KMAX)) q8_combine_kernel(const Q8CombineArgs a) {
   __shared__ float part[kDirectWarps][KMAX];
   pdl_entry();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int64_t i = a.split ? blockIdx.x : static_cast<int64_t>(blockIdx.x) * kDirectWarps + warp;
-  if (i >= a.T) return;  // whole warps; a shared token's block has all its warps
+  const int64_t i = blockIdx.x;
   const int k = a.k, width = a.c.width, chunks = (width + W - 1) / W;
   float w[KMAX], ss[KMAX];
   int row[KMAX];  // < 0: the slot holds nothing
@@ -124,7 +127,7 @@ __global__ void __launch_bounds__(kDirectWarps * 32) q8_combine_kernel(const Q8C
   const TI* x = a.x ? static_cast<const TI*>(a.x) + i * a.x_stride : nullptr;
   TI* out = static_cast<TI*>(a.out) + i * a.out_stride;
   const float* gate = a.gate ? a.gate + (i / a.seq) * a.gate_stride : nullptr;
-  for (int c = (a.split ? warp * 32 : 0) + lane; c < chunks; c += (a.split ? kDirectWarps : 1) * 32) {
+  for (int c = threadIdx.x; c < chunks; c += kDirectWarps * 32) {
     const int left = width - c * W;
     uint2 h[KMAX];
     float f[KMAX], xs[W];
@@ -182,10 +185,6 @@ __global__ void __launch_bounds__(kDirectWarps * 32) q8_combine_kernel(const Q8C
   }
   if (!a.norms) return;
   const float s = warp_sums<KMAX>(ss, lane);
-  if (!a.split) {
-    if (lane < k) a.norms[i * k + lane] = sqrtf(s);
-    return;
-  }
   if (lane < KMAX) part[warp][lane] = s;
   __syncthreads();
   if (threadIdx.x < k) {
@@ -446,16 +445,16 @@ cudaError_t combine(Q8CombineArgs a, cudaStream_t s) {
   constexpr int size = sizeof(TI);
   a.vec = q8_aligned16(a.out, a.out_stride * size) && (!a.x || q8_aligned16(a.x, a.x_stride * size));
   a.gate_vec = a.gate && q8_aligned16(a.gate, a.gate_stride * 4);
-  // A block per token below two tokens per SM; staged above, where two blocks'
-  // buffers fit an SM.
-  a.split = a.T < 152 * 2;
+  // Staged where the tokens are more than direct blocks run at once and two
+  // blocks' buffers fit an SM (2000 tokens of 16 slots and 2560 values: 40 us for
+  // 111 direct; of four slots and 9000, whose buffers do not: 48 alone on an SM, 47 direct).
   const int64_t wide = static_cast<int64_t>(a.c.width) * (a.k + 2 * size);
-  if (!a.split && wide < kStageMax / kStageWarps) {
+  if (a.T > 152 * direct_blocks(a.k) && wide < kStageMax / kStageWarps) {
     const StageLayout L = a.vec ? stage_layout<true>(a.k, a.c.width, a.x != nullptr) : stage_layout<false>(a.k, a.c.width, a.x != nullptr);
     const int smem = kStageWarps * L.bytes;
     if (smem <= kStageMax) return a.vec ? staged<E5, true>(a, smem, s) : staged<E5, false>(a, smem, s);
   }
-  const dim3 grid(a.split ? a.T : (a.T + kDirectWarps - 1) / kDirectWarps), block(kDirectWarps * 32);
+  const dim3 grid(a.T), block(kDirectWarps * 32);
   if (a.k == 1) return launch_pdl(q8_combine_kernel<E5, 1>, grid, block, 0, s, a);
   if (a.k == 2) return launch_pdl(q8_combine_kernel<E5, 2>, grid, block, 0, s, a);
   if (a.k <= 4) return launch_pdl(q8_combine_kernel<E5, 4>, grid, block, 0, s, a);

@@ -80,7 +80,7 @@ struct Shared {
   int lo[kMaxGroups], rows[kMaxGroups];   // first row, rows
   alignas(16) uint32_t top[kParts][2][4][32];         // [part][buffer][quadrant][token]: largest |z| bits
   alignas(16) uint32_t stage[kEpiWarps][256];  // a chunk on its way out: 32 x 32 bytes, or 16 x 32 bf16
-  float inv[kEpiWarps][32];   // 1 / scale of the chunk's tokens, read four at a time
+  alignas(16) float inv[kEpiWarps][32];   // 1 / scale of the chunk's tokens, read four at a time
   uint64_t full[kMaxStages], empty[kMaxStages], sf_full[kSfStages], sf_empty[kSfStages], tfull[2], tempty[2], drain;
   uint32_t tmem;
   int max_n;
