@@ -537,6 +537,31 @@ def test_two_streams_at_once(M):
             assert all(torch.equal(x, y) for x, y in zip(a, b))
 
 
+def test_two_host_threads_at_once(M):
+    """Host threads that call at the same time, each on its own stream, get the bits of calls alone."""
+    import threading
+    states = [layer_state(M, 7, T=300, D=256, F=520), layer_state(M, 8, T=260, E=8, D=384, F=640)]
+    alone = [[t.clone() for t in expert_layer(M, s)] for s in states]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(s, want):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            for _ in range(25):
+                got = expert_layer(M, s)
+                stream.synchronize()
+                if not all(torch.equal(a, b) for a, b in zip(got, want)):
+                    wrong.append(1)
+
+    threads = [threading.Thread(target=work, args=p) for p in zip(states, alone)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong
+
+
 def test_repeats_give_the_same_bits(M):
     a, _ = filled(M, 1, 777, 1500, "e4m3")
     b, _ = filled(M, 2, 3 * 500, 1500, "e4m3")
