@@ -223,6 +223,8 @@ constexpr int kStageSm = 227 * 1024, kStageMax = 112 * 1024;  // shared memory o
 // Blocks per SM that the registers allow (the grid is persistent: none may wait for another).
 constexpr int stage_blocks(int k) { return k <= 2 ? 16 : k <= 4 ? 12 : k <= 9 ? 8 : 6; }
 constexpr unsigned long long kCopyWaitNs = 1000000000ull;
+// The fewest slots that run with a kernel of `kmax` (see staged()).
+__host__ __device__ constexpr int least_slots(int kmax) { return kmax == 6 ? 5 : kmax == 8 ? 7 : kmax == 16 ? 10 : kmax; }
 
 // A warp's buffer: the slots' rows, x's, out's (VEC false), the scale words, the
 // scales as floats.
@@ -343,9 +345,16 @@ __global__ void __launch_bounds__(kStageWarps * 32, stage_blocks(KMAX)) q8_combi
       float2 y[4];
 #pragma unroll
       for (int p = 0; p < KMAX; ++p) {
-        const int at = p < k ? p : 0;  // a slot past the last reads the first with a weight of 0; its norm is not kept
+        // A slot past the last has the first one's bytes, cleared: an infinity times its weight of 0 would be NaN.
+        const int at = p < k ? p : 0;
+        uint2 h = *reinterpret_cast<const uint2*>(buf + at * L.row + c * W);
+        if (p >= least_slots(KMAX)) {
+          const uint32_t keep = p < k ? 0xffffffffu : 0u;
+          h.x &= keep;
+          h.y &= keep;
+        }
         float2 d[4];
-        decode8<E5>(*reinterpret_cast<const uint2*>(buf + at * L.row + c * W), d);
+        decode8<E5>(h, d);
         const float f = scales[at * L.blocks + (c >> 4)];
         ss[p] = p == 0 ? slot_values<true>(d, f, wp[p] * f, y, ss[p]) : slot_values<false>(d, f, wp[p] * f, y, ss[p]);
       }

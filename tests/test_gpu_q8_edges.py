@@ -1,0 +1,41 @@
+"""8-bit rows at the edges of their formats, sizes and streams, against the float64 oracle (tolerances: see
+tests/test_gpu_q8.py)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import q8 as O
+from test_gpu_q8 import HALF, M, TYPES, VALUES, activations, exps, f64, filled, ints  # noqa: F401  (M: a fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+# --- combine: infinities -----------------------------------------------------
+
+@pytest.mark.parametrize("k", [1, 2, 3, 5, 6, 7, 8, 9, 10, 13, 16])
+@pytest.mark.parametrize("unaligned", [0, 1])
+def test_combine_keeps_infinities(M, k, unaligned):
+    """An e5m2 infinity in a token's first or last slot reaches its own value with its sign and nothing else, in a
+    call of few tokens and in one of many, which agree bit for bit."""
+    D, T, few = 264, 2000, 20
+    c, h = filled(M, 5, 50, D, "e5m2")
+    for row, at, byte, v in ((0, 3, 0x7c, np.inf), (1, 130, 0xfc, -np.inf), (2, 263, 0x7c, np.inf)):
+        c.q.view(torch.uint8)[row, at] = byte
+        h[row, at] = v
+    rng = np.random.default_rng(k)
+    rows = rng.integers(3, 50, (T, k)).astype(np.int32)
+    rows[::4, 0], rows[1::4, k - 1], rows[2::4, k // 2] = 0, 1, 2
+    w = rng.uniform(0.1, 1, (T, k)).astype(np.float32)
+    x = activations(7, T, D + unaligned, "bf16")[:, unaligned:]
+    rt, wt = torch.from_numpy(rows).cuda(), torch.from_numpy(w).cuda()
+    out, norms = M.q8_combine(c, rt, wt, x=x, norms=True)
+    want, wn = O.combine(h, rows, w.astype(np.float64), f64(x))
+    inf = np.isinf(want)
+    np.testing.assert_array_equal(f64(out)[inf], want[inf])
+    big, _ = O.combine(np.abs(h), rows, w, np.abs(f64(x)))
+    err = (k + 3) * 2.0 ** -23 * big[~inf]
+    assert (np.abs(f64(out)[~inf] - want[~inf]) <= err + HALF["bf16"] * (np.abs(want[~inf]) + err)).all()
+    np.testing.assert_array_equal(np.isinf(f64(norms)), np.isinf(wn))
+    small, small_n = M.q8_combine(c, rt[:few], wt[:few], x=x[:few], norms=True)
+    assert torch.equal(small, out[:few])
+    np.testing.assert_array_equal(np.isinf(f64(small_n)), np.isinf(wn[:few]))
