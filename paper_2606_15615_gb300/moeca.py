@@ -699,6 +699,21 @@ def _call(fn, args: bytes, device: int, stream: int):
         _check(status)
 
 
+def _on(stream: int, device: int, make):
+    """make()'s tensors allocated (and filled) on the stream that the call runs on: an explicit ``stream`` is not
+    ordered with the current one."""
+    if not stream or device < 0:
+        return make()
+    torch = _TYPES["torch"]
+    with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device)):
+        return make()
+
+
+# Each call runs on ``stream`` (a raw cudaStream_t), by default the tensors' device's current stream.  Results that a
+# call allocates belong to that stream: another one waits for it before it reads them, and as with any torch tensor
+# record_stream() tells the allocator of uses elsewhere.
+
+
 def q8_write(x, cache: Q8, src=None, dst=None, count=None, stream: int = 0) -> Q8:
     """Quantise rows of ``x`` (fp32 or bf16) into ``cache`` (float8 type and scales as allocated): cache row
     dst[i] from x row src[i], int32 lists on the device (None: i), for all entries or the first ``count``
@@ -725,7 +740,7 @@ def q8_read(cache: Q8, rows=None, dtype=None, out=None, status=None, stream: int
     n = c[2] if rows is None else rows.numel()
     if out is None:
         torch = _TYPES["torch"]
-        out = torch.empty((n, c[5]), dtype=dtype or torch.bfloat16, device=cache[0].device)
+        out = _on(stream, dev, lambda: torch.empty((n, c[5]), dtype=dtype or torch.bfloat16, device=cache[0].device))
         address, stride, code = out.data_ptr(), c[5], _TYPES.get(out.dtype, -1)
         if not MOECA_F32 <= code <= MOECA_BF16:
             raise ValueError("dtype must be float32 or bfloat16")
@@ -761,7 +776,8 @@ def q8_combine(cache: Q8, rows, weights=None, x=None, gate=None, norms=False, dt
         if n_x != T or x_width != width:
             raise ValueError(f"x must be [{T}, {width}]")
     if out is None:
-        out = torch.empty((T, width), dtype=x.dtype if x is not None else dtype or torch.bfloat16, device=q.device)
+        kind = x.dtype if x is not None else dtype or torch.bfloat16
+        out = _on(stream, dev, lambda: torch.empty((T, width), dtype=kind, device=q.device))
         address, stride, o_code = out.data_ptr(), width, _TYPES.get(out.dtype, -1)
         if not MOECA_F32 <= o_code <= MOECA_BF16:
             raise ValueError("dtype must be float32 or bfloat16")
@@ -775,7 +791,7 @@ def q8_combine(cache: Q8, rows, weights=None, x=None, gate=None, norms=False, dt
             raise ValueError("gate must be float32 rows, one for each T / rows consecutive tokens")
         seq = T // n_g if T else 1
     if norms is True:
-        norms = torch.empty(shape, dtype=torch.float32, device=q.device)
+        norms = _on(stream, dev, lambda: torch.empty(shape, dtype=torch.float32, device=q.device))
         n_address = norms.data_ptr()
     else:
         norms = None if norms is False else norms
@@ -809,8 +825,8 @@ def q8_matmul(a: Q8, b: Q8, offsets=None, bias=None, act: str = "none", dst=None
         code = _TYPES.get(dtype or torch.bfloat16, -1)
         if code < 0:
             raise ValueError("dtype must be float32, bfloat16, float8_e4m3fn or float8_e5m2")
-        out = q8_empty(ra[2], cols, dtype, a[0].device) if code >= MOECA_E4M3 else \
-            torch.empty((ra[2], cols), dtype=dtype or torch.bfloat16, device=a[0].device)
+        out = _on(stream, dev, lambda: q8_empty(ra[2], cols, dtype, a[0].device) if code >= MOECA_E4M3 else
+                  torch.empty((ra[2], cols), dtype=dtype or torch.bfloat16, device=a[0].device))
     if isinstance(out, Q8):
         ro = _q8_fields(out, "out", dev)
     else:

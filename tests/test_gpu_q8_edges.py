@@ -39,3 +39,45 @@ def test_combine_keeps_infinities(M, k, unaligned):
     small, small_n = M.q8_combine(c, rt[:few], wt[:few], x=x[:few], norms=True)
     assert torch.equal(small, out[:few])
     np.testing.assert_array_equal(np.isinf(f64(small_n)), np.isinf(wn[:few]))
+
+
+# --- results on a stream that is not the current one -------------------------
+
+def held_back(side):
+    """The current stream busy for a while (a tenth of a second), `side` free."""
+    torch.cuda.synchronize()
+    torch.cuda._sleep(200_000_000)
+    return side.cuda_stream
+
+
+@pytest.mark.parametrize("dtype", [torch.float8_e4m3fn, torch.float8_e5m2])
+def test_product_on_another_stream_keeps_its_rows(M, dtype):
+    """Nothing of a product's own result is filled on the current stream after the product has run on another."""
+    a, _ = filled(M, 1, 300, 256, "e4m3")
+    b, _ = filled(M, 2, 500, 256, "e4m3")
+    want = M.q8_matmul(a, b, dtype=dtype)
+    side = torch.cuda.Stream()
+    got = M.q8_matmul(a, b, dtype=dtype, stream=held_back(side))
+    torch.cuda.synchronize()
+    assert torch.equal(got.q.view(torch.uint8), want.q.view(torch.uint8)) and torch.equal(got.scale, want.scale)
+
+
+@pytest.mark.parametrize("call", ["read", "combine", "norms", "matmul"])
+def test_results_on_another_stream_have_memory_of_their_own(M, call):
+    """Memory that the current stream has freed but may still write is not given to a result of another stream."""
+    a, _ = filled(M, 1, 1024, 512, "e4m3")
+    b, _ = filled(M, 2, 512, 512, "e4m3")
+    rows = torch.arange(1024, dtype=torch.int32, device="cuda")[:, None].expand(1024, 8).contiguous()
+    calls = dict(read=lambda s: M.q8_read(a, dtype=torch.float32, stream=s),
+                 combine=lambda s: M.q8_combine(a, rows, dtype=torch.float32, stream=s),
+                 norms=lambda s: M.q8_combine(a, rows, norms=True, stream=s)[1],
+                 matmul=lambda s: M.q8_matmul(a, b, dtype=torch.float32, stream=s))
+    want = calls[call](0).clone()
+    side = torch.cuda.Stream()
+    s = held_back(side)
+    stale = torch.empty_like(want)
+    stale.fill_(5.0)  # runs once the current stream is free again
+    del stale
+    got = calls[call](s)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
