@@ -586,10 +586,12 @@ def ddpm_step(x_t, eps, alpha: float, alpha_bar: float, sigma: float, z=None, x_
               stream: int = 0):
     """Eq. 1 on torch CUDA tensors: x_prev (fp32) = the reverse step of x_t
     (fp32) with the denoiser output eps; x_next (eps's dtype) optionally
-    receives x_prev for the next denoiser call.  Returns x_prev."""
+    receives x_prev for the next denoiser call.  Returns x_prev (without one
+    given, a new tensor that belongs to ``stream``)."""
     import torch
+    _types()
     if x_prev is None:
-        x_prev = torch.empty_like(x_t)
+        x_prev = _on(stream, x_t.get_device(), lambda: torch.empty_like(x_t))
     args = moeca_ddpm_args(
         x_t.numel(), MOECA_BF16 if eps.dtype == torch.bfloat16 else MOECA_F32, alpha, alpha_bar, sigma,
         x_t.data_ptr(), eps.data_ptr(), z.data_ptr() if z is not None else None, x_prev.data_ptr(),

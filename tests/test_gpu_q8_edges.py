@@ -74,6 +74,7 @@ def test_results_on_another_stream_have_memory_of_their_own(M, call):
                  matmul=lambda s: M.q8_matmul(a, b, dtype=torch.float32, stream=s))
     want = calls[call](0).clone()
     side = torch.cuda.Stream()
+    torch.empty_like(want).fill_(5.0)  # loads the fill's kernel, which would wait for the stream
     s = held_back(side)
     stale = torch.empty_like(want)
     stale.fill_(5.0)  # runs once the current stream is free again
