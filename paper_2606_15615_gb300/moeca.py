@@ -813,7 +813,8 @@ def q8_matmul(a: Q8, b: Q8, offsets=None, bias=None, act: str = "none", dst=None
     weight rows one group after another; ``offsets`` [groups + 1] and ``dst`` [rows of a] (the output row of
     each; out of range: dropped) are int32 on the device, ``bias`` [groups, columns] fp32.  ``out``: a tensor of
     fp32 / bf16 rows or a Q8 that takes the rows in 8 bits; without it a new tensor of ``dtype`` (bf16; float8
-    types give a Q8).  ``status`` [2] int32 on the device tells of a wait that ran out.  Returns out."""
+    types give a Q8), in which rows of no group, and rows that ``dst`` names nowhere, are zeros (offsets and dst are
+    known on the device only, so the whole of it is filled first: a given ``out`` saves that).  ``status`` [2] int32 on the device tells of a wait that ran out.  Returns out."""
     dev = a[0].get_device()
     ra, rb = _q8_fields(a, "a", dev), _q8_fields(b, "b", dev)
     groups = offsets.numel() - 1 if offsets is not None else 1
@@ -827,8 +828,9 @@ def q8_matmul(a: Q8, b: Q8, offsets=None, bias=None, act: str = "none", dst=None
         code = _TYPES.get(dtype or torch.bfloat16, -1)
         if code < 0:
             raise ValueError("dtype must be float32, bfloat16, float8_e4m3fn or float8_e5m2")
+        make = torch.empty if offsets is None and dst is None else torch.zeros
         out = _on(stream, dev, lambda: q8_empty(ra[2], cols, dtype, a[0].device) if code >= MOECA_E4M3 else
-                  torch.empty((ra[2], cols), dtype=dtype or torch.bfloat16, device=a[0].device))
+                  make((ra[2], cols), dtype=dtype or torch.bfloat16, device=a[0].device))
     if isinstance(out, Q8):
         ro = _q8_fields(out, "out", dev)
     else:

@@ -82,3 +82,26 @@ def test_results_on_another_stream_have_memory_of_their_own(M, call):
     got = calls[call](s)
     torch.cuda.synchronize()
     assert torch.equal(got, want)
+
+
+# --- rows that a product does not write --------------------------------------
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32, torch.float8_e4m3fn])
+@pytest.mark.parametrize("by", ["offsets", "dst"])
+def test_a_new_result_has_zeros_where_nothing_is_written(M, dtype, by):
+    a, _ = filled(M, 1, 200, 256, "e4m3")
+    b, _ = filled(M, 2, 2 * 128, 256, "e4m3")
+    if by == "offsets":  # rows before, between and behind the groups' ones: 10..49 and 50..119 have one
+        kw, b2, live = dict(offsets=ints([10, 50, 120])), b, range(10, 120)
+    else:
+        b2 = M.Q8(b.q[:128], b.scale[:128])
+        kw, live = dict(dst=ints([r if r % 3 else -1 for r in range(200)])), [r for r in range(200) if r % 3]
+    stale = torch.full((200, 128), 7.0, device="cuda")  # what such a result's memory may have held
+    del stale
+    stale = torch.full((200, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    del stale
+    got = M.q8_matmul(a, b2, dtype=dtype, **kw)
+    v = M.q8_read(got, dtype=torch.float32) if isinstance(got, M.Q8) else got.float()
+    rest = torch.ones(200, dtype=torch.bool)
+    rest[list(live)] = False
+    assert bool((v[rest.cuda()] == 0).all()) and bool((v[~rest.cuda()] != 0).any(1).all())
