@@ -123,7 +123,9 @@ typedef enum { MOECA_ACT_NONE = 0, MOECA_ACT_GELU = 1, MOECA_ACT_GELU_TANH = 2 }
  * out of [0, out.rows) drops its row; entries are distinct.  Rows of out that
  * no entry names, and bytes past a row's width, keep what they hold.
  * MOECA_ERR_UNSUPPORTED above 2^30 rows of a or b, or where (a.rows / 16 +
- * n_groups) x ceil(n_cols / 256) passes 2^30. */
+ * n_groups) x ceil(n_cols / 256), or (ceil(n_groups / 2) x a.rows / 224 +
+ * n_groups) x ceil(n_cols / 256), passes 2^30 (tiles are counted in 32 bits,
+ * and offsets that step back may claim every row again and again). */
 typedef struct {
   moeca_q8_rows a;         /* activations                                             */
   moeca_q8_rows b;         /* weights: rows = n_groups x n_cols, width = a.width      */

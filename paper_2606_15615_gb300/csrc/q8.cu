@@ -384,10 +384,14 @@ moeca_status moeca_q8_matmul(const moeca_q8_matmul_args* a, void* stream) {
       return refuse("out: base and row stride (bytes) aligned to the type, rows at least a row's bytes apart");
   }
   const int64_t M = a->a.rows;
-  // Rows and tiles are counted in 32 bits.
-  if (M > kMaxProductRows || a->b.rows > kMaxProductRows ||
-      (M / 16 + a->n_groups) * ((a->n_cols + 255ll) / 256) > kMaxProductRows) {
-    keep_call_error("a and b of at most 2^30 rows, (rows / 16 + n_groups) x ceil(n_cols / 256) at most 2^30");
+  // Rows and tiles are counted in 32 bits.  Offsets may step back, so that groups
+  // claim the same rows: each step back is an empty group, after which all rows
+  // may come again.
+  const int64_t wide = (a->n_cols + kQ8TileCols - 1ll) / kQ8TileCols, passes = (a->n_groups + 1) / 2;
+  if (M > kMaxProductRows || a->b.rows > kMaxProductRows || (M / 16 + a->n_groups) * wide > kMaxProductRows ||
+      (passes * M / kQ8TileRows + a->n_groups) * wide > kMaxProductRows) {
+    keep_call_error("a and b of at most 2^30 rows, (rows / 16 + n_groups) and (ceil(n_groups / 2) x rows / 224 + n_groups) "
+                    "x ceil(n_cols / 256) at most 2^30");
     return MOECA_ERR_UNSUPPORTED;
   }
   if (!a->dst && o.rows < M) return refuse("out has fewer rows than a, and there is no dst");

@@ -18,6 +18,7 @@
 namespace moeca {
 
 constexpr int kQ8Block = 128;
+constexpr int kQ8TileRows = 224, kQ8TileCols = 256;  // a tile of q8_matmul.cu: token rows, weight rows
 
 // What the launches of q8.cu and q8_matmul.cu take (checked by their C calls).
 struct Q8Rows {

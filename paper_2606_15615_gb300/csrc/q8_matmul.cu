@@ -54,7 +54,7 @@ namespace {
 
 constexpr int kBM = 128;                  // weight rows per CTA (half of the MMA's M)
 constexpr int kSub = 2;                   // K blocks of 128 per stage
-constexpr int kMaxN = 224;                // token rows per tile
+constexpr int kMaxN = kQ8TileRows;        // token rows per tile
 constexpr int kBoxes = kMaxN / 16;        // token boxes of 8, 16, .., 112 rows
 constexpr int kMaxStages = 5;
 constexpr int kRingBytes = 192 * 1024;    // weight slots first, then token slots
@@ -73,6 +73,7 @@ constexpr int kTmemCols = 512;
 constexpr int kMaxGroups = 512;
 static_assert(kSfBase + kSfStages * kSfCols <= kTmemCols, "TMEM");
 static_assert(kMaxN <= 256, "eight scale columns");
+static_assert(2 * kBM == kQ8TileCols, "tile width");
 
 // Behind the ring: what the warps share.
 struct Shared {
