@@ -14,6 +14,9 @@
  *
  * moeca_probe_hold occupies SMs for a stated time, so that tests can run the
  * library's kernels on a GPU they do not have to themselves.
+ *
+ * moeca_probe_q8_stall lets a bounded wait of the 8-bit calls run out, so that
+ * tests see what a caller sees then.
  */
 #ifndef MOECA_PROBE_H_
 #define MOECA_PROBE_H_
@@ -65,6 +68,18 @@ int32_t moeca_probe_hold(int32_t device, int32_t blocks, int32_t smem_bytes, int
  * of the fused preparation kernel with `blocks` blocks brings into L2 under
  * moeca_config.weight_prefetch_mb = setting_mb.  Runs on the host. */
 int64_t moeca_probe_prefetch_bytes(int64_t w1_bytes, int32_t setting_mb, int32_t blocks);
+
+/* Let a wait of the calling thread's later moeca_q8_read, _combine and _matmul
+ * calls run out: barriers of the named kind are set up for an arrival that never
+ * comes, every wait gives up after wait_ns (1000000 .. 1000000000), and the call's
+ * kernel ends with MOECA_ERR_TIMEOUT in its status word, its output incomplete.
+ * MOECA_Q8_NONE brings back the normal waits.  Copies: moeca_q8_read and
+ * moeca_q8_combine with so many tokens that they are staged; the others:
+ * moeca_q8_matmul.  Returns 0, or -1 (out of range). */
+typedef enum {
+  MOECA_Q8_NONE = 0, MOECA_Q8_COPIES = 1, MOECA_Q8_OPERANDS = 2, MOECA_Q8_SCALES = 3, MOECA_Q8_ACCUMULATORS = 4
+} moeca_probe_q8_barrier;
+int32_t moeca_probe_q8_stall(int32_t barrier, int64_t wait_ns);
 
 /* Tensor maps (TMA descriptors) this process has encoded, on any thread: host
  * work, done once per handle for its own buffers. */

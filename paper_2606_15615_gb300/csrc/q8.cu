@@ -4,10 +4,14 @@
 
 #include "common.cuh"
 #include "kernels.h"
+#include "moeca_probe.h"
 #include "q8.cuh"
 
 namespace moeca {
 namespace {
+
+constexpr Q8Waits kWaits{1000000000ull, 0};  // a wait gives up after a second
+thread_local Q8Waits g_waits = kWaits;
 
 // ---------------------------------------------------------------------------
 // Write.  A block of 128 values (a unit) is the work of 8 lanes: each takes 16
@@ -169,6 +173,8 @@ __global__ void __launch_bounds__(kWriteThreads, kWriteBlocks) q8_write_kernel(c
 
 }  // namespace
 
+Q8Waits q8_waits() { return g_waits; }
+
 cudaError_t launch_q8_write(const Q8WriteArgs& a, bool bf16, bool e5, cudaStream_t s) {
   if (a.n <= 0) return cudaSuccess;
   const bool vec = q8_aligned16(a.x, a.x_stride * (bf16 ? 2 : 4));
@@ -315,6 +321,7 @@ moeca_status moeca_q8_read(const moeca_q8_read_args* a, void* stream) {
   d.status = a->status;
   d.T = a->n;
   d.k = d.seq = 1;
+  d.waits = q8_waits();
   return launched([&] {
     return (a->dtype == MOECA_BF16 ? launch_q8_combine_bf16 : launch_q8_combine_f32)(d, a->cache.format == MOECA_E5M2,
                                                                                      static_cast<cudaStream_t>(stream));
@@ -355,6 +362,7 @@ moeca_status moeca_q8_combine(const moeca_q8_combine_args* a, void* stream) {
   d.norms = a->norms;
   d.status = a->status;
   d.T = T; d.k = a->n_slots; d.seq = a->gate ? a->seq : 1;
+  d.waits = q8_waits();
   return launched([&] {
     return (a->dtype == MOECA_BF16 ? launch_q8_combine_bf16 : launch_q8_combine_f32)(d, a->cache.format == MOECA_E5M2,
                                                                                      static_cast<cudaStream_t>(stream));
@@ -408,7 +416,15 @@ moeca_status moeca_q8_matmul(const moeca_q8_matmul_args* a, void* stream) {
   d.a_e5 = a->a.format == MOECA_E5M2; d.b_e5 = a->b.format == MOECA_E5M2;
   d.out_format = o.format; d.act = a->act; d.n_groups = a->n_groups; d.n_cols = a->n_cols;
   d.offsets = a->offsets; d.dst = a->dst; d.bias = a->bias; d.status = a->status;
+  d.waits = q8_waits();
   return launched([&] { return launch_q8_matmul(d, static_cast<cudaStream_t>(stream)); });
+}
+
+int32_t moeca_probe_q8_stall(int32_t barrier, int64_t wait_ns) {
+  using namespace moeca;
+  if (barrier < MOECA_Q8_NONE || barrier > MOECA_Q8_ACCUMULATORS || wait_ns < 1000000 || wait_ns > 1000000000) return -1;
+  g_waits = barrier == MOECA_Q8_NONE ? kWaits : Q8Waits{static_cast<unsigned long long>(wait_ns), barrier};
+  return 0;
 }
 
 }  // extern "C"

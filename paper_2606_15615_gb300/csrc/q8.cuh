@@ -103,6 +103,15 @@ __device__ __forceinline__ uint4 shifted(const uint4& a, const uint4& b, uint32_
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// How long a kernel's bounded waits last, and the one that is to run out (tests;
+// see moeca_probe_q8_stall): a barrier of that kind is set up for one arrival
+// more than comes.
+struct Q8Waits {
+  unsigned long long ns;
+  int stall;  // moeca_probe_q8_barrier, 0: none
+};
+Q8Waits q8_waits();  // of the calling host thread
+
 // Whether 16-byte accesses can take rows of this base and stride.
 inline bool q8_aligned16(const void* p, int64_t stride_bytes) {
   return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride_bytes % 16 == 0;
@@ -130,6 +139,7 @@ struct Q8CombineArgs {
   float* norms;
   int32_t* status;
   int T, k, seq;
+  Q8Waits waits;
   bool vec, gate_vec;  // set at the launch: 16-byte accesses of x and out, of the gate
 };
 cudaError_t launch_q8_combine_bf16(const Q8CombineArgs& a, bool e5, cudaStream_t s);
@@ -142,6 +152,7 @@ struct Q8MatmulArgs {
   const int32_t *offsets, *dst;
   const float* bias;
   int32_t* status;
+  Q8Waits waits;
 };
 cudaError_t launch_q8_matmul(const Q8MatmulArgs& a, cudaStream_t s);
 

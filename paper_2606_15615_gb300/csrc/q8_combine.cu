@@ -10,6 +10,7 @@
 
 #include "common.cuh"
 #include "kernels.h"
+#include "moeca_probe.h"
 #include "q8.cuh"
 
 namespace moeca {
@@ -222,7 +223,6 @@ constexpr int kStageWarps = 2;
 constexpr int kStageSm = 227 * 1024, kStageMax = 112 * 1024;  // shared memory of an SM, and the most a block takes
 // Blocks per SM that the registers allow (the grid is persistent: none may wait for another).
 constexpr int stage_blocks(int k) { return k <= 2 ? 16 : k <= 4 ? 12 : k <= 9 ? 8 : 6; }
-constexpr unsigned long long kCopyWaitNs = 1000000000ull;
 // The fewest slots that run with a kernel of `kmax` (see staged()).
 __host__ __device__ constexpr int least_slots(int kmax) { return kmax == 6 ? 5 : kmax == 8 ? 7 : kmax == 16 ? 10 : kmax; }
 
@@ -252,7 +252,7 @@ __global__ void __launch_bounds__(kStageWarps * 32, stage_blocks(KMAX)) q8_combi
   __shared__ __align__(8) uint64_t bars[kStageWarps];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t bar = smem_u32(&bars[warp]);
-  if (lane == 0) mbar_init(bar, 1);
+  if (lane == 0) mbar_init(bar, 1 + (a.waits.stall == MOECA_Q8_COPIES));
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   __syncwarp();
   pdl_entry();
@@ -309,7 +309,7 @@ __global__ void __launch_bounds__(kStageWarps * 32, stage_blocks(KMAX)) q8_combi
     Gate next{};
     if (GATED && lane < chunks) next = load_gate(gate + lane * W, a.gate_vec, width - lane * W);
     asm volatile("cp.async.wait_all;" ::: "memory");
-    if (!__all_sync(0xffffffffu, mbar_wait_for(bar, parity, kCopyWaitNs))) {
+    if (!__all_sync(0xffffffffu, mbar_wait_for(bar, parity, a.waits.ns))) {
       if (lane == 0) report_status(a.status, MOECA_ERR_TIMEOUT, 710);
       return;
     }

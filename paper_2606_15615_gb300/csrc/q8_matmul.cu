@@ -46,6 +46,7 @@
 
 #include "common.cuh"
 #include "kernels.h"
+#include "moeca_probe.h"
 #include "q8.cuh"
 #include "tc_common.cuh"
 
@@ -86,6 +87,7 @@ struct Shared {
   uint32_t tmem;
   int max_n;
   volatile int abort_flag;
+  unsigned long long wait_ns;
 };
 constexpr int kSmem = kRingBytes + sizeof(Shared) + 1024;
 static_assert(kSmem <= 227 * 1024, "shared memory");
@@ -155,11 +157,11 @@ __device__ __forceinline__ void mma_mx_block(uint32_t d_tmem, uint32_t a_lo, uin
       ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(acc), "r"(kHi), "r"(sf_a), "r"(sf_b), "r"(issue)
       : "memory");
 }
-__device__ __forceinline__ void commit_pair_if(uint32_t bar, uint32_t issue) {
+__device__ __forceinline__ void commit_pair_if(uint32_t bar, uint32_t issue, uint16_t ranks = 3) {
   asm volatile(
       "{\n .reg .pred e;\n setp.ne.b32 e, %2, 0;\n"
       " @e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n}" ::"r"(bar),
-      "h"(static_cast<uint16_t>(3)), "r"(issue)
+      "h"(ranks), "r"(issue)
       : "memory");
 }
 // Arrive on a barrier of either CTA without a release: what is handed over lies
@@ -168,10 +170,28 @@ __device__ __forceinline__ void commit_pair_if(uint32_t bar, uint32_t issue) {
 __device__ __forceinline__ void arrive_relaxed(uint32_t bar) {
   asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
+// Bounded wait for phase `parity` of a barrier.  False when it has run out, or
+// another of the CTA's has.
+__device__ __noinline__ bool wait_bar(uint32_t bar, uint32_t parity, Shared* sh) {
+  unsigned long long t0 = 0;
+  for (uint32_t it = 1;; ++it) {
+    if (mbar_try(bar, parity)) return true;
+    if ((it & 255u) == 0) {
+      if (sh->abort_flag) return false;
+      const unsigned long long now = globaltimer();
+      if (t0 == 0) t0 = now;
+      else if (now - t0 > sh->wait_ns) return false;
+    }
+  }
+}
+// The same with the first try inline: one thread runs a ring's loop.
+__device__ __forceinline__ bool wait_hot(uint32_t bar, uint32_t parity, Shared* sh) {
+  return mbar_try(bar, parity) || wait_bar(bar, parity, sh);
+}
 // Every lane's bounded wait, the first try inline; the same answer in all lanes.
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, Shared* sh) {
   if (__all_sync(0xffffffffu, mbar_try(bar, parity))) return true;
-  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
+  return __all_sync(0xffffffffu, wait_bar(bar, parity, sh));
 }
 
 // 2^x and 1 / x of the special-function unit (about 2^-22 relative).
@@ -268,6 +288,7 @@ struct MatmulParams {
   int64_t out_rows, out_stride, os_stride;
   bool w_e5, t_e5, wide;       // wide: 16-byte stores of bf16 rows
   int32_t* status;
+  Q8Waits waits;
 };
 
 // Stores under a predicate, without a branch (a branch per store keeps the
@@ -425,20 +446,20 @@ __global__ void __launch_bounds__(kThreads, 1) q8_matmul_kernel(const __grid_con
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
   const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
-  volatile int* abort_flag = &sh.abort_flag;
 
   if (threadIdx.x == 0) {
     sh.abort_flag = 0;
+    sh.wait_ns = p.waits.ns;
     for (int s = 0; s < kMaxStages; ++s) {
-      mbar_init(smem_u32(&sh.full[s]), 1);
+      mbar_init(smem_u32(&sh.full[s]), 1 + (p.waits.stall == MOECA_Q8_OPERANDS));
       mbar_init(smem_u32(&sh.empty[s]), 1);
     }
     for (int s = 0; s < kSfStages; ++s) {
-      mbar_init(smem_u32(&sh.sf_full[s]), 8);
+      mbar_init(smem_u32(&sh.sf_full[s]), 8 + (p.waits.stall == MOECA_Q8_SCALES));
       mbar_init(smem_u32(&sh.sf_empty[s]), 1);
     }
     for (int s = 0; s < 2; ++s) {
-      mbar_init(smem_u32(&sh.tfull[s]), 1);
+      mbar_init(smem_u32(&sh.tfull[s]), 1 + (p.waits.stall == MOECA_Q8_ACCUMULATORS));
       mbar_init(smem_u32(&sh.tempty[s]), 2 * kEpiWarps);
     }
     mbar_init(smem_u32(&sh.drain), 1);
@@ -521,7 +542,7 @@ __global__ void __launch_bounds__(kThreads, 1) q8_matmul_kernel(const __grid_con
         const int box = wts ? kWBytes : half * kQ8Block;
         const uint32_t tx = 2 * kWSlot + kSub * t.n * kQ8Block;  // both CTAs' bytes; outside the rows or K: zeros
         for (int k = 0; k < ks; ++k) {
-          if (!(ok = mbar_wait_hot(eb, par, abort_flag))) break;
+          if (!(ok = wait_hot(eb, par, &sh))) break;
           if (wts && rank == 0) mbar_expect_tx(fb, tx);
 #pragma unroll
           for (int q = 0; q < kSub; ++q) tma_load_pair(dst + q * box, map, (k * kSub + q) * kQ8Block, row, fb);
@@ -545,7 +566,7 @@ __global__ void __launch_bounds__(kThreads, 1) q8_matmul_kernel(const __grid_con
         for (int q = 0; wts && rank == 0 && q < nst && q < issued; ++q) {
           const int last = issued - 1 - (issued - 1 - q) % nst;
           const unsigned long long t0 = globaltimer();
-          while (!mbar_try(smem_u32(&sh.full[q]), (last / nst) & 1) && globaltimer() - t0 < kTcWaitNs) {
+          while (!mbar_try(smem_u32(&sh.full[q]), (last / nst) & 1) && globaltimer() - t0 < sh.wait_ns) {
           }
         }
       }
@@ -563,12 +584,12 @@ __global__ void __launch_bounds__(kThreads, 1) q8_matmul_kernel(const __grid_con
       for (int u = pair; u < units; u += n_pairs) {
         const Unit t = unit_at(sh, u, g, nw);
         g = t.g;
-        if (!(ok = warp_wait(smem_u32(&sh.tempty[acc]), acc_phase ^ 1u, abort_flag))) break;
+        if (!(ok = warp_wait(smem_u32(&sh.tempty[acc]), acc_phase ^ 1u, &sh))) break;
         const uint32_t d_tmem = tmem + static_cast<uint32_t>(acc * kMaxN);
         const uint32_t idesc = mx_desc(t.n, p.w_e5, p.t_e5), x_sub = static_cast<uint32_t>(t.n >> 1) * kQ8Block >> 4;
         for (int k = 0; k < ks; ++k) {
-          if (k % (4 / kSub) == 0 && !(ok = warp_wait(sf_full0 + sfs * 8, sf_par, abort_flag))) break;
-          if (!(ok = warp_wait(full0 + slot * 8, par, abort_flag))) break;
+          if (k % (4 / kSub) == 0 && !(ok = warp_wait(sf_full0 + sfs * 8, sf_par, &sh))) break;
+          if (!(ok = warp_wait(full0 + slot * 8, par, &sh))) break;
           tc_fence_after();
           const uint32_t sf = tmem + kSfBase + sfs * kSfCols;
           const uint32_t w_lo = w_lo0 + slot * (kWSlot >> 4), x_lo = x_lo0 + slot * (t_slot >> 4);
@@ -601,15 +622,16 @@ __global__ void __launch_bounds__(kThreads, 1) q8_matmul_kernel(const __grid_con
           acc_phase ^= 1u;
         }
       }
-      if (lane == 0) {
-        if (!ok) {
-          if (!sh.abort_flag) report_status(p.status, MOECA_ERR_TIMEOUT, 701);
-          sh.abort_flag = 1;
-        }
-        // Every MMA issued so far has completed once the drain barrier fires.
-        mma_commit_pair(smem_u32(&sh.drain), 1);
+      if (lane == 0 && !ok) {
+        if (!sh.abort_flag) report_status(p.status, MOECA_ERR_TIMEOUT, 701);
+        sh.abort_flag = 1;
+      }
+      // Every MMA issued so far has completed once the drain barrier fires: a
+      // commit covers what its own thread issued, so the issuing lane makes it.
+      commit_pair_if(smem_u32(&sh.drain), issue, 1);
+      if (issue) {
         const unsigned long long t0 = globaltimer();
-        while (!mbar_try(smem_u32(&sh.drain), 0) && globaltimer() - t0 < kTcWaitNs) {
+        while (!mbar_try(smem_u32(&sh.drain), 0) && globaltimer() - t0 < sh.wait_ns) {
         }
       }
     }
@@ -641,7 +663,7 @@ __global__ void __launch_bounds__(kThreads, 1) q8_matmul_kernel(const __grid_con
       };
       load(0);
       for (int k = 0; k < kc; ++k) {
-        if (!(ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.sf_empty[sfs]), par, abort_flag)))) break;
+        if (!(ok = __all_sync(0xffffffffu, wait_bar(smem_u32(&sh.sf_empty[sfs]), par, &sh)))) break;
         tc_fence_after();
         const uint32_t at = tmem + lanes + kSfBase + sfs * kSfCols;
         asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(ws[0]), "r"(ws[1]),
@@ -688,7 +710,7 @@ __global__ void __launch_bounds__(kThreads, 1) q8_matmul_kernel(const __grid_con
         if (m < t.m_end) rows[j] = p.dst ? __ldg(p.dst + m) : m;
         if (rows[j] >= p.out_rows) rows[j] = -1;
       }
-      ok = mbar_wait(smem_u32(&sh.tfull[acc]), acc_phase, abort_flag);
+      ok = __all_sync(0xffffffffu, wait_bar(smem_u32(&sh.tfull[acc]), acc_phase, &sh));
       if (!(ok = part_sync(part, ok))) break;  // all warps of the part, or none: the chunks' exchanges need all
       tc_fence_after();
       const uint32_t tb = tmem + (static_cast<uint32_t>(quad * 32) << 16) + static_cast<uint32_t>(acc * kMaxN);
@@ -788,6 +810,7 @@ cudaError_t launch_q8_matmul(const Q8MatmulArgs& a, cudaStream_t s) {
   p.w_e5 = a.b_e5; p.t_e5 = a.a_e5;
   p.wide = reinterpret_cast<uintptr_t>(a.out.q) % 16 == 0 && a.out.q_stride % 16 == 0;
   p.status = a.status;
+  p.waits = a.waits;
   // At most one pair per tile there can be.
   const int64_t nw = (a.n_cols + 2 * kBM - 1) / (2 * kBM);
   const int64_t most = nw * ((a.a.rows + kMaxN - 1) / kMaxN + std::min<int64_t>(a.n_groups, a.a.rows) - 1);

@@ -31,6 +31,7 @@ KERNEL_KINDS = ["router", "select", "compact", "ffn1", "ffn2", "combine", "prep"
                 "qkv", "attn", "oproj", "attn_aux", "adaln"]
 ATTN_SYNC, ATTN_STALE, ATTN_FULL = 0, 1, 2
 MOECA_E4M3, MOECA_E5M2 = 2, 3
+MOECA_Q8_NONE, MOECA_Q8_COPIES, MOECA_Q8_OPERANDS, MOECA_Q8_SCALES, MOECA_Q8_ACCUMULATORS = 0, 1, 2, 3, 4
 MOECA_ACT_NONE, MOECA_ACT_GELU, MOECA_ACT_GELU_TANH = 0, 1, 2
 
 
@@ -180,6 +181,7 @@ def _load():
         "moeca_q8_read": (C.c_int, [C.POINTER(moeca_q8_read_args), C.c_void_p]),
         "moeca_q8_combine": (C.c_int, [C.POINTER(moeca_q8_combine_args), C.c_void_p]),
         "moeca_q8_matmul": (C.c_int, [C.POINTER(moeca_q8_matmul_args), C.c_void_p]),
+        "moeca_probe_q8_stall": (C.c_int32, [C.c_int32, C.c_int64]),
         "moeca_probe_ffma": (C.c_int32, [C.c_int32, C.c_int32, C.POINTER(C.c_double), C.POINTER(C.c_double)]),
         "moeca_probe_maps_encoded": (C.c_int64, []),
         "moeca_probe_prefetch_bytes": (C.c_int64, [C.c_int64, C.c_int32, C.c_int32]),
@@ -395,6 +397,14 @@ def moeca_probe_hold(device: int, blocks: int, smem_bytes: int, us: int, stream:
     st = LIB.moeca_probe_hold(device, blocks, smem_bytes, us, stream)
     if st != MOECA_OK:
         raise MoecaError(st, "moeca_probe_hold")
+
+
+def moeca_probe_q8_stall(barrier: int, wait_ns: int = 20_000_000) -> None:
+    """Let a bounded wait of this thread's later 8-bit calls run out after ``wait_ns``, or (MOECA_Q8_NONE) none
+    (include/moeca_probe.h)."""
+    st = LIB.moeca_probe_q8_stall(barrier, wait_ns)
+    if st != MOECA_OK:
+        raise MoecaError(st, "moeca_probe_q8_stall")
 
 
 def moeca_probe_stream(device: int, n_tokens: int, rows: int, row_bytes: int, reps: int = 15) -> tuple:

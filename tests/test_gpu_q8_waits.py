@@ -1,0 +1,55 @@
+"""Bounded waits of the 8-bit calls that run out: a barrier waits for an arrival that nothing makes, the kernel gives
+up after the set limit, says so in the status word and leaves the GPU in order.  No GPU fault is made."""
+import time
+
+import pytest
+import torch
+
+from test_gpu_q8 import M, filled, ints  # noqa: F401  (M: a fixture)
+
+pytestmark = pytest.mark.gpu
+
+LIMIT = 20_000_000  # ns
+
+
+@pytest.fixture
+def stall(M):
+    yield lambda barrier: M.moeca_probe_q8_stall(barrier, LIMIT)
+    M.moeca_probe_q8_stall(M.MOECA_Q8_NONE, LIMIT)
+
+
+def status_words():
+    return torch.zeros(2, dtype=torch.int32, device="cuda")
+
+
+def test_stall_arguments(M):
+    for barrier, ns in ((-1, LIMIT), (5, LIMIT), (1, 0), (1, 1_000_000_001)):
+        with pytest.raises(M.MoecaError):
+            M.moeca_probe_q8_stall(barrier, ns)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float8_e4m3fn])
+@pytest.mark.parametrize("rows", [3, 9000])  # one tile, several a pair: the pair's MMAs run when the wait begins
+@pytest.mark.parametrize("barrier", ["MOECA_Q8_OPERANDS", "MOECA_Q8_SCALES", "MOECA_Q8_ACCUMULATORS"])
+def test_matmul_wait_runs_out(M, stall, barrier, rows, dtype):
+    a, _ = filled(M, 1, rows, 1500, "e4m3")
+    b, _ = filled(M, 2, 2 * 700, 1500, "e4m3")
+    off = ints([0, rows // 3, rows])
+    call = lambda status: M.q8_matmul(a, b, off, dtype=dtype, status=status)  # noqa: E731
+    bits = lambda r: r.q.view(torch.uint8) if isinstance(r, M.Q8) else r  # noqa: E731
+    status = status_words()
+    want = bits(call(status)).clone()
+    assert status.tolist() == [0, 0]
+    stall(getattr(M, barrier))
+    t0 = time.monotonic()
+    call(status)
+    torch.cuda.synchronize()
+    assert time.monotonic() - t0 < 20
+    assert status[0].item() == M.MOECA_ERR_TIMEOUT and 700 <= status[1].item() < 710
+    call(None)  # nobody asked: the call still ends
+    torch.cuda.synchronize()
+    stall(M.MOECA_Q8_NONE)
+    status.zero_()
+    for _ in range(3):  # all SMs' TMEM and barriers are in order again
+        assert torch.equal(bits(call(status)), want)
+    assert status.tolist() == [0, 0]
