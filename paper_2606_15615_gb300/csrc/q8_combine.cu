@@ -311,6 +311,7 @@ __global__ void __launch_bounds__(kStageWarps * 32, stage_blocks(KMAX)) q8_combi
     asm volatile("cp.async.wait_all;" ::: "memory");
     if (!__all_sync(0xffffffffu, mbar_wait_for(bar, parity, a.waits.ns))) {
       if (lane == 0) report_status(a.status, MOECA_ERR_TIMEOUT, 710);
+      mbar_wait_for(bar, parity, a.waits.ns);  // the copies still write this block's memory: as long again for them
       return;
     }
     parity ^= 1u;

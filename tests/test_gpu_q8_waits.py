@@ -53,3 +53,31 @@ def test_matmul_wait_runs_out(M, stall, barrier, rows, dtype):
     for _ in range(3):  # all SMs' TMEM and barriers are in order again
         assert torch.equal(bits(call(status)), want)
     assert status.tolist() == [0, 0]
+
+
+@pytest.mark.parametrize("call", ["read", "combine", "combine unaligned"])
+def test_staged_copies_run_out(M, stall, call):
+    """Every warp gives up on its first token, and waits as long again for the copies that are under way."""
+    width = 1001 if "unaligned" in call else 1152
+    c, _ = filled(M, 3, 3000, width, "e4m3")
+    rows = torch.arange(3000, dtype=torch.int32, device="cuda")[:, None].repeat(1, 4)
+    x = torch.randn(3000, width, device="cuda")
+    if call == "read":
+        run = lambda status: M.q8_read(c, dtype=torch.float32, status=status)  # noqa: E731
+    else:
+        run = lambda status: M.q8_combine(c, rows, x=x, status=status)  # noqa: E731
+    status = status_words()
+    want = run(status).clone()
+    assert status.tolist() == [0, 0]
+    stall(M.MOECA_Q8_COPIES)
+    torch.cuda.synchronize()
+    t0 = time.monotonic()
+    run(status)
+    torch.cuda.synchronize()
+    assert 2e-9 * LIMIT <= time.monotonic() - t0 < 10
+    assert status.tolist() == [M.MOECA_ERR_TIMEOUT, 710]
+    run(None)
+    torch.cuda.synchronize()
+    stall(M.MOECA_Q8_NONE)
+    status.zero_()
+    assert torch.equal(run(status), want) and status.tolist() == [0, 0]
