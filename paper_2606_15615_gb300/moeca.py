@@ -559,7 +559,11 @@ class Stack:
         """Load a layer's cached state, as ``get_state`` gives it (branch outputs in 8 bits are read back)."""
         n = int(state["cache_e"].shape[0])
         if isinstance(state["cache_h"], Q8):
-            rows = q8_read(state["cache_h"], dtype=self.dtype)
+            status = self.torch.zeros(2, dtype=self.torch.int32, device=self.device)
+            rows = q8_read(state["cache_h"], dtype=self.dtype, status=status)
+            code = int(status[0])  # waits for the rows: an incomplete cache is not loaded
+            if code != MOECA_OK:
+                raise MoecaError(code, "the 8-bit branch outputs were not read back")
             state = dict(state, cache_h=rows.view(n, self.cfg.top_k, self.cfg.hidden))
         keep = {k: v.contiguous() for k, v in state.items() if k != "n_tokens" and v is not None}
         st = moeca_layer_state(**{k: keep[k].data_ptr() if k in keep else None
@@ -746,7 +750,8 @@ def q8_write(x, cache: Q8, src=None, dst=None, count=None, stream: int = 0) -> Q
 
 def q8_read(cache: Q8, rows=None, dtype=None, out=None, status=None, stream: int = 0):
     """Cache rows as bf16 (default) or fp32: all of them, or those of ``rows`` (int32, on the device); zeros
-    where an entry is out of range.  ``status``: as for q8_matmul."""
+    where an entry is out of range.  ``status``: as for q8_matmul (without it a read of many rows whose copies do
+    not arrive is incomplete in silence)."""
     dev = cache[0].get_device()
     c = _q8_fields(cache, "cache", dev)
     n = c[2] if rows is None else rows.numel()
@@ -770,7 +775,7 @@ def q8_combine(cache: Q8, rows, weights=None, x=None, gate=None, norms=False, dt
     """Eq. 8 over an 8-bit branch cache: x + gate * sum_p weights[:, p] cache[rows[:, p]].  ``rows`` [T, k]
     int32 (out of range: an empty slot), ``weights`` [T, k] fp32 (None: 1), ``x`` [T, D] fp32 or bf16 (None: 0),
     ``gate`` [B, D] fp32, one row for each T / B consecutive tokens.  ``norms``: True or a [T, k] fp32 tensor
-    also gives the rows' 2-norms.  The result has x's dtype (without x: ``dtype``, default bf16); ``out`` may be
+    also gives the rows' 2-norms.  ``status``: as for q8_matmul.  The result has x's dtype (without x: ``dtype``, default bf16); ``out`` may be
     x.  Returns out, or (out, norms)."""
     q = cache[0]
     dev = q.get_device()
@@ -824,7 +829,9 @@ def q8_matmul(a: Q8, b: Q8, offsets=None, bias=None, act: str = "none", dst=None
     each; out of range: dropped) are int32 on the device, ``bias`` [groups, columns] fp32.  ``out``: a tensor of
     fp32 / bf16 rows or a Q8 that takes the rows in 8 bits; without it a new tensor of ``dtype`` (bf16; float8
     types give a Q8), in which rows of no group, and rows that ``dst`` names nowhere, are zeros (offsets and dst are
-    known on the device only, so the whole of it is filled first: a given ``out`` saves that).  ``status`` [2] int32 on the device tells of a wait that ran out.  Returns out."""
+    known on the device only, so the whole of it is filled first: a given ``out`` saves that).  ``status`` [2] int32
+    zeros on the device: its first word becomes MOECA_ERR_TIMEOUT if a wait of the kernel ran out and the result is
+    incomplete; without it nothing tells.  Returns out."""
     dev = a[0].get_device()
     ra, rb = _q8_fields(a, "a", dev), _q8_fields(b, "b", dev)
     groups = offsets.numel() - 1 if offsets is not None else 1

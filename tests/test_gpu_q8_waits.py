@@ -81,3 +81,27 @@ def test_staged_copies_run_out(M, stall, call):
     stall(M.MOECA_Q8_NONE)
     status.zero_()
     assert torch.equal(run(status), want) and status.tolist() == [0, 0]
+
+
+def test_a_snapshot_that_was_not_read_back_is_not_loaded(M, stall):
+    """Stack.set_state from 8-bit rows raises when their copies do not arrive, and leaves the stack as it was."""
+    from paper_2606_15615_gb300 import workloads as W
+    T, D, E, k, F = 512, 128, 8, 2, 256
+    w = W.tiny_layer(43, T, D, E, k, F, dtype="bf16", wscale=0.05)[0]
+    cfg = M.moeca_config_default(n_layers=1, hidden=D, ffn=F, n_experts=E, top_k=k, max_tokens=T, tau0=0.75)
+    s = M.Stack(cfg, [w])
+    x = torch.randn(T, D, device="cuda").bfloat16()
+    s.step(x, 1)
+    small = s.get_state(0, q8=torch.float8_e4m3fn)
+    s.step(2 * x, 1)
+    before = s.get_state(0)
+    stall(M.MOECA_Q8_COPIES)
+    with pytest.raises(M.MoecaError) as e:
+        s.set_state(0, small)
+    assert e.value.status == M.MOECA_ERR_TIMEOUT
+    stall(M.MOECA_Q8_NONE)
+    after = s.get_state(0)
+    assert all(torch.equal(before[n], after[n]) for n in ("cache_h", "cache_e", "cache_w", "cache_norm", "ema"))
+    s.set_state(0, small)
+    assert torch.equal(s.get_state(0)["cache_h"].view(T * k, D), M.q8_read(small["cache_h"]))
+    s.close()
