@@ -87,9 +87,12 @@ moeca_status moeca_q8_read(const moeca_q8_read_args* args, void* stream);
  *   out_i = x_i + g_(i / seq) * sum_p weights[i, p] h_(i, p)
  * with h_(i, p) the cache row rows[i, p], p < n_slots (a shared expert's
  * output is one more slot of weight 1).  A slot whose row is out of range
- * holds nothing: it adds nothing, whatever its weight.  Sums are fp32, slot
- * by slot; the result is rounded once.  norms[i, p] = ||h_(i, p)|| over the
- * row (Eq. 9's history), 0 for a slot that holds nothing. */
+ * holds nothing: it adds nothing, whatever its weight.  h is the cache's value
+ * in fp32 (exact; an infinity past fp32's largest), sums are fp32, slot by slot,
+ * and the result is rounded once.  norms[i, p] = ||h_(i, p)|| over the row
+ * (Eq. 9's history), 0 for a slot that holds nothing; the sum of squares is
+ * fp32: rows of a norm above 1.8e19 have an infinite one, squares below 1.4e-45
+ * count nothing. */
 typedef struct {
   moeca_q8_rows cache;   /* read                                                      */
   const int32_t* rows;   /* [n_tokens, n_slots]                                       */

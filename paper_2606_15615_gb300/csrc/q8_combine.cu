@@ -1,12 +1,15 @@
 // Eq. 8 over an 8-bit branch cache, and the cache read back as it is (one
 // slot, no weights, no residual) (include/moeca_q8.h):
 //   out_i = x_i + g * sum_p w_p h_p,   norm_p = ||h_p||
-// The scale of a block is a power of two, so w x scale is exact and one
-// multiply-add per value does for both; squares are summed over a lane's 8
-// values of a block before their scale.  Two values go through one packed
-// fp32 instruction.  Compiled twice: bf16 rows here, fp32 rows in
-// q8_combine_f32.cu.
+// A value h = f d is its byte times its block's power of two, exact in fp32 (but
+// past its largest value, where it is an infinity, and below its least).  Where
+// scales and weights are moderate w f is exact too, and one multiply-add does for
+// both with the same result; elsewhere w f could pass fp32's range or fall among
+// its subnormals where w h does neither, and make a NaN of a 0: there the value
+// comes first.  Two values go through one packed fp32 instruction.  Compiled
+// twice: bf16 rows here, fp32 rows in q8_combine_f32.cu.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.cuh"
 #include "kernels.h"
@@ -41,12 +44,23 @@ __device__ __forceinline__ void decode8(const uint2& h, float2 (&d)[4]) {
   }
 }
 
-// y (+)= w f h and the square sum of the 8 values times f^2.
-template <bool FIRST>
-__device__ __forceinline__ float slot_values(const float2 (&d)[4], float f, float wf, float2 (&y)[4], float ss) {
-  const float2 wf2 = make_float2(wf, wf);
+// Scale bytes and weights between which w f d is exact up to its rounding in
+// either order: 2^-63 .. 2^63 and 2^-60 .. 2^60, or a weight of 0.
+__device__ __forceinline__ bool far_scale(uint32_t byte) { return byte - 64u > 126u; }
+__device__ __forceinline__ bool far_weight(float w) { return w != 0.f && !(fabsf(w) >= 0x1p-60f && fabsf(w) <= 0x1p60f); }
+
+// y (+)= w f d, and ss plus the square sum of the 8 values: that of d times f^2,
+// which passes fp32's range only where the values' squares do.  FAR: any scale
+// and weight.
+template <bool FIRST, bool FAR>
+__device__ __forceinline__ float slot_values(const float2 (&d)[4], float f, float w, float2 (&y)[4], float ss) {
+  const float wf = FAR ? w : w * f;
+  const float2 w2 = make_float2(wf, wf), f2 = make_float2(f, f);
 #pragma unroll
-  for (int t = 0; t < 4; ++t) y[t] = FIRST ? mul2(wf2, d[t]) : fma2(wf2, d[t], y[t]);
+  for (int t = 0; t < 4; ++t) {
+    const float2 h = FAR ? mul2(f2, d[t]) : d[t];
+    y[t] = FIRST ? mul2(w2, h) : fma2(w2, h, y[t]);
+  }
   float2 sq = mul2(d[0], d[0]);
 #pragma unroll
   for (int t = 1; t < 4; ++t) sq = fma2(d[t], d[t], sq);
@@ -164,7 +178,7 @@ __global__ void __launch_bounds__(kDirectWarps * 32, direct_blocks(KMAX)) q8_com
     for (int p = 0; p < KMAX; ++p) {
       float2 d[4];
       decode8<E5>(h[p], d);
-      ss[p] = p == 0 ? slot_values<true>(d, f[p], w[p] * f[p], y, ss[p]) : slot_values<false>(d, f[p], w[p] * f[p], y, ss[p]);
+      ss[p] = p == 0 ? slot_values<true, true>(d, f[p], w[p], y, ss[p]) : slot_values<false, true>(d, f[p], w[p], y, ss[p]);
     }
     float o[W] = {y[0].x, y[0].y, y[1].x, y[1].y, y[2].x, y[2].y, y[3].x, y[3].y};
     if (gate) {
@@ -206,7 +220,9 @@ __global__ void __launch_bounds__(kDirectWarps * 32, direct_blocks(KMAX)) q8_com
 //
 // Decoding is what costs next to HBM here: a conversion of two e4m3 values
 // takes a scheduler 4 clocks, their widening 3; the loop over a token's values
-// holds no branch and no select, so that the slots' chains interleave.  For
+// holds no branch and no select, so that the slots' chains interleave (a scale ahead
+// of the weight in it: 95 -> 103 us in e5m2 at eight slots, so that tokens with
+// moderate ones have a loop of their own).  For
 // that the buffer is prepared once per token: slots that hold nothing and the
 // bytes past the row's width are zeros, and the scales are turned into floats
 // by block.
@@ -317,10 +333,13 @@ __global__ void __launch_bounds__(kStageWarps * 32, stage_blocks(KMAX)) q8_combi
     parity ^= 1u;
     __syncwarp();
     // Prepare the buffer: zeros for what is not there, scales as floats.
+    bool far = far_weight(w_now);
     float* scales = reinterpret_cast<float*>(buf + L.scale_at);
     for (int j = lane; j < k * L.blocks; j += 32) {
       const int p = j / L.blocks, b = j - p * L.blocks;
-      scales[j] = slots >> p & 1 ? scale_value(buf[L.word_at + p * L.words * 4 + b]) : 1.f;
+      const uint32_t byte = slots >> p & 1 ? buf[L.word_at + p * L.words * 4 + b] : 127u;
+      scales[j] = scale_value(byte);
+      far |= far_scale(byte);
     }
     if (lane < k && width < L.row) {
       for (int t = width; t < L.row; ++t) buf[lane * L.row + t] = 0;
@@ -331,6 +350,7 @@ __global__ void __launch_bounds__(kStageWarps * 32, stage_blocks(KMAX)) q8_combi
     float wp[KMAX];
 #pragma unroll
     for (int p = 0; p < KMAX; ++p) wp[p] = __shfl_sync(0xffffffffu, w_now, p);
+    far = __any_sync(0xffffffffu, far);
     __syncwarp();
 
     TI* out = static_cast<TI*>(a.out) + i * a.out_stride;
@@ -339,57 +359,62 @@ __global__ void __launch_bounds__(kStageWarps * 32, stage_blocks(KMAX)) q8_combi
     float ss[KMAX];
 #pragma unroll
     for (int p = 0; p < KMAX; ++p) ss[p] = 0.f;
-    for (int c = lane; c < chunks; c += 32) {
-      const int left = width - c * W;
-      const Gate now = next;
-      if (GATED && c + 32 < chunks) next = load_gate(gate + (c + 32) * W, a.gate_vec, left - 32 * W);
-      float2 y[4];
+    const auto add_up = [&](auto any) {
+      constexpr bool FAR = decltype(any)::value;
+      for (int c = lane; c < chunks; c += 32) {
+        const int left = width - c * W;
+        const Gate now = next;
+        if (GATED && c + 32 < chunks) next = load_gate(gate + (c + 32) * W, a.gate_vec, left - 32 * W);
+        float2 y[4];
 #pragma unroll
-      for (int p = 0; p < KMAX; ++p) {
-        // A slot past the last has the first one's bytes, cleared: an infinity times its weight of 0 would be NaN.
-        const int at = p < k ? p : 0;
-        uint2 h = *reinterpret_cast<const uint2*>(buf + at * L.row + c * W);
-        if (p >= least_slots(KMAX)) {
-          const uint32_t keep = p < k ? 0xffffffffu : 0u;
-          h.x &= keep;
-          h.y &= keep;
+        for (int p = 0; p < KMAX; ++p) {
+          // A slot past the last has the first one's bytes, cleared: an infinity times its weight of 0 would be NaN.
+          const int at = p < k ? p : 0;
+          uint2 h = *reinterpret_cast<const uint2*>(buf + at * L.row + c * W);
+          if (p >= least_slots(KMAX)) {
+            const uint32_t keep = p < k ? 0xffffffffu : 0u;
+            h.x &= keep;
+            h.y &= keep;
+          }
+          float2 d[4];
+          decode8<E5>(h, d);
+          const float f = scales[at * L.blocks + (c >> 4)];
+          ss[p] = p == 0 ? slot_values<true, FAR>(d, f, wp[p], y, ss[p]) : slot_values<false, FAR>(d, f, wp[p], y, ss[p]);
         }
-        float2 d[4];
-        decode8<E5>(h, d);
-        const float f = scales[at * L.blocks + (c >> 4)];
-        ss[p] = p == 0 ? slot_values<true>(d, f, wp[p] * f, y, ss[p]) : slot_values<false>(d, f, wp[p] * f, y, ss[p]);
-      }
-      float o[W] = {y[0].x, y[0].y, y[1].x, y[1].y, y[2].x, y[2].y, y[3].x, y[3].y};
-      if constexpr (GATED) {
+        float o[W] = {y[0].x, y[0].y, y[1].x, y[1].y, y[2].x, y[2].y, y[3].x, y[3].y};
+        if constexpr (GATED) {
 #pragma unroll
-        for (int t = 0; t < W; ++t) o[t] *= now.v[t];
-      }
-      if (x) {
-        float xs[W];
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-          const uint4* piece = reinterpret_cast<const uint4*>(buf + L.x_at) + c * NV + j;
-          if constexpr (VEC) unpack_vec(*piece, &xs[j * V], static_cast<TI*>(nullptr));
-          else unpack_vec(shifted<TI>(piece[0], piece[1], mx), &xs[j * V], static_cast<TI*>(nullptr));
+          for (int t = 0; t < W; ++t) o[t] *= now.v[t];
         }
+        if (x) {
+          float xs[W];
 #pragma unroll
-        for (int t = 0; t < W; ++t) o[t] += xs[t];
-      }
-      if constexpr (VEC) {
-        if (left >= W) {
+          for (int j = 0; j < NV; ++j) {
+            const uint4* piece = reinterpret_cast<const uint4*>(buf + L.x_at) + c * NV + j;
+            if constexpr (VEC) unpack_vec(*piece, &xs[j * V], static_cast<TI*>(nullptr));
+            else unpack_vec(shifted<TI>(piece[0], piece[1], mx), &xs[j * V], static_cast<TI*>(nullptr));
+          }
 #pragma unroll
-          for (int j = 0; j < NV; ++j) store_vec(out + c * W + j * V, &o[j * V]);
+          for (int t = 0; t < W; ++t) o[t] += xs[t];
+        }
+        if constexpr (VEC) {
+          if (left >= W) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j) store_vec(out + c * W + j * V, &o[j * V]);
+          } else {
+#pragma unroll
+            for (int t = 0; t < W; ++t)
+              if (t < left) out[c * W + t] = Elem<TI>::from_f(o[t]);
+          }
         } else {
 #pragma unroll
-          for (int t = 0; t < W; ++t)
-            if (t < left) out[c * W + t] = Elem<TI>::from_f(o[t]);
+          for (int j = 0; j < NV; ++j)
+            store_vec(reinterpret_cast<TI*>(buf + L.out_at + 16) + c * W + j * V, &o[j * V]);
         }
-      } else {
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
-          store_vec(reinterpret_cast<TI*>(buf + L.out_at + 16) + c * W + j * V, &o[j * V]);
       }
-    }
+    };
+    if (far) add_up(std::true_type());
+    else add_up(std::false_type());
     __syncwarp();  // all have read the slots and x
     if constexpr (!VEC) {
       // out's aligned pieces, each from the two staged ones that it straddles; its

@@ -105,3 +105,40 @@ def test_a_new_result_has_zeros_where_nothing_is_written(M, dtype, by):
     rest = torch.ones(200, dtype=torch.bool)
     rest[list(live)] = False
     assert bool((v[rest.cuda()] == 0).all()) and bool((v[~rest.cuda()] != 0).any(1).all())
+
+
+# --- combine: scales at the ends of their range ------------------------------
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("k", [1, 2, 5, 9, 16])
+@pytest.mark.parametrize("T", [30, 2000])
+def test_combine_weights_meet_values_not_scales(M, T, k, dtype, fmt):
+    """Scale bytes from 0 to 254 under weights from 0 to 2048: w h where w x scale would pass fp32's range (2^127 x 2,
+    2^118 x 2048) or lose digits among its subnormals, and zeros in such blocks stay zeros.
+    Each fp32 operation is off by 2^-24 of its result or by half of the least subnormal, 2^-150."""
+    D, R = 200, 400
+    rng = np.random.default_rng(T + k)
+    c = M.q8_empty(R, D, TYPES[fmt])
+    v = torch.from_numpy(rng.standard_normal((R, D)).astype(np.float32) / 16).clamp(-0.25, 0.25).to(TYPES[fmt])
+    c.q.copy_(v)
+    c.q.view(torch.uint8)[:, ::3] = 0
+    kinds = np.array([0, 1, 3, 20, 100, 127, 140, 240, 245, 254])
+    e = kinds[rng.integers(0, len(kinds) - 3, (R, 2))]
+    e[:40] = rng.choice(kinds[-3:], (40, 2))  # the first rows are huge
+    c.scale.copy_(torch.from_numpy(e.astype(np.uint8)))
+    h = O.dequantise(f64(c.q), e - 127)
+    assert np.isfinite(h.astype(np.float32)).all()
+    rows = rng.integers(40, R, (T, k)).astype(np.int32)
+    rows[::2, k // 2] = rng.integers(0, 40, len(rows[::2]))  # one huge row at most in a token
+    w = rng.choice(np.array([0, 1e-20, 1e-3, 0.3, 1.7], np.float32), (T, k))
+    small = np.abs(h).max(1)[rows] < 2.0 ** 116
+    w = np.where(small & (rng.random((T, k)) < 0.3), np.float32(2048), w)
+    w[::4, k // 2] = 2.0
+    out = M.q8_combine(c, torch.from_numpy(rows).cuda(), torch.from_numpy(w).cuda(), dtype=VALUES[dtype])
+    want, _ = O.combine(h, rows, w.astype(np.float64))
+    big, _ = O.combine(np.abs(h), rows, w.astype(np.float64))
+    assert (np.abs(want) < 2.0 ** 127).all()
+    err = (k + 3) * 2.0 ** -23 * big + k * 2.0 ** -149
+    bound = err + HALF[dtype] * (np.abs(want) + err) + (2.0 ** -134 if dtype == "bf16" else 2.0 ** -150)
+    assert (np.abs(f64(out) - want) <= bound).all()
