@@ -119,8 +119,11 @@ typedef enum { MOECA_ACT_NONE = 0, MOECA_ACT_GELU = 1, MOECA_ACT_GELU_TANH = 2 }
  *   out row dst[m] = act(sum_k a[m, k] b[g n_cols + c, k] + bias[g, c]), c < n_cols,
  * for the rows offsets[g] <= m < offsets[g + 1] of every group g (an expert):
  * a holds one group's rows after another's, b every group's n_cols weight
- * rows, both K = width values wide.  Sums are fp32; the result is rounded
- * once, to out's format.  Rows outside the groups are not computed.  Offsets
+ * rows, both K = width values wide.  Sums are fp32 as the tensor core adds them,
+ * truncating (relative error about 7e-8 at K = 1152 and 3e-7 at 4608, where fp32
+ * with rounding has 4e-8 and 6e-8); GELU is z (1 + h) / 2 in fp32, within 6 x 2^-24 |z|
+ * of the function and 0 where h rounds to -1; the result is rounded once, to out's
+ * format.  Rows outside the groups are not computed.  Offsets
  * are clamped to [0, a.rows], a group that would end before it starts is
  * empty; rows that two groups claim hold either's result.  An entry of dst
  * out of [0, out.rows) drops its row; entries are distinct.  Rows of out that

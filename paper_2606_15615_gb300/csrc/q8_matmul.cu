@@ -205,15 +205,25 @@ __device__ __forceinline__ float rcp(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// GELU of a chunk's values (Eq. 5), z (1 + h) / 2 with h in fp32 as gelu_f has it:
-// where h rounds to -1 the result is 0, so that an 8-bit block of nothing else
-// has the scale of zeros.  tanh form: h = 2 sigmoid(2 u) - 1, u = sqrt(2/pi) (z + 0.044715 z^3).
-// erf form: |h| = erf(|z| / sqrt 2) by Abramowitz and Stegun's formula 7.1.26,
-// 1 - P(t) exp(-z^2 / 2) with t = 1 / (1 + p |z| / sqrt 2), within 1.5e-7.
-// Two values share one reciprocal, 1/a = b / (ab): the special-function unit
-// takes 8 clocks a warp for it, and the pairs' chains interleave (28 -> 11
-// clocks a value at two warps per scheduler).  The minima keep ab finite and
-// one value's NaN out of the other.
+// GELU of a chunk's values (Eq. 5), z (1 + h) / 2 with h rounded to fp32 as in
+// gelu_f: where h is -1 the result is 0, so that an 8-bit block of nothing else has
+// the scale of zeros.
+// erf form: |h| = erf(|z| / sqrt 2) = 1 - 2^(-|z| Q(|z|)).  -log2 erfc(a / sqrt 2) / a is
+// smooth, about 1.15 + 0.46 a + .., so that a polynomial Q of degree 8, fitted for
+// the smallest largest error in h over 0 .. 5.8 (where 1 - h is below half a step of
+// fp32), is within 2.3e-9 of it, and 2^-g turns g's rounding into little of h.
+// tanh form: |h| = 1 - 2 t, t = 1 / (1 + 2^w), w = 2 sqrt(2/pi) log2(e) (|z| + 0.044715 |z|^3):
+// t is at most 1/2, and its error shrinks with it (h = 2 t - 1 of the signed w has
+// twice the error at z > 1).  Two values share one reciprocal, 1/a = b / (ab): the
+// special-function unit takes 8 clocks a warp for it.
+// The minima take |z| where h is 1 in fp32 and keep one value's NaN out of the other.
+// Largest and root mean square error over |z|, in units of 2^-24, in brackets that of
+// the same formula in fp32 with erff and tanhf:
+//   |z| < 1/2:     erf 1.3, 0.34 (1.4, 0.31)   tanh 2.2, 0.53 (1.5, 0.32)
+//   z > 1/2:       erf 1.3, 0.40 (1.9, 0.51)   tanh 1.7, 0.40 (1.9, 0.50)
+//   -1/2 .. -2:    erf 1.0, 0.21 (0.8, 0.20)   tanh 1.3, 0.26 (1.3, 0.28)
+//   z < -2:        erf 0.4, 0.13 (0.5, 0.18)   tanh 0.4, 0.13 (0.4, 0.13)
+// (a Newton step on t brings the tanh form's first line to 1.6, 0.44 and costs 1.9 us of 60).
 template <int ACT>
 __device__ __forceinline__ void activate(float (&z)[32]) {
   constexpr float kLog2e = 1.44269504f;
@@ -221,35 +231,43 @@ __device__ __forceinline__ void activate(float (&z)[32]) {
   if constexpr (ACT != MOECA_ACT_NONE) {
 #pragma unroll
     for (int i0 = 0; i0 < 32; i0 += 8) {
-      float2 v[4], d[4];
+      float2 v[4], h[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[i] = make_float2(z[i0 + 2 * i], z[i0 + 2 * i + 1]);
-        if constexpr (ACT == MOECA_ACT_GELU_TANH) {
-          const float2 w = mul2(v[i], fma2(both(-0.0713548163f * kLog2e), mul2(v[i], v[i]), both(-1.5957691216f * kLog2e)));
-          d[i] = add2(both(1.f), make_float2(ex2(fminf(w.x, 60.f)), ex2(fminf(w.y, 60.f))));  // w = -2 u log2(e)
-        } else {
-          d[i] = fma2(both(0.3275911f * 0.70710678f), make_float2(fminf(fabsf(v[i].x), 1e18f), fminf(fabsf(v[i].y), 1e18f)), both(1.f));
+      for (int i = 0; i < 4; ++i) v[i] = make_float2(z[i0 + 2 * i], z[i0 + 2 * i + 1]);
+      if constexpr (ACT == MOECA_ACT_GELU_TANH) {
+        float2 d[4], t[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float2 a = make_float2(fminf(fabsf(v[i].x), 6.f), fminf(fabsf(v[i].y), 6.f));
+          const float2 w = mul2(a, fma2(both(0.0713548163f * kLog2e), mul2(a, a), both(1.5957691216f * kLog2e)));
+          d[i] = add2(both(1.f), make_float2(ex2(w.x), ex2(w.y)));
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) t[i] = mul2(both(rcp(d[i].x * d[i].y)), make_float2(d[i].y, d[i].x));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) h[i] = fma2(both(-2.f), t[i], both(1.f));
+      } else {
+        constexpr float kQ[9] = {-1.15110421f, -0.459221452f, -0.0524347648f, 0.0069311196f, 1.49909565e-05f, -0.000284347712f, 7.49738392e-05f, -9.56023268e-06f, 5.12861789e-07f};
+        float2 a[4], q[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          a[i] = make_float2(fminf(fabsf(v[i].x), 5.8f), fminf(fabsf(v[i].y), 5.8f));
+          q[i] = both(kQ[8]);
+        }
+#pragma unroll
+        for (int c = 7; c >= 0; --c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) q[i] = fma2(q[i], a[i], both(kQ[c]));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float2 w = mul2(a[i], q[i]);
+          h[i] = add2(both(1.f), make_float2(-ex2(w.x), -ex2(w.y)));
         }
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) d[i] = mul2(both(rcp(d[i].x * d[i].y)), make_float2(d[i].y, d[i].x));
-#pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float2 t = d[i];
-        float2 r;
         const float2 half = mul2(v[i], both(0.5f));
-        if constexpr (ACT == MOECA_ACT_GELU_TANH) {
-          r = fma2(half, fma2(both(2.f), t, both(-1.f)), half);
-        } else {
-          float2 s = fma2(both(1.061405429f), t, both(-1.453152027f));
-          s = fma2(s, t, both(1.421413741f));
-          s = fma2(s, t, both(-0.284496736f));
-          s = fma2(s, t, both(0.254829592f));
-          const float2 w = mul2(v[i], mul2(half, both(-kLog2e)));
-          const float2 rest = mul2(mul2(s, t), make_float2(-ex2(w.x), -ex2(w.y)));  // -erfc(|z| / sqrt 2)
-          r = fma2(make_float2(fabsf(half.x), fabsf(half.y)), add2(both(1.f), rest), half);
-        }
+        const float2 r = fma2(make_float2(fabsf(half.x), fabsf(half.y)), h[i], half);
         z[i0 + 2 * i] = r.x;
         z[i0 + 2 * i + 1] = r.y;
       }

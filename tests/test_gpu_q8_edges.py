@@ -142,3 +142,44 @@ def test_combine_weights_meet_values_not_scales(M, T, k, dtype, fmt):
     err = (k + 3) * 2.0 ** -23 * big + k * 2.0 ** -149
     bound = err + HALF[dtype] * (np.abs(want) + err) + (2.0 ** -134 if dtype == "bf16" else 2.0 ** -150)
     assert (np.abs(f64(out) - want) <= bound).all()
+
+
+# --- GELU --------------------------------------------------------------------
+
+@pytest.mark.parametrize("act", ["gelu", "gelu_tanh"])
+def test_gelu_is_as_exact_as_fp32_functions_make_it(M, act):
+    """The product's GELU against float64, beside the same formula in fp32 with the library's erf and tanh.
+
+    Bounds, in units of u = 2^-24, for z (1 + h) / 2 = |z| / 2 x |h| + z / 2, rounded once (u |result|).
+    erf, |h| = 1 - 2^-g: the fit 0.04 u, g's three last roundings 3 ln2 g 2^-g u <= 1.6 u, 2^x 2.9 2^-g u <= 2.9 u, |h|'s
+    rounding 0.5 u: 5.1 u of h, so 2.6 u + 1 u of |z|; for z < -2, where 2^-g < 0.05, 0.04 + 0.5 + 0.15 + 0.5 = 1.2 u,
+    0.6 u + 0.05 u.
+    tanh, |h| = 1 - 2t: the exponent's roundings and constants 4 u ln2 w 2 t (1 - t) <= 1.8 u, 2^x 2.9 u 2 t (1 - t) <=
+    1.5 u, four more on t 5 u 2t <= 5 u, 0.5 u: 8.8 u, so 4.4 u + 1 u of |z|; for z < -2 (t < 0.023) 0.7 + 0.2 + 0.3 +
+    0.5 = 1.7 u, 0.9 u + 0.05 u.
+    On the mean no more than a quarter above the fp32 formula for |z| > 1/2, and below twice it near 0, where the
+    result's own rounding no longer covers the two functions' difference."""
+    n = 1 << 17
+    g = torch.Generator().manual_seed(5)
+    near = (2 * torch.rand(n // 2, generator=g) - 1) * torch.exp2(torch.randint(-10, 1, (n // 2,), generator=g).float())
+    z = torch.cat([14 * torch.rand(n // 2, generator=g) - 7, near]).cuda()
+    a, b = M.q8_write(torch.zeros(1, 1, device="cuda"), M.q8_empty(1, 1)), M.q8_empty(n, 1)
+    got = f64(M.q8_matmul(a, b, bias=z[None], act=act, dtype=torch.float32))[0]
+    if act == "gelu":
+        plain = 0.5 * z * (1 + torch.erf(z * 0.7071067811865476))
+    else:
+        plain = 0.5 * z * (1 + torch.tanh(0.7978845608028654 * (z + 0.044715 * z * z * z)))
+    z64 = f64(z)
+    if act == "gelu":  # 1 + erf and 1 + tanh cancel in float64 as well
+        from scipy.special import erfc
+        want = 0.5 * z64 * erfc(-z64 / np.sqrt(2))
+    else:
+        want = z64 / (1 + np.exp(-2 * np.sqrt(2 / np.pi) * (z64 + 0.044715 * z64 ** 3)))
+    u = 2.0 ** -24 * np.abs(z64)
+    err, err_plain = np.abs(got - want) / u, np.abs(f64(plain) - want) / u
+    low = z64 < -2
+    assert err.max() <= (3.6 if act == "gelu" else 5.4) and err[low].max() <= (0.65 if act == "gelu" else 0.95)
+    rms = lambda v: np.sqrt((v * v).mean())  # noqa: E731
+    for lo, hi, most in ((-7, -4, 1.25), (-4, -2, 1.25), (-2, -0.5, 1.25), (-0.5, 0.5, 2), (0.5, 2, 1.25), (2, 7, 1.25)):
+        at = (z64 >= lo) & (z64 < hi)
+        assert rms(err[at]) <= most * rms(err_plain[at]), (lo, hi)
