@@ -22,6 +22,9 @@ enum StatIndex {
 // uses several devices sets it on each.  Thread-safe.
 cudaError_t set_dyn_smem_on_device(const void* func, int bytes);
 
+// SMs of the current device.
+cudaError_t device_sms(int* sms);
+
 // A call without a handle failed with `why`: kept for moeca_last_error(NULL).
 void keep_call_error(const char* why) noexcept;
 

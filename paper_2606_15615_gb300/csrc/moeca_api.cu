@@ -60,6 +60,12 @@ cudaError_t set_dyn_smem_on_device(const void* func, int bytes) {
   return cudaSuccess;
 }
 
+cudaError_t device_sms(int* sms) {
+  int dev = 0;
+  const cudaError_t e = cudaGetDevice(&dev);
+  return e == cudaSuccess ? cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev) : e;
+}
+
 thread_local std::string g_create_error;
 
 void keep_call_error(const char* why) noexcept {

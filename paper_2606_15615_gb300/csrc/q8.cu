@@ -180,7 +180,10 @@ cudaError_t launch_q8_write(const Q8WriteArgs& a, bool bf16, bool e5, cudaStream
   const bool vec = q8_aligned16(a.x, a.x_stride * (bf16 ? 2 : 4));
   const int64_t units = static_cast<int64_t>(a.n) * ((a.c.width + kQ8Block - 1) / kQ8Block);
   constexpr int64_t per_block = kWriteThreads / 8;
-  const dim3 grid(static_cast<unsigned>(std::min<int64_t>((units + per_block - 1) / per_block, 152 * kWriteBlocks)));
+  int sms = 0;
+  const cudaError_t e = device_sms(&sms);
+  if (e != cudaSuccess) return e;
+  const dim3 grid(static_cast<unsigned>(std::min<int64_t>((units + per_block - 1) / per_block, sms * kWriteBlocks)));
   auto run = [&](auto kern) { return launch_pdl(kern, grid, dim3(kWriteThreads), 0, s, a); };
   auto pick = [&](auto t) {
     using TI = decltype(t);

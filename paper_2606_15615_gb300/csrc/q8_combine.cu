@@ -450,28 +450,28 @@ __global__ void __launch_bounds__(kStageWarps * 32, stage_blocks(KMAX)) q8_combi
 }
 
 template <bool E5, bool VEC, int KMAX>
-cudaError_t run_staged(const Q8CombineArgs& a, int smem, cudaStream_t s) {
+cudaError_t run_staged(const Q8CombineArgs& a, int smem, int sms, cudaStream_t s) {
   const auto kern = a.gate ? q8_combine_staged_kernel<E5, KMAX, VEC, true> : q8_combine_staged_kernel<E5, KMAX, VEC, false>;
   const cudaError_t e = set_dyn_smem_on_device(reinterpret_cast<const void*>(kern), kStageMax);
   if (e != cudaSuccess) return e;
   const int per_sm = std::max(1, std::min(kStageSm / (smem + 1088), stage_blocks(KMAX)));
-  const int64_t blocks = std::min<int64_t>((static_cast<int64_t>(a.T) + kStageWarps - 1) / kStageWarps, 152 * per_sm);
+  const int64_t blocks = std::min<int64_t>((static_cast<int64_t>(a.T) + kStageWarps - 1) / kStageWarps, sms * per_sm);
   return launch_pdl(kern, dim3(static_cast<unsigned>(blocks)), dim3(kStageWarps * 32), smem, s, a);
 }
 
 template <bool E5, bool VEC>
-cudaError_t staged(const Q8CombineArgs& a, int smem, cudaStream_t s) {
+cudaError_t staged(const Q8CombineArgs& a, int smem, int sms, cudaStream_t s) {
   switch (a.k) {
-    case 1: return run_staged<E5, VEC, 1>(a, smem, s);
-    case 2: return run_staged<E5, VEC, 2>(a, smem, s);
-    case 3: return run_staged<E5, VEC, 3>(a, smem, s);
-    case 4: return run_staged<E5, VEC, 4>(a, smem, s);
+    case 1: return run_staged<E5, VEC, 1>(a, smem, sms, s);
+    case 2: return run_staged<E5, VEC, 2>(a, smem, sms, s);
+    case 3: return run_staged<E5, VEC, 3>(a, smem, sms, s);
+    case 4: return run_staged<E5, VEC, 4>(a, smem, sms, s);
     case 5:
-    case 6: return run_staged<E5, VEC, 6>(a, smem, s);
+    case 6: return run_staged<E5, VEC, 6>(a, smem, sms, s);
     case 7:
-    case 8: return run_staged<E5, VEC, 8>(a, smem, s);
-    case 9: return run_staged<E5, VEC, 9>(a, smem, s);
-    default: return run_staged<E5, VEC, 16>(a, smem, s);
+    case 8: return run_staged<E5, VEC, 8>(a, smem, sms, s);
+    case 9: return run_staged<E5, VEC, 9>(a, smem, sms, s);
+    default: return run_staged<E5, VEC, 16>(a, smem, sms, s);
   }
 }
 
@@ -484,10 +484,13 @@ cudaError_t combine(Q8CombineArgs a, cudaStream_t s) {
   // blocks' buffers fit an SM (2000 tokens of 16 slots and 2560 values: 40 us for
   // 111 direct; of four slots and 9000, whose buffers do not: 48 alone on an SM, 47 direct).
   const int64_t wide = static_cast<int64_t>(a.c.width) * (a.k + 2 * size);
-  if (a.T > 152 * direct_blocks(a.k) && wide < kStageMax / kStageWarps) {
+  int sms = 0;
+  const cudaError_t e = device_sms(&sms);
+  if (e != cudaSuccess) return e;
+  if (a.T > sms * direct_blocks(a.k) && wide < kStageMax / kStageWarps) {
     const StageLayout L = a.vec ? stage_layout<true>(a.k, a.c.width, a.x != nullptr) : stage_layout<false>(a.k, a.c.width, a.x != nullptr);
     const int smem = kStageWarps * L.bytes;
-    if (smem <= kStageMax) return a.vec ? staged<E5, true>(a, smem, s) : staged<E5, false>(a, smem, s);
+    if (smem <= kStageMax) return a.vec ? staged<E5, true>(a, smem, sms, s) : staged<E5, false>(a, smem, sms, s);
   }
   const dim3 grid(a.T), block(kDirectWarps * 32);
   if (a.k == 1) return launch_pdl(q8_combine_kernel<E5, 1>, grid, block, 0, s, a);

@@ -814,9 +814,8 @@ cudaError_t launch_q8_matmul(const Q8MatmulArgs& a, cudaStream_t s) {
     else maps.act[i] = maps.act[0];
   }
   if (!ok) return cudaErrorInvalidValue;
-  int dev = 0, sms = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  int sms = 0;
+  const cudaError_t e = device_sms(&sms);
   if (e != cudaSuccess) return e;
   MatmulParams p{};
   p.w_scale = a.b.scale; p.w_stride = a.b.scale_stride; p.w_rows = a.b.rows;
