@@ -69,6 +69,14 @@ int32_t moeca_probe_hold(int32_t device, int32_t blocks, int32_t smem_bytes, int
  * moeca_config.weight_prefetch_mb = setting_mb.  Runs on the host. */
 int64_t moeca_probe_prefetch_bytes(int64_t w1_bytes, int32_t setting_mb, int32_t blocks);
 
+/* Which form of its kernel a moeca_q8_combine on a device of `sms` SMs takes: 1
+ * the one staged in shared memory (many tokens), 0 the direct one (few tokens, or
+ * rows too wide for the first).  residual: with x; aligned: all rows of x and out
+ * start at 16 bytes.  moeca_q8_read is the same with one slot and no residual.
+ * For tests that have to reach both.  Returns -1 out of range.  Runs on the host. */
+int32_t moeca_probe_q8_staged(int32_t sms, int32_t n_tokens, int32_t n_slots, int32_t width, int32_t dtype, int32_t residual,
+                              int32_t aligned);
+
 /* Let a wait of the calling thread's later moeca_q8_read, _combine and _matmul
  * calls run out: barriers of the named kind are set up for an arrival that never
  * comes, every wait gives up after wait_ns (1000000 .. 1000000000), and the call's

@@ -423,6 +423,19 @@ moeca_status moeca_q8_matmul(const moeca_q8_matmul_args* a, void* stream) {
   return launched([&] { return launch_q8_matmul(d, static_cast<cudaStream_t>(stream)); });
 }
 
+int32_t moeca_probe_q8_staged(int32_t sms, int32_t n_tokens, int32_t n_slots, int32_t width, int32_t dtype, int32_t residual,
+                              int32_t aligned) {
+  using namespace moeca;
+  if (sms < 1 || n_tokens < 0 || n_slots < 1 || n_slots > kMaxSlots || width < 1 || width > kMaxWidth || !is_dtype(dtype)) return -1;
+  Q8CombineArgs a{};
+  a.c.width = width;
+  a.T = n_tokens;
+  a.k = n_slots;
+  a.out = reinterpret_cast<void*>(static_cast<uintptr_t>(aligned ? 16 : 20));  // looked at, not read
+  a.x = residual ? a.out : nullptr;
+  return dtype == MOECA_BF16 ? q8_combine_is_staged_bf16(a, sms) : q8_combine_is_staged_f32(a, sms);
+}
+
 int32_t moeca_probe_q8_stall(int32_t barrier, int64_t wait_ns) {
   using namespace moeca;
   if (barrier < MOECA_Q8_NONE || barrier > MOECA_Q8_ACCUMULATORS || wait_ns < 1000000 || wait_ns > 1000000000) return -1;

@@ -142,6 +142,9 @@ struct Q8CombineArgs {
   Q8Waits waits;
   bool vec, gate_vec;  // set at the launch: 16-byte accesses of x and out, of the gate
 };
+// Whether a launch takes the staged form on a device of `sms` SMs.
+bool q8_combine_is_staged_bf16(const Q8CombineArgs& a, int sms);
+bool q8_combine_is_staged_f32(const Q8CombineArgs& a, int sms);
 cudaError_t launch_q8_combine_bf16(const Q8CombineArgs& a, bool e5, cudaStream_t s);
 cudaError_t launch_q8_combine_f32(const Q8CombineArgs& a, bool e5, cudaStream_t s);
 

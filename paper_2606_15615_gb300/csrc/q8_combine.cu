@@ -475,23 +475,32 @@ cudaError_t staged(const Q8CombineArgs& a, int smem, int sms, cudaStream_t s) {
   }
 }
 
+bool row_vec(const Q8CombineArgs& a) {
+  constexpr int size = sizeof(TI);
+  return q8_aligned16(a.out, a.out_stride * size) && (!a.x || q8_aligned16(a.x, a.x_stride * size));
+}
+
+// Shared memory of the staged form's blocks, 0 where the direct form is taken:
+// staged where the tokens are more than direct blocks run at once and two
+// blocks' buffers fit an SM (2000 tokens of 16 slots and 2560 values: 40 us for
+// 111 direct; of four slots and 9000, whose buffers do not: 48 alone on an SM, 47 direct).
+int staged_smem(const Q8CombineArgs& a, int sms) {
+  const int64_t wide = static_cast<int64_t>(a.c.width) * (a.k + 2 * static_cast<int>(sizeof(TI)));
+  if (a.T <= sms * direct_blocks(a.k) || wide >= kStageMax / kStageWarps) return 0;
+  const StageLayout L = row_vec(a) ? stage_layout<true>(a.k, a.c.width, a.x != nullptr) : stage_layout<false>(a.k, a.c.width, a.x != nullptr);
+  const int smem = kStageWarps * L.bytes;
+  return smem <= kStageMax ? smem : 0;
+}
+
 template <bool E5>
 cudaError_t combine(Q8CombineArgs a, cudaStream_t s) {
-  constexpr int size = sizeof(TI);
-  a.vec = q8_aligned16(a.out, a.out_stride * size) && (!a.x || q8_aligned16(a.x, a.x_stride * size));
+  a.vec = row_vec(a);
   a.gate_vec = a.gate && q8_aligned16(a.gate, a.gate_stride * 4);
-  // Staged where the tokens are more than direct blocks run at once and two
-  // blocks' buffers fit an SM (2000 tokens of 16 slots and 2560 values: 40 us for
-  // 111 direct; of four slots and 9000, whose buffers do not: 48 alone on an SM, 47 direct).
-  const int64_t wide = static_cast<int64_t>(a.c.width) * (a.k + 2 * size);
   int sms = 0;
   const cudaError_t e = device_sms(&sms);
   if (e != cudaSuccess) return e;
-  if (a.T > sms * direct_blocks(a.k) && wide < kStageMax / kStageWarps) {
-    const StageLayout L = a.vec ? stage_layout<true>(a.k, a.c.width, a.x != nullptr) : stage_layout<false>(a.k, a.c.width, a.x != nullptr);
-    const int smem = kStageWarps * L.bytes;
-    if (smem <= kStageMax) return a.vec ? staged<E5, true>(a, smem, sms, s) : staged<E5, false>(a, smem, sms, s);
-  }
+  const int smem = staged_smem(a, sms);
+  if (smem > 0) return a.vec ? staged<E5, true>(a, smem, sms, s) : staged<E5, false>(a, smem, sms, s);
   const dim3 grid(a.T), block(kDirectWarps * 32);
   if (a.k == 1) return launch_pdl(q8_combine_kernel<E5, 1>, grid, block, 0, s, a);
   if (a.k == 2) return launch_pdl(q8_combine_kernel<E5, 2>, grid, block, 0, s, a);
@@ -503,8 +512,10 @@ cudaError_t combine(Q8CombineArgs a, cudaStream_t s) {
 }  // namespace
 
 #ifdef MOECA_Q8_COMBINE_F32
+bool q8_combine_is_staged_f32(const Q8CombineArgs& a, int sms) { return staged_smem(a, sms) > 0; }
 cudaError_t launch_q8_combine_f32(const Q8CombineArgs& a, bool e5, cudaStream_t s) {
 #else
+bool q8_combine_is_staged_bf16(const Q8CombineArgs& a, int sms) { return staged_smem(a, sms) > 0; }
 cudaError_t launch_q8_combine_bf16(const Q8CombineArgs& a, bool e5, cudaStream_t s) {
 #endif
   if (a.T <= 0) return cudaSuccess;

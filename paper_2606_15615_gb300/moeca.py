@@ -181,6 +181,7 @@ def _load():
         "moeca_q8_read": (C.c_int, [C.POINTER(moeca_q8_read_args), C.c_void_p]),
         "moeca_q8_combine": (C.c_int, [C.POINTER(moeca_q8_combine_args), C.c_void_p]),
         "moeca_q8_matmul": (C.c_int, [C.POINTER(moeca_q8_matmul_args), C.c_void_p]),
+        "moeca_probe_q8_staged": (C.c_int32, [C.c_int32] * 7),
         "moeca_probe_q8_stall": (C.c_int32, [C.c_int32, C.c_int64]),
         "moeca_probe_ffma": (C.c_int32, [C.c_int32, C.c_int32, C.POINTER(C.c_double), C.POINTER(C.c_double)]),
         "moeca_probe_maps_encoded": (C.c_int64, []),
@@ -397,6 +398,15 @@ def moeca_probe_hold(device: int, blocks: int, smem_bytes: int, us: int, stream:
     st = LIB.moeca_probe_hold(device, blocks, smem_bytes, us, stream)
     if st != MOECA_OK:
         raise MoecaError(st, "moeca_probe_hold")
+
+
+def moeca_probe_q8_staged(sms: int, tokens: int, slots: int, width: int, dtype: int, residual: bool = True,
+                          aligned: bool = True) -> bool:
+    """Whether an 8-bit combine takes the form staged in shared memory (include/moeca_probe.h)."""
+    st = LIB.moeca_probe_q8_staged(sms, tokens, slots, width, dtype, residual, aligned)
+    if st < 0:
+        raise MoecaError(st, "moeca_probe_q8_staged")
+    return bool(st)
 
 
 def moeca_probe_q8_stall(barrier: int, wait_ns: int = 20_000_000) -> None:
