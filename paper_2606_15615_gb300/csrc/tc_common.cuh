@@ -221,15 +221,19 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
+// Threads may ask at the same time: each finds the same function.
 inline EncodeTiledFn get_encoder() {
-  static EncodeTiledFn fn = nullptr;
+  static std::atomic<EncodeTiledFn> kept{nullptr};
+  EncodeTiledFn fn = kept.load(std::memory_order_relaxed);
   if (!fn) {
     void* p = nullptr;
     cudaDriverEntryPointQueryResult q;
     if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) ==
             cudaSuccess &&
-        q == cudaDriverEntryPointSuccess)
+        q == cudaDriverEntryPointSuccess) {
       fn = reinterpret_cast<EncodeTiledFn>(p);
+      kept.store(fn, std::memory_order_relaxed);
+    }
   }
   return fn;
 }
