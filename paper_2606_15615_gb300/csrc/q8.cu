@@ -25,11 +25,12 @@ thread_local Q8Waits g_waits = kWaits;
 // shifted into place in registers.
 // 65549 x 2568 fp32 rows take 130 us (6.5 TB/s, 0.95 of a plain copy's rate),
 // 60000 x 1152 bf16 rows 42 us (5.0 TB/s with the launch: instruction issue and
-// HBM share the bound), 60000 x 1153 unaligned ones 66 us.
+// HBM share the bound), 60000 x 1153 unaligned ones 66 us (two 16-byte loads for
+// each piece, and the shifts).
 // ---------------------------------------------------------------------------
 constexpr int kWriteThreads = 256;
-constexpr int kWriteBlocks = 3;  // per SM: 45.7 us for 60000 bf16 rows of 1152; 4 with fewer registers each: the same, but 164 us for 134 in fp32
-
+// Per SM.  Four with fewer registers each: the same time in bf16, but 164 us for 134 in fp32.
+constexpr int kWriteBlocks = 3;
 
 // One unit on its way: where it goes and its raw values.
 template <int J>

@@ -220,20 +220,21 @@ __global__ void __launch_bounds__(kDirectWarps * 32, direct_blocks(KMAX)) q8_com
 //
 // Decoding is what costs next to HBM here: a conversion of two e4m3 values
 // takes a scheduler 4 clocks, their widening 3; the loop over a token's values
-// holds no branch and no select, so that the slots' chains interleave (a scale ahead
-// of the weight in it: 95 -> 103 us in e5m2 at eight slots, so that tokens with
-// moderate ones have a loop of their own).  For
-// that the buffer is prepared once per token: slots that hold nothing and the
-// bytes past the row's width are zeros, and the scales are turned into floats
-// by block.
+// holds no branch and no select, so that the slots' chains interleave.  For that
+// the buffer is prepared once per token: slots that hold nothing and the bytes
+// past the row's width are zeros, and the scales are turned into floats by block.
+// Tokens with a far scale or weight (see slot_values) have a loop of their own: one
+// loop with the value first took 103 us for 95 at eight slots in e5m2.
 //
 // Rows of x and out that do not start at 16 bytes (VEC false): x is copied in
 // the aligned pieces that hold it and shifted as it is read; out is put
 // together in the buffer and leaves it in aligned pieces.
 //
-// 32768 tokens x 8 slots x 1152 (e4m3, gated, bf16) take 103 us (4.5 TB/s, bound by
-// decoding and its latency; 172 us with loads to registers), 4096 x 3 x 2560 23 us,
-// 20000 x 1 x 1152 40 us (5.3 TB/s), 60000 rows of 1152 read back 44 us, of 1153 62 us.
+// One launch after a flush of L2: 32768 tokens x 8 slots x 1152 (e4m3, gated, bf16) 103 us
+// (4.5 TB/s, bound by decoding and its latency; 172 us with loads to registers), 4096 x
+// 3 x 2560 23 us, 20000 x 1 x 1152 40 us (5.3 TB/s), 60000 rows of 1152 read back 44 us, of
+// 1153 62 us: a read's issue slots are 0.71 busy and HBM 0.44 (a token's fixed costs
+// weigh most with one slot, and the square sums are formed for nobody).
 // ---------------------------------------------------------------------------
 constexpr int kStageWarps = 2;
 constexpr int kStageSm = 227 * 1024, kStageMax = 112 * 1024;  // shared memory of an SM, and the most a block takes
