@@ -40,7 +40,8 @@ extern "C" {
 /* Formats beside MOECA_F32 and MOECA_BF16. */
 typedef enum { MOECA_E4M3 = 2, MOECA_E5M2 = 3 } moeca_q8_format;
 
-/* Rows in 8 bits; as a product's output also rows of fp32 or bf16. */
+/* Rows in 8 bits; as a product's output also rows of fp32 or bf16.  Rows are read
+ * in pieces of 16 bytes and scales in words, the last ones to their end. */
 typedef struct {
   void* q;               /* [rows] rows of `width` bytes, 16-byte aligned             */
   uint8_t* scale;        /* [rows] rows of ceil(width / 128) bytes, 4-byte aligned    */

@@ -242,8 +242,11 @@ const char* bad_values(const void* p, int64_t rows, int64_t stride, int width, i
   if (stride < width || (rows > 0 && stride > INT64_MAX / 8 / rows)) return "a value stride is smaller than the width, or out of range";
   return nullptr;
 }
-Range q_range(const moeca_q8_rows& r) { return rows_range(r.q, r.rows, r.q_stride, r.q_stride); }
-Range scale_range(const moeca_q8_rows& r) { return rows_range(r.scale, r.rows, r.scale_stride, r.scale_stride); }
+// What the kernels touch: rows in pieces of 16 bytes, their scales in words.
+int64_t row_bytes(const moeca_q8_rows& r) { return (r.width + 15) / 16 * 16; }
+int64_t scale_bytes(const moeca_q8_rows& r) { return ((r.width + kQ8Block - 1) / kQ8Block + 3) / 4 * 4; }
+Range q_range(const moeca_q8_rows& r) { return rows_range(r.q, r.rows, r.q_stride, row_bytes(r)); }
+Range scale_range(const moeca_q8_rows& r) { return rows_range(r.scale, r.rows, r.scale_stride, scale_bytes(r)); }
 Q8Rows device_rows(const moeca_q8_rows& r) {
   return {static_cast<uint8_t*>(r.q), r.scale, r.rows, r.q_stride, r.scale_stride, r.width};
 }
@@ -409,7 +412,7 @@ moeca_status moeca_q8_matmul(const moeca_q8_matmul_args* a, void* stream) {
   if (!a->dst && o.rows < M) return refuse("out has fewer rows than a, and there is no dst");
   if (addr(a->offsets) % 4 || addr(a->dst) % 4 || addr(a->bias) % 4 || addr(a->status) % 4)
     return refuse("offsets, dst, bias or status is not 4-byte aligned");
-  const Range written[] = {rows_range(o.q, o.rows, o.q_stride, is_format(o.format) ? o.q_stride : o.width * elem_size(o.format)),
+  const Range written[] = {is_format(o.format) ? q_range(o) : rows_range(o.q, o.rows, o.q_stride, o.width * elem_size(o.format)),
                            is_format(o.format) ? scale_range(o) : Range{nullptr, 0}, {a->status, 8}};
   const Range read[] = {q_range(a->a), scale_range(a->a), q_range(a->b), scale_range(a->b),
                         {a->offsets, 4ll * (a->n_groups + 1)}, {a->dst, 4 * M}, {a->bias, 4 * a->b.rows}};

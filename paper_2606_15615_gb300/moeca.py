@@ -635,7 +635,8 @@ _ACTS = {"none": MOECA_ACT_NONE, "gelu": MOECA_ACT_GELU, "gelu_tanh": MOECA_ACT_
 class Q8(NamedTuple):
     """Rows held in 8 bits: ``q`` [rows, width] float8_e4m3fn or float8_e5m2, its row stride a multiple
     of 16 bytes; ``scale`` [rows, ceil(width / 128)] uint8, its row stride a multiple of 4, byte s for 2^(s - 127).
-    The storage under a row reaches to the next row's start."""
+    The storage under a row reaches to the next multiple of 16 bytes, under its scales of 4.  Columns of wider rows
+    that start at a multiple of 512 values are such rows too."""
     q: "torch.Tensor"  # noqa: F821
     scale: "torch.Tensor"  # noqa: F821
 
