@@ -736,15 +736,11 @@ def _on(stream: int, device: int, make):
         return make()
 
 
-# Each call runs on ``stream`` (a raw cudaStream_t), by default the tensors' device's current stream.  Results that a
-# call allocates belong to that stream: another one waits for it before it reads them, and as with any torch tensor
-# record_stream() tells the allocator of uses elsewhere.
-
-
 def q8_write(x, cache: Q8, src=None, dst=None, count=None, stream: int = 0) -> Q8:
     """Quantise rows of ``x`` (fp32 or bf16) into ``cache`` (float8 type and scales as allocated): cache row
     dst[i] from x row src[i], int32 lists on the device (None: i), for all entries or the first ``count``
-    (an int32 device tensor of one value).  Entries out of range are skipped.  Returns ``cache``."""
+    (an int32 device tensor of one value).  Entries out of range are skipped.  ``stream``: a raw cudaStream_t to run
+    on, by default the device's current stream.  Returns ``cache``."""
     dev = x.get_device()
     address, n_x, x_stride, width, dtype = _value_fields(x, "x", dev)
     rows = _q8_fields(cache, "cache", dev)
@@ -762,7 +758,8 @@ def q8_write(x, cache: Q8, src=None, dst=None, count=None, stream: int = 0) -> Q
 def q8_read(cache: Q8, rows=None, dtype=None, out=None, status=None, stream: int = 0):
     """Cache rows as bf16 (default) or fp32: all of them, or those of ``rows`` (int32, on the device); zeros
     where an entry is out of range.  ``status``: as for q8_matmul (without it a read of many rows whose copies do
-    not arrive is incomplete in silence)."""
+    not arrive is incomplete in silence).  ``stream``: as for q8_write; a result that the call allocates belongs to it
+    (another stream waits for it first, and record_stream() tells the allocator of uses there)."""
     dev = cache[0].get_device()
     c = _q8_fields(cache, "cache", dev)
     n = c[2] if rows is None else rows.numel()
@@ -786,8 +783,8 @@ def q8_combine(cache: Q8, rows, weights=None, x=None, gate=None, norms=False, dt
     """Eq. 8 over an 8-bit branch cache: x + gate * sum_p weights[:, p] cache[rows[:, p]].  ``rows`` [T, k]
     int32 (out of range: an empty slot), ``weights`` [T, k] fp32 (None: 1), ``x`` [T, D] fp32 or bf16 (None: 0),
     ``gate`` [B, D] fp32, one row for each T / B consecutive tokens.  ``norms``: True or a [T, k] fp32 tensor
-    also gives the rows' 2-norms.  ``status``: as for q8_matmul.  The result has x's dtype (without x: ``dtype``, default bf16); ``out`` may be
-    x.  Returns out, or (out, norms)."""
+    also gives the rows' 2-norms.  The result has x's dtype (without x: ``dtype``, default bf16); ``out`` may be
+    x.  ``status``: as for q8_matmul; ``stream``: as for q8_read.  Returns out, or (out, norms)."""
     q = cache[0]
     dev = q.get_device()
     c = _q8_fields(cache, "cache", dev)
@@ -842,7 +839,7 @@ def q8_matmul(a: Q8, b: Q8, offsets=None, bias=None, act: str = "none", dst=None
     types give a Q8), in which rows of no group, and rows that ``dst`` names nowhere, are zeros (offsets and dst are
     known on the device only, so the whole of it is filled first: a given ``out`` saves that).  ``status`` [2] int32
     zeros on the device: its first word becomes MOECA_ERR_TIMEOUT if a wait of the kernel ran out and the result is
-    incomplete; without it nothing tells.  Returns out."""
+    incomplete; without it nothing tells.  ``stream``: as for q8_read.  Returns out."""
     dev = a[0].get_device()
     ra, rb = _q8_fields(a, "a", dev), _q8_fields(b, "b", dev)
     groups = offsets.numel() - 1 if offsets is not None else 1
