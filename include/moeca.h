@@ -547,7 +547,8 @@ moeca_status moeca_ddpm_step(const moeca_ddpm_args* args, void* stream);
 const char* moeca_status_string(moeca_status s);
 /* Message of the last error on this handle ("" if none); NULL handle: the
  * last failure of a call without a handle on this thread (moeca_create,
- * moeca_ddpm_schedule, moeca_ddpm_step, the calls of moeca_q8.h). */
+ * moeca_ddpm_schedule, moeca_ddpm_step, the calls of moeca_q8.h, moeca_experts.h and
+ * moeca_attention.h). */
 const char* moeca_last_error(const moeca_handle* h);
 
 #ifdef __cplusplus

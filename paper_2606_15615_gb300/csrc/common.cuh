@@ -130,6 +130,23 @@ __device__ __forceinline__ void unpack_vec(const uint4& v, float* out, __nv_bflo
   }
 }
 
+// The 16 bytes from byte `m` (a multiple of the type's size, below 16) of two
+// consecutive 16-byte pieces.
+template <typename TI>
+__device__ __forceinline__ uint4 shifted(const uint4& a, const uint4& b, uint32_t m) {
+  uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+  for (int i = 0; i < 6; ++i) w[i] = m & 8 ? w[i + 2] : w[i];
+#pragma unroll
+  for (int i = 0; i < 5; ++i) w[i] = m & 4 ? w[i + 1] : w[i];
+  if (sizeof(TI) == 2) {
+    const uint32_t sel = m & 2 ? 0x5432 : 0x3210;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __byte_perm(w[i], w[i + 1], sel);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);

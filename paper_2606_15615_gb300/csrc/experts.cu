@@ -1,0 +1,599 @@
+// Tokens sorted by expert and back, with the gradients (include/moeca_experts.h).
+#include <algorithm>
+
+#include "calls.h"
+#include "common.cuh"
+#include "moeca_experts.h"
+
+namespace moeca {
+namespace {
+
+constexpr int kExpertsMost = 512;
+constexpr int64_t kMaxBranches = 1 << 30;
+
+// ---------------------------------------------------------------------------
+// Sort: a stable counting sort.  A block's warps take consecutive pieces of the
+// branches; a warp counts its piece 32 ids at a time (the lanes of one id find
+// each other with a match, the first of them adds their number to the warp's
+// count of that id).  A prefix sum over the warps and the experts turns counts
+// into first rows, and a second walk over the same ids hands the rows out in
+// order.  Few branches are one block's work; of many, a first launch counts each
+// block's piece into the workspace, and every block of the second sums the
+// counts of the blocks before it.  No atomic's order shows in a result.
+// ---------------------------------------------------------------------------
+constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
+constexpr int kSortOneBlock = 8192;  // branches that one block sorts
+constexpr int kSortPiece = 2048;     // branches of a block otherwise, at least
+constexpr int kSortBlocks = 128;     // at most
+
+struct SortArgs {
+  const int32_t* experts;
+  int n, k, E;
+  int piece;  // branches per block
+  int32_t *offsets, *place, *slot, *token, *work;
+};
+
+int sort_blocks(int64_t n) {
+  return n <= kSortOneBlock ? 1 : static_cast<int>(std::min<int64_t>(kSortBlocks, (n + kSortPiece - 1) / kSortPiece));
+}
+
+__global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const SortArgs a) {
+  extern __shared__ int32_t count[];  // [E]
+  pdl_entry();
+  for (int e = threadIdx.x; e < a.E; e += kSortThreads) count[e] = 0;
+  __syncthreads();
+  const int64_t lo = static_cast<int64_t>(blockIdx.x) * a.piece;
+  const int hi = static_cast<int>(min(lo + a.piece, static_cast<int64_t>(a.n)));
+  for (int i = static_cast<int>(min(lo, static_cast<int64_t>(hi))) + threadIdx.x; i < hi; i += kSortThreads) {
+    const int e = a.experts[i];
+    if (static_cast<unsigned>(e) < static_cast<unsigned>(a.E)) atomicAdd(&count[e], 1);
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < a.E; e += kSortThreads) a.work[blockIdx.x * a.E + e] = count[e];
+}
+
+__global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const SortArgs a) {
+  extern __shared__ int32_t next[];  // [warps][E]: counts, then the next row of the warp's branches of expert e
+  __shared__ int32_t warp_total[kSortWarps];
+  pdl_entry();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t before = (1u << lane) - 1;
+  const int E = a.E;
+  for (int i = threadIdx.x; i < kSortWarps * E; i += kSortThreads) next[i] = 0;
+  __syncthreads();
+  // This warp's piece, in steps of 32 branches.
+  const int64_t lo = static_cast<int64_t>(blockIdx.x) * a.piece;
+  const int64_t hi = min(lo + a.piece, static_cast<int64_t>(a.n));
+  const int each = (a.piece + kSortThreads - 1) / kSortThreads * 32;
+  const int64_t wlo = lo + static_cast<int64_t>(warp) * each, whi = min(wlo + each, hi);
+  int32_t* mine = next + warp * E;
+  for (int64_t i0 = wlo; i0 < whi; i0 += 32) {
+    const int64_t i = i0 + lane;
+    int e = i < whi ? a.experts[i] : -1;
+    if (static_cast<unsigned>(e) >= static_cast<unsigned>(E)) e = -1;
+    const uint32_t same = __match_any_sync(0xffffffffu, e);
+    if (e >= 0 && (same & before) == 0) mine[e] += __popc(same);
+    __syncwarp();
+  }
+  __syncthreads();
+  // Thread e < E: the warps' counts become offsets within the block, and the
+  // experts' totals offsets over all branches.
+  const int e = threadIdx.x;
+  int total = 0, earlier = 0;
+  if (e < E) {
+    for (int w = 0; w < kSortWarps; ++w) {
+      const int c = next[w * E + e];
+      next[w * E + e] = total;
+      total += c;
+    }
+    if (gridDim.x > 1) {
+      total = 0;
+      for (int b = 0; b < gridDim.x; ++b) {
+        const int c = a.work[b * E + e];
+        earlier += b < blockIdx.x ? c : 0;
+        total += c;
+      }
+    }
+  }
+  int sum = total;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int v = __shfl_up_sync(0xffffffffu, sum, o);
+    if (lane >= o) sum += v;
+  }
+  if (lane == 31) warp_total[warp] = sum;
+  __syncthreads();
+  int first = sum - total, all = 0;
+  for (int w = 0; w < kSortWarps; ++w) {
+    if (w < warp) first += warp_total[w];
+    all += warp_total[w];
+  }
+  if (e < E) {
+    for (int w = 0; w < kSortWarps; ++w) next[w * E + e] += first + earlier;
+    if (blockIdx.x == 0) a.offsets[e] = first;
+  }
+  if (blockIdx.x == 0 && e == 0) a.offsets[E] = all;
+  __syncthreads();
+  for (int64_t i0 = wlo; i0 < whi; i0 += 32) {
+    const int64_t i = i0 + lane;
+    int x = i < whi ? a.experts[i] : -1;
+    if (static_cast<unsigned>(x) >= static_cast<unsigned>(E)) x = -1;
+    const uint32_t same = __match_any_sync(0xffffffffu, x);
+    int row = -1;
+    if (x >= 0) row = mine[x] + __popc(same & before);
+    __syncwarp();
+    if (x >= 0 && (same & before) == 0) mine[x] += __popc(same);
+    __syncwarp();
+    if (i < whi) a.place[i] = row;
+    if (row >= 0) {
+      if (a.slot) a.slot[row] = static_cast<int>(i);
+      if (a.token) a.token[row] = static_cast<int>(i / a.k);
+    }
+  }
+  // Behind the last row.
+  for (int64_t r = all + static_cast<int64_t>(blockIdx.x) * kSortThreads + threadIdx.x; r < a.n;
+       r += static_cast<int64_t>(gridDim.x) * kSortThreads) {
+    if (a.slot) a.slot[r] = -1;
+    if (a.token) a.token[r] = -1;
+  }
+}
+
+cudaError_t launch_sort(SortArgs a, cudaStream_t s) {
+  const int blocks = sort_blocks(a.n);
+  // A multiple of 32 ids for every warp.
+  a.piece = static_cast<int>((static_cast<int64_t>(a.n) + blocks - 1) / blocks);
+  a.piece = std::max((a.piece + kSortThreads - 1) / kSortThreads, 1) * kSortThreads;
+  if (blocks > 1) {
+    const cudaError_t e = launch_pdl(sort_count_kernel, dim3(blocks), dim3(kSortThreads), a.E * 4, s, a);
+    if (e != cudaSuccess) return e;
+  }
+  const size_t smem = static_cast<size_t>(kSortWarps) * a.E * 4;
+  if (smem > 48 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute(sort_place_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               kSortWarps * kExpertsMost * 4);
+    if (e != cudaSuccess) return e;
+  }
+  return launch_pdl(sort_place_kernel, dim3(blocks), dim3(kSortThreads), smem, s, a);
+}
+
+// ---------------------------------------------------------------------------
+// Rows.  All three kernels move rows in units of 16 bytes, a unit of a written
+// row per thread; the written row's own 16-byte boundaries cut the units, so that
+// rows of any alignment go out in whole sectors (the first and last unit of an
+// unaligned row may be partial: value by value).  What is read is shifted into
+// place from the aligned pieces that hold it.
+// ---------------------------------------------------------------------------
+constexpr int kRowThreads = 256;
+
+template <typename T>
+__device__ __forceinline__ int misalign(const T* p) {
+  return static_cast<int>((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T));
+}
+
+// V values from p on, all of them inside their row.
+template <typename T, bool ALIGNED>
+__device__ __forceinline__ uint4 load_unit(const T* p) {
+  if (ALIGNED) return *reinterpret_cast<const uint4*>(p);
+  const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+  const uint32_t m = at & 15;
+  const uint4* piece = reinterpret_cast<const uint4*>(at - m);
+  const uint4 lo = piece[0];
+  return m ? shifted<T>(lo, piece[1], m) : lo;
+}
+// The same for a unit of which only values lo .. hi - 1 are inside the row; the others are zero.
+template <typename T>
+__device__ __forceinline__ uint4 load_part(const T* p, int lo, int hi) {
+  uint4 raw = make_uint4(0, 0, 0, 0);
+  T* v = reinterpret_cast<T*>(&raw);
+#pragma unroll
+  for (int i = 0; i < Elem<T>::kVec; ++i)
+    if (i >= lo && i < hi) v[i] = p[i];
+  return raw;
+}
+template <typename T>
+__device__ __forceinline__ uint4 pack_unit(const float* f) {
+  uint4 raw;
+  store_vec(reinterpret_cast<T*>(&raw), f);
+  return raw;
+}
+
+// A unit of a written row: values [lo, hi) of the V from `at` on.
+template <typename T, bool ALIGNED>
+struct Unit {
+  int at, lo, hi;
+  bool whole;
+  __device__ __forceinline__ Unit(int u, const T* row, int width) {
+    constexpr int V = Elem<T>::kVec;
+    at = u * V - (ALIGNED ? 0 : misalign(row));
+    lo = max(-at, 0);
+    hi = min(width - at, V);
+    whole = lo == 0 && hi == V;
+  }
+  __device__ __forceinline__ bool any() const { return lo < hi; }
+  __device__ __forceinline__ uint4 load(const T* row) const {
+    return whole ? load_unit<T, ALIGNED>(row + at) : load_part(row + at, lo, hi);
+  }
+  __device__ __forceinline__ void store(T* row, const uint4& raw) const {
+    if (whole) {
+      *reinterpret_cast<uint4*>(row + at) = raw;
+      return;
+    }
+    const T* v = reinterpret_cast<const T*>(&raw);
+#pragma unroll
+    for (int i = 0; i < Elem<T>::kVec; ++i)
+      if (i >= lo && i < hi) row[at + i] = v[i];
+  }
+};
+
+// Units that a row of any alignment needs.
+template <typename T>
+__host__ __device__ constexpr int row_units(int width, bool aligned) {
+  constexpr int V = Elem<T>::kVec;
+  return aligned ? (width + V - 1) / V : (width + 2 * V - 2) / V;
+}
+
+// The row and unit of the calling thread, the threads of all blocks numbered through.
+struct Item {
+  int64_t row;
+  int u;
+  __device__ __forceinline__ Item(int64_t block, int units) {
+    const int64_t start = block * kRowThreads;
+    int64_t row0;
+    if (start < 0x7fffffff) row0 = static_cast<uint32_t>(start) / static_cast<uint32_t>(units);
+    else row0 = start / units;
+    const uint32_t t = static_cast<uint32_t>(start - row0 * units) + threadIdx.x;
+    const uint32_t q = t / static_cast<uint32_t>(units);
+    row = row0 + q;
+    u = static_cast<int>(t - q * units);
+  }
+};
+
+// Rows from *count on become zeros.
+template <typename T, bool ALIGNED>
+__device__ __forceinline__ void clear_tail(T* rows, int64_t stride, int64_t n_rows, const int32_t* count, int units,
+                                           int width) {
+  if (!count) return;
+  const int64_t used = min(max(static_cast<int64_t>(*count), int64_t(0)), n_rows);
+  const int64_t blocks = ((n_rows - used) * units + kRowThreads - 1) / kRowThreads;
+  for (int64_t b = blockIdx.x; b < blocks; b += gridDim.x) {
+    const Item it(b, units);
+    const int64_t r = used + it.row;
+    if (r >= n_rows) break;
+    T* row = rows + r * stride;
+    const Unit<T, ALIGNED> unit(it.u, row, width);
+    if (unit.any()) unit.store(row, make_uint4(0, 0, 0, 0));
+  }
+}
+
+struct RowsArgs {
+  const void* x;
+  int64_t x_stride;
+  void* rows;
+  int64_t rows_stride, n_rows;
+  const int32_t *place, *count;
+  int T, k, width, units;
+};
+
+// x is read once and written to its k rows.  Unaligned rows start at k different
+// boundaries: there a unit belongs to a branch, and x comes from L1 or L2 again.
+template <typename T, bool ALIGNED>
+__global__ void __launch_bounds__(kRowThreads) expert_rows_kernel(const RowsArgs a) {
+  pdl_entry();
+  const int64_t items = ALIGNED ? a.T : static_cast<int64_t>(a.T) * a.k;
+  const int64_t blocks = (items * a.units + kRowThreads - 1) / kRowThreads;
+  for (int64_t b = blockIdx.x; b < blocks; b += gridDim.x) {
+    const Item it(b, a.units);
+    if (it.row >= items) break;
+    if (ALIGNED) {
+      const T* x = static_cast<const T*>(a.x) + it.row * a.x_stride;
+      const Unit<T, true> unit(it.u, x, a.width);
+      const uint4 raw = unit.load(x);
+      for (int p = 0; p < a.k; ++p) {
+        const int r = a.place[it.row * a.k + p];
+        if (static_cast<unsigned>(r) < a.n_rows) unit.store(static_cast<T*>(a.rows) + r * a.rows_stride, raw);
+      }
+    } else {
+      const int r = a.place[it.row];
+      if (static_cast<unsigned>(r) >= a.n_rows) continue;
+      T* row = static_cast<T*>(a.rows) + r * a.rows_stride;
+      const Unit<T, false> unit(it.u, row, a.width);
+      if (unit.any()) unit.store(row, unit.load(static_cast<const T*>(a.x) + it.row / a.k * a.x_stride));
+    }
+  }
+  clear_tail<T, ALIGNED>(static_cast<T*>(a.rows), a.rows_stride, a.n_rows, a.count, a.units, a.width);
+}
+
+struct BackArgs {
+  const void* rows;
+  int64_t rows_stride, n_rows;
+  const int32_t* place;
+  const float* weights;
+  const void* x;
+  int64_t x_stride;
+  void* out;
+  int64_t out_stride;
+  int T, k, width, units;
+};
+
+// A thread per unit of the result, CH branches' loads in flight.
+template <typename T, bool ALIGNED, int CH>
+__global__ void __launch_bounds__(kRowThreads) expert_combine_kernel(const BackArgs a) {
+  constexpr int V = Elem<T>::kVec;
+  pdl_entry();
+  const int64_t blocks = (static_cast<int64_t>(a.T) * a.units + kRowThreads - 1) / kRowThreads;
+  for (int64_t b = blockIdx.x; b < blocks; b += gridDim.x) {
+    const Item it(b, a.units);
+    if (it.row >= a.T) break;
+    T* out = static_cast<T*>(a.out) + it.row * a.out_stride;
+    const Unit<T, ALIGNED> unit(it.u, out, a.width);
+    if (!unit.any()) continue;
+    uint4 own = make_uint4(0, 0, 0, 0);
+    if (a.x) own = unit.load(static_cast<const T*>(a.x) + it.row * a.x_stride);
+    float sum[V] = {};
+    const int64_t s0 = it.row * a.k;
+    for (int p = 0; p < a.k; p += CH) {
+      uint4 raw[CH];
+      float w[CH];
+      bool live[CH];
+#pragma unroll
+      for (int j = 0; j < CH; ++j) {
+        const int r = p + j < a.k ? a.place[s0 + p + j] : -1;
+        live[j] = r >= 0 && r < a.n_rows;
+        if (live[j]) {
+          raw[j] = unit.load(static_cast<const T*>(a.rows) + r * a.rows_stride);
+          w[j] = a.weights ? a.weights[s0 + p + j] : 1.f;
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < CH; ++j)
+        if (live[j]) {
+          float h[V];
+          unpack_vec(raw[j], h, static_cast<T*>(nullptr));
+#pragma unroll
+          for (int i = 0; i < V; ++i) sum[i] = fmaf(w[j], h[i], sum[i]);
+        }
+    }
+    if (a.x) {
+      float f[V];
+      unpack_vec(own, f, static_cast<T*>(nullptr));
+#pragma unroll
+      for (int i = 0; i < V; ++i) sum[i] += f[i];
+    }
+    unit.store(out, pack_unit<T>(sum));
+  }
+}
+
+struct GradArgs {
+  const void* dout;
+  int64_t dout_stride;
+  const void* rows;
+  int64_t rows_stride, n_rows;
+  const int32_t* place;
+  const float* weights;
+  const int32_t* count;
+  void* drows;
+  int64_t drows_stride;
+  float* dweights;
+  int T, k, width, units;
+};
+
+// A warp per branch: dout's row (from L1 or L2 but for the token's first branch)
+// scaled into the gradient's row, and multiplied with the branch's row.
+template <typename T, bool ALIGNED>
+__global__ void __launch_bounds__(kRowThreads) expert_grad_kernel(const GradArgs a) {
+  constexpr int V = Elem<T>::kVec, J = 4;
+  pdl_entry();
+  const int lane = threadIdx.x & 31;
+  const int64_t n = static_cast<int64_t>(a.T) * a.k, step = static_cast<int64_t>(gridDim.x) * (kRowThreads / 32);
+  for (int64_t s = static_cast<int64_t>(blockIdx.x) * (kRowThreads / 32) + (threadIdx.x >> 5); s < n; s += step) {
+    const int r = a.place[s];
+    float dot = 0.f;
+    if (r >= 0 && r < a.n_rows) {
+      const float w = a.weights ? a.weights[s] : 1.f;
+      const T* dout = static_cast<const T*>(a.dout) + s / a.k * a.dout_stride;
+      const T* row = static_cast<const T*>(a.rows) + r * a.rows_stride;
+      T* drow = static_cast<T*>(a.drows) + r * a.drows_stride;
+      const T* cut = a.drows ? drow : row;  // whose boundaries the units have
+      for (int u0 = lane; u0 < a.units; u0 += 32 * J) {
+        uint4 d[J], h[J];
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+          const Unit<T, ALIGNED> unit(u0 + 32 * j, cut, a.width);
+          if (unit.any()) {
+            d[j] = unit.load(dout);
+            if (a.dweights) h[j] = unit.load(row);
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+          const Unit<T, ALIGNED> unit(u0 + 32 * j, cut, a.width);
+          if (!unit.any()) continue;
+          float f[V], g[V];
+          unpack_vec(d[j], f, static_cast<T*>(nullptr));
+          if (a.dweights) {
+            unpack_vec(h[j], g, static_cast<T*>(nullptr));
+#pragma unroll
+            for (int i = 0; i < V; ++i) dot = fmaf(f[i], g[i], dot);
+          }
+          if (a.drows) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) f[i] *= w;
+            unit.store(drow, pack_unit<T>(f));
+          }
+        }
+      }
+    }
+    if (a.dweights) {
+      dot = warp_sum(dot);
+      if (lane == 0) a.dweights[s] = dot;
+    }
+  }
+  if (a.drows) clear_tail<T, ALIGNED>(static_cast<T*>(a.drows), a.drows_stride, a.n_rows, a.count, a.units, a.width);
+}
+
+constexpr int64_t kMaxBlocks = 1 << 30;  // beyond: blocks walk on
+
+dim3 row_grid(int64_t threads) {
+  return dim3(static_cast<unsigned>(std::max<int64_t>(1, std::min((threads + kRowThreads - 1) / kRowThreads, kMaxBlocks))));
+}
+bool aligned16(const void* p, int64_t stride, int dtype) {
+  return addr(p) % 16 == 0 && stride * elem_size(dtype) % 16 == 0;
+}
+// f(T*, std::bool_constant<ALIGNED>)
+template <typename F>
+cudaError_t pick(int dtype, bool aligned, F f) {
+  if (dtype == MOECA_BF16)
+    return aligned ? f(static_cast<__nv_bfloat16*>(nullptr), std::true_type()) : f(static_cast<__nv_bfloat16*>(nullptr), std::false_type());
+  return aligned ? f(static_cast<float*>(nullptr), std::true_type()) : f(static_cast<float*>(nullptr), std::false_type());
+}
+
+const char* bad_branches(int n_tokens, int n_slots) {
+  if (n_tokens < 0 || n_slots < 1 || n_slots > kMaxSlots) return "n_tokens >= 0 and 1 <= n_slots <= 16";
+  if (static_cast<int64_t>(n_tokens) * n_slots > kMaxBranches) return "more than 2^30 branches";
+  return nullptr;
+}
+const char* bad_shape(int dtype, int n_tokens, int n_slots, int width, int64_t n_rows, const int32_t* place) {
+  if (!is_dtype(dtype)) return "dtype must be MOECA_F32 or MOECA_BF16";
+  if (const char* why = bad_branches(n_tokens, n_slots)) return why;
+  if (width < 1 || width > kMaxWidth) return "width out of range";
+  if (n_rows < 0 || n_rows > kMaxRows) return "n_rows out of range";
+  if (n_tokens > 0 && !place) return "place is NULL";
+  if (addr(place) % 4) return "place is not 4-byte aligned";
+  return nullptr;
+}
+
+}  // namespace
+}  // namespace moeca
+
+extern "C" {
+
+int64_t moeca_expert_sort_workspace(int32_t n_tokens, int32_t n_slots, int32_t n_experts) {
+  using namespace moeca;
+  if (bad_branches(n_tokens, n_slots) || n_experts < 1 || n_experts > kExpertsMost) return -1;
+  const int blocks = sort_blocks(static_cast<int64_t>(n_tokens) * n_slots);
+  return blocks > 1 ? static_cast<int64_t>(blocks) * n_experts : 0;
+}
+
+moeca_status moeca_expert_sort(const moeca_expert_sort_args* a, void* stream) {
+  using namespace moeca;
+  if (!a) return refuse("NULL argument");
+  if (const char* why = bad_branches(a->n_tokens, a->n_slots)) return refuse(why);
+  if (a->n_experts < 1 || a->n_experts > kExpertsMost) return refuse("1 <= n_experts <= 512");
+  const int64_t n = static_cast<int64_t>(a->n_tokens) * a->n_slots;
+  const int64_t work = moeca_expert_sort_workspace(a->n_tokens, a->n_slots, a->n_experts);
+  if (!a->offsets || (n > 0 && (!a->experts || !a->place)) || (work > 0 && !a->workspace))
+    return refuse("experts, offsets, place or workspace is NULL");
+  for (const void* p : {static_cast<const void*>(a->experts), static_cast<const void*>(a->offsets),
+                        static_cast<const void*>(a->place), static_cast<const void*>(a->slot),
+                        static_cast<const void*>(a->token), static_cast<const void*>(a->workspace)})
+    if (addr(p) % 4) return refuse("a list is not 4-byte aligned");
+  const Range written[] = {{a->offsets, 4ll * (a->n_experts + 1)}, {a->place, 4 * n}, {a->slot, 4 * n}, {a->token, 4 * n},
+                           {work ? a->workspace : nullptr, 4 * work}};
+  const Range read[] = {{a->experts, 4 * n}};
+  if (any_overlap(written, read)) return refuse("lists overlap");
+  SortArgs d{};
+  d.experts = a->experts;
+  d.n = static_cast<int>(n); d.k = a->n_slots; d.E = a->n_experts;
+  d.offsets = a->offsets; d.place = a->place; d.slot = a->slot; d.token = a->token; d.work = a->workspace;
+  return launched([&] { return launch_sort(d, static_cast<cudaStream_t>(stream)); });
+}
+
+moeca_status moeca_expert_rows(const moeca_expert_rows_args* a, void* stream) {
+  using namespace moeca;
+  if (!a) return refuse("NULL argument");
+  if (const char* why = bad_shape(a->dtype, a->n_tokens, a->n_slots, a->width, a->n_rows, a->place)) return refuse(why);
+  const int T = a->n_tokens, width = a->width;
+  if (const char* why = bad_values(a->x, T, a->x_stride, width, a->dtype, "x is NULL")) return refuse(why);
+  if (const char* why = bad_values(a->rows, a->n_rows, a->rows_stride, width, a->dtype, "rows is NULL")) return refuse(why);
+  if (addr(a->count) % 4) return refuse("count is not 4-byte aligned");
+  const int64_t es = elem_size(a->dtype), slots = static_cast<int64_t>(T) * a->n_slots;
+  const Range written[] = {rows_range(a->rows, a->n_rows, a->rows_stride * es, width * es)};
+  const Range read[] = {rows_range(a->x, T, a->x_stride * es, width * es), {a->place, 4 * slots}, {a->count, 4}};
+  if (any_overlap(written, read)) return refuse("rows overlaps another buffer of the call");
+  if (a->n_rows == 0 || (T == 0 && !a->count)) return MOECA_OK;
+  const RowsArgs d{a->x, a->x_stride, a->rows, a->rows_stride, a->n_rows, a->place, a->count, T, a->n_slots, width, 0};
+  const bool aligned = aligned16(a->x, a->x_stride, a->dtype) && aligned16(a->rows, a->rows_stride, a->dtype);
+  return launched([&] {
+    return pick(a->dtype, aligned, [&](auto* t, auto al) {
+      using E = std::remove_pointer_t<decltype(t)>;
+      RowsArgs k = d;
+      k.units = row_units<E>(width, al.value);
+      // The tail of an empty batch is cleared by as many threads as its units need.
+      const int64_t items = T == 0 ? a->n_rows : al.value ? T : slots;
+      return launch_pdl(expert_rows_kernel<E, al.value>, row_grid(items * k.units), dim3(kRowThreads), 0,
+                        static_cast<cudaStream_t>(stream), k);
+    });
+  });
+}
+
+moeca_status moeca_expert_combine(const moeca_expert_combine_args* a, void* stream) {
+  using namespace moeca;
+  if (!a) return refuse("NULL argument");
+  if (const char* why = bad_shape(a->dtype, a->n_tokens, a->n_slots, a->width, a->n_rows, a->place)) return refuse(why);
+  const int T = a->n_tokens, width = a->width;
+  if (const char* why = bad_values(a->rows, a->n_rows, a->rows_stride, width, a->dtype, "rows is NULL")) return refuse(why);
+  if (const char* why = bad_values(a->out, T, a->out_stride, width, a->dtype, "out is NULL")) return refuse(why);
+  if (a->x)
+    if (const char* why = bad_values(a->x, T, a->x_stride, width, a->dtype, "")) return refuse(why);
+  if (addr(a->weights) % 4) return refuse("weights is not 4-byte aligned");
+  const int64_t es = elem_size(a->dtype), slots = static_cast<int64_t>(T) * a->n_slots;
+  const bool in_place = a->x == a->out && a->x_stride == a->out_stride;
+  const Range written[] = {rows_range(a->out, T, a->out_stride * es, width * es)};
+  const Range read[] = {rows_range(a->rows, a->n_rows, a->rows_stride * es, width * es), {a->place, 4 * slots},
+                        {a->weights, 4 * slots}, rows_range(in_place ? nullptr : a->x, T, a->x_stride * es, width * es)};
+  if (any_overlap(written, read)) return refuse("out overlaps another buffer of the call");
+  if (T == 0) return MOECA_OK;
+  const BackArgs d{a->rows, a->rows_stride, a->n_rows, a->place, a->weights, a->x, a->x_stride,
+                      a->out, a->out_stride, T, a->n_slots, width, 0};
+  const bool aligned = aligned16(a->out, a->out_stride, a->dtype) &&
+                       (a->n_rows == 0 || aligned16(a->rows, a->rows_stride, a->dtype)) &&
+                       (!a->x || aligned16(a->x, a->x_stride, a->dtype));
+  return launched([&] {
+    return pick(a->dtype, aligned, [&](auto* t, auto al) {
+      using E = std::remove_pointer_t<decltype(t)>;
+      BackArgs k = d;
+      k.units = row_units<E>(width, al.value);
+      return launch_pdl(a->n_slots <= 2 ? expert_combine_kernel<E, al.value, 2> : expert_combine_kernel<E, al.value, 4>,
+                        row_grid(static_cast<int64_t>(T) * k.units), dim3(kRowThreads), 0,
+                        static_cast<cudaStream_t>(stream), k);
+    });
+  });
+}
+
+moeca_status moeca_expert_combine_grad(const moeca_expert_combine_grad_args* a, void* stream) {
+  using namespace moeca;
+  if (!a) return refuse("NULL argument");
+  if (const char* why = bad_shape(a->dtype, a->n_tokens, a->n_slots, a->width, a->n_rows, a->place)) return refuse(why);
+  const int T = a->n_tokens, width = a->width;
+  if (const char* why = bad_values(a->dout, T, a->dout_stride, width, a->dtype, "dout is NULL")) return refuse(why);
+  if (a->dweights || a->rows)
+    if (const char* why = bad_values(a->rows, a->n_rows, a->rows_stride, width, a->dtype, "rows is NULL")) return refuse(why);
+  if (a->drows)
+    if (const char* why = bad_values(a->drows, a->n_rows, a->drows_stride, width, a->dtype, "")) return refuse(why);
+  if (addr(a->weights) % 4 || addr(a->dweights) % 4 || addr(a->count) % 4)
+    return refuse("weights, dweights or count is not 4-byte aligned");
+  const int64_t es = elem_size(a->dtype), slots = static_cast<int64_t>(T) * a->n_slots;
+  const Range written[] = {rows_range(a->drows, a->n_rows, a->drows_stride * es, width * es), {a->dweights, 4 * slots}};
+  const Range read[] = {rows_range(a->dout, T, a->dout_stride * es, width * es),
+                        rows_range(a->rows, a->n_rows, a->rows_stride * es, width * es), {a->place, 4 * slots},
+                        {a->weights, 4 * slots}, {a->count, 4}};
+  if (any_overlap(written, read)) return refuse("drows or dweights overlaps another buffer of the call");
+  const bool clears = a->drows && a->count && a->n_rows > 0;
+  if ((!a->drows && !a->dweights) || (T == 0 && !clears)) return MOECA_OK;
+  const GradArgs d{a->dout, a->dout_stride, a->rows, a->rows_stride, a->n_rows, a->place, a->weights, a->count,
+                   a->drows, a->drows_stride, a->dweights, T, a->n_slots, width, 0};
+  const bool aligned = aligned16(a->dout, a->dout_stride, a->dtype) &&
+                       (!a->dweights || a->n_rows == 0 || aligned16(a->rows, a->rows_stride, a->dtype)) &&
+                       (!a->drows || aligned16(a->drows, a->drows_stride, a->dtype));
+  return launched([&] {
+    return pick(a->dtype, aligned, [&](auto* t, auto al) {
+      using E = std::remove_pointer_t<decltype(t)>;
+      GradArgs k = d;
+      k.units = row_units<E>(width, al.value);
+      return launch_pdl(expert_grad_kernel<E, al.value>, row_grid((T == 0 ? a->n_rows : slots) * 32), dim3(kRowThreads), 0,
+                        static_cast<cudaStream_t>(stream), k);
+    });
+  });
+}
+
+}  // extern "C"

@@ -1,0 +1,409 @@
+// Attention over packed sequences (include/moeca_attention.h): the call, its
+// choice of kernel, the CUDA-core kernel and the join of key chunks.
+#include <algorithm>
+
+#include "common.cuh"
+#include "packed_attn.cuh"
+
+namespace moeca {
+namespace {
+
+// ---------------------------------------------------------------------------
+// The CUDA-core kernel: fp32 values (the debug path), and bf16 rows that the
+// tensor-core kernels do not take (heads above 128 values, rows that do not
+// start at 16 bytes).  A block works on BQ queries of one head; 16 x 16 threads,
+// BQ / 16 rows and two keys each for the scores, BQ / 16 rows and four channels
+// in every 64 for the sums.  One pass over the keys, 32 at a time, with a running
+// maximum m and sum l per row:
+//   m' = max(m, max_j s_j), o <- o 2^(m - m') + sum_j 2^(s_j - m') v_j,
+// s in base 2.  Bound by FFMA and the shared-memory reads beside it.
+// ---------------------------------------------------------------------------
+constexpr int kSimtThreads = 256, kSimtKeys = 32;
+constexpr int kSimtPitch = kSimtKeys + 4;  // floats from row to row of p
+
+// Floats from row to row of q, k and v: the next multiple of 4 that is an odd
+// number of 16-byte pieces, so that eight rows' pieces fall in distinct banks.
+__host__ __device__ constexpr int simt_pitch(int dim) { return (dim + 3) / 4 % 2 ? (dim + 3) / 4 * 4 : (dim + 3) / 4 * 4 + 4; }
+constexpr size_t simt_smem(int rows, int dim) {
+  return (static_cast<size_t>(rows + 2 * kSimtKeys) * simt_pitch(dim) + rows * kSimtPitch) * 4;
+}
+
+// `rows` rows of one head into shared memory as floats, zeros from row `n` on and past dim.
+template <typename T>
+__device__ __forceinline__ void load_rows(float* dst, int pitch, const T* src, int64_t stride, int rows, int n, int dim,
+                                          bool vec) {
+  constexpr int V = Elem<T>::kVec;
+  if (vec) {
+    const int units = dim / V;
+    for (int i = threadIdx.x; i < rows * units; i += kSimtThreads) {
+      const int r = i / units, u = i - r * units;
+      float f[V] = {};
+      if (r < n) load_vec(src + r * stride + u * V, f);
+#pragma unroll
+      for (int j = 0; j < V; j += 4) store_vec(dst + r * pitch + u * V + j, f + j);
+    }
+  } else {
+    const int width = (dim + 3) / 4 * 4;
+    for (int i = threadIdx.x; i < rows * width; i += kSimtThreads) {
+      const int r = i / width, c = i - r * width;
+      dst[r * pitch + c] = r < n && c < dim ? Elem<T>::to_f(src[r * stride + c]) : 0.f;
+    }
+  }
+}
+
+__device__ __forceinline__ float group16_max(float v) {
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
+}
+__device__ __forceinline__ float group16_sum(float v) {
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+
+template <typename T, int BQ, int DC>  // DC: channels in 64s
+__global__ void __launch_bounds__(kSimtThreads) attn_simt_kernel(const PackedAttnArgs a, const bool vec) {
+  constexpr int R = BQ / 16;
+  extern __shared__ float4 smem4[];
+  pdl_entry();
+  const int64_t index = blockIdx.x / a.q.heads;
+  const int h = static_cast<int>(blockIdx.x - index * a.q.heads);
+  const AttnWork w = attn_work(a, index);
+  clear_rest<T>(a);
+  if (!w.any) return;
+  const int dim = a.dim, pitch = simt_pitch(dim);
+  float* sq = reinterpret_cast<float*>(smem4);
+  float* sk = sq + BQ * pitch;
+  float* sv = sk + kSimtKeys * pitch;
+  float* sp = sv + kSimtKeys * pitch;
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  const int rows = min(BQ, min(w.nq, a.max_q) - w.row0);
+  const T* q = static_cast<const T*>(a.q.data) + (w.q0 + w.row0) * a.q.token_stride + h * a.q.head_stride;
+  const T* k = static_cast<const T*>(a.k.data) + w.k0 * a.k.token_stride + h / a.group * a.k.head_stride;
+  const T* v = static_cast<const T*>(a.v.data) + w.k0 * a.v.token_stride + h / a.group * a.v.head_stride;
+  load_rows(sq, pitch, q, a.q.token_stride, BQ, rows, dim, vec);
+  float m[R], l[R], o[R][DC][4];
+  int see[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    m[r] = -INFINITY;
+    l[r] = 0.f;
+    see[r] = visible_keys(a, w, w.row0 + ty * R + r);
+#pragma unroll
+    for (int c = 0; c < DC; ++c)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[r][c][j] = 0.f;
+  }
+  // The last row of the tile sees the most.
+  const int end = min(w.key_hi, visible_keys(a, w, w.row0 + rows - 1));
+  const int d4 = (dim + 3) / 4;
+  for (int key0 = w.key_lo; key0 < end; key0 += kSimtKeys) {
+    const int n = min(kSimtKeys, w.key_hi - key0);
+    __syncthreads();
+    load_rows(sk, pitch, k + key0 * a.k.token_stride, a.k.token_stride, kSimtKeys, n, dim, vec);
+    load_rows(sv, pitch, v + key0 * a.v.token_stride, a.v.token_stride, kSimtKeys, n, dim, vec);
+    __syncthreads();
+    float s[R][2] = {};
+    for (int c = 0; c < d4; ++c) {
+      const float4 k0 = *reinterpret_cast<const float4*>(sk + tx * pitch + 4 * c);
+      const float4 k1 = *reinterpret_cast<const float4*>(sk + (tx + 16) * pitch + 4 * c);
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const float4 x = *reinterpret_cast<const float4*>(sq + (ty * R + r) * pitch + 4 * c);
+        s[r][0] = fmaf(x.x, k0.x, fmaf(x.y, k0.y, fmaf(x.z, k0.z, fmaf(x.w, k0.w, s[r][0]))));
+        s[r][1] = fmaf(x.x, k1.x, fmaf(x.y, k1.y, fmaf(x.z, k1.z, fmaf(x.w, k1.w, s[r][1]))));
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int limit = min(see[r], w.key_hi) - key0;
+      s[r][0] = tx < limit ? s[r][0] * a.scale_log2 : -INFINITY;
+      s[r][1] = tx + 16 < limit ? s[r][1] * a.scale_log2 : -INFINITY;
+      // A score that is not a number reaches p through s, not through the maximum.
+      const float top = fmaxf(m[r], group16_max(fmaxf(s[r][0], s[r][1])));
+      const float ref = top == -INFINITY ? 0.f : top;
+      const float keep = exp2f(m[r] - ref);
+      s[r][0] = exp2f(s[r][0] - ref);
+      s[r][1] = exp2f(s[r][1] - ref);
+      l[r] = l[r] * keep + group16_sum(s[r][0] + s[r][1]);
+      m[r] = top;
+      sp[(ty * R + r) * kSimtPitch + tx] = s[r][0];
+      sp[(ty * R + r) * kSimtPitch + tx + 16] = s[r][1];
+#pragma unroll
+      for (int c = 0; c < DC; ++c)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[r][c][j] *= keep;
+    }
+    __syncwarp();  // a row's p is written and read by the same half warp
+    for (int j = 0; j < n; j += 4) {
+      float4 p[R];
+#pragma unroll
+      for (int r = 0; r < R; ++r) p[r] = *reinterpret_cast<const float4*>(sp + (ty * R + r) * kSimtPitch + j);
+#pragma unroll
+      for (int c = 0; c < DC; ++c) {
+        const int at = c * 64 + tx * 4;
+        if (at >= dim) continue;
+#pragma unroll
+        for (int jj = 0; jj < 4; ++jj) {
+          const float4 x = *reinterpret_cast<const float4*>(sv + (j + jj) * pitch + at);
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            const float pr = jj == 0 ? p[r].x : jj == 1 ? p[r].y : jj == 2 ? p[r].z : p[r].w;
+            o[r][c][0] = fmaf(pr, x.x, o[r][c][0]);
+            o[r][c][1] = fmaf(pr, x.y, o[r][c][1]);
+            o[r][c][2] = fmaf(pr, x.z, o[r][c][2]);
+            o[r][c][3] = fmaf(pr, x.w, o[r][c][3]);
+          }
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int i = w.row0 + ty * R + r;
+    if (ty * R + r >= rows) continue;
+    const float inv = l[r] == 0.f ? 0.f : 1.f / l[r];
+    const float lse2 = l[r] == 0.f ? -INFINITY : m[r] + log2f(l[r]);
+    if (a.ks.unit) {
+      const int64_t at = (w.piece * a.max_q + i) * a.q.heads + h;
+      if (tx == 0) a.part_lse[at] = lse2;
+#pragma unroll
+      for (int c = 0; c < DC; ++c)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (c * 64 + tx * 4 + j < dim) a.part_o[at * dim + c * 64 + tx * 4 + j] = o[r][c][j] * inv;
+    } else {
+      if (tx == 0 && a.lse) a.lse[(w.q0 + i) * a.q.heads + h] = lse2 * kLn2;
+      T* out = static_cast<T*>(a.out.data) + (w.q0 + i) * a.out.token_stride + h * a.out.head_stride;
+#pragma unroll
+      for (int c = 0; c < DC; ++c)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (c * 64 + tx * 4 + j < dim) out[c * 64 + tx * 4 + j] = Elem<T>::from_f(o[r][c][j] * inv);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Join: a warp per (query, head).  With lse_j the chunks' base-2 logarithms and
+// m their maximum: o = sum_j 2^(lse_j - m) o_j / sum_j 2^(lse_j - m), chunk by chunk.
+// ---------------------------------------------------------------------------
+constexpr int kJoinThreads = 128;
+
+template <typename T>
+__global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const PackedAttnArgs a) {
+  pdl_entry();
+  const int lane = threadIdx.x & 31;
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * (kJoinThreads / 32) + (threadIdx.x >> 5);
+  const int64_t t = row / a.q.heads;
+  const int h = static_cast<int>(row - t * a.q.heads);
+  if (t >= a.qs.total) return;
+  const int b = a.qs.owner(t);
+  const int64_t i = t - a.qs.start(b);
+  if (i < 0 || i >= min(a.qs.length(b), static_cast<int64_t>(a.max_q))) return;
+  const int chunks = static_cast<int>((a.ks.length(b) + a.ks.unit - 1) / a.ks.unit);
+  const int64_t first = a.ks.base(b);
+  const auto at = [&](int j) { return ((first + j) * a.max_q + i) * a.q.heads + h; };
+  float m = -INFINITY;
+  for (int j = lane; j < chunks; j += 32) m = fmaxf(m, a.part_lse[at(j)]);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  const float ref = m == -INFINITY ? 0.f : m;
+  float sum = 0.f;
+  for (int j = 0; j < chunks; ++j) sum += exp2f(a.part_lse[at(j)] - ref);
+  if (lane == 0 && a.lse) a.lse[t * a.q.heads + h] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * kLn2;
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  T* out = static_cast<T*>(a.out.data) + t * a.out.token_stride + h * a.out.head_stride;
+  for (int c0 = 0; c0 < a.dim; c0 += 128) {
+    float o[4] = {};
+    for (int j = 0; j < chunks; ++j) {
+      const float weight = exp2f(a.part_lse[at(j)] - ref);
+      if (weight == 0.f) continue;  // that chunk's o may be anything
+      const float* part = a.part_o + at(j) * a.dim + c0;
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        if (c0 + c * 32 + lane < a.dim) o[c] = fmaf(weight, part[c * 32 + lane], o[c]);
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      if (c0 + c * 32 + lane < a.dim) out[c0 + c * 32 + lane] = Elem<T>::from_f(o[c] * inv);
+  }
+}
+
+template <typename T, int BQ>
+cudaError_t simt(const PackedAttnArgs& a, bool vec, int64_t blocks, cudaStream_t s) {
+  const size_t smem = simt_smem(BQ, a.dim);
+  const auto run = [&](auto kernel) {
+    if (smem > 48 * 1024) {
+      const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(simt_smem(BQ, 256)));
+      if (e != cudaSuccess) return e;
+    }
+    return launch_pdl(kernel, dim3(static_cast<unsigned>(blocks)), dim3(kSimtThreads), smem, s, a, vec);
+  };
+  if (a.dim <= 64) return run(attn_simt_kernel<T, BQ, 1>);
+  if (a.dim <= 128) return run(attn_simt_kernel<T, BQ, 2>);
+  return run(attn_simt_kernel<T, BQ, 4>);
+}
+
+}  // namespace
+
+cudaError_t launch_attn_simt(const PackedAttnArgs& a, int dtype, int tile, cudaStream_t s) {
+  const int64_t es = elem_size(dtype), n = 16 / es;
+  const auto fits = [&](const Heads& h) { return addr(h.data) % 16 == 0 && h.token_stride % n == 0 && h.head_stride % n == 0; };
+  const bool vec = a.dim % n == 0 && fits(a.q) && fits(a.k) && fits(a.v);
+  const int64_t blocks = (a.ks.unit ? a.k_pieces * a.tiles : a.q_pieces) * a.q.heads;
+  if (dtype == MOECA_BF16)
+    return tile == 16 ? simt<__nv_bfloat16, 16>(a, vec, blocks, s) : simt<__nv_bfloat16, 32>(a, vec, blocks, s);
+  return tile == 16 ? simt<float, 16>(a, vec, blocks, s) : simt<float, 32>(a, vec, blocks, s);
+}
+
+cudaError_t launch_attn_join(const PackedAttnArgs& a, int dtype, cudaStream_t s) {
+  const int64_t rows = a.qs.total * a.q.heads;
+  const dim3 grid(static_cast<unsigned>((rows + kJoinThreads / 32 - 1) / (kJoinThreads / 32)));
+  return launch_pdl(dtype == MOECA_BF16 ? attn_join_kernel<__nv_bfloat16> : attn_join_kernel<float>, grid, dim3(kJoinThreads), 0, s, a);
+}
+
+namespace {
+
+constexpr int64_t kMaxTokens = 1 << 30;
+constexpr int kMaxHeadDim = 256, kMaxSeqs = 1 << 20;
+constexpr int64_t kMaxWorkspace = int64_t(1) << 30;  // beyond, the key axis is not cut
+
+struct Plan {
+  int tile;           // query tokens of a tile
+  int chunk;          // keys of a chunk, 0: not cut
+  int max_q, tiles;
+  int64_t q_pieces, k_pieces;
+  int q_per, k_per;
+  int64_t blocks;
+  int64_t lse_bytes, bytes;  // workspace: the logarithms, all of it
+};
+
+int64_t pieces(const int32_t* off, int64_t total, int n, int unit, int most, int* per) {
+  // Sequences of known or bounded length have the same number of pieces, or the
+  // pieces follow the offsets, whichever are fewer.
+  const int64_t each = ((off ? std::min<int64_t>(most, total) : total / n) + unit - 1) / unit;
+  const int64_t packed = total / unit + n;
+  *per = 0;
+  if (!off || each * n <= packed) {
+    *per = static_cast<int>(std::max<int64_t>(each, 1));
+    return each * n;
+  }
+  return packed;
+}
+
+// How a call is carried out: a function of its sizes alone.
+Plan plan_attention(const moeca_attention_args& a) {
+  Plan p{};
+  const int64_t most = a.q_offsets ? (a.max_q > 0 ? std::min<int64_t>(a.max_q, a.n_queries) : a.n_queries) : a.n_queries / a.n_seqs;
+  p.max_q = static_cast<int>(a.max_q > 0 ? std::min<int64_t>(a.max_q, most) : most);
+  p.tile = p.max_q <= 16 ? 16 : 32;
+  p.q_pieces = pieces(a.q_offsets, a.n_queries, a.n_seqs, p.tile, p.max_q, &p.q_per);
+  p.tiles = (p.max_q + p.tile - 1) / p.tile;
+  p.blocks = p.q_pieces * a.q.heads;
+  // Few blocks with many keys each: the key axis is cut so that some 600 blocks share it.
+  const int64_t wanted = 608;
+  if (p.blocks > 0 && p.blocks < wanted && p.max_q > 0) {
+    const int64_t chunk = std::max<int64_t>(256, (a.n_keys * p.tiles * a.q.heads / wanted + 127) / 128 * 128);
+    const int64_t longest = a.k_offsets ? a.n_keys : a.n_keys / a.n_seqs;
+    if (chunk < longest) {
+      const int64_t n = pieces(a.k_offsets, a.n_keys, a.n_seqs, static_cast<int>(chunk), 0x7fffffff, &p.k_per);
+      const int64_t rows = n * p.max_q * a.q.heads;
+      const int64_t lse = (rows * 4 + 15) / 16 * 16, bytes = lse + rows * a.dim * 4;
+      if (rows < kMaxWorkspace && bytes <= kMaxWorkspace) {
+        p.chunk = static_cast<int>(chunk);
+        p.k_pieces = n;
+        p.blocks = n * p.tiles * a.q.heads;
+        p.lse_bytes = lse;
+        p.bytes = bytes;
+      }
+    }
+  }
+  return p;
+}
+
+// What is wrong with a call but for its buffers (null: nothing).
+const char* bad_attention(const moeca_attention_args& a) {
+  if (!is_dtype(a.dtype)) return "dtype must be MOECA_F32 or MOECA_BF16";
+  if (a.dim < 1 || a.dim > kMaxHeadDim) return "1 <= dim <= 256";
+  if (a.n_seqs < 1 || a.n_seqs > kMaxSeqs) return "1 <= n_seqs <= 2^20";
+  if (a.n_queries < 0 || a.n_keys < 0 || a.max_q < 0) return "n_queries, n_keys and max_q must not be negative";
+  if (!a.q_offsets && a.n_queries % a.n_seqs) return "n_queries must be a multiple of n_seqs without q_offsets";
+  if (!a.k_offsets && a.n_keys % a.n_seqs) return "n_keys must be a multiple of n_seqs without k_offsets";
+  if (a.q.heads < 1 || a.k.heads < 1 || a.q.heads % a.k.heads || a.v.heads != a.k.heads || a.out.heads != a.q.heads)
+    return "q.heads must be a multiple of k.heads = v.heads, and out.heads = q.heads";
+  if (a.causal < 0 || a.causal > 1 || a.clear < 0 || a.clear > 1) return "causal and clear must be 0 or 1";
+  if (!(a.scale > 0) || a.scale > 3e38f) return "scale must be positive and finite";
+  if (const char* why = bad_heads(a.q, a.n_queries, a.dim, a.dtype, false)) return why;
+  if (const char* why = bad_heads(a.k, a.n_keys, a.dim, a.dtype, false)) return why;
+  if (const char* why = bad_heads(a.v, a.n_keys, a.dim, a.dtype, false)) return why;
+  if (const char* why = bad_heads(a.out, a.n_queries, a.dim, a.dtype, true)) return why;
+  return nullptr;
+}
+
+}  // namespace
+}  // namespace moeca
+
+extern "C" {
+
+int64_t moeca_attention_workspace(const moeca_attention_args* a) {
+  using namespace moeca;
+  if (!a || bad_attention(*a) || a->n_queries > kMaxTokens || a->n_keys > kMaxTokens) return -1;
+  return a->n_queries == 0 ? 0 : plan_attention(*a).bytes;
+}
+
+moeca_status moeca_attention(const moeca_attention_args* a, void* stream) {
+  using namespace moeca;
+  if (!a) return refuse("NULL argument");
+  if (const char* why = bad_attention(*a)) return refuse(why);
+  if (addr(a->q_offsets) % 4 || addr(a->k_offsets) % 4 || addr(a->lse) % 4 || addr(a->status) % 4)
+    return refuse("offsets, lse or status is not 4-byte aligned");
+  if (a->n_queries > kMaxTokens || a->n_keys > kMaxTokens) {
+    keep_call_error("more than 2^30 tokens");
+    return MOECA_ERR_UNSUPPORTED;
+  }
+  const int64_t es = elem_size(a->dtype), nq = a->n_queries, nk = a->n_keys;
+  const int dim = a->dim;
+  const Plan p = nq > 0 ? plan_attention(*a) : Plan{};
+  if (p.bytes > 0 && (!a->workspace || addr(a->workspace) % 16)) return refuse("workspace is NULL or not 16-byte aligned");
+  const Range q_list = {a->q_offsets, 4ll * (a->n_seqs + 1)}, k_list = {a->k_offsets, 4ll * (a->n_seqs + 1)};
+  const Range lse = {a->lse, 4 * nq * a->q.heads}, work = {p.bytes ? a->workspace : nullptr, p.bytes}, status = {a->status, 8};
+  const Range written[] = {lse, work, status};
+  const Range read[] = {q_list, k_list};
+  if (any_overlap(written, read)) return refuse("lse, workspace or status overlaps another buffer of the call");
+  for (const Range& r : {lse, work, status, q_list, k_list})
+    if (heads_overlap(a->out, nq, r, dim, es)) return refuse("out overlaps another buffer of the call");
+  for (const Range& r : written)
+    if (heads_overlap(a->q, nq, r, dim, es) || heads_overlap(a->k, nk, r, dim, es) || heads_overlap(a->v, nk, r, dim, es))
+      return refuse("lse, workspace or status overlaps another buffer of the call");
+  if ((!same_heads(a->out, a->q) && heads_overlap(a->out, nq, a->q, nq, dim, es)) ||
+      heads_overlap(a->out, nq, a->k, nk, dim, es) || heads_overlap(a->out, nq, a->v, nk, dim, es))
+    return refuse("out overlaps another buffer of the call");
+  if (nq == 0 || p.max_q == 0) return MOECA_OK;
+  if (p.blocks > kMaxRows || nq * a->q.heads > kMaxRows) {
+    keep_call_error("too many tiles for one launch");
+    return MOECA_ERR_UNSUPPORTED;
+  }
+  PackedAttnArgs d{};
+  d.q = device_heads(a->q); d.k = device_heads(a->k); d.v = device_heads(a->v); d.out = device_heads(a->out);
+  d.qs = {a->q_offsets, nq, a->n_seqs, p.tile, p.q_per};
+  d.ks = {a->k_offsets, nk, a->n_seqs, p.chunk, p.k_per};
+  d.q_pieces = p.q_pieces; d.k_pieces = p.k_pieces;
+  d.lse = a->lse;
+  d.part_lse = static_cast<float*>(a->workspace);
+  d.part_o = reinterpret_cast<float*>(static_cast<uint8_t*>(a->workspace) + p.lse_bytes);
+  d.max_q = p.max_q; d.tiles = p.tiles;
+  d.group = a->q.heads / a->k.heads;
+  d.dim = dim; d.causal = a->causal; d.clear = a->clear;
+  d.scale_log2 = a->scale * kLog2e;
+  d.status = a->status;
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  return launched([&] {
+    cudaError_t e = launch_attn_simt(d, a->dtype, p.tile, s);
+    if (e == cudaSuccess && p.chunk) e = launch_attn_join(d, a->dtype, s);
+    return e;
+  });
+}
+
+}  // extern "C"

@@ -2,6 +2,7 @@
 // written, and the checks of every call's arguments.
 #include <algorithm>
 
+#include "calls.h"
 #include "common.cuh"
 #include "kernels.h"
 #include "moeca_probe.h"
@@ -199,28 +200,10 @@ cudaError_t launch_q8_write(const Q8WriteArgs& a, bool bf16, bool e5, cudaStream
 // ---------------------------------------------------------------------------
 namespace {
 
-constexpr int64_t kMaxRows = 0x7fffffff;
 constexpr int64_t kMaxProductRows = 1 << 30;
-constexpr int kMaxWidth = 1 << 20, kMaxSlots = 16, kMaxGroups = 512;
+constexpr int kMaxGroups = 512;
 
 bool is_format(int f) { return f == MOECA_E4M3 || f == MOECA_E5M2; }
-bool is_dtype(int d) { return d == MOECA_F32 || d == MOECA_BF16; }
-int64_t elem_size(int d) { return d == MOECA_BF16 ? 2 : 4; }
-uintptr_t addr(const void* p) { return reinterpret_cast<uintptr_t>(p); }
-
-// A buffer's bytes: [from, from + bytes).
-struct Range {
-  const void* from;
-  int64_t bytes;
-};
-Range rows_range(const void* p, int64_t rows, int64_t stride, int64_t row_bytes) {
-  return {p, rows > 0 ? (rows - 1) * stride + row_bytes : 0};
-}
-bool overlap(const Range& a, const Range& b) {
-  return a.from && b.from && a.bytes > 0 && b.bytes > 0 && addr(a.from) < addr(b.from) + b.bytes &&
-         addr(b.from) < addr(a.from) + a.bytes;
-}
-
 // What is wrong with 8-bit rows (null: nothing).
 const char* bad_rows(const moeca_q8_rows& r) {
   if (!is_format(r.format)) return "rows: format must be MOECA_E4M3 or MOECA_E5M2";
@@ -236,12 +219,6 @@ const char* bad_rows(const moeca_q8_rows& r) {
     return "rows: strides out of range";
   return nullptr;
 }
-const char* bad_values(const void* p, int64_t rows, int64_t stride, int width, int dtype, const char* what) {
-  if (rows > 0 && !p) return what;
-  if (addr(p) % elem_size(dtype)) return "a value buffer is not aligned to its type";
-  if (stride < width || (rows > 0 && stride > INT64_MAX / 8 / rows)) return "a value stride is smaller than the width, or out of range";
-  return nullptr;
-}
 // What the kernels touch: rows in pieces of 16 bytes, their scales in words.
 int64_t row_bytes(const moeca_q8_rows& r) { return (r.width + 15) / 16 * 16; }
 int64_t scale_bytes(const moeca_q8_rows& r) { return ((r.width + kQ8Block - 1) / kQ8Block + 3) / 4 * 4; }
@@ -250,36 +227,6 @@ Range scale_range(const moeca_q8_rows& r) { return rows_range(r.scale, r.rows, r
 Q8Rows device_rows(const moeca_q8_rows& r) {
   return {static_cast<uint8_t*>(r.q), r.scale, r.rows, r.q_stride, r.scale_stride, r.width};
 }
-moeca_status refuse(const char* why) {
-  keep_call_error(why);
-  return MOECA_ERR_INVALID_ARG;
-}
-// Runs a launch; nothing is thrown to the caller.
-template <typename F>
-moeca_status launched(F launch) {
-  try {
-    const cudaError_t e = launch();
-    if (e == cudaSuccess) return MOECA_OK;
-    cudaGetLastError();
-    keep_call_error(cudaGetErrorString(e));
-    return MOECA_ERR_CUDA;
-  } catch (...) {
-    keep_call_error("out of host memory");
-    return MOECA_ERR_OOM;
-  }
-}
-// Whether any buffer of `written` overlaps one of `read` or another one written.
-template <int NW, int NR>
-bool any_overlap(const Range (&written)[NW], const Range (&read)[NR]) {
-  for (int i = 0; i < NW; ++i) {
-    for (const Range& r : read)
-      if (overlap(written[i], r)) return true;
-    for (int j = 0; j < i; ++j)
-      if (overlap(written[i], written[j])) return true;
-  }
-  return false;
-}
-
 }  // namespace
 }  // namespace moeca
 

@@ -137,6 +137,51 @@ class moeca_q8_matmul_args(C.Structure):
                 ("n_cols", C.c_int32), ("act", C.c_int32)]
 
 
+class moeca_expert_sort_args(C.Structure):
+    _fields_ = [("experts", C.c_void_p), ("n_tokens", C.c_int32), ("n_slots", C.c_int32), ("n_experts", C.c_int32),
+                ("offsets", C.c_void_p), ("place", C.c_void_p), ("slot", C.c_void_p), ("token", C.c_void_p),
+                ("workspace", C.c_void_p)]
+
+
+class moeca_expert_rows_args(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("x_stride", C.c_int64), ("rows", C.c_void_p), ("rows_stride", C.c_int64),
+                ("n_rows", C.c_int64), ("place", C.c_void_p), ("count", C.c_void_p), ("dtype", C.c_int32),
+                ("n_tokens", C.c_int32), ("n_slots", C.c_int32), ("width", C.c_int32)]
+
+
+class moeca_expert_combine_args(C.Structure):
+    _fields_ = [("rows", C.c_void_p), ("rows_stride", C.c_int64), ("n_rows", C.c_int64), ("place", C.c_void_p),
+                ("weights", C.c_void_p), ("x", C.c_void_p), ("x_stride", C.c_int64), ("out", C.c_void_p),
+                ("out_stride", C.c_int64), ("dtype", C.c_int32), ("n_tokens", C.c_int32), ("n_slots", C.c_int32),
+                ("width", C.c_int32)]
+
+
+class moeca_expert_combine_grad_args(C.Structure):
+    _fields_ = [("dout", C.c_void_p), ("dout_stride", C.c_int64), ("rows", C.c_void_p), ("rows_stride", C.c_int64),
+                ("n_rows", C.c_int64), ("place", C.c_void_p), ("weights", C.c_void_p), ("count", C.c_void_p),
+                ("drows", C.c_void_p), ("drows_stride", C.c_int64), ("dweights", C.c_void_p), ("dtype", C.c_int32),
+                ("n_tokens", C.c_int32), ("n_slots", C.c_int32), ("width", C.c_int32)]
+
+
+class moeca_heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64), ("heads", C.c_int32)]
+
+
+class moeca_qk_norm_rope_args(C.Structure):
+    _fields_ = [("q", moeca_heads), ("k", moeca_heads), ("q_out", moeca_heads), ("k_out", moeca_heads),
+                ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("table", C.c_void_p), ("pos", C.c_void_p),
+                ("n_positions", C.c_int64), ("dtype", C.c_int32), ("n_tokens", C.c_int32), ("dim", C.c_int32),
+                ("rot", C.c_int32), ("pairs", C.c_int32), ("eps", C.c_float)]
+
+
+class moeca_attention_args(C.Structure):
+    _fields_ = [("q", moeca_heads), ("k", moeca_heads), ("v", moeca_heads), ("out", moeca_heads),
+                ("q_offsets", C.c_void_p), ("k_offsets", C.c_void_p), ("lse", C.c_void_p), ("workspace", C.c_void_p),
+                ("status", C.c_void_p), ("n_queries", C.c_int64), ("n_keys", C.c_int64), ("n_seqs", C.c_int32),
+                ("max_q", C.c_int32), ("dtype", C.c_int32), ("dim", C.c_int32), ("causal", C.c_int32),
+                ("clear", C.c_int32), ("scale", C.c_float)]
+
+
 class MoecaError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__(f"{STATUS_NAMES.get(status, status)}: {msg}")
@@ -181,6 +226,14 @@ def _load():
         "moeca_q8_read": (C.c_int, [C.POINTER(moeca_q8_read_args), C.c_void_p]),
         "moeca_q8_combine": (C.c_int, [C.POINTER(moeca_q8_combine_args), C.c_void_p]),
         "moeca_q8_matmul": (C.c_int, [C.POINTER(moeca_q8_matmul_args), C.c_void_p]),
+        "moeca_expert_sort": (C.c_int, [C.POINTER(moeca_expert_sort_args), C.c_void_p]),
+        "moeca_expert_sort_workspace": (C.c_int64, [C.c_int32, C.c_int32, C.c_int32]),
+        "moeca_expert_rows": (C.c_int, [C.POINTER(moeca_expert_rows_args), C.c_void_p]),
+        "moeca_expert_combine": (C.c_int, [C.POINTER(moeca_expert_combine_args), C.c_void_p]),
+        "moeca_expert_combine_grad": (C.c_int, [C.POINTER(moeca_expert_combine_grad_args), C.c_void_p]),
+        "moeca_qk_norm_rope": (C.c_int, [C.POINTER(moeca_qk_norm_rope_args), C.c_void_p]),
+        "moeca_attention": (C.c_int, [C.POINTER(moeca_attention_args), C.c_void_p]),
+        "moeca_attention_workspace": (C.c_int64, [C.POINTER(moeca_attention_args)]),
         "moeca_probe_q8_staged": (C.c_int32, [C.c_int32] * 7),
         "moeca_probe_q8_stall": (C.c_int32, [C.c_int32, C.c_int64]),
         "moeca_probe_ffma": (C.c_int32, [C.c_int32, C.c_int32, C.POINTER(C.c_double), C.POINTER(C.c_double)]),
@@ -382,6 +435,46 @@ def moeca_q8_combine(args: moeca_q8_combine_args, stream: int = 0):
 def moeca_q8_matmul(args: moeca_q8_matmul_args, stream: int = 0):
     """Grouped product of 8-bit rows (see include/moeca_q8.h)."""
     _check(LIB.moeca_q8_matmul(C.byref(args), stream or None))
+
+
+def moeca_expert_sort(args: moeca_expert_sort_args, stream: int = 0):
+    """Sort branches by expert (see include/moeca_experts.h)."""
+    _check(LIB.moeca_expert_sort(C.byref(args), stream or None))
+
+
+def moeca_expert_sort_workspace(n_tokens: int, n_slots: int, n_experts: int) -> int:
+    """int32 values that moeca_expert_sort works in (-1: a size out of range)."""
+    return LIB.moeca_expert_sort_workspace(n_tokens, n_slots, n_experts)
+
+
+def moeca_expert_rows(args: moeca_expert_rows_args, stream: int = 0):
+    """The tokens' rows in the experts' order (see include/moeca_experts.h)."""
+    _check(LIB.moeca_expert_rows(C.byref(args), stream or None))
+
+
+def moeca_expert_combine(args: moeca_expert_combine_args, stream: int = 0):
+    """The experts' rows back to their tokens, weighted (see include/moeca_experts.h)."""
+    _check(LIB.moeca_expert_combine(C.byref(args), stream or None))
+
+
+def moeca_expert_combine_grad(args: moeca_expert_combine_grad_args, stream: int = 0):
+    """Gradients of moeca_expert_combine (see include/moeca_experts.h)."""
+    _check(LIB.moeca_expert_combine_grad(C.byref(args), stream or None))
+
+
+def moeca_qk_norm_rope(args: moeca_qk_norm_rope_args, stream: int = 0):
+    """Norms of query and key heads with the rotation (see include/moeca_attention.h)."""
+    _check(LIB.moeca_qk_norm_rope(C.byref(args), stream or None))
+
+
+def moeca_attention(args: moeca_attention_args, stream: int = 0):
+    """Attention over packed sequences (see include/moeca_attention.h)."""
+    _check(LIB.moeca_attention(C.byref(args), stream or None))
+
+
+def moeca_attention_workspace(args: moeca_attention_args) -> int:
+    """Bytes that moeca_attention works in (-1: it would refuse the call)."""
+    return LIB.moeca_attention_workspace(C.byref(args))
 
 
 def moeca_probe_ffma(device: int = 0, iterations: int = 1 << 16) -> tuple:
@@ -714,7 +807,7 @@ def _list(t, kind: str, shape: tuple, what: str, device: int) -> int:
 def _call(fn, args: bytes, device: int, stream: int):
     """Run a C call with the tensors' device current, on ``stream`` or that device's current stream."""
     if device < 0:
-        raise ValueError("8-bit rows live on a CUDA device")
+        raise ValueError("the call's tensors must be on a CUDA device")
     torch = _TYPES["torch"]
     stream = stream or torch._C._cuda_getCurrentRawStream(device)
     if device == torch._C._cuda_getDevice():
@@ -868,3 +961,281 @@ def q8_matmul(a: Q8, b: Q8, offsets=None, bias=None, act: str = "none", dst=None
         _list(dst, "i32", (ra[2],), "dst", dev), _list(status, "i32", (2,), "status", dev), groups, cols, _ACTS[act])
     _call(_q8_packed[3], args, dev, stream)
     return out
+
+
+# ---------------------------------------------------------------------------
+# Tokens sorted by expert and back (include/moeca_experts.h) on torch CUDA tensors
+# ---------------------------------------------------------------------------
+
+_PACK_SORT = struct.Struct("@QiiiQQQQQ")
+_PACK_ROWS = struct.Struct("@QqQqqQQiiii")
+_PACK_BACK = struct.Struct("@QqqQQQqQqiiii")
+_PACK_BACK_GRAD = struct.Struct("@QqQqqQQQQqQiiii")
+_HEADS = "Qqqi4x"
+_PACK_QK = struct.Struct("@" + 4 * _HEADS + "QQQQqiiiiif")
+_PACK_ATTENTION = struct.Struct("@" + 4 * _HEADS + "QQQQQqqiiiiiif")
+for _s, _t in ((_PACK_SORT, moeca_expert_sort_args), (_PACK_ROWS, moeca_expert_rows_args),
+               (_PACK_BACK, moeca_expert_combine_args), (_PACK_BACK_GRAD, moeca_expert_combine_grad_args),
+               (_PACK_QK, moeca_qk_norm_rope_args), (_PACK_ATTENTION, moeca_attention_args)):
+    assert (_s.size + 7) // 8 * 8 == C.sizeof(_t)
+_packed = {_n: C.CFUNCTYPE(C.c_int, C.c_char_p, C.c_void_p)(C.cast(getattr(LIB, _n), C.c_void_p).value) for _n in (
+    "moeca_expert_sort", "moeca_expert_rows", "moeca_expert_combine", "moeca_expert_combine_grad", "moeca_qk_norm_rope",
+    "moeca_attention")}
+_attention_bytes = C.CFUNCTYPE(C.c_int64, C.c_char_p)(C.cast(LIB.moeca_attention_workspace, C.c_void_p).value)
+
+
+class ExpertPlan(NamedTuple):
+    """Branches sorted by expert, int32 on the device: ``offsets`` [experts + 1] (expert e's rows are offsets[e] ..
+    offsets[e + 1] - 1), ``place`` [T, k] (a branch's row, or -1), ``slot`` and ``token`` [T k] (a row's branch, token k +
+    slot, and its token; -1 behind the last row).  ``offsets``, ``slot`` and ``token`` are what q8_matmul and q8_write
+    take as offsets, dst and src."""
+    offsets: "torch.Tensor"  # noqa: F821
+    place: "torch.Tensor"  # noqa: F821
+    slot: "torch.Tensor"  # noqa: F821
+    token: "torch.Tensor"  # noqa: F821
+
+
+def expert_sort(experts, n_experts: int, plan: ExpertPlan = None, stream: int = 0) -> ExpertPlan:
+    """Sort the branches of ``experts`` [T, k] (int32 ids on the device; out of [0, n_experts): not sorted) by
+    expert, each expert's in the order of token and slot.  ``plan``: tensors to write to, by default new ones.
+    ``stream``: as for q8_read."""
+    dev = experts.get_device()
+    shape = experts.shape
+    if len(shape) != 2:
+        raise ValueError("experts must be [tokens, slots]")
+    address = _list(experts, "i32", shape, "experts", dev)
+    T, k = shape
+    n = T * k
+    work = LIB.moeca_expert_sort_workspace(T, k, n_experts) if T < 1 << 31 and 0 < k < 1 << 31 and 0 < n_experts < 1 << 31 else -1
+    if work < 0:
+        raise ValueError("1 .. 16 slots, 1 .. 512 experts and at most 2^30 branches")
+    torch = _TYPES["torch"]
+    if plan is None or work:
+        def make():
+            def new(*size):
+                return torch.empty(size, dtype=torch.int32, device=experts.device)
+            return (plan or ExpertPlan(new(n_experts + 1), new(T, k), new(n), new(n)), new(work) if work else None)
+        plan, space = _on(stream, dev, make)
+    offsets, place, slot, token = plan
+    args = _PACK_SORT.pack(
+        address, T, k, n_experts, _list(offsets, "i32", (n_experts + 1,), "offsets", dev), _list(place, "i32", shape, "place", dev),
+        _list(slot, "i32", (n,), "slot", dev), _list(token, "i32", (n,), "token", dev), space.data_ptr() if work else 0)
+    _call(_packed["moeca_expert_sort"], args, dev, stream)
+    return plan
+
+
+def _branches(plan, dev: int) -> tuple:
+    """(address of place, tokens, slots) of a plan."""
+    place = plan[1]
+    shape = place.shape
+    if len(shape) != 2:
+        raise ValueError("plan.place must be [tokens, slots]")
+    return _list(place, "i32", shape, "plan.place", dev), shape[0], shape[1]
+
+
+def _row_result(out, n: int, width: int, like, what: str, dev: int, stream: int):
+    """(tensor, address, stride) of the rows a call writes: ``out``, or a new tensor like ``like``."""
+    if out is None:
+        torch = _TYPES["torch"]
+        out = _on(stream, dev, lambda: torch.empty((n, width), dtype=like.dtype, device=like.device))
+        return out, out.data_ptr(), width
+    address, rows, stride, w, _ = _value_fields(out, what, dev)
+    if rows != n or w != width or out.dtype != like.dtype:
+        raise ValueError(f"{what} must be [{n}, {width}] of the input's dtype")
+    return out, address, stride
+
+
+def _plan_count(plan, dev: int) -> int:
+    offsets = plan[0]
+    return _list(offsets, "i32", (offsets.numel(),), "plan.offsets", dev) + 4 * (offsets.numel() - 1)
+
+
+def expert_rows(x, plan: ExpertPlan, out=None, stream: int = 0):
+    """The rows of ``x`` [T, D] (fp32 or bf16) in the plan's order: row place[t, p] is x[t].  A new result has T k rows,
+    zeros behind the plan's last; rows of a given ``out`` behind it keep what they hold.  ``stream``: as for q8_read.
+    Its gradient is expert_rows_grad."""
+    dev = x.get_device()
+    address, n_x, x_stride, width, code = _value_fields(x, "x", dev)
+    place, T, k = _branches(plan, dev)
+    if n_x != T:
+        raise ValueError(f"x must have {T} rows")
+    count = _plan_count(plan, dev) if out is None else 0
+    n = T * k if out is None else out.shape[0]
+    out, o_address, o_stride = _row_result(out, n, width, x, "out", dev, stream)
+    args = _PACK_ROWS.pack(address, x_stride, o_address, o_stride, n, place, count, code, T, k, width)
+    _call(_packed["moeca_expert_rows"], args, dev, stream)
+    return out
+
+
+def expert_combine(rows, plan: ExpertPlan, weights=None, x=None, out=None, stream: int = 0):
+    """x + sum_p weights[:, p] rows[place[:, p]]: ``rows`` [n, D] fp32 or bf16 in the plan's order, ``weights`` [T, k] fp32
+    (None: 1), ``x`` [T, D] of rows' dtype (None: 0); a branch without a row adds nothing.  ``out`` may be x.
+    ``stream``: as for q8_read.  Its gradients are expert_combine_grad's."""
+    dev = rows.get_device()
+    address, n, stride, width, code = _value_fields(rows, "rows", dev)
+    place, T, k = _branches(plan, dev)
+    x_address = x_stride = 0
+    if x is not None:
+        x_address, n_x, x_stride, x_width, x_code = _value_fields(x, "x", dev)
+        if n_x != T or x_width != width or x_code != code:
+            raise ValueError(f"x must be [{T}, {width}] of rows' dtype")
+    w = _list(weights, "f32", (T, k), "weights", dev)
+    out, o_address, o_stride = _row_result(out, T, width, rows, "out", dev, stream)
+    args = _PACK_BACK.pack(address, stride, n, place, w, x_address, x_stride, o_address, o_stride, code, T, k, width)
+    _call(_packed["moeca_expert_combine"], args, dev, stream)
+    return out
+
+
+def expert_rows_grad(drows, plan: ExpertPlan, out=None, stream: int = 0):
+    """The gradient of expert_rows' x for the gradient ``drows`` of its result: each token's branches' rows added."""
+    return expert_combine(drows, plan, out=out, stream=stream)
+
+
+def expert_combine_grad(dout, rows, plan: ExpertPlan, weights=None, drows=None, dweights=True, stream: int = 0):
+    """The gradients of expert_combine's rows and weights for the gradient ``dout`` [T, D] of its result (x's is dout
+    itself).  ``drows``: rows to write to (those behind the plan's last keep what they hold), by default new ones
+    (zeros there).  ``dweights``: True, False or a [T, k] fp32 tensor.  Returns (drows, dweights or None)."""
+    dev = dout.get_device()
+    address, n_d, d_stride, width, code = _value_fields(dout, "dout", dev)
+    r_address, n, r_stride, r_width, r_code = _value_fields(rows, "rows", dev)
+    place, T, k = _branches(plan, dev)
+    if n_d != T or r_width != width or r_code != code:
+        raise ValueError(f"dout must be [{T}, {r_width}] of rows' dtype")
+    w = _list(weights, "f32", (T, k), "weights", dev)
+    count = _plan_count(plan, dev) if drows is None else 0
+    drows, g_address, g_stride = _row_result(drows, n, width, rows, "drows", dev, stream)
+    if dweights is True:
+        torch = _TYPES["torch"]
+        dweights = _on(stream, dev, lambda: torch.empty((T, k), dtype=torch.float32, device=rows.device))
+    elif dweights is False:
+        dweights = None
+    dw = _list(dweights, "f32", (T, k), "dweights", dev)
+    args = _PACK_BACK_GRAD.pack(address, d_stride, r_address, r_stride, n, place, w, count, g_address, g_stride, dw, code, T, k,
+                                width)
+    _call(_packed["moeca_expert_combine_grad"], args, dev, stream)
+    return drows, dweights
+
+
+# ---------------------------------------------------------------------------
+# Attention on packed tokens (include/moeca_attention.h) on torch CUDA tensors
+# ---------------------------------------------------------------------------
+
+
+def _head_fields(t, what: str, device: int) -> tuple:
+    """((address, token stride, head stride, heads), tokens, dim, type code) of [tokens, heads, dim] values."""
+    shape, stride, code = t.shape, t.stride(), (_TYPES or _types()).get(t.dtype, -1)
+    if code not in (MOECA_F32, MOECA_BF16) or len(shape) != 3 or (stride[2] != 1 and shape[2] > 1) or t.get_device() != device:
+        raise ValueError(f"{what} must be a [tokens, heads, dim] float32 or bfloat16 tensor on the call's device whose heads "
+                         "are consecutive values")
+    n, heads, dim = shape
+    return (t.data_ptr(), stride[0] if n > 1 else 0, stride[1] if heads > 1 else 0, heads), n, dim, code
+
+
+def rope_table(positions, dims, theta: float = 10000.0):
+    """Cosines and sines [P, sum(dims) / 2, 2] fp32 for qk_norm_rope: ``positions`` [P] or [P, axes] (any numbers), axis a
+    turning dims[a] / 2 pairs with the frequencies theta^(-2 i / dims[a]), one axis' pairs after another's.  The angles
+    are formed in 64 bits."""
+    import torch
+    p = torch.as_tensor(positions)
+    p = p[:, None] if p.dim() == 1 else p
+    dims = [dims] if isinstance(dims, int) else list(dims)
+    if p.dim() != 2 or p.shape[1] != len(dims) or any(d < 0 or d % 2 for d in dims):
+        raise ValueError("positions must be [P] or [P, axes], dims an even number for each axis")
+    angles = [p[:, a:a + 1].double() * theta ** (-torch.arange(0, d, 2, dtype=torch.float64, device=p.device) / max(d, 1))
+              for a, d in enumerate(dims)]
+    angle = torch.cat(angles, 1)
+    return torch.stack([angle.cos(), angle.sin()], -1).float()
+
+
+def qk_norm_rope(q, k, table=None, q_weight=None, k_weight=None, pos=None, eps: float = 1e-6, pairs: bool = False,
+                 q_out=None, k_out=None, stream: int = 0):
+    """RMS norm of every head of ``q`` [T, H, d] and ``k`` [T, Hk, d] (fp32 or bf16, or k None; views of a fused
+    projection, say), times ``q_weight`` / ``k_weight`` [d] fp32 (None: 1), and the rotation of the first 2 P values by
+    ``table`` [positions, P, 2] fp32 (cosines and sines, see rope_table; None: no rotation).  Pair i is (i, i + P), or
+    (2 i, 2 i + 1) with ``pairs``.  ``pos`` [T] int32: the tokens' rows of the table (None: their numbers); a token whose
+    position is outside it is left out.  ``q_out`` and ``k_out`` may be q and k.  ``stream``: as for q8_read.  Returns
+    (q_out, k_out)."""
+    dev = q.get_device()
+    fq, T, dim, code = _head_fields(q, "q", dev)
+    torch = _TYPES["torch"]
+
+    def result(out, x, fields, what):
+        if out is None:
+            out = _on(stream, dev, lambda: torch.empty(x.shape, dtype=x.dtype, device=x.device))
+        f, n, d, c = _head_fields(out, what, dev)
+        if n != T or d != dim or c != code or f[3] != fields[3]:
+            raise ValueError(f"{what} must have the shape and dtype of what it comes from")
+        return out, f
+
+    fk = fk_out = (0, 0, 0, 0)
+    if k is not None:
+        fk, n, d, c = _head_fields(k, "k", dev)
+        if n != T or d != dim or c != code:
+            raise ValueError("k must have q's tokens, dim and dtype")
+    n_pos = rot = t_address = 0
+    if table is not None:
+        if table.dim() != 3 or table.shape[2] != 2:
+            raise ValueError("table must be [positions, pairs, 2]")
+        n_pos, rot = table.shape[0], 2 * table.shape[1]
+        t_address = _list(table, "f32", table.shape, "table", dev)
+    p_address = _list(pos, "i32", (T,), "pos", dev)
+    w = _list(q_weight, "f32", (dim,), "q_weight", dev), _list(k_weight, "f32", (dim,), "k_weight", dev)
+    q_out, fq_out = result(q_out, q, fq, "q_out")
+    if k is not None:
+        k_out, fk_out = result(k_out, k, fk, "k_out")
+    args = _PACK_QK.pack(*fq, *fk, *fq_out, *fk_out, *w, t_address, p_address, n_pos, code, T, dim, rot, bool(pairs), eps)
+    _call(_packed["moeca_qk_norm_rope"], args, dev, stream)
+    return q_out, k_out
+
+
+def attention(q, k, v, q_offsets=None, k_offsets=None, n_seqs: int = None, causal: bool = False, scale: float = None,
+              max_q: int = 0, lse=False, out=None, status=None, stream: int = 0):
+    """Attention over packed sequences: ``q`` [Tq, H, d], ``k`` and ``v`` [Tk, Hk, d] (fp32 or bf16, any token and head
+    strides, H a multiple of Hk), sequence b's tokens from offsets[b] to offsets[b + 1] - 1.  ``q_offsets`` and
+    ``k_offsets`` [B + 1] int32 on the device; without them the tokens are split evenly among ``n_seqs`` sequences (1, or as
+    many as the other offsets say).  ``causal``: the last query of a sequence sees its last key, each earlier one a key
+    less.  ``scale``: d^-0.5 by default.  ``max_q``: the longest query, if known (queries behind a sequence's first max_q are
+    not computed).  ``lse``: True or a [Tq, H] fp32 tensor also gives the log of the sum of exponentials.  A row that
+    sees no key is 0 with lse = -inf.  ``out`` may be q; query tokens before the first and behind the last sequence keep
+    what a given ``out`` holds and are 0 (lse -inf) with a new one.  ``status``: as for q8_matmul; ``stream``: as for q8_read.  Returns out, or
+    (out, lse)."""
+    dev = q.get_device()
+    fq, n_q, dim, code = _head_fields(q, "q", dev)
+    fk, n_k, k_dim, k_code = _head_fields(k, "k", dev)
+    fv, n_v, v_dim, v_code = _head_fields(v, "v", dev)
+    if n_k != n_v or not dim == k_dim == v_dim or not code == k_code == v_code:
+        raise ValueError("k and v must have the same tokens, and q's dim and dtype")
+    for offsets in (q_offsets, k_offsets):
+        if offsets is not None:
+            if n_seqs is None:
+                n_seqs = offsets.numel() - 1
+            if n_seqs < 1 or offsets.numel() != n_seqs + 1:
+                raise ValueError("offsets must have one entry more than there are sequences")
+    n_seqs = 1 if n_seqs is None else n_seqs
+    torch = _TYPES["torch"]
+    offs = _list(q_offsets, "i32", (n_seqs + 1,), "q_offsets", dev), _list(k_offsets, "i32", (n_seqs + 1,), "k_offsets", dev)
+    clear = out is None
+    if clear:
+        out = _on(stream, dev, lambda: torch.empty(q.shape, dtype=q.dtype, device=q.device))
+    fo, n_o, o_dim, o_code = _head_fields(out, "out", dev)
+    if n_o != n_q or o_dim != dim or o_code != code or fo[3] != fq[3]:
+        raise ValueError("out must have q's shape and dtype")
+    if lse is True:
+        lse = _on(stream, dev, lambda: torch.empty((n_q, fq[3]), dtype=torch.float32, device=q.device))
+    elif lse is False:
+        lse = None
+    s_address = _list(status, "i32", (2,), "status", dev)
+    l_address = _list(lse, "f32", (n_q, fq[3]), "lse", dev)
+    scale = dim ** -0.5 if scale is None and dim else scale or 0.0
+
+    def pack(space):
+        return _PACK_ATTENTION.pack(*fq, *fk, *fv, *fo, *offs, l_address, space, s_address, n_q, n_k, n_seqs, max_q, code, dim,
+                                    bool(causal), clear, scale)
+
+    args = pack(0)
+    size = _attention_bytes(args)
+    if size > 0:
+        space = _on(stream, dev, lambda: torch.empty(size, dtype=torch.uint8, device=q.device))
+        args = pack(space.data_ptr())
+    _call(_packed["moeca_attention"], args, dev, stream)
+    return out if lse is None else (out, lse)
