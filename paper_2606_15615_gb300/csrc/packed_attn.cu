@@ -271,6 +271,7 @@ constexpr int kMaxHeadDim = 256, kMaxSeqs = 1 << 20;
 constexpr int64_t kMaxWorkspace = int64_t(1) << 30;  // beyond, the key axis is not cut
 
 struct Plan {
+  int rows;           // tiles of 128 rows per block of the tensor-core kernel, 0: the CUDA-core kernel
   int tile;           // query tokens of a tile
   int chunk;          // keys of a chunk, 0: not cut
   int max_q, tiles;
@@ -293,20 +294,42 @@ int64_t pieces(const int32_t* off, int64_t total, int n, int unit, int most, int
   return packed;
 }
 
-// How a call is carried out: a function of its sizes alone.
+// Whether the tensor-core kernel can take the heads: pieces of 16 bytes everywhere.
+bool fits_tc(const moeca_heads& h, int64_t tokens) {
+  return tokens == 0 || (addr(h.data) % 16 == 0 && (tokens == 1 || h.token_stride % 8 == 0) && (h.heads == 1 || h.head_stride % 8 == 0));
+}
+
+constexpr int kSms = 152;
+
+// How a call is carried out: a function of its sizes, type and alignment.
 Plan plan_attention(const moeca_attention_args& a) {
   Plan p{};
-  const int64_t most = a.q_offsets ? (a.max_q > 0 ? std::min<int64_t>(a.max_q, a.n_queries) : a.n_queries) : a.n_queries / a.n_seqs;
+  const int64_t most = a.q_offsets ? a.n_queries : a.n_queries / a.n_seqs;
   p.max_q = static_cast<int>(a.max_q > 0 ? std::min<int64_t>(a.max_q, most) : most);
-  p.tile = p.max_q <= 16 ? 16 : 32;
+  const int group = a.q.heads / a.k.heads;
+  int heads, fill, least;  // blocks of a tile, blocks that fill the GPU, keys of a chunk at least
+  if (a.dtype == MOECA_BF16 && a.dim % 8 == 0 && a.dim <= 128 && group <= 128 && fits_tc(a.q, a.n_queries) &&
+      fits_tc(a.k, a.n_keys) && fits_tc(a.v, a.n_keys) && fits_tc(a.out, a.n_queries)) {
+    const int each = 128 / group;
+    p.rows = p.max_q <= each ? 1 : 2;
+    p.tile = p.rows * each;
+    heads = a.k.heads;
+    fill = kSms;
+    least = 512;
+  } else {
+    p.tile = p.max_q <= 16 ? 16 : 32;
+    heads = a.q.heads;
+    fill = 4 * kSms;
+    least = 256;
+  }
   p.q_pieces = pieces(a.q_offsets, a.n_queries, a.n_seqs, p.tile, p.max_q, &p.q_per);
   p.tiles = (p.max_q + p.tile - 1) / p.tile;
-  p.blocks = p.q_pieces * a.q.heads;
-  // Few blocks with many keys each: the key axis is cut so that some 600 blocks share it.
-  const int64_t wanted = 608;
-  if (p.blocks > 0 && p.blocks < wanted && p.max_q > 0) {
-    const int64_t chunk = std::max<int64_t>(256, (a.n_keys * p.tiles * a.q.heads / wanted + 127) / 128 * 128);
-    const int64_t longest = a.k_offsets ? a.n_keys : a.n_keys / a.n_seqs;
+  p.blocks = p.q_pieces * heads;
+  // Few blocks with many keys each: the key axis is cut so that the chunks' blocks fill the GPU once.
+  if (p.blocks > 0 && 2 * p.blocks <= fill) {
+    const int64_t cuts = fill / p.blocks, mean = a.n_keys / a.n_seqs;
+    const int64_t chunk = std::max<int64_t>(least, ((mean + cuts - 1) / cuts + 127) / 128 * 128);
+    const int64_t longest = a.k_offsets ? a.n_keys : mean;
     if (chunk < longest) {
       const int64_t n = pieces(a.k_offsets, a.n_keys, a.n_seqs, static_cast<int>(chunk), 0x7fffffff, &p.k_per);
       const int64_t rows = n * p.max_q * a.q.heads;
@@ -314,7 +337,7 @@ Plan plan_attention(const moeca_attention_args& a) {
       if (rows < kMaxWorkspace && bytes <= kMaxWorkspace) {
         p.chunk = static_cast<int>(chunk);
         p.k_pieces = n;
-        p.blocks = n * p.tiles * a.q.heads;
+        p.blocks = n * p.tiles * heads;
         p.lse_bytes = lse;
         p.bytes = bytes;
       }
@@ -400,7 +423,7 @@ moeca_status moeca_attention(const moeca_attention_args* a, void* stream) {
   d.status = a->status;
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   return launched([&] {
-    cudaError_t e = launch_attn_simt(d, a->dtype, p.tile, s);
+    cudaError_t e = p.rows ? launch_attn_packed_tc(d, p.rows, s) : launch_attn_simt(d, a->dtype, p.tile, s);
     if (e == cudaSuccess && p.chunk) e = launch_attn_join(d, a->dtype, s);
     return e;
   });

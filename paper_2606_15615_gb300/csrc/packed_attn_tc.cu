@@ -1,0 +1,439 @@
+// Attention over packed sequences on the tensor cores (include/moeca_attention.h):
+// bf16, heads of up to 128 values.
+//
+// A CTA works on one key head and NT tiles of 128 rows, over the sequence's keys
+// or one chunk of them.  A tile's rows are (query, head) pairs: 128 / G queries
+// with the G query heads that share the key head, so that every key block that
+// comes in serves all of them, and a single new token fills G rows instead of one.
+//   warp 0      TMA: the tiles' queries once, then key and value blocks of 128 keys
+//               through one ring of 32 KB (16 KB) slots, in the order of their use
+//   warp 1      allocates TMEM and issues tcgen05.mma from one thread:
+//               S_i = Q_i K_j^T (128 x 128, fp32), then O_i += P_i V_j
+//   warps 2 ..  softmax: four warps per tile, a row per thread.  A thread takes its
+//               row of S from TMEM, keeps the running maximum m and sum l, and
+//               writes P = 2^(s - m) in bf16 over S, where the second product
+//               reads it as its A operand.
+// With two tiles the tensor core works on one tile while the other's softmax
+// runs; S, and O beside it, take 256 TMEM columns a tile.  V is taken as it lies in
+// memory (keys x channels): the product reads it as an MN-major operand.
+// The row's maximum moves only when it rises by more than 2^8 (O is then rescaled
+// in TMEM; P stays below 2^8): after the first blocks that is rare.  S_{j+1}'s
+// completion is committed after the product with P_j was issued, so a thread
+// that sees S_{j+1} knows that O is quiet.
+// P is rounded to bf16, the operand's type; l adds the unrounded values in fp32.
+// Keys behind the sequence's end are masked; value rows there are zeroed in shared
+// memory before the product, as they belong to another sequence and may hold
+// infinities or NaN.
+// Every wait is bounded (about one second); a wait that runs out records
+// MOECA_ERR_TIMEOUT, raises the CTA's abort flag, lets what was issued finish,
+// frees TMEM and returns.
+#include <algorithm>
+
+#include "attn_tc.cuh"
+#include "packed_attn.cuh"
+
+namespace moeca {
+namespace {
+
+constexpr int kTileRows = 128;               // rows of a tile (MMA M)
+constexpr int kBlockKeys = 128;              // keys of a block
+constexpr int kPart = 128 * 128;             // bytes of 128 rows x 64 channels
+constexpr int kMaxStages = 8;
+constexpr size_t kSmemMost = 227 * 1024 - 2048;  // less the static part
+
+template <int DK, int NT>  // DK: 16-channel steps of a head
+struct TcShape {
+  static constexpr int DP = DK * 16;
+  static constexpr int SUBS = (DP + 63) / 64;
+  static constexpr int SLOT = SUBS * kPart;    // a tile of queries, a block of keys or of values
+  static constexpr int STAGES_FIT = static_cast<int>((kSmemMost - 1024 - NT * SLOT) / SLOT);
+  static constexpr int STAGES = STAGES_FIT < kMaxStages ? STAGES_FIT : kMaxStages;
+  static constexpr size_t SMEM = static_cast<size_t>(NT + STAGES) * SLOT + 1024;
+  static constexpr int COLUMNS = 256 * NT;     // TMEM
+  static constexpr int THREADS = 64 + 128 * NT;
+};
+
+// Instruction descriptor: B with its N values side by side (MN-major), or with its K values (K-major).
+__device__ __forceinline__ uint32_t instr_desc_b(int N, bool mn_major) {
+  return instr_desc(kTileRows, 16) - (16u >> 3 << 17) + (static_cast<uint32_t>(N >> 3) << 17) + (mn_major ? 1u << 16 : 0u);
+}
+// 16 keys of a value block as an MN-major operand: 128-byte swizzle, 64 channels a
+// row, the next 8 keys 1024 bytes on, the next 64 channels a sub-block on.
+__device__ __forceinline__ uint64_t smem_desc_mn(uint32_t at) {
+  uint64_t d = 0;
+  d |= static_cast<uint64_t>((at & 0x3FFFFu) >> 4);
+  d |= static_cast<uint64_t>(kPart >> 4) << 16;
+  d |= static_cast<uint64_t>(1024 >> 4) << 32;
+  d |= static_cast<uint64_t>(1) << 46;
+  d |= static_cast<uint64_t>(2) << 61;
+  return d;
+}
+__device__ __forceinline__ void tma_load_heads(uint32_t dst, const CUtensorMap* map, int channel, int head, int token, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(channel), "r"(head), "r"(token), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
+// Slots of the ring are filled and used in this order: K_0, K_1, V_0, K_2, V_1, ...
+__device__ __forceinline__ int place_of_k(int j) { return j == 0 ? 0 : 2 * j - 1; }
+__device__ __forceinline__ int place_of_v(int j, int blocks) { return j + 1 < blocks ? 2 * j + 2 : 2 * j + 1; }
+
+template <int DK, int NT>
+__global__ void __launch_bounds__(64 + 128 * NT, 1)
+    attn_packed_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
+                          const __grid_constant__ CUtensorMap vmap, const PackedAttnArgs a) {
+  using Sh = TcShape<DK, NT>;
+  constexpr int ST = Sh::STAGES;
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  __shared__ __align__(8) uint64_t q_full[NT], s_full[NT], p_full[NT], o_full[NT], full[ST], empty[ST], v_clean, drain;
+  __shared__ int issued;          // slots that the producer filled (for the drain)
+  __shared__ uint32_t tmem_sh;
+  __shared__ volatile int abort_flag;
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* ring = smem + NT * Sh::SLOT;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    abort_flag = 0;
+    issued = 0;
+    for (int i = 0; i < NT; ++i) {
+      mbar_init(smem_u32(&q_full[i]), 1);
+      mbar_init(smem_u32(&s_full[i]), 1);
+      mbar_init(smem_u32(&p_full[i]), kTileRows);
+      mbar_init(smem_u32(&o_full[i]), 1);
+    }
+    for (int i = 0; i < ST; ++i) {
+      mbar_init(smem_u32(&full[i]), 1);
+      mbar_init(smem_u32(&empty[i]), 1);
+    }
+    mbar_init(smem_u32(&v_clean), 1);
+    mbar_init(smem_u32(&drain), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  pdl_entry();
+  clear_rest<__nv_bfloat16>(a);
+  // The heaviest tiles of a causal sequence are its last: they start first.
+  const int64_t pieces = gridDim.x / a.k.heads;
+  const int64_t turn = blockIdx.x / a.k.heads;
+  const int kvh = static_cast<int>(blockIdx.x - turn * a.k.heads);
+  const AttnWork w = attn_work(a, a.causal && !a.ks.unit ? pieces - 1 - turn : turn);
+  if (!w.any) return;  // uniform over the CTA, before TMEM is taken
+  const int G = a.group, per_tile = a.qs.unit / NT;  // queries of a tile
+  const int n_q = min(w.nq, a.max_q);
+  // Blocks of keys that each tile's rows see.
+  int nb[NT], blocks = 0;
+#pragma unroll
+  for (int i = 0; i < NT; ++i) {
+    const int first = w.row0 + i * per_tile, last = min(first + per_tile, n_q) - 1;
+    nb[i] = first < n_q ? max(0, min(w.key_hi, visible_keys(a, w, last)) - w.key_lo + kBlockKeys - 1) / kBlockKeys : 0;
+    blocks = max(blocks, nb[i]);
+  }
+  // Keys of the last block, in 16s, and whether foreign value rows are among them.
+  const int last_keys = min(kBlockKeys, w.key_hi - (w.key_lo + (blocks - 1) * kBlockKeys));
+  const bool dirty = blocks > 0 && last_keys % 16 != 0;
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_sh)),
+                 "r"(Sh::COLUMNS)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    tc_fence_before();
+  }
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_sh;
+  const auto give_up = [&](int where) {
+    if (!abort_flag) report_status(a.status, MOECA_ERR_TIMEOUT, where);
+    abort_flag = 1;
+  };
+
+  if (warp == 0) {
+    if (lane == 0) {
+      const int token = static_cast<int>(w.q0) + w.row0;
+#pragma unroll
+      for (int i = 0; i < NT; ++i)
+        if (nb[i] > 0) {
+          mbar_expect_tx(smem_u32(&q_full[i]), Sh::SUBS * G * per_tile * 128);
+          for (int s = 0; s < Sh::SUBS; ++s)
+            tma_load_heads(smem_u32(smem + i * Sh::SLOT + s * kPart), &qmap, s * 64, kvh * G, token + i * per_tile, smem_u32(&q_full[i]));
+        }
+      int n = 0;
+      bool ok = true;
+      const auto fill = [&](const CUtensorMap* map, int block) {
+        const int s = n % ST;
+        if (n >= ST && !mbar_wait(smem_u32(&empty[s]), ((n / ST) - 1) & 1, &abort_flag)) {
+          give_up(710);
+          ok = false;
+          return;
+        }
+        const uint32_t bar = smem_u32(&full[s]);
+        mbar_expect_tx(bar, Sh::SLOT);
+        for (int c = 0; c < Sh::SUBS; ++c)
+          tma_load_heads(smem_u32(ring + s * Sh::SLOT + c * kPart), map, c * 64, kvh,
+                         static_cast<int>(w.k0) + w.key_lo + block * kBlockKeys, bar);
+        ++n;
+      };
+      if (blocks > 0) fill(&kmap, 0);
+      for (int j = 0; ok && j < blocks; ++j) {
+        if (j + 1 < blocks) fill(&kmap, j + 1);
+        if (ok) fill(&vmap, j);
+      }
+      issued = n;
+    }
+    __syncwarp();
+    if (dirty && !abort_flag) {
+      // Value rows last_keys .. of the last block's 16s are another sequence's, or nobody's.
+      const int n = place_of_v(blocks - 1, blocks), s = n % ST;
+      if (warp_wait(smem_u32(&full[s]), (n / ST) & 1, &abort_flag)) {
+        const int rows = (last_keys + 15) / 16 * 16 - last_keys;
+        for (int i = lane; i < rows * 8 * Sh::SUBS; i += 32) {
+          const int c = i / (rows * 8), at = i - c * rows * 8;
+          *reinterpret_cast<uint4*>(ring + s * Sh::SLOT + c * kPart + last_keys * 128 + at * 16) = make_uint4(0, 0, 0, 0);
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&v_clean));
+      } else if (lane == 0) {
+        give_up(711);
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      bool ok = true;
+      const auto wait = [&](uint64_t* bar, int phase) {
+        if (ok && !mbar_wait_hot(smem_u32(bar), phase & 1, &abort_flag)) ok = false;
+        return ok;
+      };
+      // S_i of block j (its K is there).
+      const auto scores = [&](int i, int j) {
+        const int n = place_of_k(j);
+        const uint32_t qa = smem_u32(smem + i * Sh::SLOT), kb = smem_u32(ring + n % ST * Sh::SLOT);
+        const int keys = j + 1 < blocks ? kBlockKeys : (last_keys + 15) / 16 * 16;
+        const uint32_t id = instr_desc_b(keys, false);
+        tc_fence_after();
+#pragma unroll
+        for (int kk = 0; kk < DK; ++kk) {
+          const int off = (kk >> 2) * kPart + (kk & 3) * 32;
+          mma_bf16(tmem + i * 256, smem_desc(qa + off), smem_desc(kb + off), id, kk > 0);
+        }
+        mma_commit(smem_u32(&s_full[i]));
+      };
+      const auto ring_wait = [&](int n) { return wait(&full[n % ST], n / ST); };
+      if (blocks > 0 && ring_wait(0)) {
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+          if (nb[i] > 0 && wait(&q_full[i], 0)) scores(i, 0);
+        if (ok) mma_commit(smem_u32(&empty[0]));
+      }
+      const uint32_t id_o = instr_desc_b(Sh::DP, true);
+      for (int j = 0; ok && j < blocks; ++j) {
+        const int nv = place_of_v(j, blocks), nk = place_of_k(j + 1);
+        const bool last = j + 1 == blocks;
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+          if (j < nb[i] && wait(&p_full[i], j) && ring_wait(nv) && (!last || !dirty || wait(&v_clean, 0))) {
+            tc_fence_after();
+            const uint32_t vb = smem_u32(ring + nv % ST * Sh::SLOT);
+            const int steps = last ? (last_keys + 15) / 16 : kBlockKeys / 16;
+            if (steps == kBlockKeys / 16) {
+#pragma unroll
+              for (int kk = 0; kk < kBlockKeys / 16; ++kk)
+                mma_bf16_ta(tmem + i * 256 + 128, tmem + i * 256 + kk * 8, smem_desc_mn(vb + kk * 2048), id_o, j > 0 || kk > 0);
+            } else {
+              for (int kk = 0; kk < steps; ++kk)
+                mma_bf16_ta(tmem + i * 256 + 128, tmem + i * 256 + kk * 8, smem_desc_mn(vb + kk * 2048), id_o, j > 0 || kk > 0);
+            }
+            if (j + 1 == nb[i]) mma_commit(smem_u32(&o_full[i]));
+          }
+          if (ok && j + 1 < nb[i] && ring_wait(nk)) scores(i, j + 1);
+        }
+        if (ok) {
+          mma_commit(smem_u32(&empty[nv % ST]));
+          if (!last) mma_commit(smem_u32(&empty[nk % ST]));
+        }
+      }
+      if (!ok) give_up(712);
+      // Every MMA issued so far has completed once this barrier fires.
+      mma_commit(smem_u32(&drain));
+      drain_wait(smem_u32(&drain), 0);
+    }
+  } else {
+    const int tile = (warp - 2) >> 2, quad = warp & 3;
+    const int r = quad * 32 + lane;
+    const uint32_t t_s = tmem + (static_cast<uint32_t>(quad * 32) << 16) + tile * 256, t_o = t_s + 128;
+    const int own_blocks = NT == 1 ? nb[0] : (tile == 0 ? nb[0] : nb[NT - 1]);
+    const int query = w.row0 + tile * per_tile + r / G, head = kvh * G + r % G;
+    const bool live = r < per_tile * G && query < n_q;
+    const int see = min(live ? visible_keys(a, w, query) : w.nk, w.key_hi) - w.key_lo;
+    const float sc = a.scale_log2;
+    float m = -INFINITY;
+    float2 l2[2] = {{0.f, 0.f}, {0.f, 0.f}};
+    bool ok = true;
+    for (int j = 0; j < own_blocks; ++j) {
+      if (!warp_wait(smem_u32(&s_full[tile]), j & 1, &abort_flag)) {
+        ok = false;
+        break;
+      }
+      tc_fence_after();
+      uint32_t sv[128];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tmem_ld32_async(t_s + c * 32, sv + c * 32);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tmem_wait32(sv + c * 32);
+      const int limit = see - j * kBlockKeys;  // keys of the block that this row sees
+      if (!__all_sync(0xffffffffu, limit >= kBlockKeys)) {
+#pragma unroll
+        for (int q = 0; q < 128; ++q)
+          if (q >= limit) sv[q] = 0xff800000u;  // -infinity
+      }
+      float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+      for (int q = 0; q < 128; q += 8)
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          top[u] = max3(top[u], __uint_as_float(sv[q + 2 * u]), __uint_as_float(sv[q + 2 * u + 1]));
+      const float cand = fmaxf(m, max3(fmaxf(top[0], top[1]), top[2], top[3]));
+      if (j == 0) {
+        m = cand;
+      } else if (__any_sync(0xffffffffu, (cand - m) * sc > 8.f)) {
+        const float alpha = m == cand ? 1.f : ex2f_approx((m - cand) * sc);
+#pragma unroll
+        for (int c = 0; c < DK; ++c) {
+          uint32_t v[16];
+          tmem_ld16(t_o + c * 16, v);
+#pragma unroll
+          for (int q = 0; q < 16; ++q) v[q] = __float_as_uint(__uint_as_float(v[q]) * alpha);
+          tmem_st16(t_o + c * 16, v);
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) l2[u] = mul2(l2[u], make_float2(alpha, alpha));
+        m = cand;
+      }
+      const float ref = m == -INFINITY ? 0.f : m * sc;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        uint32_t pk[16];
+#pragma unroll
+        for (int q = 0; q < 16; ++q) {
+          const int at = c * 32 + 2 * q;
+          float2 p = fma2(make_float2(__uint_as_float(sv[at]), __uint_as_float(sv[at + 1])), make_float2(sc, sc), make_float2(-ref, -ref));
+          p.x = ex2f_approx(p.x);
+          p.y = ex2f_approx(p.y);
+          l2[q & 1] = add2(l2[q & 1], p);
+          pk[q] = pack2(p.x, p.y);
+        }
+        tmem_st16(t_s + c * 16, pk);
+      }
+      tc_fence_before();
+      mbar_arrive(smem_u32(&p_full[tile]));
+    }
+    if (ok && own_blocks > 0) ok = warp_wait(smem_u32(&o_full[tile]), 0, &abort_flag);
+    if (ok) {
+      tc_fence_after();
+      const float l = (l2[0].x + l2[0].y) + (l2[1].x + l2[1].y);
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const float lse2 = l == 0.f ? -INFINITY : m * sc + log2f(l);
+      const bool cut = a.ks.unit != 0;
+      const int64_t part = (w.piece * a.max_q + query) * a.q.heads + head;
+      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out.data) + (w.q0 + query) * a.out.token_stride + head * a.out.head_stride;
+      float* part_o = a.part_o + part * a.dim;
+      if (live) {
+        if (cut) a.part_lse[part] = lse2;
+        else if (a.lse) a.lse[(w.q0 + query) * a.q.heads + head] = lse2 * kLn2;
+      }
+#pragma unroll
+      for (int c = 0; c < DK; ++c) {
+        uint32_t v[16] = {};
+        if (own_blocks > 0) tmem_ld16(t_o + c * 16, v);  // every lane: the load is warp-collective
+        float f[16];
+#pragma unroll
+        for (int q = 0; q < 16; ++q) f[q] = __uint_as_float(v[q]) * inv;
+        if (!live) continue;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int at = c * 16 + h * 8;
+          if (at >= a.dim) continue;
+          if (cut) {
+            store_vec(part_o + at, f + h * 8);
+            store_vec(part_o + at + 4, f + h * 8 + 4);
+          } else {
+            store_vec(out + at, f + h * 8);
+          }
+        }
+      }
+    } else if (lane == 0) {
+      give_up(713);
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (threadIdx.x == 0 && abort_flag) {
+    // Copies issued but never used still land in shared memory.
+    for (int i = 0; i < NT; ++i)
+      if (nb[i] > 0) drain_wait(smem_u32(&q_full[i]), 0);
+    for (int s = 0; s < ST && s < issued; ++s) {
+      const int last = issued - 1 - (issued - 1 - s) % ST;  // the newest copy into slot s
+      drain_wait(smem_u32(&full[s]), (last / ST) & 1);
+    }
+  }
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(Sh::COLUMNS) : "memory");
+  }
+}
+
+// A map of heads: {channel, head, token}, boxes of 64 channels x `heads` x `tokens`, channels past dim zero-filled.
+bool encode_heads(CUtensorMap* m, const Heads& h, int64_t tokens, int dim, int heads, int box_tokens) {
+  EncodeTiledFn enc = get_encoder();
+  if (!enc) return false;
+  const auto stride = [&](int64_t s, int64_t n) { return static_cast<cuuint64_t>(n > 1 ? s * 2 : (dim * 2 + 15) / 16 * 16); };
+  cuuint64_t dims[3] = {static_cast<cuuint64_t>(dim), static_cast<cuuint64_t>(h.heads), static_cast<cuuint64_t>(tokens)};
+  cuuint64_t strides[2] = {stride(h.head_stride, h.heads), stride(h.token_stride, tokens)};
+  cuuint32_t box[3] = {64, static_cast<cuuint32_t>(heads), static_cast<cuuint32_t>(box_tokens)};
+  cuuint32_t estr[3] = {1, 1, 1};
+  return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, h.data, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int DK, int NT>
+cudaError_t run(const PackedAttnArgs& a, cudaStream_t s) {
+  using Sh = TcShape<DK, NT>;
+  static_assert(Sh::STAGES >= 4, "a ring that holds two blocks of keys and of values");
+  CUtensorMap qm, km, vm;
+  // Without keys nothing is loaded; the maps still want a tensor.
+  const Heads& k = a.ks.total > 0 ? a.k : a.q;
+  const Heads& v = a.ks.total > 0 ? a.v : a.q;
+  const int64_t keys = a.ks.total > 0 ? a.ks.total : a.qs.total;
+  if (!encode_heads(&qm, a.q, a.qs.total, a.dim, a.group, a.qs.unit / NT) || !encode_heads(&km, k, keys, a.dim, 1, kBlockKeys) ||
+      !encode_heads(&vm, v, keys, a.dim, 1, kBlockKeys))
+    return cudaErrorInvalidValue;
+  const auto kernel = attn_packed_tc_kernel<DK, NT>;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(Sh::SMEM));
+  if (e != cudaSuccess) return e;
+  const int64_t blocks = (a.ks.unit ? a.k_pieces * a.tiles : a.q_pieces) * a.k.heads;
+  return launch_pdl(kernel, dim3(static_cast<unsigned>(blocks)), dim3(Sh::THREADS), Sh::SMEM, s, qm, km, vm, a);
+}
+
+}  // namespace
+
+cudaError_t launch_attn_packed_tc(const PackedAttnArgs& a, int tiles, cudaStream_t s) {
+  const int dk = (a.dim + 15) / 16;
+  if (tiles == 2) {
+    if (dk <= 4) return run<4, 2>(a, s);
+    if (dk == 5) return run<5, 2>(a, s);
+    if (dk == 6) return run<6, 2>(a, s);
+    return run<8, 2>(a, s);
+  }
+  if (dk <= 4) return run<4, 1>(a, s);
+  if (dk == 5) return run<5, 1>(a, s);
+  if (dk == 6) return run<6, 1>(a, s);
+  return run<8, 1>(a, s);
+}
+
+}  // namespace moeca
