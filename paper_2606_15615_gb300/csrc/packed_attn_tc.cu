@@ -57,16 +57,34 @@ struct TcShape {
 __device__ __forceinline__ uint32_t instr_desc_b(int N, bool mn_major) {
   return instr_desc(kTileRows, 16) - (16u >> 3 << 17) + (static_cast<uint32_t>(N >> 3) << 17) + (mn_major ? 1u << 16 : 0u);
 }
-// 16 keys of a value block as an MN-major operand: 128-byte swizzle, 64 channels a
-// row, the next 8 keys 1024 bytes on, the next 64 channels a sub-block on.
-__device__ __forceinline__ uint64_t smem_desc_mn(uint32_t at) {
-  uint64_t d = 0;
-  d |= static_cast<uint64_t>((at & 0x3FFFFu) >> 4);
-  d |= static_cast<uint64_t>(kPart >> 4) << 16;
-  d |= static_cast<uint64_t>(1024 >> 4) << 32;
-  d |= static_cast<uint64_t>(1) << 46;
-  d |= static_cast<uint64_t>(2) << 61;
-  return d;
+// Low word of a shared-memory matrix descriptor (128-byte swizzle, 8 rows 1024
+// bytes on; the high word is the same for all).  K-major operands (queries, keys)
+// do not use `lead`; for the MN-major values (64 channels a row, 8 keys 1024
+// bytes on) it is the way to the next 64 channels.
+__device__ __forceinline__ uint32_t desc_lo(uint32_t at, uint32_t lead) { return ((at & 0x3FFFFu) >> 4) | (lead >> 4 << 16); }
+constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
+// One MMA, issued by the lane that has `issue` set.
+__device__ __forceinline__ void mma_ss_if(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t acc, uint32_t issue) {
+  asm volatile(
+      "{\n .reg .pred p, e;\n .reg .b64 a, b;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 e, %6, 0;\n"
+      " mov.b64 a, {%1, %5};\n mov.b64 b, {%2, %5};\n"
+      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n}"
+      ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(acc), "r"(kDescHi), "r"(issue)
+      : "memory");
+}
+__device__ __forceinline__ void mma_ts_if(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t idesc, uint32_t acc, uint32_t issue) {
+  asm volatile(
+      "{\n .reg .pred p, e;\n .reg .b64 b;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 e, %6, 0;\n"
+      " mov.b64 b, {%2, %5};\n"
+      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n}"
+      ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(idesc), "r"(acc), "r"(kDescHi), "r"(issue)
+      : "memory");
+}
+__device__ __forceinline__ void commit_if(uint32_t bar, uint32_t issue) {
+  asm volatile(
+      "{\n .reg .pred e;\n setp.ne.b32 e, %1, 0;\n"
+      " @e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}" ::"r"(bar), "r"(issue)
+      : "memory");
 }
 __device__ __forceinline__ void tma_load_heads(uint32_t dst, const CUtensorMap* map, int channel, int head, int token, uint32_t bar) {
   asm volatile(
@@ -80,6 +98,19 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 
+// mbar_wait without a call.
+__device__ __forceinline__ bool wait_here(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  if (mbar_try(bar, parity)) return true;
+  const unsigned long long t0 = globaltimer();
+#pragma unroll 1
+  for (uint32_t it = 1; !mbar_try(bar, parity); ++it)
+    if ((it & 255u) == 0 && (*abort_flag || globaltimer() - t0 > kTcWaitNs)) return false;
+  return true;
+}
+__device__ __forceinline__ bool warp_wait_here(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  return __all_sync(0xffffffffu, wait_here(bar, parity, abort_flag));
+}
+
 // Slots of the ring are filled and used in this order: K_0, K_1, V_0, K_2, V_1, ...
 __device__ __forceinline__ int place_of_k(int j) { return j == 0 ? 0 : 2 * j - 1; }
 __device__ __forceinline__ int place_of_v(int j, int blocks) { return j + 1 < blocks ? 2 * j + 2 : 2 * j + 1; }
@@ -91,7 +122,7 @@ __global__ void __launch_bounds__(64 + 128 * NT, 1)
   using Sh = TcShape<DK, NT>;
   constexpr int ST = Sh::STAGES;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t q_full[NT], s_full[NT], p_full[NT], o_full[NT], full[ST], empty[ST], v_clean, drain;
+  __shared__ __align__(8) uint64_t q_full[NT], s_full[NT], p_full[NT][2], o_full[NT], full[ST], empty[ST], v_clean, drain;
   __shared__ int issued;          // slots that the producer filled (for the drain)
   __shared__ uint32_t tmem_sh;
   __shared__ volatile int abort_flag;
@@ -104,7 +135,8 @@ __global__ void __launch_bounds__(64 + 128 * NT, 1)
     for (int i = 0; i < NT; ++i) {
       mbar_init(smem_u32(&q_full[i]), 1);
       mbar_init(smem_u32(&s_full[i]), 1);
-      mbar_init(smem_u32(&p_full[i]), kTileRows);
+      mbar_init(smem_u32(&p_full[i][0]), kTileRows);
+      mbar_init(smem_u32(&p_full[i][1]), kTileRows);
       mbar_init(smem_u32(&o_full[i]), 1);
     }
     for (int i = 0; i < ST; ++i) {
@@ -166,7 +198,7 @@ __global__ void __launch_bounds__(64 + 128 * NT, 1)
       bool ok = true;
       const auto fill = [&](const CUtensorMap* map, int block) {
         const int s = n % ST;
-        if (n >= ST && !mbar_wait(smem_u32(&empty[s]), ((n / ST) - 1) & 1, &abort_flag)) {
+        if (n >= ST && !wait_here(smem_u32(&empty[s]), ((n / ST) - 1) & 1, &abort_flag)) {
           give_up(710);
           ok = false;
           return;
@@ -189,7 +221,7 @@ __global__ void __launch_bounds__(64 + 128 * NT, 1)
     if (dirty && !abort_flag) {
       // Value rows last_keys .. of the last block's 16s are another sequence's, or nobody's.
       const int n = place_of_v(blocks - 1, blocks), s = n % ST;
-      if (warp_wait(smem_u32(&full[s]), (n / ST) & 1, &abort_flag)) {
+      if (warp_wait_here(smem_u32(&full[s]), (n / ST) & 1, &abort_flag)) {
         const int rows = (last_keys + 15) / 16 * 16 - last_keys;
         for (int i = lane; i < rows * 8 * Sh::SUBS; i += 32) {
           const int c = i / (rows * 8), at = i - c * rows * 8;
@@ -203,65 +235,85 @@ __global__ void __launch_bounds__(64 + 128 * NT, 1)
       }
     }
   } else if (warp == 1) {
-    if (lane == 0) {
-      bool ok = true;
-      const auto wait = [&](uint64_t* bar, int phase) {
-        if (ok && !mbar_wait_hot(smem_u32(bar), phase & 1, &abort_flag)) ok = false;
-        return ok;
-      };
-      // S_i of block j (its K is there).
-      const auto scores = [&](int i, int j) {
-        const int n = place_of_k(j);
-        const uint32_t qa = smem_u32(smem + i * Sh::SLOT), kb = smem_u32(ring + n % ST * Sh::SLOT);
-        const int keys = j + 1 < blocks ? kBlockKeys : (last_keys + 15) / 16 * 16;
-        const uint32_t id = instr_desc_b(keys, false);
-        tc_fence_after();
+    // All lanes run the loop, so that operands stay in uniform registers; one issues.
+    uint32_t issue;
+    asm volatile("{\n .reg .pred e;\n elect.sync _|e, 0xffffffff;\n selp.u32 %0, 1, 0, e;\n}" : "=r"(issue));
+    bool ok = true;
+    const auto wait = [&](uint64_t* bar, int phase) {
+      if (ok && !warp_wait_here(smem_u32(bar), phase & 1, &abort_flag)) ok = false;
+      return ok;
+    };
+    const uint32_t q_lo = desc_lo(smem_u32(smem), 16), ring_k = desc_lo(smem_u32(ring), 16), ring_v = desc_lo(smem_u32(ring), kPart);
+    const uint32_t id_s = instr_desc_b(kBlockKeys, false), id_o = instr_desc_b(Sh::DP, true);
+    // S_i of block j, whose keys are in slot `at`.
+    const auto scores = [&](int i, int j, int at) {
+      const uint32_t id = j + 1 < blocks ? id_s : instr_desc_b((last_keys + 15) / 16 * 16, false);
+      const uint32_t qa = q_lo + i * (Sh::SLOT >> 4), kb = ring_k + at * (Sh::SLOT >> 4);
+      tc_fence_after();
 #pragma unroll
-        for (int kk = 0; kk < DK; ++kk) {
-          const int off = (kk >> 2) * kPart + (kk & 3) * 32;
-          mma_bf16(tmem + i * 256, smem_desc(qa + off), smem_desc(kb + off), id, kk > 0);
-        }
-        mma_commit(smem_u32(&s_full[i]));
-      };
-      const auto ring_wait = [&](int n) { return wait(&full[n % ST], n / ST); };
-      if (blocks > 0 && ring_wait(0)) {
-#pragma unroll
-        for (int i = 0; i < NT; ++i)
-          if (nb[i] > 0 && wait(&q_full[i], 0)) scores(i, 0);
-        if (ok) mma_commit(smem_u32(&empty[0]));
+      for (int kk = 0; kk < DK; ++kk) {
+        const int off = ((kk >> 2) * kPart + (kk & 3) * 32) >> 4;
+        mma_ss_if(tmem + i * 256, qa + off, kb + off, id, kk > 0, issue);
       }
-      const uint32_t id_o = instr_desc_b(Sh::DP, true);
-      for (int j = 0; ok && j < blocks; ++j) {
-        const int nv = place_of_v(j, blocks), nk = place_of_k(j + 1);
-        const bool last = j + 1 == blocks;
-#pragma unroll
-        for (int i = 0; i < NT; ++i) {
-          if (j < nb[i] && wait(&p_full[i], j) && ring_wait(nv) && (!last || !dirty || wait(&v_clean, 0))) {
-            tc_fence_after();
-            const uint32_t vb = smem_u32(ring + nv % ST * Sh::SLOT);
-            const int steps = last ? (last_keys + 15) / 16 : kBlockKeys / 16;
-            if (steps == kBlockKeys / 16) {
-#pragma unroll
-              for (int kk = 0; kk < kBlockKeys / 16; ++kk)
-                mma_bf16_ta(tmem + i * 256 + 128, tmem + i * 256 + kk * 8, smem_desc_mn(vb + kk * 2048), id_o, j > 0 || kk > 0);
-            } else {
-              for (int kk = 0; kk < steps; ++kk)
-                mma_bf16_ta(tmem + i * 256 + 128, tmem + i * 256 + kk * 8, smem_desc_mn(vb + kk * 2048), id_o, j > 0 || kk > 0);
-            }
-            if (j + 1 == nb[i]) mma_commit(smem_u32(&o_full[i]));
-          }
-          if (ok && j + 1 < nb[i] && ring_wait(nk)) scores(i, j + 1);
-        }
-        if (ok) {
-          mma_commit(smem_u32(&empty[nv % ST]));
-          if (!last) mma_commit(smem_u32(&empty[nk % ST]));
-        }
+      commit_if(smem_u32(&s_full[i]), issue);
+    };
+    // Slots are used in the order in which they are filled; a barrier is waited for once.
+    int at = 0, seen = -1;
+    uint32_t parity = 0;
+    const auto ring_wait = [&](int n) {  // n: seen, or seen + 1
+      if (n == seen) return ok;
+      if (seen >= 0 && ++at == ST) {
+        at = 0;
+        parity ^= 1;
       }
-      if (!ok) give_up(712);
-      // Every MMA issued so far has completed once this barrier fires.
-      mma_commit(smem_u32(&drain));
-      drain_wait(smem_u32(&drain), 0);
+      seen = n;
+      return wait(&full[at], parity);
+    };
+    if (blocks > 0 && ring_wait(0)) {
+#pragma unroll
+      for (int i = 0; i < NT; ++i)
+        if (nb[i] > 0 && wait(&q_full[i], 0)) scores(i, 0, 0);
+      if (ok) commit_if(smem_u32(&empty[0]), issue);
     }
+    for (int j = 0; ok && j < blocks; ++j) {
+      const bool last = j + 1 == blocks;
+      // The next keys come before this block's values.
+      int k_at = 0;
+      if (!last) {
+        ring_wait(place_of_k(j + 1));
+        k_at = at;
+      }
+      if (!ring_wait(place_of_v(j, blocks)) || (last && dirty && !wait(&v_clean, 0))) break;
+      const uint32_t vb = ring_v + at * (Sh::SLOT >> 4);
+      const int steps = last ? (last_keys + 15) / 16 : kBlockKeys / 16;
+#pragma unroll
+      for (int i = 0; i < NT; ++i) {
+        if (j < nb[i]) {
+          // P comes in halves of 64 keys.
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            if (!wait(&p_full[i][half], j)) break;
+            tc_fence_after();
+#pragma unroll
+            for (int kk = half * 4; kk < half * 4 + 4; ++kk)
+              if (kk < steps)
+                mma_ts_if(tmem + i * 256 + 128, tmem + i * 256 + kk * 8, vb + kk * (2048 >> 4), id_o, j > 0 || kk > 0, issue);
+          }
+          if (ok && j + 1 == nb[i]) commit_if(smem_u32(&o_full[i]), issue);
+        }
+        if (ok && j + 1 < nb[i]) scores(i, j + 1, k_at);
+      }
+      if (ok) {
+        commit_if(smem_u32(&empty[at]), issue);
+        if (!last) commit_if(smem_u32(&empty[k_at]), issue);
+      }
+    }
+    if (!ok && lane == 0) give_up(712);
+    // Every MMA issued so far has completed once this barrier fires: a commit
+    // covers what its own thread issued, so the issuing lane makes it.
+    commit_if(smem_u32(&drain), issue);
+    if (issue) drain_wait(smem_u32(&drain), 0);
+    __syncwarp();
   } else {
     const int tile = (warp - 2) >> 2, quad = warp & 3;
     const int r = quad * 32 + lane;
@@ -275,7 +327,7 @@ __global__ void __launch_bounds__(64 + 128 * NT, 1)
     float2 l2[2] = {{0.f, 0.f}, {0.f, 0.f}};
     bool ok = true;
     for (int j = 0; j < own_blocks; ++j) {
-      if (!warp_wait(smem_u32(&s_full[tile]), j & 1, &abort_flag)) {
+      if (!warp_wait_here(smem_u32(&s_full[tile]), j & 1, &abort_flag)) {
         ok = false;
         break;
       }
@@ -327,12 +379,15 @@ __global__ void __launch_bounds__(64 + 128 * NT, 1)
           l2[q & 1] = add2(l2[q & 1], p);
           pk[q] = pack2(p.x, p.y);
         }
-        tmem_st16(t_s + c * 16, pk);
+        tmem_st16_async(t_s + c * 16, pk);
+        if (c & 1) {
+          tmem_wait_st();
+          tc_fence_before();
+          mbar_arrive(smem_u32(&p_full[tile][c >> 1]));
+        }
       }
-      tc_fence_before();
-      mbar_arrive(smem_u32(&p_full[tile]));
     }
-    if (ok && own_blocks > 0) ok = warp_wait(smem_u32(&o_full[tile]), 0, &abort_flag);
+    if (ok && own_blocks > 0) ok = warp_wait_here(smem_u32(&o_full[tile]), 0, &abort_flag);
     if (ok) {
       tc_fence_after();
       const float l = (l2[0].x + l2[0].y) + (l2[1].x + l2[1].y);
