@@ -98,13 +98,17 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 
-// mbar_wait without a call.
+// mbar_wait without a call, the clock looked at every 256 tries (reading it takes longer than most waits).
 __device__ __forceinline__ bool wait_here(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
   if (mbar_try(bar, parity)) return true;
-  const unsigned long long t0 = globaltimer();
+  unsigned long long t0 = 0;
 #pragma unroll 1
   for (uint32_t it = 1; !mbar_try(bar, parity); ++it)
-    if ((it & 255u) == 0 && (*abort_flag || globaltimer() - t0 > kTcWaitNs)) return false;
+    if ((it & 255u) == 0) {
+      const unsigned long long now = globaltimer();
+      if (*abort_flag || (t0 != 0 && now - t0 > kTcWaitNs)) return false;
+      if (t0 == 0) t0 = now;
+    }
   return true;
 }
 __device__ __forceinline__ bool warp_wait_here(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
@@ -112,7 +116,6 @@ __device__ __forceinline__ bool warp_wait_here(uint32_t bar, uint32_t parity, vo
 }
 
 // Slots of the ring are filled and used in this order: K_0, K_1, V_0, K_2, V_1, ...
-__device__ __forceinline__ int place_of_k(int j) { return j == 0 ? 0 : 2 * j - 1; }
 __device__ __forceinline__ int place_of_v(int j, int blocks) { return j + 1 < blocks ? 2 * j + 2 : 2 * j + 1; }
 
 template <int DK, int NT>
@@ -235,77 +238,90 @@ __global__ void __launch_bounds__(64 + 128 * NT, 1)
       }
     }
   } else if (warp == 1) {
-    // All lanes run the loop, so that operands stay in uniform registers; one issues.
+    // All lanes run the loop and one issues; what the loop turns on is read from
+    // lane 0, so that the compiler knows it to be the same in all and keeps the
+    // MMAs' operands in uniform registers (else each is moved there anew, and the
+    // loop alone takes 3300 clocks for two tiles' block, at 64 channels and at 128).
+    const auto uniform = [](auto x) { return static_cast<decltype(x)>(__shfl_sync(0xffffffffu, x, 0)); };
     uint32_t issue;
     asm volatile("{\n .reg .pred e;\n elect.sync _|e, 0xffffffff;\n selp.u32 %0, 1, 0, e;\n}" : "=r"(issue));
+    const int n_blocks = uniform(blocks), n_last = uniform((last_keys + 15) / 16);
+    int n_own[NT];
+#pragma unroll
+    for (int i = 0; i < NT; ++i) n_own[i] = uniform(nb[i]);
+    const bool clean_first = uniform(static_cast<int>(dirty)) != 0;
+    const uint32_t t = uniform(tmem);
     bool ok = true;
-    const auto wait = [&](uint64_t* bar, int phase) {
-      if (ok && !warp_wait_here(smem_u32(bar), phase & 1, &abort_flag)) ok = false;
-      return ok;
-    };
+    const auto wait = [&](uint32_t bar, uint32_t phase) { return ok = warp_wait_here(bar, phase & 1, &abort_flag); };
     const uint32_t q_lo = desc_lo(smem_u32(smem), 16), ring_k = desc_lo(smem_u32(ring), 16), ring_v = desc_lo(smem_u32(ring), kPart);
     const uint32_t id_s = instr_desc_b(kBlockKeys, false), id_o = instr_desc_b(Sh::DP, true);
-    // S_i of block j, whose keys are in slot `at`.
-    const auto scores = [&](int i, int j, int at) {
-      const uint32_t id = j + 1 < blocks ? id_s : instr_desc_b((last_keys + 15) / 16 * 16, false);
+    const uint32_t full0 = smem_u32(&full[0]), empty0 = smem_u32(&empty[0]), p0 = smem_u32(&p_full[0][0]), s0 = smem_u32(&s_full[0]);
+    // S_i, for the keys in slot `at`.
+    const auto scores = [&](int i, uint32_t at, uint32_t id) {
       const uint32_t qa = q_lo + i * (Sh::SLOT >> 4), kb = ring_k + at * (Sh::SLOT >> 4);
-      tc_fence_after();
 #pragma unroll
       for (int kk = 0; kk < DK; ++kk) {
         const int off = ((kk >> 2) * kPart + (kk & 3) * 32) >> 4;
-        mma_ss_if(tmem + i * 256, qa + off, kb + off, id, kk > 0, issue);
+        mma_ss_if(t + i * 256, qa + off, kb + off, id, kk > 0, issue);
       }
-      commit_if(smem_u32(&s_full[i]), issue);
+      commit_if(s0 + i * 8, issue);
     };
-    // Slots are used in the order in which they are filled; a barrier is waited for once.
-    int at = 0, seen = -1;
-    uint32_t parity = 0;
-    const auto ring_wait = [&](int n) {  // n: seen, or seen + 1
-      if (n == seen) return ok;
-      if (seen >= 0 && ++at == ST) {
+    // The second product with 64 keys' P, `steps` of 16 keys of them.
+    const auto values = [&](int i, int half, uint32_t vb, bool first, int steps) {
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk)
+        if (kk < steps)
+          mma_ts_if(t + i * 256 + 128, t + i * 256 + (half * 4 + kk) * 8, vb + (half * 4 + kk) * (2048 >> 4), id_o,
+                    !first || half > 0 || kk > 0, issue);
+    };
+    // Slots are used in the order in which they are filled.
+    uint32_t at = 0, parity = 0;
+    const auto next = [&] {
+      if (++at == ST) {
         at = 0;
         parity ^= 1;
       }
-      seen = n;
-      return wait(&full[at], parity);
     };
-    if (blocks > 0 && ring_wait(0)) {
+    const auto id_of = [&](int j) { return j + 1 < n_blocks ? id_s : instr_desc_b(n_last * 16, false); };
+    if (n_blocks > 0 && wait(full0, 0)) {
 #pragma unroll
       for (int i = 0; i < NT; ++i)
-        if (nb[i] > 0 && wait(&q_full[i], 0)) scores(i, 0, 0);
-      if (ok) commit_if(smem_u32(&empty[0]), issue);
+        if (ok && n_own[i] > 0 && wait(smem_u32(&q_full[i]), 0)) {
+          tc_fence_after();
+          scores(i, 0, id_of(0));
+        }
+      if (ok) commit_if(empty0, issue);
     }
-    for (int j = 0; ok && j < blocks; ++j) {
-      const bool last = j + 1 == blocks;
+    for (int j = 0; ok && j < n_blocks; ++j) {
+      const bool last = j + 1 == n_blocks;
+      const uint32_t id_next = id_of(j + 1);
+      const int steps = last ? n_last : kBlockKeys / 16;
       // The next keys come before this block's values.
-      int k_at = 0;
+      uint32_t k_at = 0;
       if (!last) {
-        ring_wait(place_of_k(j + 1));
+        next();
         k_at = at;
+        if (!wait(full0 + at * 8, parity)) break;
       }
-      if (!ring_wait(place_of_v(j, blocks)) || (last && dirty && !wait(&v_clean, 0))) break;
+      next();
+      if (!wait(full0 + at * 8, parity) || (last && clean_first && !wait(smem_u32(&v_clean), 0))) break;
       const uint32_t vb = ring_v + at * (Sh::SLOT >> 4);
-      const int steps = last ? (last_keys + 15) / 16 : kBlockKeys / 16;
 #pragma unroll
       for (int i = 0; i < NT; ++i) {
-        if (j < nb[i]) {
-          // P comes in halves of 64 keys.
-#pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            if (!wait(&p_full[i][half], j)) break;
-            tc_fence_after();
-#pragma unroll
-            for (int kk = half * 4; kk < half * 4 + 4; ++kk)
-              if (kk < steps)
-                mma_ts_if(tmem + i * 256 + 128, tmem + i * 256 + kk * 8, vb + kk * (2048 >> 4), id_o, j > 0 || kk > 0, issue);
-          }
-          if (ok && j + 1 == nb[i]) commit_if(smem_u32(&o_full[i]), issue);
-        }
-        if (ok && j + 1 < nb[i]) scores(i, j + 1, k_at);
+        if (j >= n_own[i]) continue;
+        // P comes in halves of 64 keys.
+        if (!wait(p0 + i * 16, j)) break;
+        tc_fence_after();
+        values(i, 0, vb, j == 0, steps);
+        if (!wait(p0 + i * 16 + 8, j)) break;
+        tc_fence_after();
+        values(i, 1, vb, j == 0, steps - 4);
+        if (j + 1 == n_own[i]) commit_if(smem_u32(&o_full[i]), issue);
+        else scores(i, k_at, id_next);
       }
       if (ok) {
-        commit_if(smem_u32(&empty[at]), issue);
-        if (!last) commit_if(smem_u32(&empty[k_at]), issue);
+        commit_if(empty0 + at * 8, issue);
+        if (!last) commit_if(empty0 + k_at * 8, issue);
       }
     }
     if (!ok && lane == 0) give_up(712);
