@@ -25,6 +25,7 @@ constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
 constexpr int kSortOneBlock = 8192;  // branches that one block sorts
 constexpr int kSortPiece = 2048;     // branches of a block otherwise, at least
 constexpr int kSortBlocks = 128;     // at most
+constexpr int kSortSteps = 8;
 
 struct SortArgs {
   const int32_t* experts;
@@ -67,13 +68,25 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const SortArgs
   const int each = (a.piece + kSortThreads - 1) / kSortThreads * 32;
   const int64_t wlo = lo + static_cast<int64_t>(warp) * each, whi = min(wlo + each, hi);
   int32_t* mine = next + warp * E;
-  for (int64_t i0 = wlo; i0 < whi; i0 += 32) {
-    const int64_t i = i0 + lane;
-    int e = i < whi ? a.experts[i] : -1;
-    if (static_cast<unsigned>(e) >= static_cast<unsigned>(E)) e = -1;
-    const uint32_t same = __match_any_sync(0xffffffffu, e);
-    if (e >= 0 && (same & before) == 0) mine[e] += __popc(same);
-    __syncwarp();
+  // kSortSteps steps' ids are loaded at once, and kept for the second walk where that is all of the piece.
+  int ids[kSortSteps];
+  const auto load = [&](int64_t i0) {
+#pragma unroll
+    for (int u = 0; u < kSortSteps; ++u) {
+      const int64_t i = i0 + u * 32 + lane;
+      ids[u] = i < whi ? a.experts[i] : -1;
+      if (static_cast<unsigned>(ids[u]) >= static_cast<unsigned>(E)) ids[u] = -1;
+    }
+  };
+  for (int64_t i0 = wlo; i0 < whi; i0 += 32 * kSortSteps) {
+    load(i0);
+#pragma unroll
+    for (int u = 0; u < kSortSteps; ++u) {
+      if (i0 + u * 32 >= whi) break;
+      const uint32_t same = __match_any_sync(0xffffffffu, ids[u]);
+      if (ids[u] >= 0 && (same & before) == 0) mine[ids[u]] += __popc(same);
+      __syncwarp();
+    }
   }
   __syncthreads();
   // Thread e < E: the warps' counts become offsets within the block, and the
@@ -114,20 +127,25 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const SortArgs
   }
   if (blockIdx.x == 0 && e == 0) a.offsets[E] = all;
   __syncthreads();
-  for (int64_t i0 = wlo; i0 < whi; i0 += 32) {
-    const int64_t i = i0 + lane;
-    int x = i < whi ? a.experts[i] : -1;
-    if (static_cast<unsigned>(x) >= static_cast<unsigned>(E)) x = -1;
-    const uint32_t same = __match_any_sync(0xffffffffu, x);
-    int row = -1;
-    if (x >= 0) row = mine[x] + __popc(same & before);
-    __syncwarp();
-    if (x >= 0 && (same & before) == 0) mine[x] += __popc(same);
-    __syncwarp();
-    if (i < whi) a.place[i] = row;
-    if (row >= 0) {
-      if (a.slot) a.slot[row] = static_cast<int>(i);
-      if (a.token) a.token[row] = static_cast<int>(i / a.k);
+  const bool kept = whi - wlo <= 32 * kSortSteps;
+  for (int64_t i0 = wlo; i0 < whi; i0 += 32 * kSortSteps) {
+    if (!kept) load(i0);
+#pragma unroll
+    for (int u = 0; u < kSortSteps; ++u) {
+      if (i0 + u * 32 >= whi) break;
+      const int64_t i = i0 + u * 32 + lane;
+      const int x = ids[u];
+      const uint32_t same = __match_any_sync(0xffffffffu, x);
+      int row = -1;
+      if (x >= 0) row = mine[x] + __popc(same & before);
+      __syncwarp();
+      if (x >= 0 && (same & before) == 0) mine[x] += __popc(same);
+      __syncwarp();
+      if (i < whi) a.place[i] = row;
+      if (row >= 0) {
+        if (a.slot) a.slot[row] = static_cast<int>(i);
+        if (a.token) a.token[row] = static_cast<int>(static_cast<uint32_t>(i) / static_cast<uint32_t>(a.k));
+      }
     }
   }
   // Behind the last row.
@@ -170,25 +188,19 @@ __device__ __forceinline__ int misalign(const T* p) {
   return static_cast<int>((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T));
 }
 
-// V values from p on, all of them inside their row.
+// The V values from p on, of which lo .. hi - 1 are inside their row; the others
+// are anything.  Unaligned ones are shifted into place from the aligned pieces
+// that hold values of the row (no other piece is read).
 template <typename T, bool ALIGNED>
-__device__ __forceinline__ uint4 load_unit(const T* p) {
-  if (ALIGNED) return *reinterpret_cast<const uint4*>(p);
+__device__ __forceinline__ uint4 load_unit(const T* p, int lo, int hi) {
   const uintptr_t at = reinterpret_cast<uintptr_t>(p);
-  const uint32_t m = at & 15;
+  if (ALIGNED) return *reinterpret_cast<const uint4*>(p);
+  const int m = static_cast<int>(at & 15);
   const uint4* piece = reinterpret_cast<const uint4*>(at - m);
-  const uint4 lo = piece[0];
-  return m ? shifted<T>(lo, piece[1], m) : lo;
-}
-// The same for a unit of which only values lo .. hi - 1 are inside the row; the others are zero.
-template <typename T>
-__device__ __forceinline__ uint4 load_part(const T* p, int lo, int hi) {
-  uint4 raw = make_uint4(0, 0, 0, 0);
-  T* v = reinterpret_cast<T*>(&raw);
-#pragma unroll
-  for (int i = 0; i < Elem<T>::kVec; ++i)
-    if (i >= lo && i < hi) v[i] = p[i];
-  return raw;
+  uint4 a = make_uint4(0, 0, 0, 0), b = a;
+  if (m + lo * static_cast<int>(sizeof(T)) < 16) a = piece[0];
+  if (m + hi * static_cast<int>(sizeof(T)) > 16) b = piece[1];
+  return shifted<T>(a, b, m);
 }
 template <typename T>
 __device__ __forceinline__ uint4 pack_unit(const float* f) {
@@ -211,7 +223,7 @@ struct Unit {
   }
   __device__ __forceinline__ bool any() const { return lo < hi; }
   __device__ __forceinline__ uint4 load(const T* row) const {
-    return whole ? load_unit<T, ALIGNED>(row + at) : load_part(row + at, lo, hi);
+    return load_unit<T, ALIGNED>(row + at, lo, hi);
   }
   __device__ __forceinline__ void store(T* row, const uint4& raw) const {
     if (whole) {
@@ -334,19 +346,20 @@ __global__ void __launch_bounds__(kRowThreads) expert_combine_kernel(const BackA
     for (int p = 0; p < a.k; p += CH) {
       uint4 raw[CH];
       float w[CH];
-      bool live[CH];
+      int r[CH];
 #pragma unroll
       for (int j = 0; j < CH; ++j) {
-        const int r = p + j < a.k ? a.place[s0 + p + j] : -1;
-        live[j] = r >= 0 && r < a.n_rows;
-        if (live[j]) {
-          raw[j] = unit.load(static_cast<const T*>(a.rows) + r * a.rows_stride);
-          w[j] = a.weights ? a.weights[s0 + p + j] : 1.f;
-        }
+        r[j] = p + j < a.k ? a.place[s0 + p + j] : -1;
+        w[j] = p + j < a.k && a.weights ? a.weights[s0 + p + j] : 1.f;
+      }
+#pragma unroll
+      for (int j = 0; j < CH; ++j) {
+        if (r[j] >= a.n_rows) r[j] = -1;
+        if (r[j] >= 0) raw[j] = unit.load(static_cast<const T*>(a.rows) + r[j] * a.rows_stride);
       }
 #pragma unroll
       for (int j = 0; j < CH; ++j)
-        if (live[j]) {
+        if (r[j] >= 0) {
           float h[V];
           unpack_vec(raw[j], h, static_cast<T*>(nullptr));
 #pragma unroll
@@ -413,7 +426,8 @@ __global__ void __launch_bounds__(kRowThreads) expert_grad_kernel(const GradArgs
           if (a.dweights) {
             unpack_vec(h[j], g, static_cast<T*>(nullptr));
 #pragma unroll
-            for (int i = 0; i < V; ++i) dot = fmaf(f[i], g[i], dot);
+            for (int i = 0; i < V; ++i)
+              if (unit.whole || (i >= unit.lo && i < unit.hi)) dot = fmaf(f[i], g[i], dot);
           }
           if (a.drows) {
 #pragma unroll
@@ -553,7 +567,9 @@ moeca_status moeca_expert_combine(const moeca_expert_combine_args* a, void* stre
       using E = std::remove_pointer_t<decltype(t)>;
       BackArgs k = d;
       k.units = row_units<E>(width, al.value);
-      return launch_pdl(a->n_slots <= 2 ? expert_combine_kernel<E, al.value, 2> : expert_combine_kernel<E, al.value, 4>,
+      return launch_pdl(a->n_slots <= 2   ? expert_combine_kernel<E, al.value, 2>
+                        : a->n_slots <= 4 ? expert_combine_kernel<E, al.value, 4>
+                                          : expert_combine_kernel<E, al.value, 8>,
                         row_grid(static_cast<int64_t>(T) * k.units), dim3(kRowThreads), 0,
                         static_cast<cudaStream_t>(stream), k);
     });

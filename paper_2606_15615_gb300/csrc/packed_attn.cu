@@ -186,48 +186,54 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_kernel(const PackedAtt
 }
 
 // ---------------------------------------------------------------------------
-// Join: a warp per (query, head).  With lse_j the chunks' base-2 logarithms and
-// m their maximum: o = sum_j 2^(lse_j - m) o_j / sum_j 2^(lse_j - m), chunk by chunk.
+// Join: a block per (query, head).  With lse_j the chunks' base-2 logarithms and
+// m their maximum: o = sum_j 2^(lse_j - m) o_j / sum_j 2^(lse_j - m).  Each of the
+// four warps adds every fourth chunk, and the four sums are added in their order:
+// the loads of many chunks are in flight at once (one warp for all of them took
+// 80 us for 171 chunks of 32 rows).
 // ---------------------------------------------------------------------------
-constexpr int kJoinThreads = 128;
+constexpr int kJoinThreads = 128, kJoinWarps = kJoinThreads / 32;
 
-template <typename T>
+template <typename T, int C>  // C: channels of a lane, 32 apart
 __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const PackedAttnArgs a) {
+  __shared__ float sh[kJoinWarps][32 * C];
   pdl_entry();
-  const int lane = threadIdx.x & 31;
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * (kJoinThreads / 32) + (threadIdx.x >> 5);
-  const int64_t t = row / a.q.heads;
-  const int h = static_cast<int>(row - t * a.q.heads);
-  if (t >= a.qs.total) return;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t t = blockIdx.x / a.q.heads;
+  const int h = static_cast<int>(blockIdx.x - t * a.q.heads);
   const int b = a.qs.owner(t);
   const int64_t i = t - a.qs.start(b);
   if (i < 0 || i >= min(a.qs.length(b), static_cast<int64_t>(a.max_q))) return;
   const int chunks = static_cast<int>((a.ks.length(b) + a.ks.unit - 1) / a.ks.unit);
-  const int64_t first = a.ks.base(b);
-  const auto at = [&](int j) { return ((first + j) * a.max_q + i) * a.q.heads + h; };
+  const int64_t first = (a.ks.base(b) * a.max_q + i) * a.q.heads + h, step = static_cast<int64_t>(a.max_q) * a.q.heads;
   float m = -INFINITY;
-  for (int j = lane; j < chunks; j += 32) m = fmaxf(m, a.part_lse[at(j)]);
+  for (int j = lane; j < chunks; j += 32) m = fmaxf(m, a.part_lse[first + j * step]);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
   const float ref = m == -INFINITY ? 0.f : m;
   float sum = 0.f;
-  for (int j = 0; j < chunks; ++j) sum += exp2f(a.part_lse[at(j)] - ref);
-  if (lane == 0 && a.lse) a.lse[t * a.q.heads + h] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * kLn2;
+  for (int j = lane; j < chunks; j += 32) sum += exp2f(a.part_lse[first + j * step] - ref);
+  sum = warp_sum(sum);
+  float o[C] = {};
+#pragma unroll 4
+  for (int j = warp; j < chunks; j += kJoinWarps) {
+    const float weight = exp2f(a.part_lse[first + j * step] - ref);
+    const float* part = a.part_o + (first + j * step) * a.dim;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+      if (c * 32 + lane < a.dim) o[c] = fmaf(weight, part[c * 32 + lane], o[c]);
+  }
+#pragma unroll
+  for (int c = 0; c < C; ++c) sh[warp][c * 32 + lane] = o[c];
+  __syncthreads();
+  if (threadIdx.x == 0 && a.lse) a.lse[t * a.q.heads + h] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * kLn2;
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   T* out = static_cast<T*>(a.out.data) + t * a.out.token_stride + h * a.out.head_stride;
-  for (int c0 = 0; c0 < a.dim; c0 += 128) {
-    float o[4] = {};
-    for (int j = 0; j < chunks; ++j) {
-      const float weight = exp2f(a.part_lse[at(j)] - ref);
-      if (weight == 0.f) continue;  // that chunk's o may be anything
-      const float* part = a.part_o + at(j) * a.dim + c0;
+  for (int c = threadIdx.x; c < a.dim; c += kJoinThreads) {
+    float v = 0.f;
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
-        if (c0 + c * 32 + lane < a.dim) o[c] = fmaf(weight, part[c * 32 + lane], o[c]);
-    }
-#pragma unroll
-    for (int c = 0; c < 4; ++c)
-      if (c0 + c * 32 + lane < a.dim) out[c0 + c * 32 + lane] = Elem<T>::from_f(o[c] * inv);
+    for (int u = 0; u < kJoinWarps; ++u) v += sh[u][c];
+    out[c] = Elem<T>::from_f(v * inv);
   }
 }
 
@@ -259,9 +265,10 @@ cudaError_t launch_attn_simt(const PackedAttnArgs& a, int dtype, int tile, cudaS
 }
 
 cudaError_t launch_attn_join(const PackedAttnArgs& a, int dtype, cudaStream_t s) {
-  const int64_t rows = a.qs.total * a.q.heads;
-  const dim3 grid(static_cast<unsigned>((rows + kJoinThreads / 32 - 1) / (kJoinThreads / 32)));
-  return launch_pdl(dtype == MOECA_BF16 ? attn_join_kernel<__nv_bfloat16> : attn_join_kernel<float>, grid, dim3(kJoinThreads), 0, s, a);
+  const dim3 grid(static_cast<unsigned>(a.qs.total * a.q.heads));
+  const auto run = [&](auto kernel) { return launch_pdl(kernel, grid, dim3(kJoinThreads), 0, s, a); };
+  if (dtype == MOECA_BF16) return run(a.dim <= 128 ? attn_join_kernel<__nv_bfloat16, 4> : attn_join_kernel<__nv_bfloat16, 8>);
+  return run(a.dim <= 128 ? attn_join_kernel<float, 4> : attn_join_kernel<float, 8>);
 }
 
 namespace {
@@ -271,7 +278,7 @@ constexpr int kMaxHeadDim = 256, kMaxSeqs = 1 << 20;
 constexpr int64_t kMaxWorkspace = int64_t(1) << 30;  // beyond, the key axis is not cut
 
 struct Plan {
-  int rows;           // tiles of 128 rows per block of the tensor-core kernel, 0: the CUDA-core kernel
+  int rows;           // tiles of 128 rows per block of the tensor-core kernel; 0: the CUDA-core kernel, -1: the one for few rows
   int tile;           // query tokens of a tile
   int chunk;          // keys of a chunk, 0: not cut
   int max_q, tiles;
@@ -310,12 +317,19 @@ Plan plan_attention(const moeca_attention_args& a) {
   int heads, fill, least;  // blocks of a tile, blocks that fill the GPU, keys of a chunk at least
   if (a.dtype == MOECA_BF16 && a.dim % 8 == 0 && a.dim <= 128 && group <= 128 && fits_tc(a.q, a.n_queries) &&
       fits_tc(a.k, a.n_keys) && fits_tc(a.v, a.n_keys) && fits_tc(a.out, a.n_queries)) {
-    const int each = 128 / group;
-    p.rows = p.max_q <= each ? 1 : 2;
-    p.tile = p.rows * each;
     heads = a.k.heads;
-    fill = kSms;
-    least = 512;
+    if (static_cast<int64_t>(p.max_q) * group <= 16) {
+      p.rows = -1;
+      p.tile = std::max(p.max_q, 1);
+      fill = 0;
+      least = 512;
+    } else {
+      const int each = 128 / group;
+      p.rows = p.max_q <= each ? 1 : 2;
+      p.tile = p.rows * each;
+      fill = kSms;
+      least = 512;
+    }
   } else {
     p.tile = p.max_q <= 16 ? 16 : 32;
     heads = a.q.heads;
@@ -326,9 +340,20 @@ Plan plan_attention(const moeca_attention_args& a) {
   p.tiles = (p.max_q + p.tile - 1) / p.tile;
   p.blocks = p.q_pieces * heads;
   // Few blocks with many keys each: the key axis is cut so that the chunks' blocks fill the GPU once.
-  if (p.blocks > 0 && 2 * p.blocks <= fill) {
-    const int64_t cuts = fill / p.blocks, mean = a.n_keys / a.n_seqs;
-    const int64_t chunk = std::max<int64_t>(least, ((mean + cuts - 1) / cuts + 127) / 128 * 128);
+  // For few rows, whose blocks are small, it is cut wherever a chunk is shorter than a sequence may be: into
+  // two blocks an SM (as many as run at once; four sequences of 131072 keys, 8 x 128, take 93 us, with six
+  // blocks an SM 98), and six of up to 64 channels (four run at once, and sequences of different lengths share
+  // the GPU more evenly: 64 sequences of 131072 keys, 8 x 64, take 54 us, with two 60).
+  if (p.blocks > 0 && (p.rows < 0 || 2 * p.blocks <= fill)) {
+    const int64_t mean = a.n_keys / a.n_seqs;
+    int64_t chunk;
+    if (p.rows < 0) {
+      chunk = a.n_keys * heads / ((a.dim <= 64 ? 6 : 2) * kSms);
+    } else {
+      const int64_t cuts = fill / p.blocks;
+      chunk = (mean + cuts - 1) / cuts;
+    }
+    chunk = std::max<int64_t>(least, (chunk + 127) / 128 * 128);
     const int64_t longest = a.k_offsets ? a.n_keys : mean;
     if (chunk < longest) {
       const int64_t n = pieces(a.k_offsets, a.n_keys, a.n_seqs, static_cast<int>(chunk), 0x7fffffff, &p.k_per);
@@ -423,7 +448,9 @@ moeca_status moeca_attention(const moeca_attention_args* a, void* stream) {
   d.status = a->status;
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   return launched([&] {
-    cudaError_t e = p.rows ? launch_attn_packed_tc(d, p.rows, s) : launch_attn_simt(d, a->dtype, p.tile, s);
+    cudaError_t e = p.rows > 0    ? launch_attn_packed_tc(d, p.rows, s)
+                    : p.rows < 0 ? launch_attn_rows(d, s)
+                                 : launch_attn_simt(d, a->dtype, p.tile, s);
     if (e == cudaSuccess && p.chunk) e = launch_attn_join(d, a->dtype, s);
     return e;
   });

@@ -142,6 +142,7 @@ __device__ __forceinline__ void clear_rest(const PackedAttnArgs& a) {
 cudaError_t launch_attn_simt(const PackedAttnArgs& a, int dtype, int tile, cudaStream_t s);
 // tiles: of 128 rows in a block, 1 or 2.
 cudaError_t launch_attn_packed_tc(const PackedAttnArgs& a, int tiles, cudaStream_t s);
+cudaError_t launch_attn_rows(const PackedAttnArgs& a, cudaStream_t s);
 cudaError_t launch_attn_join(const PackedAttnArgs& a, int dtype, cudaStream_t s);
 
 }  // namespace moeca

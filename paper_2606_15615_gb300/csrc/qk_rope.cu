@@ -28,27 +28,35 @@ struct QkArgs {
   bool table16;  // rows of the table can be read 16 bytes at a time
 };
 
+// W values of a head: as loaded, and in fp32.
 template <typename T, int W>
 struct Chunk {
-  float f[W];
+  static constexpr int WORDS = (W * sizeof(T) + 3) / 4;
+  uint32_t raw[WORDS];
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) raw[i] = 0;
+  }
   __device__ __forceinline__ void load(const T* p) {
     if constexpr (W * sizeof(T) == 16) {
-      load_vec(p, f);
+      const uint4 v = *reinterpret_cast<const uint4*>(p);
+      raw[0] = v.x; raw[1] = v.y; raw[2] = v.z; raw[3] = v.w;
     } else if constexpr (W * sizeof(T) == 8) {
       const uint2 v = *reinterpret_cast<const uint2*>(p);
-      if constexpr (sizeof(T) == 4) {
-        f[0] = __uint_as_float(v.x); f[1] = __uint_as_float(v.y);
-      } else {
-        const float2 a = __bfloat1622float2(reinterpret_cast<const __nv_bfloat162&>(v.x));
-        const float2 b = __bfloat1622float2(reinterpret_cast<const __nv_bfloat162&>(v.y));
-        f[0] = a.x; f[1] = a.y; f[2] = b.x; f[3] = b.y;
-      }
+      raw[0] = v.x; raw[1] = v.y;
+    } else if constexpr (sizeof(T) == 4) {
+      raw[0] = *reinterpret_cast<const uint32_t*>(p);
     } else {
-#pragma unroll
-      for (int i = 0; i < W; ++i) f[i] = Elem<T>::to_f(p[i]);
+      raw[0] = *reinterpret_cast<const uint16_t*>(p);
     }
   }
-  __device__ __forceinline__ void store(T* p) const {
+  __device__ __forceinline__ void get(float* f) const {
+#pragma unroll
+    for (int i = 0; i < W; ++i)
+      f[i] = sizeof(T) == 4 ? __uint_as_float(raw[i])
+                            : __uint_as_float(i & 1 ? raw[i / 2] & 0xffff0000u : raw[i / 2] << 16);  // bf16: the upper half
+  }
+  __device__ __forceinline__ static void store(T* p, const float* f) {
     if constexpr (W * sizeof(T) == 16) {
       store_vec(p, f);
     } else if constexpr (W * sizeof(T) == 8) {
@@ -61,8 +69,7 @@ struct Chunk {
       }
       *reinterpret_cast<uint2*>(p) = v;
     } else {
-#pragma unroll
-      for (int i = 0; i < W; ++i) p[i] = Elem<T>::from_f(f[i]);
+      p[0] = Elem<T>::from_f(f[0]);
     }
   }
 };
@@ -85,7 +92,7 @@ __device__ __forceinline__ float group_sum(float v, int lane, int n) {
 // weights in registers.  One pass: every value is read and written once, the table
 // comes from L1 / L2 but for the first token at a position.
 template <typename T, int W, int U, bool PAIRS>
-__global__ void __launch_bounds__(kQkThreads) qk_norm_rope_kernel(const QkArgs a) {
+__global__ void __launch_bounds__(kQkThreads, U == 1 ? 3 : 1) qk_norm_rope_kernel(const QkArgs a) {
   pdl_entry();
   const int warp_lane = threadIdx.x & 31, per_warp = 32 / a.lanes;
   const int in_warp = warp_lane / a.lanes, lane = warp_lane - in_warp * a.lanes;
@@ -129,24 +136,32 @@ __global__ void __launch_bounds__(kQkThreads) qk_norm_rope_kernel(const QkArgs a
     }
   }
   float weight[U][2][W];
+  const int heads = a.q.heads + a.k.heads;
+  Chunk<T, W> next[U][2];
+  const auto fetch = [&](int h) {
+    const bool live = on && h < heads, is_q = h < a.q.heads;
+    const T* x = static_cast<const T*>(is_q ? a.q.data : a.k.data) + t * (is_q ? a.q.token_stride : a.k.token_stride) +
+                 (is_q ? h * a.q.head_stride : (h - a.q.heads) * a.k.head_stride);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      next[u][0].clear();
+      next[u][1].clear();
+      if (live && lo[u] < a.dim) next[u][0].load(x + lo[u]);
+      if (live && hi[u] < a.dim) next[u][1].load(x + hi[u]);
+    }
+  };
+  fetch(part * a.per);
   // Every lane of the warp takes the same number of rounds: the sums are shuffles of whole warps.
   for (int i = 0; i < a.per; ++i) {
     const int h = part * a.per + i;
-    const bool is_q = h < a.q.heads;
-    const bool live = on && h < a.q.heads + a.k.heads;
-    const int hh = is_q ? h : h - a.q.heads;
-    const T* x = static_cast<const T*>(is_q ? a.q.data : a.k.data) + t * (is_q ? a.q.token_stride : a.k.token_stride) +
-                 hh * (is_q ? a.q.head_stride : a.k.head_stride);
-    T* y = static_cast<T*>(is_q ? a.q_out.data : a.k_out.data) +
-           t * (is_q ? a.q_out.token_stride : a.k_out.token_stride) + hh * (is_q ? a.q_out.head_stride : a.k_out.head_stride);
-    Chunk<T, W> c[U][2];
+    const bool is_q = h < a.q.heads, live = on && h < heads;
+    float c[U][2][W];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-#pragma unroll
-      for (int j = 0; j < W; ++j) c[u][0].f[j] = c[u][1].f[j] = 0.f;
-      if (live && lo[u] < a.dim) c[u][0].load(x + lo[u]);
-      if (live && hi[u] < a.dim) c[u][1].load(x + hi[u]);
+      next[u][0].get(c[u][0]);
+      next[u][1].get(c[u][1]);
     }
+    if (i + 1 < a.per) fetch(h + 1);  // in flight while this head is worked on
     if (i == 0 || h == a.q.heads) {
       const float* w = is_q ? a.q_weight : a.k_weight;
 #pragma unroll
@@ -162,16 +177,18 @@ __global__ void __launch_bounds__(kQkThreads) qk_norm_rope_kernel(const QkArgs a
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int j = 0; j < W; ++j)
-        sum = fmaf(c[u][0].f[j], c[u][0].f[j], fmaf(c[u][1].f[j], c[u][1].f[j], sum));
+      for (int j = 0; j < W; ++j) sum = fmaf(c[u][0][j], c[u][0][j], fmaf(c[u][1][j], c[u][1][j], sum));
     sum = group_sum(sum, lane, a.lanes);
     const float r = 1.f / sqrtf(sum / static_cast<float>(a.dim) + a.eps);
+    T* y = static_cast<T*>(is_q ? a.q_out.data : a.k_out.data) +
+           t * (is_q ? a.q_out.token_stride : a.k_out.token_stride) +
+           (is_q ? h * a.q_out.head_stride : (h - a.q.heads) * a.k_out.head_stride);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
 #pragma unroll
       for (int e = 0; e < 2; ++e)
 #pragma unroll
-        for (int j = 0; j < W; ++j) c[u][e].f[j] = c[u][e].f[j] * r * weight[u][e][j];
+        for (int j = 0; j < W; ++j) c[u][e][j] = c[u][e][j] * r * weight[u][e][j];
       if (lane + u * a.lanes < turned) {
         if (PAIRS && W > 1) {
 #pragma unroll
@@ -179,22 +196,22 @@ __global__ void __launch_bounds__(kQkThreads) qk_norm_rope_kernel(const QkArgs a
 #pragma unroll
             for (int j = 0; j + 1 < W; j += 2) {
               const float2 cs = turn[u][(e * W + j) / 2];
-              const float p = c[u][e].f[j], q = c[u][e].f[j + 1];
-              c[u][e].f[j] = p * cs.x - q * cs.y;
-              c[u][e].f[j + 1] = q * cs.x + p * cs.y;
+              const float p = c[u][e][j], q = c[u][e][j + 1];
+              c[u][e][j] = p * cs.x - q * cs.y;
+              c[u][e][j + 1] = q * cs.x + p * cs.y;
             }
         } else {
 #pragma unroll
           for (int j = 0; j < W; ++j) {
             const float2 cs = turn[u][j];
-            const float p = c[u][0].f[j], q = c[u][1].f[j];
-            c[u][0].f[j] = p * cs.x - q * cs.y;
-            c[u][1].f[j] = q * cs.x + p * cs.y;
+            const float p = c[u][0][j], q = c[u][1][j];
+            c[u][0][j] = p * cs.x - q * cs.y;
+            c[u][1][j] = q * cs.x + p * cs.y;
           }
         }
       }
-      if (live && lo[u] < a.dim) c[u][0].store(y + lo[u]);
-      if (live && hi[u] < a.dim) c[u][1].store(y + hi[u]);
+      if (live && lo[u] < a.dim) Chunk<T, W>::store(y + lo[u], c[u][0]);
+      if (live && hi[u] < a.dim) Chunk<T, W>::store(y + hi[u], c[u][1]);
     }
   }
 }
