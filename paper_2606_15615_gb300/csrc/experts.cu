@@ -175,11 +175,10 @@ cudaError_t launch_sort(SortArgs a, cudaStream_t s) {
 }
 
 // ---------------------------------------------------------------------------
-// Rows.  All three kernels move rows in units of 16 bytes, a unit of a written
-// row per thread; the written row's own 16-byte boundaries cut the units, so that
-// rows of any alignment go out in whole sectors (the first and last unit of an
-// unaligned row may be partial: value by value).  What is read is shifted into
-// place from the aligned pieces that hold it.
+// Rows.  All three kernels move rows in units of 16 bytes; the written row's own
+// 16-byte boundaries cut the units, so that rows of any alignment go out in whole
+// sectors (the first and last unit of an unaligned row may be partial: value by
+// value).  What is read is shifted into place from the aligned pieces that hold it.
 // ---------------------------------------------------------------------------
 constexpr int kRowThreads = 256;
 
@@ -277,42 +276,77 @@ __device__ __forceinline__ void clear_tail(T* rows, int64_t stride, int64_t n_ro
   }
 }
 
+// Work of a group of L lanes: a token and a segment of its units, J of them a lane.  A lane below k holds the place (and weight) of the token's branch;
+// branches without a row are passed over by the whole group.
+struct Segments {
+  int units, segs, per;  // units of a row, its segments, units of a segment
+};
+Segments segments(int units, int lanes, int j) {
+  const int segs = (units + j * lanes - 1) / (j * lanes);
+  return {units, segs, (units + segs - 1) / segs};
+}
+
+template <int L>
+struct Group {
+  uint32_t mask, live;  // lanes of the group; branches that have a row
+  int lane, place;
+  __device__ __forceinline__ Group() {
+    lane = threadIdx.x & (L - 1);
+    mask = L == 32 ? 0xffffffffu : ((1u << (L & 31)) - 1) << (threadIdx.x & 31 & ~(L - 1));
+  }
+  __device__ __forceinline__ void load(const int32_t* places, int k, int64_t n_rows) {
+    place = lane < k ? places[lane] : -1;
+    if (place >= n_rows) place = -1;
+    live = __ballot_sync(mask, place >= 0) >> (threadIdx.x & 31 & ~(L - 1));
+    if (L < 32) live &= (1u << (L & 31)) - 1;
+  }
+  template <typename V>
+  __device__ __forceinline__ V from(V v, int p) const {
+    return __shfl_sync(mask, v, p, L);
+  }
+};
+
 struct RowsArgs {
   const void* x;
   int64_t x_stride;
   void* rows;
   int64_t rows_stride, n_rows;
   const int32_t *place, *count;
-  int T, k, width, units;
+  int T, k, width;
+  Segments seg;
 };
 
-// x is read once and written to its k rows.  Unaligned rows start at k different
-// boundaries: there a unit belongs to a branch, and x comes from L1 or L2 again.
-template <typename T, bool ALIGNED>
+// x is read once and written to its rows (unaligned rows start at boundaries of
+// their own: x then comes from L1 again for each).
+constexpr int kRowsUnits = 2;
+
+template <typename T, bool ALIGNED, int L>
 __global__ void __launch_bounds__(kRowThreads) expert_rows_kernel(const RowsArgs a) {
+  constexpr int J = kRowsUnits;
   pdl_entry();
-  const int64_t items = ALIGNED ? a.T : static_cast<int64_t>(a.T) * a.k;
-  const int64_t blocks = (items * a.units + kRowThreads - 1) / kRowThreads;
-  for (int64_t b = blockIdx.x; b < blocks; b += gridDim.x) {
-    const Item it(b, a.units);
-    if (it.row >= items) break;
+  Group<L> g;
+  const int64_t tasks = static_cast<int64_t>(a.T) * a.seg.segs, step = static_cast<int64_t>(gridDim.x) * (kRowThreads / L);
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * (kRowThreads / L) + threadIdx.x / L; i < tasks; i += step) {
+    const int64_t t = i < 0x7fffffff ? static_cast<uint32_t>(i) / static_cast<uint32_t>(a.seg.segs) : i / a.seg.segs;
+    const int u0 = static_cast<int>(i - t * a.seg.segs) * a.seg.per, end = min(u0 + a.seg.per, a.seg.units);
+    const T* x = static_cast<const T*>(a.x) + t * a.x_stride;
+    uint4 raw[J];
     if (ALIGNED) {
-      const T* x = static_cast<const T*>(a.x) + it.row * a.x_stride;
-      const Unit<T, true> unit(it.u, x, a.width);
-      const uint4 raw = unit.load(x);
-      for (int p = 0; p < a.k; ++p) {
-        const int r = a.place[it.row * a.k + p];
-        if (static_cast<unsigned>(r) < a.n_rows) unit.store(static_cast<T*>(a.rows) + r * a.rows_stride, raw);
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+        if (u0 + g.lane + j * L < end) raw[j] = Unit<T, true>(u0 + g.lane + j * L, x, a.width).load(x);
+    }
+    g.load(a.place + t * a.k, a.k, a.n_rows);
+    for (uint32_t live = g.live; live; live &= live - 1) {
+      T* row = static_cast<T*>(a.rows) + static_cast<int64_t>(g.from(g.place, __ffs(live) - 1)) * a.rows_stride;
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        const Unit<T, ALIGNED> unit(u0 + g.lane + j * L, row, a.width);
+        if (u0 + g.lane + j * L < end && unit.any()) unit.store(row, ALIGNED ? raw[j] : unit.load(x));
       }
-    } else {
-      const int r = a.place[it.row];
-      if (static_cast<unsigned>(r) >= a.n_rows) continue;
-      T* row = static_cast<T*>(a.rows) + r * a.rows_stride;
-      const Unit<T, false> unit(it.u, row, a.width);
-      if (unit.any()) unit.store(row, unit.load(static_cast<const T*>(a.x) + it.row / a.k * a.x_stride));
     }
   }
-  clear_tail<T, ALIGNED>(static_cast<T*>(a.rows), a.rows_stride, a.n_rows, a.count, a.units, a.width);
+  clear_tail<T, ALIGNED>(static_cast<T*>(a.rows), a.rows_stride, a.n_rows, a.count, a.seg.units, a.width);
 }
 
 struct BackArgs {
@@ -324,55 +358,80 @@ struct BackArgs {
   int64_t x_stride;
   void* out;
   int64_t out_stride;
-  int T, k, width, units;
+  int T, k, width;
+  Segments seg;
 };
 
-// A thread per unit of the result, CH branches' loads in flight.
-template <typename T, bool ALIGNED, int CH>
-__global__ void __launch_bounds__(kRowThreads) expert_combine_kernel(const BackArgs a) {
+// A lane's loads in flight are those of CH branches for its J units; the rest of
+// what HBM needs is other warps', so registers are held down.  32768 tokens with
+// 8 slots of 1152 (bf16): four branches of one unit and five blocks an SM 128 us, with
+// what the compiler takes (three blocks, two units) 232, eight branches of one unit on four blocks 145.  4096
+// tokens with two of 2560: two branches of two units on four blocks 11.9 us, of one unit on six 13.0.
+template <typename T, bool ALIGNED, int L, int CH, int J>
+__global__ void __launch_bounds__(kRowThreads, CH == 2 ? 4 : ALIGNED ? 5 : 6) expert_combine_kernel(const BackArgs a) {
   constexpr int V = Elem<T>::kVec;
   pdl_entry();
-  const int64_t blocks = (static_cast<int64_t>(a.T) * a.units + kRowThreads - 1) / kRowThreads;
-  for (int64_t b = blockIdx.x; b < blocks; b += gridDim.x) {
-    const Item it(b, a.units);
-    if (it.row >= a.T) break;
-    T* out = static_cast<T*>(a.out) + it.row * a.out_stride;
-    const Unit<T, ALIGNED> unit(it.u, out, a.width);
-    if (!unit.any()) continue;
-    uint4 own = make_uint4(0, 0, 0, 0);
-    if (a.x) own = unit.load(static_cast<const T*>(a.x) + it.row * a.x_stride);
-    float sum[V] = {};
-    const int64_t s0 = it.row * a.k;
-    for (int p = 0; p < a.k; p += CH) {
-      uint4 raw[CH];
+  Group<L> g;
+  const int64_t tasks = static_cast<int64_t>(a.T) * a.seg.segs, step = static_cast<int64_t>(gridDim.x) * (kRowThreads / L);
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * (kRowThreads / L) + threadIdx.x / L; i < tasks; i += step) {
+    const int64_t t = i < 0x7fffffff ? static_cast<uint32_t>(i) / static_cast<uint32_t>(a.seg.segs) : i / a.seg.segs;
+    const int u0 = static_cast<int>(i - t * a.seg.segs) * a.seg.per, end = min(u0 + a.seg.per, a.seg.units);
+    T* out = static_cast<T*>(a.out) + t * a.out_stride;
+    g.load(a.place + t * a.k, a.k, a.n_rows);
+    const float weight = a.weights && g.lane < a.k ? a.weights[t * a.k + g.lane] : 1.f;
+    bool on[J];
+    uint4 own[J];
+    float sum[J][V];
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const Unit<T, ALIGNED> unit(u0 + g.lane + j * L, out, a.width);
+      on[j] = u0 + g.lane + j * L < end && unit.any();
+      if (a.x && on[j]) own[j] = unit.load(static_cast<const T*>(a.x) + t * a.x_stride);
+#pragma unroll
+      for (int v = 0; v < V; ++v) sum[j][v] = 0.f;
+    }
+    for (uint32_t live = g.live; live;) {
+      uint4 raw[CH][J];
       float w[CH];
       int r[CH];
 #pragma unroll
-      for (int j = 0; j < CH; ++j) {
-        r[j] = p + j < a.k ? a.place[s0 + p + j] : -1;
-        w[j] = p + j < a.k && a.weights ? a.weights[s0 + p + j] : 1.f;
+      for (int c = 0; c < CH; ++c) {
+        r[c] = -1;
+        if (live) {
+          const int p = __ffs(live) - 1;
+          live &= live - 1;
+          r[c] = g.from(g.place, p);
+          w[c] = g.from(weight, p);
+          const T* row = static_cast<const T*>(a.rows) + r[c] * a.rows_stride;
+#pragma unroll
+          for (int j = 0; j < J; ++j)
+            if (on[j]) raw[c][j] = Unit<T, ALIGNED>(u0 + g.lane + j * L, out, a.width).load(row);
+        }
       }
 #pragma unroll
-      for (int j = 0; j < CH; ++j) {
-        if (r[j] >= a.n_rows) r[j] = -1;
-        if (r[j] >= 0) raw[j] = unit.load(static_cast<const T*>(a.rows) + r[j] * a.rows_stride);
-      }
+      for (int c = 0; c < CH; ++c)
+        if (r[c] >= 0) {
 #pragma unroll
-      for (int j = 0; j < CH; ++j)
-        if (r[j] >= 0) {
-          float h[V];
-          unpack_vec(raw[j], h, static_cast<T*>(nullptr));
+          for (int j = 0; j < J; ++j) {
+            if (!on[j]) continue;
+            float h[V];
+            unpack_vec(raw[c][j], h, static_cast<T*>(nullptr));
 #pragma unroll
-          for (int i = 0; i < V; ++i) sum[i] = fmaf(w[j], h[i], sum[i]);
+            for (int v = 0; v < V; ++v) sum[j][v] = fmaf(w[c], h[v], sum[j][v]);
+          }
         }
     }
-    if (a.x) {
-      float f[V];
-      unpack_vec(own, f, static_cast<T*>(nullptr));
 #pragma unroll
-      for (int i = 0; i < V; ++i) sum[i] += f[i];
+    for (int j = 0; j < J; ++j) {
+      if (!on[j]) continue;
+      if (a.x) {
+        float f[V];
+        unpack_vec(own[j], f, static_cast<T*>(nullptr));
+#pragma unroll
+        for (int v = 0; v < V; ++v) sum[j][v] += f[v];
+      }
+      Unit<T, ALIGNED>(u0 + g.lane + j * L, out, a.width).store(out, pack_unit<T>(sum[j]));
     }
-    unit.store(out, pack_unit<T>(sum));
   }
 }
 
@@ -392,9 +451,13 @@ struct GradArgs {
 
 // A warp per branch: dout's row (from L1 or L2 but for the token's first branch)
 // scaled into the gradient's row, and multiplied with the branch's row.
+// As in the combine, warps are worth more than registers: 8191 tokens with 8
+// slots of 768 (fp32) with two units a lane on five blocks an SM 106 us (both
+// gradients), four on what the compiler takes 121; 20011 tokens with 3 unaligned slots of 1001
+// (bf16) with one unit on six blocks 128 us, two on five 138, four 172.
 template <typename T, bool ALIGNED>
-__global__ void __launch_bounds__(kRowThreads) expert_grad_kernel(const GradArgs a) {
-  constexpr int V = Elem<T>::kVec, J = 4;
+__global__ void __launch_bounds__(kRowThreads, ALIGNED ? 5 : 6) expert_grad_kernel(const GradArgs a) {
+  constexpr int V = Elem<T>::kVec, J = ALIGNED ? 2 : 1;
   pdl_entry();
   const int lane = threadIdx.x & 31;
   const int64_t n = static_cast<int64_t>(a.T) * a.k, step = static_cast<int64_t>(gridDim.x) * (kRowThreads / 32);
@@ -461,6 +524,12 @@ cudaError_t pick(int dtype, bool aligned, F f) {
   return aligned ? f(static_cast<float*>(nullptr), std::true_type()) : f(static_cast<float*>(nullptr), std::false_type());
 }
 
+// f(std::integral_constant<lanes>): half a warp a token where a row has no more units.
+template <typename F>
+cudaError_t by_group(int units, F f) {
+  return units <= 16 ? f(std::integral_constant<int, 16>()) : f(std::integral_constant<int, 32>());
+}
+
 const char* bad_branches(int n_tokens, int n_slots) {
   if (n_tokens < 0 || n_slots < 1 || n_slots > kMaxSlots) return "n_tokens >= 0 and 1 <= n_slots <= 16";
   if (static_cast<int64_t>(n_tokens) * n_slots > kMaxBranches) return "more than 2^30 branches";
@@ -525,17 +594,19 @@ moeca_status moeca_expert_rows(const moeca_expert_rows_args* a, void* stream) {
   const Range read[] = {rows_range(a->x, T, a->x_stride * es, width * es), {a->place, 4 * slots}, {a->count, 4}};
   if (any_overlap(written, read)) return refuse("rows overlaps another buffer of the call");
   if (a->n_rows == 0 || (T == 0 && !a->count)) return MOECA_OK;
-  const RowsArgs d{a->x, a->x_stride, a->rows, a->rows_stride, a->n_rows, a->place, a->count, T, a->n_slots, width, 0};
   const bool aligned = aligned16(a->x, a->x_stride, a->dtype) && aligned16(a->rows, a->rows_stride, a->dtype);
   return launched([&] {
     return pick(a->dtype, aligned, [&](auto* t, auto al) {
       using E = std::remove_pointer_t<decltype(t)>;
-      RowsArgs k = d;
-      k.units = row_units<E>(width, al.value);
-      // The tail of an empty batch is cleared by as many threads as its units need.
-      const int64_t items = T == 0 ? a->n_rows : al.value ? T : slots;
-      return launch_pdl(expert_rows_kernel<E, al.value>, row_grid(items * k.units), dim3(kRowThreads), 0,
-                        static_cast<cudaStream_t>(stream), k);
+      const int units = row_units<E>(width, al.value);
+      return by_group(units, [&](auto lanes) {
+        const RowsArgs d{a->x, a->x_stride, a->rows, a->rows_stride, a->n_rows, a->place, a->count, T, a->n_slots, width,
+                         segments(units, lanes.value, kRowsUnits)};
+        // The tail of an empty batch is cleared by as many threads as its units need.
+        const int64_t threads = T == 0 ? a->n_rows * units : static_cast<int64_t>(T) * d.seg.segs * lanes.value;
+        return launch_pdl(expert_rows_kernel<E, al.value, lanes.value>, row_grid(threads), dim3(kRowThreads), 0,
+                          static_cast<cudaStream_t>(stream), d);
+      });
     });
   });
 }
@@ -557,21 +628,22 @@ moeca_status moeca_expert_combine(const moeca_expert_combine_args* a, void* stre
                         {a->weights, 4 * slots}, rows_range(in_place ? nullptr : a->x, T, a->x_stride * es, width * es)};
   if (any_overlap(written, read)) return refuse("out overlaps another buffer of the call");
   if (T == 0) return MOECA_OK;
-  const BackArgs d{a->rows, a->rows_stride, a->n_rows, a->place, a->weights, a->x, a->x_stride,
-                      a->out, a->out_stride, T, a->n_slots, width, 0};
   const bool aligned = aligned16(a->out, a->out_stride, a->dtype) &&
                        (a->n_rows == 0 || aligned16(a->rows, a->rows_stride, a->dtype)) &&
                        (!a->x || aligned16(a->x, a->x_stride, a->dtype));
   return launched([&] {
     return pick(a->dtype, aligned, [&](auto* t, auto al) {
       using E = std::remove_pointer_t<decltype(t)>;
-      BackArgs k = d;
-      k.units = row_units<E>(width, al.value);
-      return launch_pdl(a->n_slots <= 2   ? expert_combine_kernel<E, al.value, 2>
-                        : a->n_slots <= 4 ? expert_combine_kernel<E, al.value, 4>
-                                          : expert_combine_kernel<E, al.value, 8>,
-                        row_grid(static_cast<int64_t>(T) * k.units), dim3(kRowThreads), 0,
-                        static_cast<cudaStream_t>(stream), k);
+      const int units = row_units<E>(width, al.value);
+      return by_group(units, [&](auto lanes) {
+        constexpr int L = lanes.value;
+        const bool two = a->n_slots <= 2;
+        const BackArgs d{a->rows, a->rows_stride, a->n_rows, a->place, a->weights, a->x, a->x_stride,
+                         a->out, a->out_stride, T, a->n_slots, width, segments(units, L, two ? 2 : 1)};
+        return launch_pdl(two ? expert_combine_kernel<E, al.value, L, 2, 2> : expert_combine_kernel<E, al.value, L, 4, 1>,
+                          row_grid(static_cast<int64_t>(T) * d.seg.segs * L), dim3(kRowThreads), 0,
+                          static_cast<cudaStream_t>(stream), d);
+      });
     });
   });
 }

@@ -12,7 +12,7 @@ namespace {
 constexpr int kQkThreads = 256;
 constexpr int kMaxDim = 512;
 constexpr int kQkGroups = 32768;   // groups of lanes from which on a group takes several heads
-constexpr int kQkMostHeads = 4;
+constexpr int kQkMostHeads = 8;
 
 struct QkArgs {
   Heads q, k, q_out, k_out;
@@ -24,8 +24,8 @@ struct QkArgs {
   int lanes;   // lanes that share a head: its units, at most 32
   int per;     // heads that a group of lanes takes one after another
   int parts;   // groups per token
-  float eps;
-  bool table16;  // rows of the table can be read 16 bytes at a time
+  float eps, inv_dim;
+  bool table16, weight16;  // rows of the table, the weights' chunks can be read 16 bytes at a time
 };
 
 // W values of a head: as loaded, and in fp32.
@@ -89,10 +89,14 @@ __device__ __forceinline__ float group_sum(float v, int lane, int n) {
 // turned (rot .. dim - 1) is cut into units of neighbouring chunks either way.
 // A group of `lanes` lanes takes the units of one head, U units a lane, and works
 // through `per` heads of its token with the token's cosines and sines and the
-// weights in registers.  One pass: every value is read and written once, the table
+// weights in registers: up to eight (16384 tokens of 20 + 4 heads of 128, rot 96
+// in pairs: 47 us; with four 50, with two 69, as table and weights are loaded for
+// each group).  The next head is loaded while one is worked on.  Blocks an SM: three
+// with chunks of eight values (four spill: 55 us), five with four (16384 tokens
+// of 32 heads of 72: 44 us, with three 51).  One pass: every value is read and written once, the table
 // comes from L1 / L2 but for the first token at a position.
 template <typename T, int W, int U, bool PAIRS>
-__global__ void __launch_bounds__(kQkThreads, U == 1 ? 3 : 1) qk_norm_rope_kernel(const QkArgs a) {
+__global__ void __launch_bounds__(kQkThreads, U > 1 ? 1 : W == 8 ? 3 : 5) qk_norm_rope_kernel(const QkArgs a) {
   pdl_entry();
   const int warp_lane = threadIdx.x & 31, per_warp = 32 / a.lanes;
   const int in_warp = warp_lane / a.lanes, lane = warp_lane - in_warp * a.lanes;
@@ -138,10 +142,18 @@ __global__ void __launch_bounds__(kQkThreads, U == 1 ? 3 : 1) qk_norm_rope_kerne
   float weight[U][2][W];
   const int heads = a.q.heads + a.k.heads;
   Chunk<T, W> next[U][2];
+  // Where the next head to fetch and the one to write lie; the first key follows the last query.
+  const int h0 = part * a.per;
+  const bool from_q = h0 < a.q.heads;
+  const int64_t hh = from_q ? h0 : h0 - a.q.heads;
+  const T* x = static_cast<const T*>(from_q ? a.q.data : a.k.data) +
+               (from_q ? t * a.q.token_stride + hh * a.q.head_stride : t * a.k.token_stride + hh * a.k.head_stride);
+  T* y = static_cast<T*>(from_q ? a.q_out.data : a.k_out.data) +
+         (from_q ? t * a.q_out.token_stride + hh * a.q_out.head_stride : t * a.k_out.token_stride + hh * a.k_out.head_stride);
   const auto fetch = [&](int h) {
-    const bool live = on && h < heads, is_q = h < a.q.heads;
-    const T* x = static_cast<const T*>(is_q ? a.q.data : a.k.data) + t * (is_q ? a.q.token_stride : a.k.token_stride) +
-                 (is_q ? h * a.q.head_stride : (h - a.q.heads) * a.k.head_stride);
+    const bool live = on && h < heads;
+    if (h > h0) x = h == a.q.heads ? static_cast<const T*>(a.k.data) + t * a.k.token_stride
+                                   : x + (h < a.q.heads ? a.q.head_stride : a.k.head_stride);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       next[u][0].clear();
@@ -150,11 +162,13 @@ __global__ void __launch_bounds__(kQkThreads, U == 1 ? 3 : 1) qk_norm_rope_kerne
       if (live && hi[u] < a.dim) next[u][1].load(x + hi[u]);
     }
   };
-  fetch(part * a.per);
+  fetch(h0);
   // Every lane of the warp takes the same number of rounds: the sums are shuffles of whole warps.
   for (int i = 0; i < a.per; ++i) {
-    const int h = part * a.per + i;
+    const int h = h0 + i;
     const bool is_q = h < a.q.heads, live = on && h < heads;
+    if (i > 0) y = h == a.q.heads ? static_cast<T*>(a.k_out.data) + t * a.k_out.token_stride
+                                  : y + (is_q ? a.q_out.head_stride : a.k_out.head_stride);
     float c[U][2][W];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -170,7 +184,16 @@ __global__ void __launch_bounds__(kQkThreads, U == 1 ? 3 : 1) qk_norm_rope_kerne
         for (int e = 0; e < 2; ++e) {
           const int at = e ? hi[u] : lo[u];
 #pragma unroll
-          for (int j = 0; j < W; ++j) weight[u][e][j] = w && live && at < a.dim ? w[at + j] : 1.f;
+          for (int j = 0; j < W; ++j) weight[u][e][j] = 1.f;
+          if (w && live && at < a.dim) {
+            if (W >= 4 && a.weight16) {
+#pragma unroll
+              for (int j = 0; j + 3 < W; j += 4) load_vec(w + at + j, weight[u][e] + j);
+            } else {
+#pragma unroll
+              for (int j = 0; j < W; ++j) weight[u][e][j] = w[at + j];
+            }
+          }
         }
     }
     float sum = 0.f;
@@ -179,10 +202,7 @@ __global__ void __launch_bounds__(kQkThreads, U == 1 ? 3 : 1) qk_norm_rope_kerne
 #pragma unroll
       for (int j = 0; j < W; ++j) sum = fmaf(c[u][0][j], c[u][0][j], fmaf(c[u][1][j], c[u][1][j], sum));
     sum = group_sum(sum, lane, a.lanes);
-    const float r = 1.f / sqrtf(sum / static_cast<float>(a.dim) + a.eps);
-    T* y = static_cast<T*>(is_q ? a.q_out.data : a.k_out.data) +
-           t * (is_q ? a.q_out.token_stride : a.k_out.token_stride) +
-           (is_q ? h * a.q_out.head_stride : (h - a.q.heads) * a.k_out.head_stride);
+    const float r = rsqrtf(fmaf(sum, a.inv_dim, a.eps));
 #pragma unroll
     for (int u = 0; u < U; ++u) {
 #pragma unroll
@@ -279,7 +299,7 @@ extern "C" moeca_status moeca_qk_norm_rope(const moeca_qk_norm_rope_args* a, voi
   d.q_weight = a->q_weight; d.k_weight = a->k_weight;
   d.table = reinterpret_cast<const float2*>(a->table);
   d.pos = a->pos; d.n_pos = a->n_positions;
-  d.T = a->n_tokens; d.dim = dim; d.rot = a->rot; d.eps = a->eps;
+  d.T = a->n_tokens; d.dim = dim; d.rot = a->rot; d.eps = a->eps; d.inv_dim = 1.f / static_cast<float>(dim);
   // Chunks of 16 bytes, of 8, or single values.
   int w = static_cast<int>(16 / es);
   const auto fits = [&](int n) {
@@ -288,6 +308,7 @@ extern "C" moeca_status moeca_qk_norm_rope(const moeca_qk_norm_rope_args* a, voi
   };
   if (!fits(w)) w = fits(w / 2) ? w / 2 : 1;
   d.table16 = addr(a->table) % 16 == 0 && a->rot % 4 == 0;
+  d.weight16 = addr(a->q_weight) % 16 == 0 && addr(a->k_weight) % 16 == 0 && a->rot / 2 % 4 == 0 && a->rot % 4 == 0;
   const int units = a->rot / (2 * w) + (dim - a->rot + 2 * w - 1) / (2 * w), heads = a->q.heads + a->k.heads;
   d.lanes = std::min(units, 32);
   d.per = static_cast<int>(std::clamp<int64_t>(T * heads / kQkGroups, 1, kQkMostHeads));
