@@ -67,8 +67,7 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_kernel(const PackedAtt
   constexpr int R = BQ / 16;
   extern __shared__ float4 smem4[];
   pdl_entry();
-  const int64_t index = blockIdx.x / a.q.heads;
-  const int h = static_cast<int>(blockIdx.x - index * a.q.heads);
+  const int index = blockIdx.x / static_cast<uint32_t>(a.q.heads), h = blockIdx.x - index * a.q.heads;
   const AttnWork w = attn_work(a, index);
   clear_rest<T>(a);
   if (!w.any) return;
@@ -79,9 +78,9 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_kernel(const PackedAtt
   float* sp = sv + kSimtKeys * pitch;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   const int rows = min(BQ, min(w.nq, a.max_q) - w.row0);
-  const T* q = static_cast<const T*>(a.q.data) + (w.q0 + w.row0) * a.q.token_stride + h * a.q.head_stride;
-  const T* k = static_cast<const T*>(a.k.data) + w.k0 * a.k.token_stride + h / a.group * a.k.head_stride;
-  const T* v = static_cast<const T*>(a.v.data) + w.k0 * a.v.token_stride + h / a.group * a.v.head_stride;
+  const T* q = static_cast<const T*>(a.q.data) + static_cast<int64_t>(w.q0 + w.row0) * a.q.token_stride + h * a.q.head_stride;
+  const T* k = static_cast<const T*>(a.k.data) + static_cast<int64_t>(w.k0) * a.k.token_stride + h / a.group * a.k.head_stride;
+  const T* v = static_cast<const T*>(a.v.data) + static_cast<int64_t>(w.k0) * a.v.token_stride + h / a.group * a.v.head_stride;
   load_rows(sq, pitch, q, a.q.token_stride, BQ, rows, dim, vec);
   float m[R], l[R], o[R][DC][4];
   int see[R];
@@ -166,7 +165,7 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_kernel(const PackedAtt
     const float inv = l[r] == 0.f ? 0.f : 1.f / l[r];
     const float lse2 = l[r] == 0.f ? -INFINITY : m[r] + log2f(l[r]);
     if (a.ks.unit) {
-      const int64_t at = (w.piece * a.max_q + i) * a.q.heads + h;
+      const int64_t at = (static_cast<int64_t>(w.piece) * a.max_q + i) * a.q.heads + h;
       if (tx == 0) a.part_lse[at] = lse2;
 #pragma unroll
       for (int c = 0; c < DC; ++c)
@@ -174,8 +173,8 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_kernel(const PackedAtt
         for (int j = 0; j < 4; ++j)
           if (c * 64 + tx * 4 + j < dim) a.part_o[at * dim + c * 64 + tx * 4 + j] = o[r][c][j] * inv;
     } else {
-      if (tx == 0 && a.lse) a.lse[(w.q0 + i) * a.q.heads + h] = lse2 * kLn2;
-      T* out = static_cast<T*>(a.out.data) + (w.q0 + i) * a.out.token_stride + h * a.out.head_stride;
+      if (tx == 0 && a.lse) a.lse[static_cast<int64_t>(w.q0 + i) * a.q.heads + h] = lse2 * kLn2;
+      T* out = static_cast<T*>(a.out.data) + static_cast<int64_t>(w.q0 + i) * a.out.token_stride + h * a.out.head_stride;
 #pragma unroll
       for (int c = 0; c < DC; ++c)
 #pragma unroll
@@ -199,13 +198,11 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const PackedAtt
   __shared__ float sh[kJoinWarps][32 * C];
   pdl_entry();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int64_t t = blockIdx.x / a.q.heads;
-  const int h = static_cast<int>(blockIdx.x - t * a.q.heads);
-  const int b = a.qs.owner(t);
-  const int64_t i = t - a.qs.start(b);
-  if (i < 0 || i >= min(a.qs.length(b), static_cast<int64_t>(a.max_q))) return;
-  const int chunks = static_cast<int>((a.ks.length(b) + a.ks.unit - 1) / a.ks.unit);
-  const int64_t first = (a.ks.base(b) * a.max_q + i) * a.q.heads + h, step = static_cast<int64_t>(a.max_q) * a.q.heads;
+  const int t = blockIdx.x / static_cast<uint32_t>(a.q.heads), h = blockIdx.x - t * a.q.heads;
+  const int b = a.qs.owner(t), i = t - a.qs.start(b);
+  if (i < 0 || i >= min(a.qs.length(b), a.max_q)) return;
+  const int chunks = static_cast<int>((static_cast<uint32_t>(a.ks.length(b)) + a.ks.unit - 1) / a.ks.unit);
+  const int64_t first = (static_cast<int64_t>(a.ks.base(b)) * a.max_q + i) * a.q.heads + h, step = static_cast<int64_t>(a.max_q) * a.q.heads;
   float m = -INFINITY;
   for (int j = lane; j < chunks; j += 32) m = fmaxf(m, a.part_lse[first + j * step]);
 #pragma unroll
@@ -226,7 +223,7 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const PackedAtt
 #pragma unroll
   for (int c = 0; c < C; ++c) sh[warp][c * 32 + lane] = o[c];
   __syncthreads();
-  if (threadIdx.x == 0 && a.lse) a.lse[t * a.q.heads + h] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * kLn2;
+  if (threadIdx.x == 0 && a.lse) a.lse[static_cast<int64_t>(t) * a.q.heads + h] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * kLn2;
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   T* out = static_cast<T*>(a.out.data) + t * a.out.token_stride + h * a.out.head_stride;
   for (int c = threadIdx.x; c < a.dim; c += kJoinThreads) {
@@ -265,7 +262,7 @@ cudaError_t launch_attn_simt(const PackedAttnArgs& a, int dtype, int tile, cudaS
 }
 
 cudaError_t launch_attn_join(const PackedAttnArgs& a, int dtype, cudaStream_t s) {
-  const dim3 grid(static_cast<unsigned>(a.qs.total * a.q.heads));
+  const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(a.qs.total) * a.q.heads));
   const auto run = [&](auto kernel) { return launch_pdl(kernel, grid, dim3(kJoinThreads), 0, s, a); };
   if (dtype == MOECA_BF16) return run(a.dim <= 128 ? attn_join_kernel<__nv_bfloat16, 4> : attn_join_kernel<__nv_bfloat16, 8>);
   return run(a.dim <= 128 ? attn_join_kernel<float, 4> : attn_join_kernel<float, 8>);
@@ -327,7 +324,7 @@ Plan plan_attention(const moeca_attention_args& a) {
       const int each = 128 / group;
       p.rows = p.max_q <= each ? 1 : 2;
       p.tile = p.rows * each;
-      fill = kSms;
+      fill = p.rows == 1 ? 2 * kSms : kSms;
       least = 512;
     }
   } else {
@@ -435,8 +432,8 @@ moeca_status moeca_attention(const moeca_attention_args* a, void* stream) {
   }
   PackedAttnArgs d{};
   d.q = device_heads(a->q); d.k = device_heads(a->k); d.v = device_heads(a->v); d.out = device_heads(a->out);
-  d.qs = {a->q_offsets, nq, a->n_seqs, p.tile, p.q_per};
-  d.ks = {a->k_offsets, nk, a->n_seqs, p.chunk, p.k_per};
+  d.qs = {a->q_offsets, static_cast<int>(nq), a->n_seqs, static_cast<int>(nq / a->n_seqs), p.tile, p.q_per};
+  d.ks = {a->k_offsets, static_cast<int>(nk), a->n_seqs, static_cast<int>(nk / a->n_seqs), p.chunk, p.k_per};
   d.q_pieces = p.q_pieces; d.k_pieces = p.k_pieces;
   d.lse = a->lse;
   d.part_lse = static_cast<float*>(a->workspace);

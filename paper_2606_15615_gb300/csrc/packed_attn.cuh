@@ -17,49 +17,44 @@ namespace moeca {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-// The sequences' share of the tokens, and their pieces of `unit` tokens, numbered through.
+// The sequences' share of the tokens, and their pieces of `unit` tokens, numbered
+// through.  Tokens and pieces are counted in 32 bits (the call takes 2^30 tokens at
+// most): index arithmetic is a sizeable part of a short sequence's time.
 struct Seqs {
-  const int32_t* off;  // [n + 1], or null: total / n tokens each
-  int64_t total;
-  int n;
+  const int32_t* off;  // [n + 1], or null: `each` tokens each
+  int total, n, each;
   int unit;
   int per;  // pieces of each sequence, or 0: sequence b's begin at off[b] / unit + b
 
-  __device__ __forceinline__ int64_t start(int b) const {
-    if (!off) return b * (total / n);
-    return min(max(static_cast<int64_t>(off[b]), int64_t(0)), total);
+  __device__ __forceinline__ int start(int b) const { return off ? min(max(off[b], 0), total) : b * each; }
+  __device__ __forceinline__ int length(int b) const { return off ? max(start(b + 1) - start(b), 0) : each; }
+  __device__ __forceinline__ int base(int b) const {
+    return per ? b * per : static_cast<int>(static_cast<uint32_t>(start(b)) / static_cast<uint32_t>(unit)) + b;
   }
-  __device__ __forceinline__ int64_t length(int b) const { return max(start(b + 1) - start(b), int64_t(0)); }
-  __device__ __forceinline__ int64_t base(int b) const {
-    return per ? static_cast<int64_t>(b) * per : start(b) / unit + b;
-  }
-  // The sequence whose piece `p` is (all lanes of a warp; the same answer in all):
-  // the last one whose pieces begin at p or before, found 32 sequences at a time.
-  // ceil(len / unit) pieces fit before the next sequence's, wherever it begins.
-  __device__ __forceinline__ int find(int64_t p) const {
-    if (per) return static_cast<int>(p / per);
+  // The last sequence with value(b) <= p, found 32 sequences at a time (all lanes of
+  // a warp; the same answer in all).
+  template <typename F>
+  __device__ __forceinline__ int last(int p, F value) const {
     int lo = 0, hi = n;
     while (hi - lo > 1) {
       const int step = (hi - lo + 31) / 32, b = lo + static_cast<int>(threadIdx.x & 31) * step;
-      const uint32_t ok = __ballot_sync(0xffffffffu, b < hi && base(b) <= p);
+      const uint32_t ok = __ballot_sync(0xffffffffu, b < hi && value(b) <= p);
       const int count = __ffs(~ok) - 1;  // lanes 0 .. count - 1 hold; -1: all 32
       lo += max((count < 0 ? 32 : count) - 1, 0) * step;
       hi = min(lo + step, hi);
     }
     return lo;
   }
-  // The sequence of a token (as find, for pieces of one token).
-  __device__ __forceinline__ int owner(int64_t t) const {
-    if (!off) return static_cast<int>(min(t / (total / n), static_cast<int64_t>(n - 1)));
-    int lo = 0, hi = n;
-    while (hi - lo > 1) {
-      const int step = (hi - lo + 31) / 32, b = lo + static_cast<int>(threadIdx.x & 31) * step;
-      const uint32_t ok = __ballot_sync(0xffffffffu, b < hi && start(b) <= t);
-      const int count = __ffs(~ok) - 1;
-      lo += max((count < 0 ? 32 : count) - 1, 0) * step;
-      hi = min(lo + step, hi);
-    }
-    return lo;
+  // The sequence whose piece `p` is.  ceil(len / unit) pieces fit before the next
+  // sequence's, wherever it begins.
+  __device__ __forceinline__ int find(int p) const {
+    if (per) return static_cast<int>(static_cast<uint32_t>(p) / static_cast<uint32_t>(per));
+    return last(p, [this](int b) { return base(b); });
+  }
+  // The sequence of a token.
+  __device__ __forceinline__ int owner(int t) const {
+    if (!off) return min(static_cast<int>(static_cast<uint32_t>(t) / static_cast<uint32_t>(max(each, 1))), n - 1);
+    return last(t, [this](int b) { return start(b); });
   }
 };
 
@@ -82,45 +77,46 @@ struct PackedAttnArgs {
 
 // One block's work.
 struct AttnWork {
-  int64_t q0, k0;        // first tokens of the sequence
+  int q0, k0;            // first tokens of the sequence
   int nq, nk;            // its queries (of which the first max_q count) and keys
   int row0;              // first query of the tile
   int key_lo, key_hi;    // keys of the chunk
-  int64_t piece;         // the chunk's number
+  int piece;             // the chunk's number
   bool any;              // whether the tile and the chunk exist
 };
 // index: the tile (no chunks), or chunk x tiles + tile.  All lanes of a warp.
-__device__ __forceinline__ AttnWork attn_work(const PackedAttnArgs& a, int64_t index) {
+__device__ __forceinline__ AttnWork attn_work(const PackedAttnArgs& a, int index) {
   AttnWork w;
-  int b;
+  int b, tile;
   if (a.ks.unit == 0) {
     b = a.qs.find(index);
-    w.row0 = static_cast<int>(min((index - a.qs.base(b)) * a.qs.unit, int64_t(0x7fffffff)));
+    tile = index - a.qs.base(b);
     w.piece = 0;
   } else {
-    w.piece = index / a.tiles;
+    w.piece = static_cast<int>(static_cast<uint32_t>(index) / static_cast<uint32_t>(a.tiles));
     b = a.ks.find(w.piece);
-    w.row0 = static_cast<int>((index - w.piece * a.tiles) * a.qs.unit);
+    tile = index - w.piece * a.tiles;
   }
   w.q0 = a.qs.start(b);
   w.k0 = a.ks.start(b);
-  w.nq = static_cast<int>(a.qs.length(b));
-  w.nk = static_cast<int>(a.ks.length(b));
-  w.any = w.row0 >= 0 && w.row0 < min(w.nq, a.max_q);
+  w.nq = a.qs.length(b);
+  w.nk = a.ks.length(b);
+  const int64_t row0 = static_cast<int64_t>(tile) * a.qs.unit;
+  w.any = row0 >= 0 && row0 < min(w.nq, a.max_q);
+  w.row0 = w.any ? static_cast<int>(row0) : 0;
   w.key_lo = 0;
   w.key_hi = w.nk;
   if (a.ks.unit) {
-    const int64_t j = w.piece - a.ks.base(b);
-    w.any = w.any && j >= 0 && j * a.ks.unit < w.nk;
-    w.key_lo = w.any ? static_cast<int>(j * a.ks.unit) : 0;
-    w.key_hi = w.any ? static_cast<int>(min(static_cast<int64_t>(w.key_lo) + a.ks.unit, static_cast<int64_t>(w.nk))) : 0;
+    const int64_t lo = static_cast<int64_t>(w.piece - a.ks.base(b)) * a.ks.unit;
+    w.any = w.any && lo >= 0 && lo < w.nk;
+    w.key_lo = w.any ? static_cast<int>(lo) : 0;
+    w.key_hi = w.any ? min(w.key_lo + a.ks.unit, w.nk) : 0;
   }
   return w;
 }
 // Keys that query i of the sequence sees: 0 .. visible - 1.
 __device__ __forceinline__ int visible_keys(const PackedAttnArgs& a, const AttnWork& w, int i) {
-  return a.causal ? static_cast<int>(min(max(static_cast<int64_t>(i) + 1 + w.nk - w.nq, int64_t(0)), static_cast<int64_t>(w.nk)))
-                  : w.nk;
+  return a.causal ? min(max(i + 1 - w.nq + w.nk, 0), w.nk) : w.nk;
 }
 
 // Query tokens before the first and behind the last sequence become 0, the blocks
@@ -128,7 +124,7 @@ __device__ __forceinline__ int visible_keys(const PackedAttnArgs& a, const AttnW
 template <typename T>
 __device__ __forceinline__ void clear_rest(const PackedAttnArgs& a) {
   if (!a.clear || !a.qs.off) return;
-  const int64_t lo = a.qs.start(0), hi = max(a.qs.start(a.qs.n), lo), rest = lo + a.qs.total - hi;
+  const int lo = a.qs.start(0), hi = max(a.qs.start(a.qs.n), lo), rest = lo + a.qs.total - hi;
   for (int64_t r = blockIdx.x; r < rest; r += gridDim.x) {
     const int64_t t = r < lo ? r : hi + (r - lo);
     T* out = static_cast<T*>(a.out.data) + t * a.out.token_stride;

@@ -55,8 +55,7 @@ __global__ void __launch_bounds__(kRowsThreads, DK <= 4 ? 4 : 2) attn_rows_kerne
   __shared__ float sh_m[kRowsWarps][16], sh_l[kRowsWarps][16];
   pdl_entry();
   clear_rest<__nv_bfloat16>(a);
-  const int64_t index = blockIdx.x / a.k.heads;
-  const int kvh = static_cast<int>(blockIdx.x - index * a.k.heads);
+  const int index = blockIdx.x / static_cast<uint32_t>(a.k.heads), kvh = blockIdx.x - index * a.k.heads;
   const AttnWork w = attn_work(a, index);
   if (!w.any) return;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -69,8 +68,8 @@ __global__ void __launch_bounds__(kRowsThreads, DK <= 4 ? 4 : 2) attn_rows_kerne
     const int row = i / (2 * DK - chunks), c = chunks + i - row * (2 * DK - chunks);
     *reinterpret_cast<uint4*>(ring + row * Sh::PITCH + c * 16) = make_uint4(0, 0, 0, 0);
   }
-  const __nv_bfloat16* k = static_cast<const __nv_bfloat16*>(a.k.data) + w.k0 * a.k.token_stride + kvh * a.k.head_stride;
-  const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(a.v.data) + w.k0 * a.v.token_stride + kvh * a.v.head_stride;
+  const __nv_bfloat16* k = static_cast<const __nv_bfloat16*>(a.k.data) + static_cast<int64_t>(w.k0) * a.k.token_stride + kvh * a.k.head_stride;
+  const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(a.v.data) + static_cast<int64_t>(w.k0) * a.v.token_stride + kvh * a.v.head_stride;
   // The last query sees the most.
   const int end = min(w.key_hi, visible_keys(a, w, n_q - 1));
   const int tiles = (max(end - w.key_lo, 0) + kRowsKeys - 1) / kRowsKeys;
@@ -99,7 +98,7 @@ __global__ void __launch_bounds__(kRowsThreads, DK <= 4 ? 4 : 2) attn_rows_kerne
   for (int h = 0; h < 2; ++h) {
     const int r = lane / 4 + 8 * h, i = min(r, rows - 1) / G, g = min(r, rows - 1) - i * G;
     see[h] = min(visible_keys(a, w, i), w.key_hi);
-    const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q.data) + (w.q0 + i) * a.q.token_stride + (kvh * G + g) * a.q.head_stride;
+    const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q.data) + static_cast<int64_t>(w.q0 + i) * a.q.token_stride + (kvh * G + g) * a.q.head_stride;
 #pragma unroll
     for (int kk = 0; kk < DK; ++kk)
 #pragma unroll
@@ -218,13 +217,13 @@ __global__ void __launch_bounds__(kRowsThreads, DK <= 4 ? 4 : 2) attn_rows_kerne
     const int q_i = r / G, head = kvh * G + r - q_i * G;
     const float lse2 = sum == 0.f ? -INFINITY : top + log2f(sum);
     if (a.ks.unit) {
-      const int64_t part = (w.piece * a.max_q + q_i) * a.q.heads + head;
+      const int64_t part = (static_cast<int64_t>(w.piece) * a.max_q + q_i) * a.q.heads + head;
       if (c == 0) a.part_lse[part] = lse2;
       store_vec(a.part_o + part * a.dim + c, f);
       store_vec(a.part_o + part * a.dim + c + 4, f + 4);
     } else {
-      if (c == 0 && a.lse) a.lse[(w.q0 + q_i) * a.q.heads + head] = lse2 * kLn2;
-      store_vec(static_cast<__nv_bfloat16*>(a.out.data) + (w.q0 + q_i) * a.out.token_stride + head * a.out.head_stride + c, f);
+      if (c == 0 && a.lse) a.lse[static_cast<int64_t>(w.q0 + q_i) * a.q.heads + head] = lse2 * kLn2;
+      store_vec(static_cast<__nv_bfloat16*>(a.out.data) + static_cast<int64_t>(w.q0 + q_i) * a.out.token_stride + head * a.out.head_stride + c, f);
     }
   }
 }

@@ -39,14 +39,15 @@ constexpr int kTileRows = 128;               // rows of a tile (MMA M)
 constexpr int kBlockKeys = 128;              // keys of a block
 constexpr int kPart = 128 * 128;             // bytes of 128 rows x 64 channels
 constexpr int kMaxStages = 8;
-constexpr size_t kSmemMost = 227 * 1024 - 2048;  // less the static part
+// Shared memory of a block less the static part: two blocks an SM with one tile, one with two.
+constexpr size_t smem_most(int tiles) { return tiles == 1 ? 227 * 1024 / 2 - 3072 : 227 * 1024 - 2048; }
 
 template <int DK, int NT>  // DK: 16-channel steps of a head
 struct TcShape {
   static constexpr int DP = DK * 16;
   static constexpr int SUBS = (DP + 63) / 64;
   static constexpr int SLOT = SUBS * kPart;    // a tile of queries, a block of keys or of values
-  static constexpr int STAGES_FIT = static_cast<int>((kSmemMost - 1024 - NT * SLOT) / SLOT);
+  static constexpr int STAGES_FIT = static_cast<int>((smem_most(NT) - 1024 - NT * SLOT) / SLOT);
   static constexpr int STAGES = STAGES_FIT < kMaxStages ? STAGES_FIT : kMaxStages;
   static constexpr size_t SMEM = static_cast<size_t>(NT + STAGES) * SLOT + 1024;
   static constexpr int COLUMNS = 256 * NT;     // TMEM
@@ -119,7 +120,7 @@ __device__ __forceinline__ bool warp_wait_here(uint32_t bar, uint32_t parity, vo
 __device__ __forceinline__ int place_of_v(int j, int blocks) { return j + 1 < blocks ? 2 * j + 2 : 2 * j + 1; }
 
 template <int DK, int NT>
-__global__ void __launch_bounds__(64 + 128 * NT, 1)
+__global__ void __launch_bounds__(64 + 128 * NT, NT == 1 ? 2 : 1)
     attn_packed_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
                           const __grid_constant__ CUtensorMap vmap, const PackedAttnArgs a) {
   using Sh = TcShape<DK, NT>;
@@ -151,13 +152,17 @@ __global__ void __launch_bounds__(64 + 128 * NT, 1)
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
+  if (threadIdx.x == 32) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&qmap)) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&kmap)) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&vmap)) : "memory");
+  }
+  __syncthreads();
   pdl_entry();
   clear_rest<__nv_bfloat16>(a);
   // The heaviest tiles of a causal sequence are its last: they start first.
-  const int64_t pieces = gridDim.x / a.k.heads;
-  const int64_t turn = blockIdx.x / a.k.heads;
-  const int kvh = static_cast<int>(blockIdx.x - turn * a.k.heads);
-  const AttnWork w = attn_work(a, a.causal && !a.ks.unit ? pieces - 1 - turn : turn);
+  const int turn = blockIdx.x / static_cast<uint32_t>(a.k.heads), kvh = blockIdx.x - turn * a.k.heads;
+  const AttnWork w = attn_work(a, a.causal && !a.ks.unit ? static_cast<int>(a.q_pieces) - 1 - turn : turn);
   if (!w.any) return;  // uniform over the CTA, before TMEM is taken
   const int G = a.group, per_tile = a.qs.unit / NT;  // queries of a tile
   const int n_q = min(w.nq, a.max_q);
@@ -172,16 +177,20 @@ __global__ void __launch_bounds__(64 + 128 * NT, 1)
   // Keys of the last block, in 16s, and whether foreign value rows are among them.
   const int last_keys = min(kBlockKeys, w.key_hi - (w.key_lo + (blocks - 1) * kBlockKeys));
   const bool dirty = blocks > 0 && last_keys % 16 != 0;
-  if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_sh)),
-                 "r"(Sh::COLUMNS)
-                 : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-    tc_fence_before();
+  // TMEM's address is waited for by the warps that use it; the copies start beside.
+  uint32_t tmem = 0;
+  if (warp != 0) {
+    if (warp == 1) {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_sh)),
+                   "r"(Sh::COLUMNS)
+                   : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+      tc_fence_before();
+    }
+    asm volatile("bar.sync 1, %0;" ::"n"(Sh::THREADS - 32) : "memory");
+    tc_fence_after();
+    tmem = tmem_sh;
   }
-  __syncthreads();
-  tc_fence_after();
-  const uint32_t tmem = tmem_sh;
   const auto give_up = [&](int where) {
     if (!abort_flag) report_status(a.status, MOECA_ERR_TIMEOUT, where);
     abort_flag = 1;
@@ -189,7 +198,7 @@ __global__ void __launch_bounds__(64 + 128 * NT, 1)
 
   if (warp == 0) {
     if (lane == 0) {
-      const int token = static_cast<int>(w.q0) + w.row0;
+      const int token = w.q0 + w.row0;
 #pragma unroll
       for (int i = 0; i < NT; ++i)
         if (nb[i] > 0) {
@@ -210,7 +219,7 @@ __global__ void __launch_bounds__(64 + 128 * NT, 1)
         mbar_expect_tx(bar, Sh::SLOT);
         for (int c = 0; c < Sh::SUBS; ++c)
           tma_load_heads(smem_u32(ring + s * Sh::SLOT + c * kPart), map, c * 64, kvh,
-                         static_cast<int>(w.k0) + w.key_lo + block * kBlockKeys, bar);
+                         w.k0 + w.key_lo + block * kBlockKeys, bar);
         ++n;
       };
       if (blocks > 0) fill(&kmap, 0);
@@ -410,30 +419,32 @@ __global__ void __launch_bounds__(64 + 128 * NT, 1)
       const float inv = l == 0.f ? 0.f : 1.f / l;
       const float lse2 = l == 0.f ? -INFINITY : m * sc + log2f(l);
       const bool cut = a.ks.unit != 0;
-      const int64_t part = (w.piece * a.max_q + query) * a.q.heads + head;
-      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out.data) + (w.q0 + query) * a.out.token_stride + head * a.out.head_stride;
+      const int64_t part = (static_cast<int64_t>(w.piece) * a.max_q + query) * a.q.heads + head;
+      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out.data) + static_cast<int64_t>(w.q0 + query) * a.out.token_stride + head * a.out.head_stride;
       float* part_o = a.part_o + part * a.dim;
       if (live) {
         if (cut) a.part_lse[part] = lse2;
-        else if (a.lse) a.lse[(w.q0 + query) * a.q.heads + head] = lse2 * kLn2;
+        else if (a.lse) a.lse[static_cast<int64_t>(w.q0 + query) * a.q.heads + head] = lse2 * kLn2;
       }
+      uint32_t v[DK][16] = {};
+      if (own_blocks > 0) {  // every lane: the loads are warp-collective
 #pragma unroll
-      for (int c = 0; c < DK; ++c) {
-        uint32_t v[16] = {};
-        if (own_blocks > 0) tmem_ld16(t_o + c * 16, v);  // every lane: the load is warp-collective
-        float f[16];
+        for (int c = 0; c < DK; ++c) tmem_ld16_async(t_o + c * 16, v[c]);
 #pragma unroll
-        for (int q = 0; q < 16; ++q) f[q] = __uint_as_float(v[q]) * inv;
-        if (!live) continue;
+        for (int c = 0; c < DK; ++c) tmem_wait16(v[c]);
+      }
+      if (live) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int at = c * 16 + h * 8;
+        for (int at = 0; at < Sh::DP; at += 8) {
           if (at >= a.dim) continue;
+          float f[8];
+#pragma unroll
+          for (int q = 0; q < 8; ++q) f[q] = __uint_as_float(v[at / 16][at % 16 + q]) * inv;
           if (cut) {
-            store_vec(part_o + at, f + h * 8);
-            store_vec(part_o + at + 4, f + h * 8 + 4);
+            store_vec(part_o + at, f);
+            store_vec(part_o + at + 4, f + 4);
           } else {
-            store_vec(out + at, f + h * 8);
+            store_vec(out + at, f);
           }
         }
       }
@@ -475,7 +486,7 @@ bool encode_heads(CUtensorMap* m, const Heads& h, int64_t tokens, int dim, int h
 template <int DK, int NT>
 cudaError_t run(const PackedAttnArgs& a, cudaStream_t s) {
   using Sh = TcShape<DK, NT>;
-  static_assert(Sh::STAGES >= 4, "a ring that holds two blocks of keys and of values");
+  static_assert(Sh::STAGES >= 2, "keys of a block beside the values of the one before");
   CUtensorMap qm, km, vm;
   // Without keys nothing is loaded; the maps still want a tensor.
   const Heads& k = a.ks.total > 0 ? a.k : a.q;
