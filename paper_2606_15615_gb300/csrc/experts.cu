@@ -22,8 +22,8 @@ constexpr int64_t kMaxBranches = 1 << 30;
 // counts of the blocks before it.  No atomic's order shows in a result.
 // ---------------------------------------------------------------------------
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
-constexpr int kSortOneBlock = 8192;  // branches that one block sorts
-constexpr int kSortPiece = 2048;     // branches of a block otherwise, at least
+constexpr int kSortOneBlock = 2048;  // branches that one block sorts
+constexpr int kSortPiece = 1024;     // branches of a block otherwise, at least
 constexpr int kSortBlocks = 128;     // at most
 constexpr int kSortSteps = 8;
 
