@@ -32,7 +32,8 @@ typedef struct {
  * and the first `rot` values of y are turned by the token's row of the table,
  *   (a, b) -> (a cos - b sin, b cos + a sin),
  * pair i being (y[i], y[i + rot / 2]), or (y[2 i], y[2 i + 1]) with `pairs`.
- * All in fp32, rounded once.  A token whose position is outside
+ * All in fp32, rounded once; heads whose sum of squares passes fp32's largest value
+ * become 0.  A token whose position is outside
  * [0, n_positions) is left out: nothing is written for it.  q_out and k_out may
  * be q and k themselves (same base and strides).  With rot = 0 positions are not
  * looked at. */

@@ -298,9 +298,11 @@ int64_t pieces(const int32_t* off, int64_t total, int n, int unit, int most, int
   return packed;
 }
 
-// Whether the tensor-core kernel can take the heads: pieces of 16 bytes everywhere.
+// Whether the tensor-core kernels can take the heads: pieces of 16 bytes everywhere, and
+// strides that a tensor map takes (one value for several tokens or heads, stride 0, is none).
 bool fits_tc(const moeca_heads& h, int64_t tokens) {
-  return tokens == 0 || (addr(h.data) % 16 == 0 && (tokens == 1 || h.token_stride % 8 == 0) && (h.heads == 1 || h.head_stride % 8 == 0));
+  const auto stride = [](int64_t s, int64_t n) { return n == 1 || (s > 0 && s % 8 == 0 && s < (int64_t(1) << 38)); };
+  return tokens == 0 || (addr(h.data) % 16 == 0 && stride(h.token_stride, tokens) && stride(h.head_stride, h.heads));
 }
 
 constexpr int kSms = 152;

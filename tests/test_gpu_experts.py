@@ -270,3 +270,20 @@ def test_results_repeat(M):
         now = (*plan, rows, M.expert_combine(rows, plan, w), *M.expert_combine_grad(x, rows, plan, w))
         first = first or now
         assert all(torch.equal(u, v) for u, v in zip(first, now))
+
+
+def test_rows_beyond_32_bits(M):
+    """Rows 16400 values apart: the last lie 2.4e9 values into their buffer."""
+    T, D, stride = 147_000, 24, 16_400
+    e = torch.from_numpy(ids(9, T, 1, 3)).cuda()
+    plan = M.expert_sort(e, 3)
+    x, w = values(3, T, D, "bf16"), torch.rand(T, 1, device="cuda")
+    want = M.expert_rows(x, plan)
+    buf = torch.empty(T * stride, dtype=torch.bfloat16, device="cuda")
+    far = buf.as_strided((T, D), (stride, 1), 0)
+    assert torch.equal(M.expert_rows(x, plan, out=far), want)
+    assert torch.equal(M.expert_combine(far, plan, w), M.expert_combine(want, plan, w))
+    got, want = M.expert_combine_grad(x, far, plan, w), M.expert_combine_grad(x, want, plan, w)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    far.copy_(x)
+    assert torch.equal(M.expert_rows(far, plan), M.expert_rows(x, plan))

@@ -372,3 +372,29 @@ def test_attention_captured_twice_and_side_by_side(M, q_n):
         res.append(last)
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(res, want))
+
+
+@pytest.mark.parametrize("q_n", [1, 200])
+def test_keys_beyond_32_bits(M, q_n):
+    """Tokens 16400 values apart: the last keys lie 2.4e9 values into their buffer."""
+    n, stride = 147_000, 16_400
+    q, k, v = qkv(30, q_n, n, 1, 1, 64, "bf16")
+    buf = torch.empty(n * stride, dtype=torch.bfloat16, device="cuda")
+    kf, vf = (buf.as_strided((n, 1, 64), (stride, 64, 1), at) for at in (0, 8192))
+    kf.copy_(k)
+    vf.copy_(v)
+    off = [1000, n - 1000 - 300, 300]
+    args = dict(q_offsets=offsets([0, 0, q_n]), k_offsets=offsets(off), causal=True)
+    assert torch.equal(M.attention(q, kf, vf, **args), M.attention(q, k, v, **args))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("q_n", [1, 40])
+def test_one_key_head_expanded(M, q_n, dtype):
+    """Heads and tokens that share their memory (stride 0)."""
+    q, k, v = qkv(31, q_n, 700, 4, 1, 64, dtype)
+    want = check(M, q, k, v, [q_n], [700], True)
+    got = check(M, q, k.expand(-1, 4, -1), v.expand(-1, 4, -1), [q_n], [700], True)
+    assert got.shape == want.shape
+    check(M, q[:1].expand(q_n, -1, -1), k, v, [q_n], [700])
+    check(M, q, k[:1].expand(700, -1, -1), v, [q_n], [700])
