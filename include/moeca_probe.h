@@ -16,7 +16,8 @@
  * library's kernels on a GPU they do not have to themselves.
  *
  * moeca_probe_q8_stall lets a bounded wait of the 8-bit calls run out, so that
- * tests see what a caller sees then.
+ * tests see what a caller sees then; moeca_probe_attention_stall one of the
+ * packed attention's.
  */
 #ifndef MOECA_PROBE_H_
 #define MOECA_PROBE_H_
@@ -88,6 +89,17 @@ typedef enum {
   MOECA_Q8_NONE = 0, MOECA_Q8_COPIES = 1, MOECA_Q8_OPERANDS = 2, MOECA_Q8_SCALES = 3, MOECA_Q8_ACCUMULATORS = 4
 } moeca_probe_q8_barrier;
 int32_t moeca_probe_q8_stall(int32_t barrier, int64_t wait_ns);
+
+/* The same for moeca_attention's tensor-core kernel: let a bounded wait of the
+ * calling thread's later calls run out.  The named barrier is set up for one
+ * arrival more than comes (the queries' copies, the scores, the weights P, a
+ * ring slot's release), and every wait lasts wait_ns (1 ms .. 1 s).
+ * MOECA_ATTENTION_NONE: as ever.  Returns 0, or -1 (an argument out of range). */
+typedef enum {
+  MOECA_ATTENTION_NONE = 0, MOECA_ATTENTION_COPIES = 1, MOECA_ATTENTION_SCORES = 2, MOECA_ATTENTION_WEIGHTS = 3,
+  MOECA_ATTENTION_SLOTS = 4
+} moeca_probe_attention_barrier;
+int32_t moeca_probe_attention_stall(int32_t barrier, int64_t wait_ns);
 
 /* Tensor maps (TMA descriptors) this process has encoded, on any thread: host
  * work, done once per handle for its own buffers. */

@@ -3,6 +3,7 @@
 #include <algorithm>
 
 #include "common.cuh"
+#include "moeca_probe.h"
 #include "packed_attn.cuh"
 
 namespace moeca {
@@ -270,6 +271,10 @@ cudaError_t launch_attn_join(const PackedAttnArgs& a, int dtype, cudaStream_t s)
 
 namespace {
 
+constexpr unsigned long long kWaitNs = 1000000000ull;  // a wait gives up after a second
+thread_local unsigned long long g_wait_ns = kWaitNs;
+thread_local int g_stall = MOECA_ATTENTION_NONE;
+
 constexpr int64_t kMaxTokens = 1 << 30;
 constexpr int kMaxHeadDim = 256, kMaxSeqs = 1 << 20;
 constexpr int64_t kMaxWorkspace = int64_t(1) << 30;  // beyond, the key axis is not cut
@@ -445,6 +450,8 @@ moeca_status moeca_attention(const moeca_attention_args* a, void* stream) {
   d.dim = dim; d.causal = a->causal; d.clear = a->clear;
   d.scale_log2 = a->scale * kLog2e;
   d.status = a->status;
+  d.wait_ns = g_wait_ns;
+  d.stall = g_stall;
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   return launched([&] {
     cudaError_t e = p.rows > 0    ? launch_attn_packed_tc(d, p.rows, s)
@@ -453,6 +460,14 @@ moeca_status moeca_attention(const moeca_attention_args* a, void* stream) {
     if (e == cudaSuccess && p.chunk) e = launch_attn_join(d, a->dtype, s);
     return e;
   });
+}
+
+int32_t moeca_probe_attention_stall(int32_t barrier, int64_t wait_ns) {
+  using namespace moeca;
+  if (barrier < MOECA_ATTENTION_NONE || barrier > MOECA_ATTENTION_SLOTS || wait_ns < 1000000 || wait_ns > 1000000000) return -1;
+  g_wait_ns = barrier == MOECA_ATTENTION_NONE ? kWaitNs : static_cast<unsigned long long>(wait_ns);
+  g_stall = barrier;
+  return 0;
 }
 
 }  // extern "C"

@@ -73,6 +73,10 @@ struct PackedAttnArgs {
   int causal, clear;
   float scale_log2; // scale log2(e)
   int32_t* status;
+  // How long a bounded wait lasts, and the barrier whose wait is to run out (tests; see
+  // moeca_probe_attention_stall): it is set up for one arrival more than comes.
+  unsigned long long wait_ns;
+  int stall;
 };
 
 // One block's work.

@@ -30,6 +30,7 @@
 #include <algorithm>
 
 #include "attn_tc.cuh"
+#include "moeca_probe.h"
 #include "packed_attn.cuh"
 
 namespace moeca {
@@ -100,20 +101,20 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 }
 
 // mbar_wait without a call, the clock looked at every 256 tries (reading it takes longer than most waits).
-__device__ __forceinline__ bool wait_here(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+__device__ __forceinline__ bool wait_here(uint32_t bar, uint32_t parity, volatile int* abort_flag, unsigned long long limit) {
   if (mbar_try(bar, parity)) return true;
   unsigned long long t0 = 0;
 #pragma unroll 1
   for (uint32_t it = 1; !mbar_try(bar, parity); ++it)
     if ((it & 255u) == 0) {
       const unsigned long long now = globaltimer();
-      if (*abort_flag || (t0 != 0 && now - t0 > kTcWaitNs)) return false;
+      if (*abort_flag || (t0 != 0 && now - t0 > limit)) return false;
       if (t0 == 0) t0 = now;
     }
   return true;
 }
-__device__ __forceinline__ bool warp_wait_here(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-  return __all_sync(0xffffffffu, wait_here(bar, parity, abort_flag));
+__device__ __forceinline__ bool warp_wait_here(uint32_t bar, uint32_t parity, volatile int* abort_flag, unsigned long long limit) {
+  return __all_sync(0xffffffffu, wait_here(bar, parity, abort_flag, limit));
 }
 
 // Slots of the ring are filled and used in this order: K_0, K_1, V_0, K_2, V_1, ...
@@ -137,15 +138,15 @@ __global__ void __launch_bounds__(64 + 128 * NT, NT == 1 ? 2 : 1)
     abort_flag = 0;
     issued = 0;
     for (int i = 0; i < NT; ++i) {
-      mbar_init(smem_u32(&q_full[i]), 1);
-      mbar_init(smem_u32(&s_full[i]), 1);
+      mbar_init(smem_u32(&q_full[i]), 1 + (a.stall == MOECA_ATTENTION_COPIES));
+      mbar_init(smem_u32(&s_full[i]), 1 + (a.stall == MOECA_ATTENTION_SCORES));
       mbar_init(smem_u32(&p_full[i][0]), kTileRows);
-      mbar_init(smem_u32(&p_full[i][1]), kTileRows);
+      mbar_init(smem_u32(&p_full[i][1]), kTileRows + (a.stall == MOECA_ATTENTION_WEIGHTS));
       mbar_init(smem_u32(&o_full[i]), 1);
     }
     for (int i = 0; i < ST; ++i) {
       mbar_init(smem_u32(&full[i]), 1);
-      mbar_init(smem_u32(&empty[i]), 1);
+      mbar_init(smem_u32(&empty[i]), 1 + (a.stall == MOECA_ATTENTION_SLOTS));
     }
     mbar_init(smem_u32(&v_clean), 1);
     mbar_init(smem_u32(&drain), 1);
@@ -210,7 +211,7 @@ __global__ void __launch_bounds__(64 + 128 * NT, NT == 1 ? 2 : 1)
       bool ok = true;
       const auto fill = [&](const CUtensorMap* map, int block) {
         const int s = n % ST;
-        if (n >= ST && !wait_here(smem_u32(&empty[s]), ((n / ST) - 1) & 1, &abort_flag)) {
+        if (n >= ST && !wait_here(smem_u32(&empty[s]), ((n / ST) - 1) & 1, &abort_flag, a.wait_ns)) {
           give_up(710);
           ok = false;
           return;
@@ -233,7 +234,7 @@ __global__ void __launch_bounds__(64 + 128 * NT, NT == 1 ? 2 : 1)
     if (dirty && !abort_flag) {
       // Value rows last_keys .. of the last block's 16s are another sequence's, or nobody's.
       const int n = place_of_v(blocks - 1, blocks), s = n % ST;
-      if (warp_wait_here(smem_u32(&full[s]), (n / ST) & 1, &abort_flag)) {
+      if (warp_wait_here(smem_u32(&full[s]), (n / ST) & 1, &abort_flag, a.wait_ns)) {
         const int rows = (last_keys + 15) / 16 * 16 - last_keys;
         for (int i = lane; i < rows * 8 * Sh::SUBS; i += 32) {
           const int c = i / (rows * 8), at = i - c * rows * 8;
@@ -261,7 +262,7 @@ __global__ void __launch_bounds__(64 + 128 * NT, NT == 1 ? 2 : 1)
     const bool clean_first = uniform(static_cast<int>(dirty)) != 0;
     const uint32_t t = uniform(tmem);
     bool ok = true;
-    const auto wait = [&](uint32_t bar, uint32_t phase) { return ok = warp_wait_here(bar, phase & 1, &abort_flag); };
+    const auto wait = [&](uint32_t bar, uint32_t phase) { return ok = warp_wait_here(bar, phase & 1, &abort_flag, a.wait_ns); };
     const uint32_t q_lo = desc_lo(smem_u32(smem), 16), ring_k = desc_lo(smem_u32(ring), 16), ring_v = desc_lo(smem_u32(ring), kPart);
     const uint32_t id_s = instr_desc_b(kBlockKeys, false), id_o = instr_desc_b(Sh::DP, true);
     const uint32_t full0 = smem_u32(&full[0]), empty0 = smem_u32(&empty[0]), p0 = smem_u32(&p_full[0][0]), s0 = smem_u32(&s_full[0]);
@@ -352,7 +353,7 @@ __global__ void __launch_bounds__(64 + 128 * NT, NT == 1 ? 2 : 1)
     float2 l2[2] = {{0.f, 0.f}, {0.f, 0.f}};
     bool ok = true;
     for (int j = 0; j < own_blocks; ++j) {
-      if (!warp_wait_here(smem_u32(&s_full[tile]), j & 1, &abort_flag)) {
+      if (!warp_wait_here(smem_u32(&s_full[tile]), j & 1, &abort_flag, a.wait_ns)) {
         ok = false;
         break;
       }
@@ -412,7 +413,7 @@ __global__ void __launch_bounds__(64 + 128 * NT, NT == 1 ? 2 : 1)
         }
       }
     }
-    if (ok && own_blocks > 0) ok = warp_wait_here(smem_u32(&o_full[tile]), 0, &abort_flag);
+    if (ok && own_blocks > 0) ok = warp_wait_here(smem_u32(&o_full[tile]), 0, &abort_flag, a.wait_ns);
     if (ok) {
       tc_fence_after();
       const float l = (l2[0].x + l2[0].y) + (l2[1].x + l2[1].y);
