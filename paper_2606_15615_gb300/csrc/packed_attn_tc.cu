@@ -24,6 +24,13 @@
 // Keys behind the sequence's end are masked; value rows there are zeroed in shared
 // memory before the product, as they belong to another sequence and may hold
 // infinities or NaN.
+// 4 x 4096 tokens, 16 heads of 128: 379 us, 1.45 PFLOP/s (0.76 of the measured burst
+// rate, 0.85 of the sustained one); of 64: 311 us, 0.88 PFLOP/s, where a block's
+// exponentials (1024 clocks for two tiles), the softmax threads' 590 instructions a
+// block and the hand-over between them and the MMAs weigh as much as its 1024 clocks
+// of products. Causal, 8192 tokens, 32 heads of 128 on 8: 370 us, 1.49 PFLOP/s. Short sequences
+// are bound by a CTA's start and end (index, TMEM, first copies 3 us, the result's
+// rows 1.3): 16 of 256, 16 heads of 72, 19 us.
 // Every wait is bounded (about one second); a wait that runs out records
 // MOECA_ERR_TIMEOUT, raises the CTA's abort flag, lets what was issued finish,
 // frees TMEM and returns.
@@ -52,6 +59,10 @@ struct TcShape {
   static constexpr int STAGES = STAGES_FIT < kMaxStages ? STAGES_FIT : kMaxStages;
   static constexpr size_t SMEM = static_cast<size_t>(NT + STAGES) * SLOT + 1024;
   static constexpr int COLUMNS = 256 * NT;     // TMEM
+  // The result's rows on their way out: powers of two of 16-byte pieces are swizzled, others one piece further apart.
+  static constexpr bool OUT_SWIZZLED = DP % 64 == 0;
+  static constexpr int OUT_PITCH = DP * 2 + (OUT_SWIZZLED ? 0 : 16);
+  static_assert(kTileRows * OUT_PITCH <= SLOT);
   static constexpr int THREADS = 64 + 128 * NT;
 };
 
@@ -250,8 +261,8 @@ __global__ void __launch_bounds__(64 + 128 * NT, NT == 1 ? 2 : 1)
   } else if (warp == 1) {
     // All lanes run the loop and one issues; what the loop turns on is read from
     // lane 0, so that the compiler knows it to be the same in all and keeps the
-    // MMAs' operands in uniform registers (else each is moved there anew, and the
-    // loop alone takes 3300 clocks for two tiles' block, at 64 channels and at 128).
+    // MMAs' operands in uniform registers (else each is moved there anew: the loop
+    // alone took 3300 clocks for a block of two tiles of 64 channels, 2500 so).
     const auto uniform = [](auto x) { return static_cast<decltype(x)>(__shfl_sync(0xffffffffu, x, 0)); };
     uint32_t issue;
     asm volatile("{\n .reg .pred e;\n elect.sync _|e, 0xffffffff;\n selp.u32 %0, 1, 0, e;\n}" : "=r"(issue));
@@ -434,18 +445,44 @@ __global__ void __launch_bounds__(64 + 128 * NT, NT == 1 ? 2 : 1)
 #pragma unroll
         for (int c = 0; c < DK; ++c) tmem_wait16(v[c]);
       }
-      if (live) {
+      if (cut) {
+#pragma unroll
+        for (int at = 0; at < Sh::DP; at += 8) {
+          if (!live || at >= a.dim) continue;
+          float f[8];
+#pragma unroll
+          for (int q = 0; q < 8; ++q) f[q] = __uint_as_float(v[at / 16][at % 16 + q]) * inv;
+          store_vec(part_o + at, f);
+          store_vec(part_o + at + 4, f + 4);
+        }
+      } else {
+        // Through the tile's query slot, which the MMAs have done with: a warp's 32
+        // rows then leave as whole rows, 32 pieces of 16 bytes side by side, not as one piece of each.
+        uint8_t* stage = smem + tile * Sh::SLOT;
+        const auto place = [&](int row, int piece) {
+          return stage + row * Sh::OUT_PITCH + (Sh::OUT_SWIZZLED ? piece ^ (row & 7) : piece) * 16;
+        };
 #pragma unroll
         for (int at = 0; at < Sh::DP; at += 8) {
           if (at >= a.dim) continue;
           float f[8];
 #pragma unroll
           for (int q = 0; q < 8; ++q) f[q] = __uint_as_float(v[at / 16][at % 16 + q]) * inv;
-          if (cut) {
-            store_vec(part_o + at, f);
-            store_vec(part_o + at + 4, f + 4);
-          } else {
-            store_vec(out + at, f);
+          store_vec(reinterpret_cast<__nv_bfloat16*>(place(r, at / 8)), f);
+        }
+        __syncwarp();
+        const uint32_t rows = __ballot_sync(0xffffffffu, live);
+        const int pieces = a.dim / 8, skip_rows = 32 / pieces, skip = 32 - skip_rows * pieces;
+        int row = lane / pieces, piece = lane - row * pieces;
+        const uint64_t own = reinterpret_cast<uint64_t>(out);
+        for (int n = 0; n < pieces; ++n) {
+          __nv_bfloat16* to = reinterpret_cast<__nv_bfloat16*>(__shfl_sync(0xffffffffu, own, row));
+          if (rows >> row & 1) *reinterpret_cast<uint4*>(to + piece * 8) = *reinterpret_cast<const uint4*>(place(quad * 32 + row, piece));
+          row += skip_rows;
+          piece += skip;
+          if (piece >= pieces) {
+            piece -= pieces;
+            ++row;
           }
         }
       }
