@@ -24,13 +24,12 @@
 // Keys behind the sequence's end are masked; value rows there are zeroed in shared
 // memory before the product, as they belong to another sequence and may hold
 // infinities or NaN.
-// 4 x 4096 tokens, 16 heads of 128: 379 us, 1.45 PFLOP/s (0.76 of the measured burst
-// rate, 0.85 of the sustained one); of 64: 311 us, 0.88 PFLOP/s, where a block's
-// exponentials (1024 clocks for two tiles), the softmax threads' 590 instructions a
-// block and the hand-over between them and the MMAs weigh as much as its 1024 clocks
-// of products. Causal, 8192 tokens, 32 heads of 128 on 8: 370 us, 1.49 PFLOP/s. Short sequences
-// are bound by a CTA's start and end (index, TMEM, first copies 3 us, the result's
-// rows 1.3): 16 of 256, 16 heads of 72, 19 us.
+// 4 x 4096 tokens, 16 heads of 128: 365 us, 1.50 PFLOP/s (0.78 of the measured burst
+// rate, 0.88 of the sustained one); of 64: 308 us, 0.89 PFLOP/s: a tile's chain from
+// its scores through its softmax (1500 clocks a block) and the hand-over to the next scores
+// is longer there than the products of both tiles (1024). Causal, 8192 tokens, 32 heads
+// of 128 on 8: 358 us, 1.54 PFLOP/s. Short sequences are bound by a CTA's start and end
+// (index, TMEM and first copies some 3 us): 16 of 256, 16 heads of 72, 18 us.
 // Every wait is bounded (about one second); a wait that runs out records
 // MOECA_ERR_TIMEOUT, raises the CTA's abort flag, lets what was issued finish,
 // frees TMEM and returns.
@@ -318,14 +317,20 @@ __global__ void __launch_bounds__(64 + 128 * NT, NT == 1 ? 2 : 1)
       const uint32_t id_next = id_of(j + 1);
       const int steps = last ? n_last : kBlockKeys / 16;
       // The next keys come before this block's values.
-      uint32_t k_at = 0;
+      uint32_t k_at = 0, k_parity = 0;
       if (!last) {
         next();
         k_at = at;
-        if (!wait(full0 + at * 8, parity)) break;
+        k_parity = parity;
       }
       next();
-      if (!wait(full0 + at * 8, parity) || (last && clean_first && !wait(smem_u32(&v_clean), 0))) break;
+      // Most often both are there: one vote for two barriers.
+      const bool there = mbar_try(full0 + at * 8, parity) && (last || mbar_try(full0 + k_at * 8, k_parity));
+      if (!__all_sync(0xffffffffu, there)) {
+        if (!last && !wait(full0 + k_at * 8, k_parity)) break;
+        if (!wait(full0 + at * 8, parity)) break;
+      }
+      if (last && clean_first && !wait(smem_u32(&v_clean), 0)) break;
       const uint32_t vb = ring_v + at * (Sh::SLOT >> 4);
 #pragma unroll
       for (int i = 0; i < NT; ++i) {
@@ -517,6 +522,7 @@ bool encode_heads(CUtensorMap* m, const Heads& h, int64_t tokens, int dim, int h
   cuuint64_t strides[2] = {stride(h.head_stride, h.heads), stride(h.token_stride, tokens)};
   cuuint32_t box[3] = {64, static_cast<cuuint32_t>(heads), static_cast<cuuint32_t>(box_tokens)};
   cuuint32_t estr[3] = {1, 1, 1};
+  g_maps_encoded.fetch_add(1, std::memory_order_relaxed);
   return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, h.data, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }

@@ -398,3 +398,35 @@ def test_one_key_head_expanded(M, q_n, dtype):
     assert got.shape == want.shape
     check(M, q[:1].expand(q_n, -1, -1), k, v, [q_n], [700])
     check(M, q, k[:1].expand(700, -1, -1), v, [q_n], [700])
+
+
+def test_two_host_threads_at_once(M):
+    """Two threads, each with its stream and its inputs: cut and whole key axes, sorts and rows, side by side."""
+    import threading
+
+    def work(seed, stream):
+        q, k, v = qkv(seed, 1 + 200 * seed, 4000 + seed, 4, 2, 128, "bf16")
+        ids = torch.randint(0, 16, (5000, 2), dtype=torch.int32, generator=torch.Generator().manual_seed(seed)).cuda()
+        x = torch.randn(5000, 72, generator=torch.Generator().manual_seed(seed)).cuda()
+        torch.cuda.synchronize()
+
+        def run():
+            plan = M.expert_sort(ids, 16, stream=stream.cuda_stream)
+            return (M.attention(q, k, v, causal=True, stream=stream.cuda_stream), M.expert_rows(x, plan, stream=stream.cuda_stream),
+                    plan.place)
+
+        first = run()
+        stream.synchronize()
+        for _ in range(20):
+            again = run()
+            stream.synchronize()
+            if not all(torch.equal(a, b) for a, b in zip(first, again)):
+                bad.append(seed)
+
+    bad = []
+    threads = [threading.Thread(target=work, args=(i, torch.cuda.Stream())) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not bad
