@@ -72,7 +72,7 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_kernel(const PackedAtt
   pdl_entry();
   const int index = blockIdx.x / static_cast<uint32_t>(a.q.heads), h = blockIdx.x - index * a.q.heads;
   const AttnWork w = attn_work(a, index);
-  clear_rest<T>(a);
+  clear_rest<T>(a, threadIdx.x, blockDim.x);
   if (!w.any) return;
   const int dim = a.dim, pitch = simt_pitch(dim);
   float* sq = reinterpret_cast<float*>(smem4);

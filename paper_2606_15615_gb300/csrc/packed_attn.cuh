@@ -123,19 +123,19 @@ __device__ __forceinline__ int visible_keys(const PackedAttnArgs& a, const AttnW
   return a.causal ? min(max(i + 1 - w.nq + w.nk, 0), w.nk) : w.nk;
 }
 
-// Query tokens before the first and behind the last sequence become 0, the blocks
-// taking them in turn.
+// Query tokens before the first and behind the last sequence become 0: the blocks
+// take them in turn, `threads` of a block's threads each.
 template <typename T>
-__device__ __forceinline__ void clear_rest(const PackedAttnArgs& a) {
+__device__ __forceinline__ void clear_rest(const PackedAttnArgs& a, int thread, int threads) {
   if (!a.clear || !a.qs.off) return;
   const int lo = a.qs.start(0), hi = max(a.qs.start(a.qs.n), lo), rest = lo + a.qs.total - hi;
   for (int64_t r = blockIdx.x; r < rest; r += gridDim.x) {
     const int64_t t = r < lo ? r : hi + (r - lo);
     T* out = static_cast<T*>(a.out.data) + t * a.out.token_stride;
     for (int h = 0; h < a.out.heads; ++h)
-      for (int c = threadIdx.x; c < a.dim; c += blockDim.x) out[h * a.out.head_stride + c] = T(0.f);
+      for (int c = thread; c < a.dim; c += threads) out[h * a.out.head_stride + c] = T(0.f);
     if (a.lse)
-      for (int h = threadIdx.x; h < a.out.heads; h += blockDim.x) a.lse[t * a.out.heads + h] = -INFINITY;
+      for (int h = thread; h < a.out.heads; h += threads) a.lse[t * a.out.heads + h] = -INFINITY;
   }
 }
 

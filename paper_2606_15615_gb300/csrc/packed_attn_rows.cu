@@ -57,7 +57,7 @@ __global__ void __launch_bounds__(kRowsThreads, DK <= 4 ? 4 : 2) attn_rows_kerne
   extern __shared__ __align__(16) uint8_t rows_smem[];
   __shared__ float sh_m[kRowsWarps][16], sh_l[kRowsWarps][16];
   pdl_entry();
-  clear_rest<__nv_bfloat16>(a);
+  clear_rest<__nv_bfloat16>(a, threadIdx.x, blockDim.x);
   const int index = blockIdx.x / static_cast<uint32_t>(a.k.heads), kvh = blockIdx.x - index * a.k.heads;
   const AttnWork w = attn_work(a, index);
   if (!w.any) return;

@@ -170,11 +170,13 @@ __global__ void __launch_bounds__(64 + 128 * NT, NT == 1 ? 2 : 1)
   }
   __syncthreads();
   pdl_entry();
-  clear_rest<__nv_bfloat16>(a);
   // The heaviest tiles of a causal sequence are its last: they start first.
   const int turn = blockIdx.x / static_cast<uint32_t>(a.k.heads), kvh = blockIdx.x - turn * a.k.heads;
   const AttnWork w = attn_work(a, a.causal && !a.ks.unit ? static_cast<int>(a.q_pieces) - 1 - turn : turn);
-  if (!w.any) return;  // uniform over the CTA, before TMEM is taken
+  if (!w.any) {  // uniform over the CTA, before TMEM is taken
+    clear_rest<__nv_bfloat16>(a, threadIdx.x, blockDim.x);
+    return;
+  }
   const int G = a.group, per_tile = a.qs.unit / NT;  // queries of a tile
   const int n_q = min(w.nq, a.max_q);
   // Blocks of keys that each tile's rows see.
@@ -210,13 +212,12 @@ __global__ void __launch_bounds__(64 + 128 * NT, NT == 1 ? 2 : 1)
   if (warp == 0) {
     if (lane == 0) {
       const int token = w.q0 + w.row0;
-#pragma unroll
-      for (int i = 0; i < NT; ++i)
-        if (nb[i] > 0) {
-          mbar_expect_tx(smem_u32(&q_full[i]), Sh::SUBS * G * per_tile * 128);
-          for (int s = 0; s < Sh::SUBS; ++s)
-            tma_load_heads(smem_u32(smem + i * Sh::SLOT + s * kPart), &qmap, s * 64, kvh * G, token + i * per_tile, smem_u32(&q_full[i]));
-        }
+      const auto queries = [&](int i) {
+        if (nb[i] == 0) return;
+        mbar_expect_tx(smem_u32(&q_full[i]), Sh::SUBS * G * per_tile * 128);
+        for (int s = 0; s < Sh::SUBS; ++s)
+          tma_load_heads(smem_u32(smem + i * Sh::SLOT + s * kPart), &qmap, s * 64, kvh * G, token + i * per_tile, smem_u32(&q_full[i]));
+      };
       int n = 0;
       bool ok = true;
       const auto fill = [&](const CUtensorMap* map, int block) {
@@ -233,7 +234,9 @@ __global__ void __launch_bounds__(64 + 128 * NT, NT == 1 ? 2 : 1)
                          w.k0 + w.key_lo + block * kBlockKeys, bar);
         ++n;
       };
+      queries(0);
       if (blocks > 0) fill(&kmap, 0);
+      if constexpr (NT == 2) queries(1);
       for (int j = 0; ok && j < blocks; ++j) {
         if (j + 1 < blocks) fill(&kmap, j + 1);
         if (ok) fill(&vmap, j);
@@ -257,6 +260,7 @@ __global__ void __launch_bounds__(64 + 128 * NT, NT == 1 ? 2 : 1)
         give_up(711);
       }
     }
+    clear_rest<__nv_bfloat16>(a, lane, 32);
   } else if (warp == 1) {
     // All lanes run the loop and one issues; what the loop turns on is read from
     // lane 0, so that the compiler knows it to be the same in all and keeps the
