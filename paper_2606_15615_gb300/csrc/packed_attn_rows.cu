@@ -13,7 +13,7 @@
 // memory at the end.
 // Four tokens over 131072 keys in all, 32 heads of 128 on 8 (537 MB): 91 us with the
 // join, 5.9 TB/s, 0.87 of the measured copy rate; one over 65536 keys on 4 key heads (134
-// MB) 34 us, a quarter of it the join's launch and its dependent loads; one over 300 keys 5.9 us.
+// MB) 32 us, a fifth of it the join's launch and its dependent loads; one over 300 keys 5.7 us.
 #include <algorithm>
 
 #include "attn_tc.cuh"

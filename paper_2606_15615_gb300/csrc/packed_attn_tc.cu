@@ -25,11 +25,11 @@
 // memory before the product, as they belong to another sequence and may hold
 // infinities or NaN.
 // 4 x 4096 tokens, 16 heads of 128: 365 us, 1.50 PFLOP/s (0.78 of the measured burst
-// rate, 0.88 of the sustained one); of 64: 308 us, 0.89 PFLOP/s: a tile's chain from
+// rate, 0.88 of the sustained one); of 64: 307 us, 0.89 PFLOP/s: a tile's chain from
 // its scores through its softmax (1500 clocks a block) and the hand-over to the next scores
 // is longer there than the products of both tiles (1024). Causal, 8192 tokens, 32 heads
-// of 128 on 8: 358 us, 1.54 PFLOP/s. Short sequences are bound by a CTA's start and end
-// (index, TMEM and first copies some 3 us): 16 of 256, 16 heads of 72, 18 us.
+// of 128 on 8: 356 us, 1.54 PFLOP/s. Short sequences are bound by a CTA's start and end
+// (index, TMEM and first copies some 3 us): 16 of 256, 16 heads of 72, 17 us.
 // Every wait is bounded (about one second); a wait that runs out records
 // MOECA_ERR_TIMEOUT, raises the CTA's abort flag, lets what was issued finish,
 // frees TMEM and returns.
