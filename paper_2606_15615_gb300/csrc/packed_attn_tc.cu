@@ -47,7 +47,7 @@ constexpr int kBlockKeys = 128;              // keys of a block
 constexpr int kPart = 128 * 128;             // bytes of 128 rows x 64 channels
 constexpr int kMaxStages = 8;
 // Shared memory of a block less the static part: two blocks an SM with one tile, one with two.
-constexpr size_t smem_most(int tiles) { return tiles == 1 ? 227 * 1024 / 2 - 3072 : 227 * 1024 - 2048; }
+constexpr size_t smem_most(int tiles) { return (tiles == 1 ? 110 : 225) * 1024; }
 
 template <int DK, int NT>  // DK: 16-channel steps of a head
 struct TcShape {

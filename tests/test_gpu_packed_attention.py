@@ -225,6 +225,14 @@ def test_attention_of_other_heads(M, H, Hk, d, dtype):
     check(M, q[:2], k, v, [1, 1], [50, 40], True, max_q=1)
 
 
+@pytest.mark.parametrize("H,Hk,d", [(17, 1, 64), (48, 1, 72), (96, 1, 128), (128, 2, 64), (128, 1, 80), (100, 4, 96)])
+def test_large_groups(M, H, Hk, d):
+    """Tiles of one to seven queries with all of their heads, full and with rows to spare."""
+    q, k, v = qkv(H, 30, 300, H, Hk, d, "bf16")
+    check(M, q, k, v, [9, 1, 20], [9, 130, 161], True)
+    check(M, q[:2], k, v, [1, 1], [1, 299], True, max_q=1)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("causal", [False, True])
 def test_equal_lengths_need_no_offsets(M, causal, dtype):
