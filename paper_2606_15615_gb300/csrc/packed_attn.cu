@@ -188,21 +188,26 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_kernel(const PackedAtt
 }
 
 // ---------------------------------------------------------------------------
-// Join: a block per (query, head).  With lse_j the chunks' base-2 logarithms and
-// m their maximum: o = sum_j 2^(lse_j - m) o_j / sum_j 2^(lse_j - m).  Each of the
-// eight warps adds every eighth chunk, and the eight sums are added in their order:
-// the loads of many chunks are in flight at once (171 chunks of 32 rows took one warp a
-// row 80 us; 74 chunks of 32 rows take this 2.5 us less than four warps).
+// Join of a (query, head)'s chunks.  With lse_j the chunks' base-2 logarithms and
+// m their maximum: o = sum_j 2^(lse_j - m) o_j / sum_j 2^(lse_j - m).
+// W warps share a row: each adds every W-th chunk, and the W sums are added in
+// their order.  Few rows with many chunks take a block of eight, so that the loads of
+// many chunks are in flight at once (171 chunks of 32 rows took one warp a row 80 us);
+// many rows, whose chunks are few, a warp each (2048 tokens, 8 heads of 128 in two
+// chunks: 29 us with the kernel before it, 66 with a block each).
 // ---------------------------------------------------------------------------
 constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32;
+constexpr int64_t kJoinFewRows = 2048;  // up to here a block per row
 
-template <typename T, int C>  // C: channels of a lane, 32 apart
+template <typename T, int C, int W>  // C: channels of a lane, 32 apart
 __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const PackedAttnArgs a) {
-  __shared__ float sh[kJoinWarps][32 * C];
+  __shared__ float sh[W > 1 ? W : 1][32 * C];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int t = blockIdx.x / static_cast<uint32_t>(a.q.heads), h = blockIdx.x - t * a.q.heads;
+  const uint32_t row = W > 1 ? blockIdx.x : blockIdx.x * kJoinWarps + warp;
+  const int t = row / static_cast<uint32_t>(a.q.heads), h = row - t * a.q.heads;
   // Offsets are the caller's: the kernel before this one only writes the workspace.
-  const int b = a.qs.owner(t), i = t - a.qs.start(b);
+  const bool some = t < a.qs.total;
+  const int b = some ? a.qs.owner(t) : 0, i = some ? t - a.qs.start(b) : -1;
   const bool mine = i >= 0 && i < min(a.qs.length(b), a.max_q);
   const int chunks = static_cast<int>((static_cast<uint32_t>(a.ks.length(b)) + a.ks.unit - 1) / a.ks.unit);
   const int64_t first = (static_cast<int64_t>(a.ks.base(b)) * a.max_q + i) * a.q.heads + h, step = static_cast<int64_t>(a.max_q) * a.q.heads;
@@ -217,25 +222,32 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const PackedAtt
   for (int j = lane; j < chunks; j += 32) sum += exp2f(a.part_lse[first + j * step] - ref);
   sum = warp_sum(sum);
   float o[C] = {};
-#pragma unroll 8
-  for (int j = warp; j < chunks; j += kJoinWarps) {
+#pragma unroll W > 1 ? 8 : 2
+  for (int j = W > 1 ? warp : 0; j < chunks; j += W) {
     const float weight = exp2f(a.part_lse[first + j * step] - ref);
     const float* part = a.part_o + (first + j * step) * a.dim;
 #pragma unroll
     for (int c = 0; c < C; ++c)
       if (c * 32 + lane < a.dim) o[c] = fmaf(weight, part[c * 32 + lane], o[c]);
   }
-#pragma unroll
-  for (int c = 0; c < C; ++c) sh[warp][c * 32 + lane] = o[c];
-  __syncthreads();
-  if (threadIdx.x == 0 && a.lse) a.lse[static_cast<int64_t>(t) * a.q.heads + h] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * kLn2;
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   T* out = static_cast<T*>(a.out.data) + t * a.out.token_stride + h * a.out.head_stride;
-  for (int c = threadIdx.x; c < a.dim; c += kJoinThreads) {
-    float v = 0.f;
+  if (lane == 0 && (W == 1 || warp == 0) && a.lse)
+    a.lse[static_cast<int64_t>(t) * a.q.heads + h] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * kLn2;
+  if constexpr (W == 1) {
 #pragma unroll
-    for (int u = 0; u < kJoinWarps; ++u) v += sh[u][c];
-    out[c] = Elem<T>::from_f(v * inv);
+    for (int c = 0; c < C; ++c)
+      if (c * 32 + lane < a.dim) out[c * 32 + lane] = Elem<T>::from_f(o[c] * inv);
+  } else {
+#pragma unroll
+    for (int c = 0; c < C; ++c) sh[warp][c * 32 + lane] = o[c];
+    __syncthreads();
+    for (int c = threadIdx.x; c < a.dim; c += kJoinThreads) {
+      float v = 0.f;
+#pragma unroll
+      for (int u = 0; u < W; ++u) v += sh[u][c];
+      out[c] = Elem<T>::from_f(v * inv);
+    }
   }
 }
 
@@ -267,10 +279,23 @@ cudaError_t launch_attn_simt(const PackedAttnArgs& a, int dtype, int tile, cudaS
 }
 
 cudaError_t launch_attn_join(const PackedAttnArgs& a, int dtype, cudaStream_t s) {
-  const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(a.qs.total) * a.q.heads));
-  const auto run = [&](auto kernel) { return launch_pdl(kernel, grid, dim3(kJoinThreads), 0, s, a); };
-  if (dtype == MOECA_BF16) return run(a.dim <= 128 ? attn_join_kernel<__nv_bfloat16, 4> : attn_join_kernel<__nv_bfloat16, 8>);
-  return run(a.dim <= 128 ? attn_join_kernel<float, 4> : attn_join_kernel<float, 8>);
+  const int64_t rows = static_cast<int64_t>(a.qs.total) * a.q.heads;
+  const auto run = [&](auto kernel, int64_t blocks) {
+    return launch_pdl(kernel, dim3(static_cast<unsigned>(blocks)), dim3(kJoinThreads), 0, s, a);
+  };
+  const auto pick = [&](auto* t, auto c) {
+    using T = std::remove_pointer_t<decltype(t)>;
+    if (rows <= kJoinFewRows) return run(attn_join_kernel<T, c.value, kJoinWarps>, rows);
+    return run(attn_join_kernel<T, c.value, 1>, (rows + kJoinWarps - 1) / kJoinWarps);
+  };
+  using Four = std::integral_constant<int, 4>;
+  using Eight = std::integral_constant<int, 8>;
+  if (dtype == MOECA_BF16) {
+    __nv_bfloat16* t = nullptr;
+    return a.dim <= 128 ? pick(t, Four()) : pick(t, Eight());
+  }
+  float* t = nullptr;
+  return a.dim <= 128 ? pick(t, Four()) : pick(t, Eight());
 }
 
 namespace {
@@ -315,6 +340,7 @@ bool fits_tc(const moeca_heads& h, int64_t tokens) {
 }
 
 constexpr int kSms = 152;
+constexpr int64_t kLongKeys = 4096, kKeysSaved = 1536;
 
 // How a call is carried out: a function of its sizes, type and alignment.
 Plan plan_attention(const moeca_attention_args& a) {
@@ -333,7 +359,11 @@ Plan plan_attention(const moeca_attention_args& a) {
       least = 512;
     } else {
       const int each = 128 / group;
-      p.rows = p.max_q <= each ? 1 : 2;
+      // One tile a block where all blocks then run at once, two an SM, and keys are too few to be cut (2 x 1024
+      // tokens, 8 heads of 64: 13.2 us, with two tiles 14.4; 2048 tokens, 8 heads of 128: 26.3 and 28.4).
+      int per;
+      const bool at_once = pieces(a.q_offsets, a.n_queries, a.n_seqs, each, p.max_q, &per) * heads <= 2 * kSms;
+      p.rows = p.max_q <= each || (at_once && a.n_keys < a.n_seqs * kLongKeys) ? 1 : 2;
       p.tile = p.rows * each;
       fill = p.rows == 1 ? 2 * kSms : kSms;
       least = 512;
@@ -362,6 +392,9 @@ Plan plan_attention(const moeca_attention_args& a) {
       chunk = (mean + cuts - 1) / cuts;
     }
     chunk = std::max<int64_t>(least, (chunk + 127) / 128 * 128);
+    // Writing and joining the tiles' partial results costs what some 1500 keys do: 2048 tokens, 8 heads of 128, cut
+    // in two 29.5 us, whole 28.4; 4096 tokens, 4 heads, 40.6 and 50.9.
+    if (p.rows > 0 && mean - chunk < kKeysSaved) chunk = kMaxTokens;
     const int64_t longest = a.k_offsets ? a.n_keys : mean;
     if (chunk < longest) {
       const int64_t n = pieces(a.k_offsets, a.n_keys, a.n_seqs, static_cast<int>(chunk), 0x7fffffff, &p.k_per);
