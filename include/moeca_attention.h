@@ -71,7 +71,7 @@ moeca_status moeca_qk_norm_rope(const moeca_qk_norm_rope_args* args, void* strea
  * a sequence's queries behind its first max_q.
  *
  * Scores, softmax statistics and sums are fp32 (the exponential's argument in
- * base 2); with bf16 values p is rounded to bf16 before it meets v, the sum of p
+ * base 2; a row's highest score gives 0 within 2^-17, whatever its size); with bf16 values p is rounded to bf16 before it meets v, the sum of p
  * is not.  Keys and values behind a sequence's end are never looked at, whatever they
  * hold; a value that is not finite may reach, by 0 x infinity, rows of its own
  * sequence that `causal` hides it from.

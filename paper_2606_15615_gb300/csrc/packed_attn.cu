@@ -16,8 +16,10 @@ namespace {
 // BQ / 16 rows and two keys each for the scores, BQ / 16 rows and four channels
 // in every 64 for the sums.  One pass over the keys, 32 at a time, with a running
 // maximum m and sum l per row:
-//   m' = max(m, max_j s_j), o <- o 2^(m - m') + sum_j 2^(s_j - m') v_j,
-// s in base 2.  Bound by FFMA and the shared-memory reads beside it (24.3 ms for
+//   m' = max(m, max_j s_j), o <- o 2^((m - m') c) + sum_j 2^((s_j - m') c) v_j,
+// s = q . k, c = scale log2(e).  The difference comes before the product: of s c - m c
+// the compiler would make a fused multiply-add, whose exponent at s = m is the rounding of
+// m c, a power of two of its own for scores of 2^31.  Bound by FFMA and the shared-memory reads beside it (24.3 ms for
 // prompts of 16384 tokens, 32 heads of 128, bf16: 24 TFLOP/s); four texts of 16 to 121 tokens,
 // 12 heads of 64 in fp32, take 27 us, the latency of four blocks of keys.
 // ---------------------------------------------------------------------------
@@ -120,14 +122,14 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_kernel(const PackedAtt
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       const int limit = min(see[r], w.key_hi) - key0;
-      s[r][0] = tx < limit ? s[r][0] * a.scale_log2 : -INFINITY;
-      s[r][1] = tx + 16 < limit ? s[r][1] * a.scale_log2 : -INFINITY;
+      if (tx >= limit) s[r][0] = -INFINITY;
+      if (tx + 16 >= limit) s[r][1] = -INFINITY;
       // A score that is not a number reaches p through s, not through the maximum.
       const float top = fmaxf(m[r], group16_max(fmaxf(s[r][0], s[r][1])));
       const float ref = top == -INFINITY ? 0.f : top;
-      const float keep = exp2f(m[r] - ref);
-      s[r][0] = exp2f(s[r][0] - ref);
-      s[r][1] = exp2f(s[r][1] - ref);
+      const float keep = exp2f((m[r] - ref) * a.scale_log2);
+      s[r][0] = exp2f((s[r][0] - ref) * a.scale_log2);
+      s[r][1] = exp2f((s[r][1] - ref) * a.scale_log2);
       l[r] = l[r] * keep + group16_sum(s[r][0] + s[r][1]);
       m[r] = top;
       sp[(ty * R + r) * kSimtPitch + tx] = s[r][0];
@@ -166,7 +168,7 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_kernel(const PackedAtt
     const int i = w.row0 + ty * R + r;
     if (ty * R + r >= rows) continue;
     const float inv = l[r] == 0.f ? 0.f : 1.f / l[r];
-    const float lse2 = l[r] == 0.f ? -INFINITY : m[r] + log2f(l[r]);
+    const float lse2 = l[r] == 0.f ? -INFINITY : m[r] * a.scale_log2 + log2f(l[r]);
     if (a.ks.unit) {
       const int64_t at = (static_cast<int64_t>(w.piece) * a.max_q + i) * a.q.heads + h;
       if (tx == 0) a.part_lse[at] = lse2;

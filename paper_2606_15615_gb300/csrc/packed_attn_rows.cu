@@ -8,8 +8,9 @@
 // fourth tile of 16 keys through a ring of its own (cp.async, two tiles in flight,
 // no barrier between warps), so that two to four blocks an SM keep HBM
 // busy.  A warp's 16 rows are one m16n8k16 fragment: S = Q K^T, the
-// running maximum and sum per row in registers, P in bf16 straight from the
-// scores' fragment into the product with V.  The four warps' results meet in shared
+// running maximum m and sum per row in registers, P = 2^((s - m) scale) in bf16 straight
+// from the scores' fragment into the product with V (the difference first: 1 at s = m,
+// however large the scores).  The four warps' results meet in shared
 // memory at the end.
 // Four tokens over 131072 keys in all, 32 heads of 128 on 8 (537 MB): 91 us with the
 // join, 5.9 TB/s, 0.87 of the measured copy rate; one over 65536 keys on 4 key heads (134
@@ -141,20 +142,20 @@ __global__ void __launch_bounds__(kRowsThreads, DK <= 4 ? 4 : 2) attn_rows_kerne
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           float& x = s[n][2 * h + e];
-          x = key0 + n * 8 + e < see[h] ? x * a.scale_log2 : -INFINITY;
+          if (key0 + n * 8 + e >= see[h]) x = -INFINITY;
           top = fmaxf(top, x);
         }
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = fmaxf(m[h], fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2)));
       const float ref = top == -INFINITY ? 0.f : top;
-      keep[h] = ex2f_approx(m[h] - ref);
+      keep[h] = ex2f_approx((m[h] - ref) * a.scale_log2);
       m[h] = top;
       float sum = 0.f;
 #pragma unroll
       for (int n = 0; n < 2; ++n)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          p[n][2 * h + e] = ex2f_approx(s[n][2 * h + e] - ref);
+          p[n][2 * h + e] = ex2f_approx((s[n][2 * h + e] - ref) * a.scale_log2);
           sum += p[n][2 * h + e];
         }
       l[h] = l[h] * keep[h] + sum;
@@ -208,7 +209,7 @@ __global__ void __launch_bounds__(kRowsThreads, DK <= 4 ? 4 : 2) attn_rows_kerne
     float sum = 0.f, f[8] = {};
 #pragma unroll
     for (int u = 0; u < kRowsWarps; ++u) {
-      const float weight = ex2f_approx(sh_m[u][r] - ref);
+      const float weight = ex2f_approx((sh_m[u][r] - ref) * a.scale_log2);
       sum += weight * sh_l[u][r];
       const float* part = reinterpret_cast<const float*>(rows_smem + u * Sh::RING) + r * Sh::DP + c;
 #pragma unroll
@@ -218,7 +219,7 @@ __global__ void __launch_bounds__(kRowsThreads, DK <= 4 ? 4 : 2) attn_rows_kerne
 #pragma unroll
     for (int j = 0; j < 8; ++j) f[j] *= inv;
     const int q_i = r / G, head = kvh * G + r - q_i * G;
-    const float lse2 = sum == 0.f ? -INFINITY : top + log2f(sum);
+    const float lse2 = sum == 0.f ? -INFINITY : top * a.scale_log2 + log2f(sum);
     if (a.ks.unit) {
       const int64_t part = (static_cast<int64_t>(w.piece) * a.max_q + q_i) * a.q.heads + head;
       if (c == 0) a.part_lse[part] = lse2;

@@ -46,6 +46,7 @@ constexpr int kTileRows = 128;               // rows of a tile (MMA M)
 constexpr int kBlockKeys = 128;              // keys of a block
 constexpr int kPart = 128 * 128;             // bytes of 128 rows x 64 channels
 constexpr int kMaxStages = 8;
+constexpr float kFusedMost = 256.f;          // |m sc| up to which the exponent is one fused multiply-add
 // Shared memory of a block less the static part: two blocks an SM with one tile, one with two.
 constexpr size_t smem_most(int tiles) { return (tiles == 1 ? 110 : 225) * 1024; }
 
@@ -369,7 +370,7 @@ __global__ void __launch_bounds__(64 + 128 * NT, NT == 1 ? 2 : 1)
     const bool live = r < per_tile * G && query < n_q;
     const int see = min(live ? visible_keys(a, w, query) : w.nk, w.key_hi) - w.key_lo;
     const float sc = a.scale_log2;
-    float m = -INFINITY;
+    float m = -INFINITY, ref = 0.f, calm = -1.f;
     float2 l2[2] = {{0.f, 0.f}, {0.f, 0.f}};
     bool ok = true;
     for (int j = 0; j < own_blocks; ++j) {
@@ -396,23 +397,42 @@ __global__ void __launch_bounds__(64 + 128 * NT, NT == 1 ? 2 : 1)
         for (int u = 0; u < 4; ++u)
           top[u] = max3(top[u], __uint_as_float(sv[q + 2 * u]), __uint_as_float(sv[q + 2 * u + 1]));
       const float cand = fmaxf(m, max3(fmaxf(top[0], top[1]), top[2], top[3]));
-      if (j == 0) {
-        m = cand;
-      } else if (__any_sync(0xffffffffu, (cand - m) * sc > 8.f)) {
-        const float alpha = m == cand ? 1.f : ex2f_approx((m - cand) * sc);
+      // P = 2^((s - m) sc).  Fused as s sc - fl(m sc), the rounding of m sc stays in every exponent and changes with m:
+      // 2^-17 at most while |m sc| is below kFusedMost, but whole powers of two (P infinite, or 0 in every column) for
+      // scores of 2^31.  Where a row of the warp is beyond the limit the difference is formed first, so that s = m
+      // gives 1, and `calm` sends every later block this way.  One vote stands for that, a risen maximum and the first
+      // block (the comparison is also taken where both maxima are infinite).
+      if (__any_sync(0xffffffffu, !((cand - m) * sc <= calm))) {
+        if (j == 0) {
+          m = cand;
+        } else if (__any_sync(0xffffffffu, (cand - m) * sc > 8.f)) {
+          const float alpha = m == cand ? 1.f : ex2f_approx((m - cand) * sc);
 #pragma unroll
-        for (int c = 0; c < DK; ++c) {
-          uint32_t v[16];
-          tmem_ld16(t_o + c * 16, v);
+          for (int c = 0; c < DK; ++c) {
+            uint32_t v[16];
+            tmem_ld16(t_o + c * 16, v);
 #pragma unroll
-          for (int q = 0; q < 16; ++q) v[q] = __float_as_uint(__uint_as_float(v[q]) * alpha);
-          tmem_st16(t_o + c * 16, v);
+            for (int q = 0; q < 16; ++q) v[q] = __float_as_uint(__uint_as_float(v[q]) * alpha);
+            tmem_st16(t_o + c * 16, v);
+          }
+#pragma unroll
+          for (int u = 0; u < 2; ++u) l2[u] = mul2(l2[u], make_float2(alpha, alpha));
+          m = cand;
         }
+        const float base = m == -INFINITY ? 0.f : m;
+        ref = base * sc;
+        const bool apart = __any_sync(0xffffffffu, fabsf(ref) > kFusedMost);
+        calm = apart ? -1.f : 8.f;
+        if (apart) {
+          ref = 0.f;
 #pragma unroll
-        for (int u = 0; u < 2; ++u) l2[u] = mul2(l2[u], make_float2(alpha, alpha));
-        m = cand;
+          for (int q = 0; q < 128; q += 2) {
+            const float2 d = add2(make_float2(__uint_as_float(sv[q]), __uint_as_float(sv[q + 1])), make_float2(-base, -base));
+            sv[q] = __float_as_uint(d.x);
+            sv[q + 1] = __float_as_uint(d.y);
+          }
+        }
       }
-      const float ref = m == -INFINITY ? 0.f : m * sc;
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
         uint32_t pk[16];
