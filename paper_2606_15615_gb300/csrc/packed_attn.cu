@@ -171,7 +171,7 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_kernel(const PackedAtt
     const float lse2 = l[r] == 0.f ? -INFINITY : m[r] * a.scale_log2 + log2f(l[r]);
     if (a.ks.unit) {
       const int64_t at = (static_cast<int64_t>(w.piece) * a.max_q + i) * a.q.heads + h;
-      if (tx == 0) a.part_lse[at] = lse2;
+      if (tx == 0) a.part_ml[at] = make_float2(m[r], l[r]);
 #pragma unroll
       for (int c = 0; c < DC; ++c)
 #pragma unroll
@@ -190,8 +190,9 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_kernel(const PackedAtt
 }
 
 // ---------------------------------------------------------------------------
-// Join of a (query, head)'s chunks.  With lse_j the chunks' base-2 logarithms and
-// m their maximum: o = sum_j 2^(lse_j - m) o_j / sum_j 2^(lse_j - m).
+// Join of a (query, head)'s chunks.  With m_j and l_j the chunks' maxima and sums, m the
+// largest maximum, c = scale log2(e) and w_j = 2^((m_j - m) c) l_j:
+//   o = sum_j w_j o_j / sum_j w_j.
 // W warps share a row: each adds every W-th chunk, and the W sums are added in
 // their order.  Few rows with many chunks take a block of eight, so that the loads of
 // many chunks are in flight at once (171 chunks of 32 rows took one warp a row 80 us);
@@ -216,26 +217,34 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const PackedAtt
   pdl_entry();
   if (!mine) return;
   float m = -INFINITY;
-  for (int j = lane; j < chunks; j += 32) m = fmaxf(m, a.part_lse[first + j * step]);
+  for (int j = lane; j < chunks; j += 32) m = fmaxf(m, a.part_ml[first + j * step].x);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
   const float ref = m == -INFINITY ? 0.f : m;
-  float sum = 0.f;
-  for (int j = lane; j < chunks; j += 32) sum += exp2f(a.part_lse[first + j * step] - ref);
-  sum = warp_sum(sum);
-  float o[C] = {};
-#pragma unroll W > 1 ? 8 : 2
-  for (int j = W > 1 ? warp : 0; j < chunks; j += W) {
-    const float weight = exp2f(a.part_lse[first + j * step] - ref);
-    const float* part = a.part_o + (first + j * step) * a.dim;
+  // A lane forms the weight of one chunk in 32, and all lanes take it from there.
+  float sum = 0.f, o[C] = {};
+  for (int j0 = 0; j0 < chunks; j0 += 32) {
+    float own = 0.f;
+    if (j0 + lane < chunks) {
+      const float2 ml = a.part_ml[first + (j0 + lane) * step];
+      own = exp2f((ml.x - ref) * a.scale_log2) * ml.y;
+    }
+    sum += own;
+    const int n = min(32, chunks - j0);
+#pragma unroll W > 1 ? 4 : 2
+    for (int j = W > 1 ? warp : 0; j < n; j += W) {
+      const float w = __shfl_sync(0xffffffffu, own, j);
+      const float* part = a.part_o + (first + (j0 + j) * step) * a.dim;
 #pragma unroll
-    for (int c = 0; c < C; ++c)
-      if (c * 32 + lane < a.dim) o[c] = fmaf(weight, part[c * 32 + lane], o[c]);
+      for (int c = 0; c < C; ++c)
+        if (c * 32 + lane < a.dim) o[c] = fmaf(w, part[c * 32 + lane], o[c]);
+    }
   }
+  sum = warp_sum(sum);
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   T* out = static_cast<T*>(a.out.data) + t * a.out.token_stride + h * a.out.head_stride;
   if (lane == 0 && (W == 1 || warp == 0) && a.lse)
-    a.lse[static_cast<int64_t>(t) * a.q.heads + h] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * kLn2;
+    a.lse[static_cast<int64_t>(t) * a.q.heads + h] = sum == 0.f ? -INFINITY : (ref * a.scale_log2 + log2f(sum)) * kLn2;
   if constexpr (W == 1) {
 #pragma unroll
     for (int c = 0; c < C; ++c)
@@ -318,7 +327,7 @@ struct Plan {
   int64_t q_pieces, k_pieces;
   int q_per, k_per;
   int64_t blocks;
-  int64_t lse_bytes, bytes;  // workspace: the logarithms, all of it
+  int64_t ml_bytes, bytes;  // workspace: the maxima and sums, all of it
 };
 
 int64_t pieces(const int32_t* off, int64_t total, int n, int unit, int most, int* per) {
@@ -401,12 +410,12 @@ Plan plan_attention(const moeca_attention_args& a) {
     if (chunk < longest) {
       const int64_t n = pieces(a.k_offsets, a.n_keys, a.n_seqs, static_cast<int>(chunk), 0x7fffffff, &p.k_per);
       const int64_t rows = n * p.max_q * a.q.heads;
-      const int64_t lse = (rows * 4 + 15) / 16 * 16, bytes = lse + rows * a.dim * 4;
+      const int64_t ml = (rows * 8 + 15) / 16 * 16, bytes = ml + rows * a.dim * 4;
       if (rows < kMaxWorkspace && bytes <= kMaxWorkspace) {
         p.chunk = static_cast<int>(chunk);
         p.k_pieces = n;
         p.blocks = n * p.tiles * heads;
-        p.lse_bytes = lse;
+        p.ml_bytes = ml;
         p.bytes = bytes;
       }
     }
@@ -482,8 +491,8 @@ moeca_status moeca_attention(const moeca_attention_args* a, void* stream) {
   d.ks = {a->k_offsets, static_cast<int>(nk), a->n_seqs, static_cast<int>(nk / a->n_seqs), p.chunk, p.k_per};
   d.q_pieces = p.q_pieces; d.k_pieces = p.k_pieces;
   d.lse = a->lse;
-  d.part_lse = static_cast<float*>(a->workspace);
-  d.part_o = reinterpret_cast<float*>(static_cast<uint8_t*>(a->workspace) + p.lse_bytes);
+  d.part_ml = static_cast<float2*>(a->workspace);
+  d.part_o = reinterpret_cast<float*>(static_cast<uint8_t*>(a->workspace) + p.ml_bytes);
   d.max_q = p.max_q; d.tiles = p.tiles;
   d.group = a->q.heads / a->k.heads;
   d.dim = dim; d.causal = a->causal; d.clear = a->clear;

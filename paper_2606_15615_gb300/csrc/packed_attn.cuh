@@ -2,9 +2,10 @@
 //
 // Every kernel works on (a tile of one sequence's query rows, a key head or query
 // head, and either all of the sequence's keys or one chunk of them).  Where the
-// key axis is cut into chunks, each chunk's kernel leaves its normalised result
-// and the base-2 logarithm of its sum in the workspace, and a last kernel joins
-// the chunks of a row in their order.
+// key axis is cut into chunks, each chunk's kernel leaves its normalised result,
+// its maximum and its sum in the workspace, and a last kernel joins
+// the chunks of a row in their order.  (Maximum and sum apart: in a logarithm of
+// the sum that holds both, a score of 2^20 leaves the sum three bits.)
 #pragma once
 
 #include <cuda_bf16.h>
@@ -65,7 +66,7 @@ struct PackedAttnArgs {
   int64_t q_pieces, k_pieces;
   float* lse;       // [queries, heads] or null
   float* part_o;    // [k_pieces, max_q, heads, dim]
-  float* part_lse;  // [k_pieces, max_q, heads], base 2
+  float2* part_ml;  // [k_pieces, max_q, heads]: the maximum of q . k, -infinity where no key is seen, and the sum
   int max_q;        // queries of a sequence that are computed
   int tiles;        // with chunks: tiles of max_q queries
   int group;        // query heads per key head

@@ -222,7 +222,7 @@ __global__ void __launch_bounds__(kRowsThreads, DK <= 4 ? 4 : 2) attn_rows_kerne
     const float lse2 = sum == 0.f ? -INFINITY : top * a.scale_log2 + log2f(sum);
     if (a.ks.unit) {
       const int64_t part = (static_cast<int64_t>(w.piece) * a.max_q + q_i) * a.q.heads + head;
-      if (c == 0) a.part_lse[part] = lse2;
+      if (c == 0) a.part_ml[part] = make_float2(top, sum);
       store_vec(a.part_o + part * a.dim + c, f);
       store_vec(a.part_o + part * a.dim + c + 4, f + 4);
     } else {

@@ -464,7 +464,7 @@ __global__ void __launch_bounds__(64 + 128 * NT, NT == 1 ? 2 : 1)
       __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out.data) + static_cast<int64_t>(w.q0 + query) * a.out.token_stride + head * a.out.head_stride;
       float* part_o = a.part_o + part * a.dim;
       if (live) {
-        if (cut) a.part_lse[part] = lse2;
+        if (cut) a.part_ml[part] = make_float2(m, l);
         else if (a.lse) a.lse[static_cast<int64_t>(w.q0 + query) * a.q.heads + head] = lse2 * kLn2;
       }
       uint32_t v[DK][16] = {};

@@ -28,8 +28,8 @@ def offsets(lengths):
     return torch.tensor(np.concatenate([[0], np.cumsum(lengths)]), dtype=torch.int32, device="cuda")
 
 
-def check(M, q_len, k_len, H, Hk, d, dtype, power, sign, order, by, causal):
-    """Scores of sign 2^power in base 2 (times 1, 2 and 3 along the keys, in the given order)."""
+def check(M, q_len, k_len, H, Hk, d, dtype, power, sign, order, by, causal, drift=0.0):
+    """Scores of sign 2^power in base 2 (times 1, 2 and 3 along the keys, in the given order); values that drift along the keys."""
     g = torch.Generator().manual_seed(d + power)
     product = 2.0 ** power / np.log2(np.e) / d ** 0.5  # |q k| of a channel, with scale d^-0.5
     scale = d ** -0.5
@@ -39,7 +39,8 @@ def check(M, q_len, k_len, H, Hk, d, dtype, power, sign, order, by, causal):
     factor = torch.cat([torch.tensor(order, dtype=torch.float32).repeat_interleave(-(-n // len(order)))[:n] for n in k_len])
     q = torch.full((sum(q_len), H, d), a).to(TYPES[dtype]).cuda()
     k = (factor[:, None, None] * (sign * b)).to(torch.bfloat16).expand(-1, Hk, d).contiguous().to(TYPES[dtype]).cuda()
-    v = torch.randn(sum(k_len), Hk, d, generator=g).to(TYPES[dtype]).cuda()
+    v = torch.randn(sum(k_len), Hk, d, generator=g) + drift * torch.linspace(-1, 1, sum(k_len))[:, None, None]
+    v = v.to(TYPES[dtype]).cuda()
     out, lse = M.attention(q, k, v, q_offsets=offsets(q_len), k_offsets=offsets(k_len), causal=causal, scale=scale, lse=True)
     got, got_lse, v6 = out.double().cpu().numpy(), lse.double().cpu().numpy(), v.double().cpu().numpy()
     key = k[:, 0, 0].double().cpu().numpy()
@@ -78,3 +79,18 @@ WHOLE = [([1], [250], 4, 2), ([40], [250], 4, 2), ([250], [255], 2, 2), ([200] *
     (40, 1, (1, 2), "values", True), (40, -1, (3, 2, 1), "scale", False), (100, 1, (1, 2), "scale", True)])
 def test_scores_beyond_the_exponent(M, q_len, k_len, H, Hk, d, dtype, power, sign, order, by, causal):
     check(M, q_len, k_len, H, Hk, d, dtype, power, sign, order, by, causal)
+
+
+# Key axes that are cut: chunks of different lengths, and rows (causal) that see a part of their last chunk.
+CUT = [([1], [5000], 4, 2), ([3, 1], [2600, 9001], 4, 1), ([40], [5000], 4, 2), ([300], [9001], 2, 2), ([17, 250], [700, 12000], 2, 1)]
+
+
+@pytest.mark.parametrize("q_len,k_len,H,Hk", CUT, ids=["one", "few", "tile", "tiles", "uneven"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [64, 72, 128])
+@pytest.mark.parametrize("power,sign,order,by,causal", [
+    (10, 1, (1,), "values", False), (16, -1, (1,), "scale", True), (20, 1, (1, 3, 2), "values", True), (24, -1, (1,), "values", False),
+    (31, 1, (1,), "scale", True), (34, 1, (1, 2), "values", False), (40, -1, (2, 1), "scale", True), (100, 1, (1,), "scale", False)])
+def test_chunks_are_joined_by_their_sums(M, q_len, k_len, H, Hk, d, dtype, power, sign, order, by, causal):
+    """The same score everywhere: a chunk weighs what its number of keys says, at any score."""
+    check(M, q_len, k_len, H, Hk, d, dtype, power, sign, order, by, causal, drift=2.0)
