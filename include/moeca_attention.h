@@ -100,7 +100,7 @@ typedef struct {
   int32_t causal;            /* 0 / 1                                                */
   int32_t clear;             /* 1: query tokens before q_offsets[0] and from
                                 q_offsets[n_seqs] on become 0 (lse -infinity)        */
-  float scale;               /* > 0                                                  */
+  float scale;               /* > 0, scale log2(e) at most fp32's largest value      */
 } moeca_attention_args;
 moeca_status moeca_attention(const moeca_attention_args* args, void* stream);
 /* Bytes that moeca_attention with these arguments works in (device pointers are

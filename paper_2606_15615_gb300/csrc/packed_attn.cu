@@ -1,6 +1,7 @@
 // Attention over packed sequences (include/moeca_attention.h): the call, its
 // choice of kernel, the CUDA-core kernel and the join of key chunks.
 #include <algorithm>
+#include <cmath>
 
 #include "common.cuh"
 #include "moeca_probe.h"
@@ -434,7 +435,8 @@ const char* bad_attention(const moeca_attention_args& a) {
   if (a.q.heads < 1 || a.k.heads < 1 || a.q.heads % a.k.heads || a.v.heads != a.k.heads || a.out.heads != a.q.heads)
     return "q.heads must be a multiple of k.heads = v.heads, and out.heads = q.heads";
   if (a.causal < 0 || a.causal > 1 || a.clear < 0 || a.clear > 1) return "causal and clear must be 0 or 1";
-  if (!(a.scale > 0) || a.scale > 3e38f) return "scale must be positive and finite";
+  // The kernels take it in base 2, where an infinite one would make NaN of a score of 0.
+  if (!(a.scale > 0) || !std::isfinite(a.scale * kLog2e)) return "scale must be positive, and scale log2(e) finite";
   if (const char* why = bad_heads(a.q, a.n_queries, a.dim, a.dtype, false)) return why;
   if (const char* why = bad_heads(a.k, a.n_keys, a.dim, a.dtype, false)) return why;
   if (const char* why = bad_heads(a.v, a.n_keys, a.dim, a.dtype, false)) return why;

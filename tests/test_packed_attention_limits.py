@@ -1,0 +1,36 @@
+"""Limits of the packed attention's arguments, checked on the host: no GPU, and nothing is launched."""
+import math
+
+import pytest
+
+from paper_2606_15615_gb300 import build
+
+A = 1 << 20  # device addresses that are never read: megabytes apart
+
+
+@pytest.fixture(scope="module")
+def M():
+    build.build()
+    from paper_2606_15615_gb300 import moeca
+    return moeca
+
+
+def args(M, n_queries=0, n_keys=50, n_seqs=1, H=4, Hk=2, d=64, dtype=None, max_q=0, causal=1, offsets=False, scale=0.125):
+    h = M.moeca_heads
+    return M.moeca_attention_args(
+        h(16 * A, H * d, d, H), h(1 << 40, 2 * Hk * d, d, Hk), h((1 << 40) + 2 * Hk * d, 2 * Hk * d, d, Hk), h(1 << 41, H * d, d, H),
+        A if offsets else None, 2 * A if offsets else None, None, 1 << 42, None, n_queries, n_keys, n_seqs, max_q,
+        M.MOECA_BF16 if dtype is None else dtype, d, causal, 0, scale)
+
+
+@pytest.mark.parametrize("scale", [2.36e38, 3e38, 3.4e38, math.inf, math.nan, 0.0, -1e-3])
+def test_scales_without_a_finite_base_2_form_are_refused(M, scale):
+    with pytest.raises(M.MoecaError, match="scale") as e:
+        M.moeca_attention(args(M, scale=scale))
+    assert e.value.status == M.MOECA_ERR_INVALID_ARG and M.moeca_attention_workspace(args(M, scale=scale)) == -1
+
+
+@pytest.mark.parametrize("scale", [2.35e38, 1.0, 1e-45])
+def test_scales_up_to_the_largest_are_taken(M, scale):
+    M.moeca_attention(args(M, scale=scale))
+    assert M.moeca_attention_workspace(args(M, scale=scale)) == 0
