@@ -396,7 +396,8 @@ __global__ void __launch_bounds__(64 + 128 * NT, NT == 1 ? 2 : 1)
 #pragma unroll
         for (int u = 0; u < 4; ++u)
           top[u] = max3(top[u], __uint_as_float(sv[q + 2 * u]), __uint_as_float(sv[q + 2 * u + 1]));
-      const float cand = fmaxf(m, max3(fmaxf(top[0], top[1]), top[2], top[3]));
+      // Rows of no query hold other sequences' queries or what shared memory held: they have no say in the votes.
+      const float cand = live ? fmaxf(m, max3(fmaxf(top[0], top[1]), top[2], top[3])) : 0.f;
       // P = 2^((s - m) sc).  Fused as s sc - fl(m sc), the rounding of m sc stays in every exponent and changes with m:
       // 2^-17 at most while |m sc| is below kFusedMost, but whole powers of two (P infinite, or 0 in every column) for
       // scores of 2^31.  Where a row of the warp is beyond the limit the difference is formed first, so that s = m
