@@ -67,8 +67,9 @@ moeca_status moeca_qk_norm_rope(const moeca_qk_norm_rope_args* args, void* strea
  * Sequence b's queries are tokens q_offsets[b] .. q_offsets[b + 1] - 1, its keys
  * k_offsets[b] .. k_offsets[b + 1] - 1; offsets ascend and are clamped to the
  * tokens there are.  Without offsets all sequences are equally long.  Query
- * tokens of no sequence keep what out and lse hold, unless `clear` is set; so do
- * a sequence's queries behind its first max_q.
+ * tokens that are not computed keep what out and lse hold, unless `clear` says
+ * otherwise: those of no sequence (before q_offsets[0], from q_offsets[n_seqs]
+ * on), and a sequence's behind its first max_q.
  *
  * Scores, softmax statistics and sums are fp32 (the exponential's argument in
  * base 2; a row's highest score gives 0 within 2^-17, whatever its size); with bf16 values p is rounded to bf16 before it meets v, the sum of p
@@ -98,8 +99,8 @@ typedef struct {
   int32_t dtype;             /* moeca_dtype of q, k, v and out                       */
   int32_t dim;               /* values per head, 1 .. 256                            */
   int32_t causal;            /* 0 / 1                                                */
-  int32_t clear;             /* 1: query tokens before q_offsets[0] and from
-                                q_offsets[n_seqs] on become 0 (lse -infinity)        */
+  int32_t clear;             /* 1: query tokens that are not computed become 0 (lse
+                                -infinity); 2: only their lse is written; 0: nothing */
   float scale;               /* > 0, scale log2(e) at most fp32's largest value      */
 } moeca_attention_args;
 moeca_status moeca_attention(const moeca_attention_args* args, void* stream);

@@ -69,13 +69,13 @@ __device__ __forceinline__ float group16_sum(float v) {
 }
 
 template <typename T, int BQ, int DC>  // DC: channels in 64s
-__global__ void __launch_bounds__(kSimtThreads) attn_simt_kernel(const PackedAttnArgs a, const bool vec) {
+__global__ void __launch_bounds__(kSimtThreads) attn_simt_kernel(const __grid_constant__ PackedAttnArgs a, const bool vec) {
   constexpr int R = BQ / 16;
   extern __shared__ float4 smem4[];
   pdl_entry();
   const int index = blockIdx.x / static_cast<uint32_t>(a.q.heads), h = blockIdx.x - index * a.q.heads;
   const AttnWork w = attn_work(a, index);
-  clear_rest<T>(a, threadIdx.x, blockDim.x);
+  clear_rest<T>(a, w, index, h, a.q.heads, threadIdx.x, kSimtThreads);
   if (!w.any) return;
   const int dim = a.dim, pitch = simt_pitch(dim);
   float* sq = reinterpret_cast<float*>(smem4);
@@ -434,7 +434,8 @@ const char* bad_attention(const moeca_attention_args& a) {
   if (!a.k_offsets && a.n_keys % a.n_seqs) return "n_keys must be a multiple of n_seqs without k_offsets";
   if (a.q.heads < 1 || a.k.heads < 1 || a.q.heads % a.k.heads || a.v.heads != a.k.heads || a.out.heads != a.q.heads)
     return "q.heads must be a multiple of k.heads = v.heads, and out.heads = q.heads";
-  if (a.causal < 0 || a.causal > 1 || a.clear < 0 || a.clear > 1) return "causal and clear must be 0 or 1";
+  if (a.causal < 0 || a.causal > 1) return "causal must be 0 or 1";
+  if (a.clear < 0 || a.clear > 2) return "clear must be 0, 1 or 2";
   // The kernels take it in base 2, where an infinite one would make NaN of a score of 0.
   if (!(a.scale > 0) || !std::isfinite(a.scale * kLog2e)) return "scale must be positive, and scale log2(e) finite";
   if (const char* why = bad_heads(a.q, a.n_queries, a.dim, a.dtype, false)) return why;

@@ -68,10 +68,11 @@ struct PackedAttnArgs {
   float* part_o;    // [k_pieces, max_q, heads, dim]
   float2* part_ml;  // [k_pieces, max_q, heads]: the maximum of q . k, -infinity where no key is seen, and the sum
   int max_q;        // queries of a sequence that are computed
-  int tiles;        // with chunks: tiles of max_q queries
+  int tiles;        // tiles of max_q queries
   int group;        // query heads per key head
   int dim;
-  int causal, clear;
+  int causal;
+  int clear;        // what becomes of query tokens that are not computed: 0 nothing, 1 out and lse, 2 lse
   float scale_log2; // scale log2(e)
   int32_t* status;
   // How long a bounded wait lasts, and the barrier whose wait is to run out (tests; see
@@ -124,20 +125,49 @@ __device__ __forceinline__ int visible_keys(const PackedAttnArgs& a, const AttnW
   return a.causal ? min(max(i + 1 - w.nq + w.nk, 0), w.nk) : w.nk;
 }
 
-// Query tokens before the first and behind the last sequence become 0: the blocks
-// take them in turn, `threads` of a block's threads each.
+// Query tokens that are not computed: their rows become 0 (clear 1), the logs of their sums -infinity.
+// Those before the first and behind the last sequence: the blocks take them in turn.  A sequence's
+// behind its first max_q: its own blocks do.  index: as for attn_work; head: of the `heads` that a tile has a block for;
+// `threads` of the block's threads, whole warps, share a token.  A call: rare, and its loops would cost the kernels
+// registers.
 template <typename T>
-__device__ __forceinline__ void clear_rest(const PackedAttnArgs& a, int thread, int threads) {
-  if (!a.clear || !a.qs.off) return;
-  const int lo = a.qs.start(0), hi = max(a.qs.start(a.qs.n), lo), rest = lo + a.qs.total - hi;
-  for (int64_t r = blockIdx.x; r < rest; r += gridDim.x) {
-    const int64_t t = r < lo ? r : hi + (r - lo);
-    T* out = static_cast<T*>(a.out.data) + t * a.out.token_stride;
-    for (int h = 0; h < a.out.heads; ++h)
-      for (int c = thread; c < a.dim; c += threads) out[h * a.out.head_stride + c] = T(0.f);
-    if (a.lse)
-      for (int h = thread; h < a.out.heads; h += threads) a.lse[t * a.out.heads + h] = -INFINITY;
+__device__ __noinline__ void clear_tokens(const PackedAttnArgs& a, int index, int head, int heads, int thread, int threads) {
+  const auto clear = [&](int64_t first, int64_t step, int64_t end) {
+    for (int64_t t = first; t < end; t += step) {
+      if (a.clear == 1) {
+        T* out = static_cast<T*>(a.out.data) + t * a.out.token_stride;
+        for (int h = 0; h < a.out.heads; ++h)
+          for (int c = thread; c < a.dim; c += threads) out[h * a.out.head_stride + c] = T(0.f);
+      }
+      if (a.lse)
+        for (int h = thread; h < a.out.heads; h += threads) a.lse[t * a.out.heads + h] = -INFINITY;
+    }
+  };
+  if (a.qs.off) {
+    const int lo = a.qs.start(0), hi = max(a.qs.start(a.qs.n), lo);
+    clear(blockIdx.x, gridDim.x, lo);
+    clear(static_cast<int64_t>(hi) + blockIdx.x, gridDim.x, a.qs.total);
   }
+  int b, tile, chunk = 0, chunks = 1;
+  if (a.ks.unit == 0) {
+    b = a.qs.find(index);
+    tile = index - a.qs.base(b);
+  } else {
+    const int piece = static_cast<int>(static_cast<uint32_t>(index) / static_cast<uint32_t>(a.tiles));
+    b = a.ks.find(piece);
+    tile = index - piece * a.tiles;
+    chunk = piece - a.ks.base(b);
+    chunks = max((a.ks.length(b) - 1) / a.ks.unit + 1, 1);  // a sequence without keys still has its first chunk's block
+  }
+  if (tile < 0 || tile >= a.tiles || chunk < 0 || chunk >= chunks) return;
+  const int64_t share = (static_cast<int64_t>(chunk) * a.tiles + tile) * heads + head, first = a.qs.start(b);
+  clear(first + a.max_q + share, static_cast<int64_t>(chunks) * a.tiles * heads, first + a.qs.length(b));
+}
+template <typename T>
+__device__ __forceinline__ void clear_rest(const PackedAttnArgs& a, const AttnWork& w, int index, int head, int heads, int thread,
+                                           int threads) {
+  if (a.clear && (w.nq > a.max_q || (a.qs.off && (a.qs.start(0) > 0 || a.qs.start(a.qs.n) < a.qs.total))))
+    clear_tokens<T>(a, index, head, heads, thread, threads);
 }
 
 cudaError_t launch_attn_simt(const PackedAttnArgs& a, int dtype, int tile, cudaStream_t s);

@@ -53,14 +53,14 @@ __device__ __forceinline__ void ldsm_x4_trans(uint32_t addr, uint32_t* r) {
 }
 
 template <int DK>
-__global__ void __launch_bounds__(kRowsThreads, DK <= 4 ? 4 : 2) attn_rows_kernel(const PackedAttnArgs a) {
+__global__ void __launch_bounds__(kRowsThreads, DK <= 4 ? 4 : 2) attn_rows_kernel(const __grid_constant__ PackedAttnArgs a) {
   using Sh = RowsShape<DK>;
   extern __shared__ __align__(16) uint8_t rows_smem[];
   __shared__ float sh_m[kRowsWarps][16], sh_l[kRowsWarps][16];
   pdl_entry();
-  clear_rest<__nv_bfloat16>(a, threadIdx.x, blockDim.x);
   const int index = blockIdx.x / static_cast<uint32_t>(a.k.heads), kvh = blockIdx.x - index * a.k.heads;
   const AttnWork w = attn_work(a, index);
+  clear_rest<__nv_bfloat16>(a, w, index, kvh, a.k.heads, threadIdx.x, kRowsThreads);
   if (!w.any) return;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int G = a.group, n_q = min(w.nq, a.max_q), rows = n_q * G;

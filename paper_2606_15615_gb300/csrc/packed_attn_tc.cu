@@ -134,7 +134,7 @@ __device__ __forceinline__ int place_of_v(int j, int blocks) { return j + 1 < bl
 template <int DK, int NT>
 __global__ void __launch_bounds__(64 + 128 * NT, NT == 1 ? 2 : 1)
     attn_packed_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
-                          const __grid_constant__ CUtensorMap vmap, const PackedAttnArgs a) {
+                          const __grid_constant__ CUtensorMap vmap, const __grid_constant__ PackedAttnArgs a) {
   using Sh = TcShape<DK, NT>;
   constexpr int ST = Sh::STAGES;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
@@ -173,9 +173,10 @@ __global__ void __launch_bounds__(64 + 128 * NT, NT == 1 ? 2 : 1)
   pdl_entry();
   // The heaviest tiles of a causal sequence are its last: they start first.
   const int turn = blockIdx.x / static_cast<uint32_t>(a.k.heads), kvh = blockIdx.x - turn * a.k.heads;
-  const AttnWork w = attn_work(a, a.causal && !a.ks.unit ? static_cast<int>(a.q_pieces) - 1 - turn : turn);
+  const int index = a.causal && !a.ks.unit ? static_cast<int>(a.q_pieces) - 1 - turn : turn;
+  const AttnWork w = attn_work(a, index);
   if (!w.any) {  // uniform over the CTA, before TMEM is taken
-    clear_rest<__nv_bfloat16>(a, threadIdx.x, blockDim.x);
+    clear_rest<__nv_bfloat16>(a, w, index, kvh, a.k.heads, threadIdx.x, blockDim.x);
     return;
   }
   const int G = a.group, per_tile = a.qs.unit / NT;  // queries of a tile
@@ -261,7 +262,7 @@ __global__ void __launch_bounds__(64 + 128 * NT, NT == 1 ? 2 : 1)
         give_up(711);
       }
     }
-    clear_rest<__nv_bfloat16>(a, lane, 32);
+    clear_rest<__nv_bfloat16>(a, w, index, kvh, a.k.heads, lane, 32);
   } else if (warp == 1) {
     // All lanes run the loop and one issues; what the loop turns on is read from
     // lane 0, so that the compiler knows it to be the same in all and keeps the

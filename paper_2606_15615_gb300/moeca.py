@@ -1206,8 +1206,9 @@ def attention(q, k, v, q_offsets=None, k_offsets=None, n_seqs: int = None, causa
     many as the other offsets say).  ``causal``: the last query of a sequence sees its last key, each earlier one a key
     less.  ``scale``: d^-0.5 by default.  ``max_q``: the longest query, if known (queries behind a sequence's first max_q are
     not computed).  ``lse``: True or a [Tq, H] fp32 tensor also gives the log of the sum of exponentials.  A row that
-    sees no key is 0 with lse = -inf.  ``out`` may be q; query tokens before the first and behind the last sequence keep
-    what a given ``out`` holds and are 0 (lse -inf) with a new one.  ``status``: as for q8_matmul; ``stream``: as for q8_read.  Returns out, or
+    sees no key is 0 with lse = -inf.  ``out`` may be q; query tokens that are not computed (before the first and behind the
+    last sequence, and behind a sequence's first max_q) keep what a given ``out`` holds and are 0 with a new one; their lse
+    is -inf, and kept where both tensors are given.  ``status``: as for q8_matmul; ``stream``: as for q8_read.  Returns out, or
     (out, lse)."""
     dev = q.get_device()
     fq, n_q, dim, code = _head_fields(q, "q", dev)
@@ -1224,8 +1225,8 @@ def attention(q, k, v, q_offsets=None, k_offsets=None, n_seqs: int = None, causa
     n_seqs = 1 if n_seqs is None else n_seqs
     torch = _TYPES["torch"]
     offs = _list(q_offsets, "i32", (n_seqs + 1,), "q_offsets", dev), _list(k_offsets, "i32", (n_seqs + 1,), "k_offsets", dev)
-    clear = out is None
-    if clear:
+    clear = 1 if out is None else 2 if lse is True else 0  # tokens that are not computed: new tensors are whole
+    if out is None:
         out = _on(stream, dev, lambda: torch.empty(q.shape, dtype=q.dtype, device=q.device))
     fo, n_o, o_dim, o_code = _head_fields(out, "out", dev)
     if n_o != n_q or o_dim != dim or o_code != code or fo[3] != fq[3]:

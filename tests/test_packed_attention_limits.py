@@ -34,3 +34,14 @@ def test_scales_without_a_finite_base_2_form_are_refused(M, scale):
 def test_scales_up_to_the_largest_are_taken(M, scale):
     M.moeca_attention(args(M, scale=scale))
     assert M.moeca_attention_workspace(args(M, scale=scale)) == 0
+
+
+@pytest.mark.parametrize("clear", [-1, 3, 1 << 30])
+def test_what_clear_may_be(M, clear):
+    bad = args(M)
+    bad.clear = clear
+    with pytest.raises(M.MoecaError, match="clear"):
+        M.moeca_attention(bad)
+    for good in (0, 1, 2):
+        bad.clear = good
+        M.moeca_attention(bad)
