@@ -34,7 +34,7 @@ typedef struct {
  * pair i being (y[i], y[i + rot / 2]), or (y[2 i], y[2 i + 1]) with `pairs`.
  * All in fp32, rounded once; heads whose sum of squares passes fp32's largest value
  * become 0.  A token whose position is outside
- * [0, n_positions) is left out: nothing is written for it.  q_out and k_out may
+ * [0, n_positions) is left out: nothing is written for it, or zeros (`clear`).  q_out and k_out may
  * be q and k themselves (same base and strides).  With rot = 0 positions are not
  * looked at. */
 typedef struct {
@@ -53,6 +53,8 @@ typedef struct {
   int32_t rot;             /* values turned, even, 0 .. dim                          */
   int32_t pairs;           /* 0 / 1                                                  */
   float eps;               /* >= 0                                                   */
+  int32_t clear;           /* results in which tokens that are left out become 0: the sum
+                              of 1 (q_out) and 2 (k_out), or 0                       */
 } moeca_qk_norm_rope_args;
 moeca_status moeca_qk_norm_rope(const moeca_qk_norm_rope_args* args, void* stream);
 

@@ -25,6 +25,7 @@ struct QkArgs {
   int per;     // heads that a group of lanes takes one after another
   int parts;   // groups per token
   float eps, inv_dim;
+  int clear;   // results whose tokens without a position become 0: 1 of q, 2 of k
   bool table16, weight16;  // rows of the table, the weights' chunks can be read 16 bytes at a time
 };
 
@@ -137,6 +138,20 @@ __global__ void __launch_bounds__(kQkThreads, U > 1 ? 1 : W == 8 ? 3 : 5) qk_nor
     } else if (i < units) {
       lo[u] = a.rot + 2 * W * (i - turned);
       hi[u] = min(lo[u] + W, a.dim);
+    }
+  }
+  if (a.clear && !on && in_warp < per_warp && t < a.T) {  // a token without a position
+    const float zeros[W] = {};
+    for (int h = part * a.per; h < min((part + 1) * a.per, a.q.heads + a.k.heads); ++h) {
+      const bool is_q = h < a.q.heads;
+      if (!(a.clear & (is_q ? 1 : 2))) continue;
+      const Heads& out = is_q ? a.q_out : a.k_out;
+      T* z = static_cast<T*>(out.data) + t * out.token_stride + (is_q ? h : h - a.q.heads) * out.head_stride;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (lo[u] < a.dim) Chunk<T, W>::store(z + lo[u], zeros);
+        if (hi[u] < a.dim) Chunk<T, W>::store(z + hi[u], zeros);
+      }
     }
   }
   float weight[U][2][W];
@@ -271,6 +286,7 @@ extern "C" moeca_status moeca_qk_norm_rope(const moeca_qk_norm_rope_args* a, voi
   if (a->rot < 0 || a->rot > a->dim || a->rot % 2) return refuse("rot must be even, 0 .. dim");
   if (!(a->eps >= 0)) return refuse("eps must not be negative");
   if (a->pairs < 0 || a->pairs > 1) return refuse("pairs must be 0 or 1");
+  if (a->clear < 0 || a->clear > 3) return refuse("clear must be 0 .. 3");
   if (a->n_positions < 0 || a->n_positions > kMaxRows) return refuse("n_positions out of range");
   const int64_t T = a->n_tokens, es = elem_size(a->dtype);
   const int dim = a->dim;
@@ -299,7 +315,7 @@ extern "C" moeca_status moeca_qk_norm_rope(const moeca_qk_norm_rope_args* a, voi
   d.q_weight = a->q_weight; d.k_weight = a->k_weight;
   d.table = reinterpret_cast<const float2*>(a->table);
   d.pos = a->pos; d.n_pos = a->n_positions;
-  d.T = a->n_tokens; d.dim = dim; d.rot = a->rot; d.eps = a->eps; d.inv_dim = 1.f / static_cast<float>(dim);
+  d.T = a->n_tokens; d.dim = dim; d.rot = a->rot; d.eps = a->eps; d.clear = a->clear; d.inv_dim = 1.f / static_cast<float>(dim);
   // Chunks of 16 bytes, of 8, or single values.
   int w = static_cast<int>(16 / es);
   const auto fits = [&](int n) {

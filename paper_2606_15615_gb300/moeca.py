@@ -172,7 +172,7 @@ class moeca_qk_norm_rope_args(C.Structure):
     _fields_ = [("q", moeca_heads), ("k", moeca_heads), ("q_out", moeca_heads), ("k_out", moeca_heads),
                 ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("table", C.c_void_p), ("pos", C.c_void_p),
                 ("n_positions", C.c_int64), ("dtype", C.c_int32), ("n_tokens", C.c_int32), ("dim", C.c_int32),
-                ("rot", C.c_int32), ("pairs", C.c_int32), ("eps", C.c_float)]
+                ("rot", C.c_int32), ("pairs", C.c_int32), ("eps", C.c_float), ("clear", C.c_int32)]
 
 
 class moeca_attention_args(C.Structure):
@@ -982,7 +982,7 @@ _PACK_ROWS = struct.Struct("@QqQqqQQiiii")
 _PACK_BACK = struct.Struct("@QqqQQQqQqiiii")
 _PACK_BACK_GRAD = struct.Struct("@QqQqqQQQQqQiiii")
 _HEADS = "Qqqi4x"
-_PACK_QK = struct.Struct("@" + 4 * _HEADS + "QQQQqiiiiif")
+_PACK_QK = struct.Struct("@" + 4 * _HEADS + "QQQQqiiiiifi")
 _PACK_ATTENTION = struct.Struct("@" + 4 * _HEADS + "QQQQQqqiiiiiif")
 for _s, _t in ((_PACK_SORT, moeca_expert_sort_args), (_PACK_ROWS, moeca_expert_rows_args),
                (_PACK_BACK, moeca_expert_combine_args), (_PACK_BACK_GRAD, moeca_expert_combine_grad_args),
@@ -1163,7 +1163,8 @@ def qk_norm_rope(q, k, table=None, q_weight=None, k_weight=None, pos=None, eps: 
     projection, say), times ``q_weight`` / ``k_weight`` [d] fp32 (None: 1), and the rotation of the first 2 P values by
     ``table`` [positions, P, 2] fp32 (cosines and sines, see rope_table; None: no rotation).  Pair i is (i, i + P), or
     (2 i, 2 i + 1) with ``pairs``.  ``pos`` [T] int32: the tokens' rows of the table (None: their numbers); a token whose
-    position is outside it is left out.  ``q_out`` and ``k_out`` may be q and k.  ``stream``: as for q8_read.  Returns
+    position is outside it is left out: a new result is 0 there, a given one keeps what it holds.  ``q_out`` and ``k_out`` may
+    be q and k.  ``stream``: as for q8_read.  Returns
     (q_out, k_out)."""
     dev = q.get_device()
     fq, T, dim, code = _head_fields(q, "q", dev)
@@ -1190,10 +1191,11 @@ def qk_norm_rope(q, k, table=None, q_weight=None, k_weight=None, pos=None, eps: 
         t_address = _list(table, "f32", table.shape, "table", dev)
     p_address = _list(pos, "i32", (T,), "pos", dev)
     w = _list(q_weight, "f32", (dim,), "q_weight", dev), _list(k_weight, "f32", (dim,), "k_weight", dev)
+    clear = (q_out is None) + 2 * (k is not None and k_out is None)
     q_out, fq_out = result(q_out, q, fq, "q_out")
     if k is not None:
         k_out, fk_out = result(k_out, k, fk, "k_out")
-    args = _PACK_QK.pack(*fq, *fk, *fq_out, *fk_out, *w, t_address, p_address, n_pos, code, T, dim, rot, bool(pairs), eps)
+    args = _PACK_QK.pack(*fq, *fk, *fq_out, *fk_out, *w, t_address, p_address, n_pos, code, T, dim, rot, bool(pairs), eps, clear)
     _call(_packed["moeca_qk_norm_rope"], args, dev, stream)
     return q_out, k_out
 

@@ -79,3 +79,34 @@ def test_attention_in_place_keeps_its_queries(M, max_q):
     done = torch.zeros(100, dtype=torch.bool)
     done[5:5 + max_q] = done[65:65 + max_q] = True
     assert torch.equal(own[~done], q[~done]) and not bool((own[done.cuda()] == q[done.cuda()]).all(-1).any())
+
+
+@pytest.mark.parametrize("T,H,Hk,d,rot", [(40, 3, 2, 64, 64), (40, 3, 2, 72, 36), (9, 1, 1, 5, 2), (33, 2, 2, 512, 512), (2000, 16, 8, 128, 96),
+                                          (3, 2, 1, 511, 254)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("pairs", [False, True])
+@pytest.mark.parametrize("new_q,new_k", [(True, True), (True, False), (False, True), (False, False)])
+def test_norm_of_tokens_without_a_position(M, T, H, Hk, d, rot, dtype, pairs, new_q, new_k):
+    g = torch.Generator().manual_seed(T)
+    q, k = (torch.randn(T, h, d, generator=g).to(TYPES[dtype]).cuda() for h in (H, Hk))
+    table = M.rope_table(torch.arange(20), rot).cuda()
+    pos = torch.randint(-15, 35, (T,), generator=g).to(torch.int32)
+    out = ((pos < 0) | (pos >= 20)).cuda()
+    pos = pos.cuda()
+    given_q, given_k = torch.full_like(q, 5.0), torch.full_like(k, 5.0)
+    poison(q, k)
+    got = M.qk_norm_rope(q, k, table, pos=pos, pairs=pairs, eps=0.0, q_out=None if new_q else given_q, k_out=None if new_k else given_k)
+    want = M.qk_norm_rope(q, k, table, pos=pos.clamp(0, 19), pairs=pairs, eps=0.0)
+    for x, w, new in zip(got, want, (new_q, new_k)):
+        assert torch.equal(x[~out], w[~out]) and bool((x[out] == (0.0 if new else 5.0)).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_norm_behind_a_short_table(M, dtype):
+    q = torch.randn(30, 2, 48, device="cuda").to(TYPES[dtype])
+    poison(q)
+    y, _ = M.qk_norm_rope(q, None, M.rope_table(torch.arange(11), 48).cuda())  # the tokens' numbers are the positions
+    assert bool((y[11:] == 0).all()) and bool(y[:11].isfinite().all()) and not bool((y[:11] == 0).all(-1).any())
+    poison(q)
+    z, _ = M.qk_norm_rope(q, q.clone(), torch.empty(0, 24, 2, device="cuda"))
+    assert bool((z == 0).all())

@@ -45,3 +45,15 @@ def test_what_clear_may_be(M, clear):
     for good in (0, 1, 2):
         bad.clear = good
         M.moeca_attention(bad)
+
+
+@pytest.mark.parametrize("clear", [-1, 4, 1 << 30])
+def test_what_the_norm_may_clear(M, clear):
+    h = M.moeca_heads
+    bad = M.moeca_qk_norm_rope_args(h(16 * A, 512, 64, 4), h(17 * A, 512, 64, 2), h(18 * A, 256, 64, 4), h(19 * A, 128, 64, 2), A, 2 * A,
+                                    3 * A, 4 * A, 50, M.MOECA_BF16, 0, 64, 64, 0, 1e-6, clear)
+    with pytest.raises(M.MoecaError, match="clear"):
+        M.moeca_qk_norm_rope(bad)
+    for good in range(4):
+        bad.clear = good
+        M.moeca_qk_norm_rope(bad)
