@@ -209,13 +209,12 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const PackedAtt
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t row = W > 1 ? blockIdx.x : blockIdx.x * kJoinWarps + warp;
   const int t = row / static_cast<uint32_t>(a.q.heads), h = row - t * a.q.heads;
-  // Offsets are the caller's: the kernel before this one only writes the workspace.
+  pdl_entry();
   const bool some = t < a.qs.total;
   const int b = some ? a.qs.owner(t) : 0, i = some ? t - a.qs.start(b) : -1;
   const bool mine = i >= 0 && i < min(a.qs.length(b), a.max_q);
   const int chunks = static_cast<int>((static_cast<uint32_t>(a.ks.length(b)) + a.ks.unit - 1) / a.ks.unit);
   const int64_t first = (static_cast<int64_t>(a.ks.base(b)) * a.max_q + i) * a.q.heads + h, step = static_cast<int64_t>(a.max_q) * a.q.heads;
-  pdl_entry();
   if (!mine) return;
   float m = -INFINITY;
   for (int j = lane; j < chunks; j += 32) m = fmaxf(m, a.part_ml[first + j * step].x);

@@ -46,3 +46,39 @@ def test_rows_do_not_depend_on_what_shared_memory_held(M, H, d):
         M.attention(fill[0], fill[1], torch.full_like(fill[2], value), n_seqs=320)  # results leave through shared memory
         res.append(M.attention(q, k, v))
     assert all(torch.equal(r, res[0]) for r in res) and bool(res[0].isfinite().all())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("most", [3, 40, 300])
+def test_offsets_written_right_before_the_call(M, dtype, most):
+    """Offsets that a kernel of the same graph writes before the call, others in every replay; the key axis is cut."""
+    n, keys, B = 3 * most, 20_000, 3
+    q, k, v = qkv(most, n, keys, 4, 2, 64, dtype)
+    rng = np.random.default_rng(most)
+
+    def cuts(total, longest):
+        while True:
+            c = np.concatenate([[0], np.sort(rng.integers(0, total + 1, B - 1)), [total]])
+            if np.diff(c).max() <= longest:
+                return torch.tensor(c, dtype=torch.int32, device="cuda")
+
+    source = [torch.zeros(B + 1, dtype=torch.int32, device="cuda") for _ in range(2)]
+    off = [torch.zeros_like(s) for s in source]
+
+    def step():
+        for a, b in zip(off, source):
+            torch.add(b, 0, out=a)
+        return M.attention(q, k, v, q_offsets=off[0], k_offsets=off[1], causal=True, max_q=most, lse=True)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out, lse = step()
+    for _ in range(6):
+        new = [cuts(n, most), cuts(keys, keys)]
+        for s, c in zip(source, new):
+            s.copy_(c)
+        graph.replay()
+        want = M.attention(q, k, v, q_offsets=new[0], k_offsets=new[1], causal=True, max_q=most, lse=True)
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
