@@ -17,12 +17,14 @@
  *
  * moeca_probe_q8_stall lets a bounded wait of the 8-bit calls run out, so that
  * tests see what a caller sees then; moeca_probe_attention_stall one of the
- * packed attention's.
+ * packed attention's.  moeca_probe_attention_form says which of its kernels takes a call.
  */
 #ifndef MOECA_PROBE_H_
 #define MOECA_PROBE_H_
 
 #include <stdint.h>
+
+#include "moeca_attention.h"
 
 #ifdef __cplusplus
 extern "C" {
@@ -100,6 +102,18 @@ typedef enum {
   MOECA_ATTENTION_SLOTS = 4
 } moeca_probe_attention_barrier;
 int32_t moeca_probe_attention_stall(int32_t barrier, int64_t wait_ns);
+
+/* How moeca_attention carries out a call with these arguments (device pointers are
+ * not looked at but for their alignment): the kernel, and in *chunk (may be
+ * NULL) the keys of a chunk where the key axis is cut, else 0.  -1: a NULL argument,
+ * or sizes, types or strides that moeca_attention refuses. */
+typedef enum {
+  MOECA_ATTENTION_FORM_CORES = 0, /* CUDA cores                                          */
+  MOECA_ATTENTION_FORM_ROWS = 1,  /* a fragment of 16 (query, head) rows                 */
+  MOECA_ATTENTION_FORM_TILE = 2,  /* a tile of 128 rows a block                          */
+  MOECA_ATTENTION_FORM_TILES = 3  /* two tiles a block                                   */
+} moeca_probe_attention_forms;
+int32_t moeca_probe_attention_form(const moeca_attention_args* args, int32_t* chunk);
 
 /* Tensor maps (TMA descriptors) this process has encoded, on any thread: host
  * work, done once per handle for its own buffers. */

@@ -512,6 +512,16 @@ moeca_status moeca_attention(const moeca_attention_args* a, void* stream) {
   });
 }
 
+int32_t moeca_probe_attention_form(const moeca_attention_args* a, int32_t* chunk) {
+  using namespace moeca;
+  if (chunk) *chunk = 0;
+  if (!a || bad_attention(*a) || a->n_queries > kMaxTokens || a->n_keys > kMaxTokens || a->n_queries == 0) return -1;
+  const Plan p = plan_attention(*a);
+  if (chunk) *chunk = p.chunk;
+  return p.rows == 2 ? MOECA_ATTENTION_FORM_TILES : p.rows == 1 ? MOECA_ATTENTION_FORM_TILE
+                     : p.rows < 0 ? MOECA_ATTENTION_FORM_ROWS : MOECA_ATTENTION_FORM_CORES;
+}
+
 int32_t moeca_probe_attention_stall(int32_t barrier, int64_t wait_ns) {
   using namespace moeca;
   if (barrier < MOECA_ATTENTION_NONE || barrier > MOECA_ATTENTION_SLOTS || wait_ns < 1000000 || wait_ns > 1000000000) return -1;

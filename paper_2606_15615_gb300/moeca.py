@@ -33,6 +33,8 @@ ATTN_SYNC, ATTN_STALE, ATTN_FULL = 0, 1, 2
 MOECA_E4M3, MOECA_E5M2 = 2, 3
 MOECA_Q8_NONE, MOECA_Q8_COPIES, MOECA_Q8_OPERANDS, MOECA_Q8_SCALES, MOECA_Q8_ACCUMULATORS = 0, 1, 2, 3, 4
 MOECA_ATTENTION_NONE, MOECA_ATTENTION_COPIES, MOECA_ATTENTION_SCORES, MOECA_ATTENTION_WEIGHTS, MOECA_ATTENTION_SLOTS = range(5)
+(MOECA_ATTENTION_FORM_CORES, MOECA_ATTENTION_FORM_ROWS, MOECA_ATTENTION_FORM_TILE,
+ MOECA_ATTENTION_FORM_TILES) = range(4)
 MOECA_ACT_NONE, MOECA_ACT_GELU, MOECA_ACT_GELU_TANH = 0, 1, 2
 
 
@@ -238,6 +240,7 @@ def _load():
         "moeca_probe_q8_staged": (C.c_int32, [C.c_int32] * 7),
         "moeca_probe_q8_stall": (C.c_int32, [C.c_int32, C.c_int64]),
         "moeca_probe_attention_stall": (C.c_int32, [C.c_int32, C.c_int64]),
+        "moeca_probe_attention_form": (C.c_int32, [C.POINTER(moeca_attention_args), C.POINTER(C.c_int32)]),
         "moeca_probe_ffma": (C.c_int32, [C.c_int32, C.c_int32, C.POINTER(C.c_double), C.POINTER(C.c_double)]),
         "moeca_probe_maps_encoded": (C.c_int64, []),
         "moeca_probe_prefetch_bytes": (C.c_int64, [C.c_int64, C.c_int32, C.c_int32]),
@@ -518,6 +521,15 @@ def moeca_probe_attention_stall(barrier: int, wait_ns: int = 20_000_000) -> None
     st = LIB.moeca_probe_attention_stall(barrier, wait_ns)
     if st != MOECA_OK:
         raise MoecaError(st, "moeca_probe_attention_stall")
+
+
+def moeca_probe_attention_form(args: moeca_attention_args) -> tuple:
+    """(form, keys of a chunk or 0) in which moeca_attention carries out a call (include/moeca_probe.h)."""
+    chunk = C.c_int32()
+    form = LIB.moeca_probe_attention_form(C.byref(args), C.byref(chunk))
+    if form < 0:
+        raise MoecaError(MOECA_ERR_INVALID_ARG, "moeca_probe_attention_form")
+    return form, chunk.value
 
 
 def moeca_probe_stream(device: int, n_tokens: int, rows: int, row_bytes: int, reps: int = 15) -> tuple:

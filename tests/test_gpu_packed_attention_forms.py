@@ -3,6 +3,8 @@ import numpy as np
 import pytest
 import torch
 
+from test_gpu_packed_attention import check as against_64_bits
+
 pytestmark = pytest.mark.gpu
 
 
@@ -52,15 +54,14 @@ def test_rows_do_not_depend_on_what_shared_memory_held(M, H, d):
 @pytest.mark.parametrize("most", [3, 40, 300])
 def test_offsets_written_right_before_the_call(M, dtype, most):
     """Offsets that a kernel of the same graph writes before the call, others in every replay; the key axis is cut."""
-    n, keys, B = 3 * most, 20_000, 3
+    n, keys, B = 2 * most, 20_000, 3
     q, k, v = qkv(most, n, keys, 4, 2, 64, dtype)
     rng = np.random.default_rng(most)
 
-    def cuts(total, longest):
-        while True:
-            c = np.concatenate([[0], np.sort(rng.integers(0, total + 1, B - 1)), [total]])
-            if np.diff(c).max() <= longest:
-                return torch.tensor(c, dtype=torch.int32, device="cuda")
+    def cuts(total, longest):  # lengths of at most `longest` each
+        a = int(rng.integers(max(total - 2 * longest, 0), min(total, longest) + 1))
+        b = int(rng.integers(max(total - longest, a), min(total, a + longest) + 1))
+        return torch.tensor([0, a, b, total], dtype=torch.int32, device="cuda")
 
     source = [torch.zeros(B + 1, dtype=torch.int32, device="cuda") for _ in range(2)]
     off = [torch.zeros_like(s) for s in source]
@@ -82,3 +83,72 @@ def test_offsets_written_right_before_the_call(M, dtype, most):
         graph.replay()
         want = M.attention(q, k, v, q_offsets=new[0], k_offsets=new[1], causal=True, max_q=most, lse=True)
         assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+
+
+def form(M, q, k, v, q_len, k_len, max_q=0):
+    """The form of a call with offsets."""
+    def heads(t):
+        return M.moeca_heads(t.data_ptr(), t.stride(0), t.stride(1), t.shape[1])
+    out = torch.empty_like(q)
+    off = offsets(q_len)
+    return M.moeca_probe_attention_form(M.moeca_attention_args(
+        heads(q), heads(k), heads(v), heads(out), off.data_ptr(), off.data_ptr(), None, None, None, q.shape[0], k.shape[0], len(q_len),
+        max_q, M.MOECA_BF16, q.shape[2], 1, 0, 0.1))
+
+
+# Shapes of two tiles a block: whole and cut keys, one and more sequences, tails of every kind, blocks whose second
+# tile has no queries or fewer keys.
+PAIRS = [
+    ([129 + 11 * i % 72 for i in range(20)], [129 + 11 * i % 72 for i in range(20)], 8, 8, False),
+    ([200 - 3 * i for i in range(20)], [150 + 17 * i for i in range(20)], 16, 8, False),
+    ([513, 700, 0, 300], [513, 700, 9, 300], 24, 24, False),
+    ([300, 17, 260, 1], [4100, 4500, 4097, 5003], 2, 2, True),
+    ([300], [9001], 2, 2, True),
+    ([150, 290], [9000, 5007], 4, 2, True),
+]
+
+
+@pytest.mark.parametrize("q_len,k_len,H,Hk,cut", PAIRS, ids=range(len(PAIRS)))
+@pytest.mark.parametrize("causal,d", [(False, 40), (False, 72), (False, 128), (True, 64), (True, 96), (True, 128)])
+def test_two_tiles_a_block(M, q_len, k_len, H, Hk, cut, causal, d):
+    q, k, v = qkv(d, sum(q_len), sum(k_len), H, Hk, d)
+    got, chunk = form(M, q, k, v, q_len, k_len, max(q_len))
+    assert got == M.MOECA_ATTENTION_FORM_TILES and (chunk > 0) == cut
+    against_64_bits(M, q, k, v, q_len, k_len, causal, max_q=max(q_len))
+
+
+@pytest.mark.parametrize("causal,d", [(False, 72), (True, 64)])
+def test_two_tiles_a_block_over_long_keys(M, causal, d):
+    """Whole key axes above 4096 keys, tiles of 1 to 256 queries."""
+    q_len, k_len = [150, 17, 260, 1], [4100, 4500, 4097, 5003]
+    q, k, v = qkv(d, sum(q_len), sum(k_len), 16, 16, d)
+    assert form(M, q, k, v, q_len, k_len, max(q_len)) == (M.MOECA_ATTENTION_FORM_TILES, 0)
+    against_64_bits(M, q, k, v, q_len, k_len, causal, max_q=max(q_len))
+
+
+@pytest.mark.parametrize("causal,d", [(False, 64), (False, 96), (True, 72), (True, 128)])
+def test_two_tiles_a_block_of_equal_lengths(M, causal, d):
+    q, k, v = qkv(d, 21 * 150, 21 * 170, 8, 8, d)
+    assert form(M, q, k, v, [150] * 21, [170] * 21, 150) == (M.MOECA_ATTENTION_FORM_TILES, 0)
+    against_64_bits(M, q, k, v, [150] * 21, [170] * 21, causal, given=False, n_seqs=21)
+    own = q.clone()
+    want = M.attention(q, k, v, n_seqs=21, causal=causal)
+    assert M.attention(own, k, v, n_seqs=21, causal=causal, out=own) is own and torch.equal(own, want)
+
+
+@pytest.mark.parametrize("d", [64, 72, 128])
+def test_two_tiles_a_block_with_foreign_values(M, d):
+    """Rising maxima, and NaN and infinities in every other sequence."""
+    n = 20
+    q_len, k_len = [140 + i for i in range(n)], [200 + 7 * i for i in range(n)]
+    q, k, v = qkv(d, sum(q_len), sum(k_len), 8, 8, d)
+    assert form(M, q, k, v, q_len, k_len, max(q_len))[0] == M.MOECA_ATTENTION_FORM_TILES
+    at = torch.cat([torch.linspace(0.1, 20, m) for m in k_len]).cuda()
+    k *= at[:, None, None].to(k.dtype)
+    against_64_bits(M, q, k, v, q_len, k_len, True, max_q=max(q_len))
+    args = dict(q_offsets=offsets(q_len), k_offsets=offsets(k_len), max_q=max(q_len))
+    want = M.attention(q, k, v, **args)
+    bad_q, bad_k = (torch.cat([torch.full((m,), i % 2 == 1) for i, m in enumerate(x)]).cuda() for x in (q_len, k_len))
+    k[bad_k], v[bad_k] = float("inf"), float("nan")
+    out = M.attention(q, k, v, **args)
+    assert torch.equal(out[~bad_q], want[~bad_q]) and bool(out[bad_q].isnan().all())

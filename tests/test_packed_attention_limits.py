@@ -57,3 +57,26 @@ def test_what_the_norm_may_clear(M, clear):
     for good in range(4):
         bad.clear = good
         M.moeca_qk_norm_rope(bad)
+
+
+# Sizes and the form they reach: (queries, keys, sequences, heads, key heads, dim, max_q), form, whether keys are cut.
+FORMS = [((1, 300, 1, 4, 2, 64, 0), "ROWS", False), ((1, 65536, 1, 4, 4, 128, 0), "ROWS", True), ((16, 300, 1, 2, 2, 64, 0), "ROWS", False),
+         ((17, 300, 1, 2, 2, 64, 0), "TILE", False), ((128, 128, 1, 1, 1, 72, 0), "TILE", False), ((64, 32768, 1, 8, 8, 128, 0), "TILE", True),
+         ((4096, 4096, 16, 16, 16, 72, 256), "TILES", False), ((16384, 16384, 5, 32, 8, 128, 6000), "TILES", False),
+         ((300, 9001, 1, 2, 2, 64, 0), "TILES", True), ((300, 300, 1, 2, 2, 130, 0), "CORES", True), ((40, 40, 1, 2, 2, 36, 0), "CORES", False)]
+
+
+@pytest.mark.parametrize("size,form,cut", FORMS, ids=str)
+def test_forms(M, size, form, cut):
+    n, m, seqs, H, Hk, d, max_q = size
+    a = args(M, n, m, seqs, H, Hk, d, max_q=max_q, offsets=True)
+    got, chunk = M.moeca_probe_attention_form(a)
+    assert got == getattr(M, "MOECA_ATTENTION_FORM_" + form) and (chunk > 0) == cut
+    assert (M.moeca_attention_workspace(a) > 0) == cut
+    assert M.moeca_probe_attention_form(args(M, n, m, seqs, H, Hk, d, max_q=max_q, offsets=True, dtype=M.MOECA_F32))[0] == 0
+
+
+def test_form_refusals(M):
+    for bad in (args(M), args(M, 1, d=257), args(M, 1, scale=-1.0), args(M, (1 << 30) + 1)):
+        with pytest.raises(M.MoecaError):
+            M.moeca_probe_attention_form(bad)
