@@ -246,7 +246,8 @@ __global__ void __launch_bounds__(64 + 128 * NT, NT == 1 ? 2 : 1)
       issued = n;
     }
     __syncwarp();
-    if (dirty && !abort_flag) {
+    // The lanes vote on the flag, which other warps may set meanwhile: what follows is a wait of the whole warp.
+    if (dirty && !__any_sync(0xffffffffu, abort_flag != 0)) {
       // Value rows last_keys .. of the last block's 16s are another sequence's, or nobody's.
       const int n = place_of_v(blocks - 1, blocks), s = n % ST;
       if (warp_wait_here(smem_u32(&full[s]), (n / ST) & 1, &abort_flag, a.wait_ns)) {
