@@ -170,7 +170,7 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_kernel(const __grid_co
     if (ty * R + r >= rows) continue;
     const float inv = l[r] == 0.f ? 0.f : 1.f / l[r];
     const float lse2 = l[r] == 0.f ? -INFINITY : m[r] * a.scale_log2 + log2f(l[r]);
-    if (a.ks.unit) {
+    if (a.ks.unit && w.nk > a.ks.unit) {
       const int64_t at = (static_cast<int64_t>(w.piece) * a.max_q + i) * a.q.heads + h;
       if (tx == 0) a.part_ml[at] = make_float2(m[r], l[r]);
 #pragma unroll
@@ -214,10 +214,11 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const PackedAtt
   const int b = some ? a.qs.owner(t) : 0, i = some ? t - a.qs.start(b) : -1;
   const bool mine = i >= 0 && i < min(a.qs.length(b), a.max_q);
   const int chunks = static_cast<int>((static_cast<uint32_t>(a.ks.length(b)) + a.ks.unit - 1) / a.ks.unit);
-  const int64_t first = (static_cast<int64_t>(a.ks.base(b)) * a.max_q + i) * a.q.heads + h, step = static_cast<int64_t>(a.max_q) * a.q.heads;
-  if (!mine) return;
+  if (!mine || chunks == 1) return;  // one chunk: the kernel before this one wrote it
+  const int first = a.ks.chunk(b, 0), others = a.ks.chunk(b, 1) - 1;
+  const auto at = [&](int j) { return (static_cast<int64_t>(j == 0 ? first : others + j) * a.max_q + i) * a.q.heads + h; };
   float m = -INFINITY;
-  for (int j = lane; j < chunks; j += 32) m = fmaxf(m, a.part_ml[first + j * step].x);
+  for (int j = lane; j < chunks; j += 32) m = fmaxf(m, a.part_ml[at(j)].x);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
   const float ref = m == -INFINITY ? 0.f : m;
@@ -226,7 +227,7 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const PackedAtt
   for (int j0 = 0; j0 < chunks; j0 += 32) {
     float own = 0.f;
     if (j0 + lane < chunks) {
-      const float2 ml = a.part_ml[first + (j0 + lane) * step];
+      const float2 ml = a.part_ml[at(j0 + lane)];
       own = exp2f((ml.x - ref) * a.scale_log2) * ml.y;
     }
     sum += own;
@@ -234,7 +235,7 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const PackedAtt
 #pragma unroll W > 1 ? 4 : 2
     for (int j = W > 1 ? warp : 0; j < n; j += W) {
       const float w = __shfl_sync(0xffffffffu, own, j);
-      const float* part = a.part_o + (first + (j0 + j) * step) * a.dim;
+      const float* part = a.part_o + at(j0 + j) * a.dim;
 #pragma unroll
       for (int c = 0; c < C; ++c)
         if (c * 32 + lane < a.dim) o[c] = fmaf(w, part[c * 32 + lane], o[c]);
@@ -326,6 +327,7 @@ struct Plan {
   int max_q, tiles;
   int64_t q_pieces, k_pieces;
   int q_per, k_per;
+  int firsts;         // chunks are numbered with every sequence's first in front
   int64_t blocks;
   int64_t ml_bytes, bytes;  // workspace: the maxima and sums, all of it
 };
@@ -351,7 +353,7 @@ bool fits_tc(const moeca_heads& h, int64_t tokens) {
 }
 
 constexpr int kSms = 152;
-constexpr int64_t kLongKeys = 4096, kKeysSaved = 1536;
+constexpr int64_t kLongKeys = 4096, kKeysSaved = 1536, kKeysUneven = 8192;
 
 // How a call is carried out: a function of its sizes, type and alignment.
 Plan plan_attention(const moeca_attention_args& a) {
@@ -403,10 +405,18 @@ Plan plan_attention(const moeca_attention_args& a) {
       chunk = (mean + cuts - 1) / cuts;
     }
     chunk = std::max<int64_t>(least, (chunk + 127) / 128 * 128);
+    const int64_t longest = a.k_offsets ? a.n_keys : mean;
+    bool uneven = false;
     // Writing and joining the tiles' partial results costs what some 1500 keys do: 2048 tokens, 8 heads of 128, cut
     // in two 29.5 us, whole 28.4; 4096 tokens, 4 heads, 40.6 and 50.9.
-    if (p.rows > 0 && mean - chunk < kKeysSaved) chunk = kMaxTokens;
-    const int64_t longest = a.k_offsets ? a.n_keys : mean;
+    if (p.rows > 0 && mean - chunk < kKeysSaved) {
+      // Where one sequence may hold most of the keys, those far above the mean are cut all the same, the others being
+      // one chunk each: 32 queries of 32 heads on 2 (64 channels) in each of 16 sequences, one of 32768 keys among ones of
+      // 512, take 50 us, whole 263; of 2528 keys each 29.6, whole 25.5.
+      chunk = (mean + kKeysSaved + 127) / 128 * 128;
+      uneven = longest - chunk >= kKeysUneven;
+      if (!uneven) chunk = kMaxTokens;
+    }
     if (chunk < longest) {
       const int64_t n = pieces(a.k_offsets, a.n_keys, a.n_seqs, static_cast<int>(chunk), 0x7fffffff, &p.k_per);
       const int64_t rows = n * p.max_q * a.q.heads;
@@ -414,6 +424,7 @@ Plan plan_attention(const moeca_attention_args& a) {
       if (rows < kMaxWorkspace && bytes <= kMaxWorkspace) {
         p.chunk = static_cast<int>(chunk);
         p.k_pieces = n;
+        p.firsts = uneven && p.k_per == 0;
         p.blocks = n * p.tiles * heads;
         p.ml_bytes = ml;
         p.bytes = bytes;
@@ -489,8 +500,8 @@ moeca_status moeca_attention(const moeca_attention_args* a, void* stream) {
   }
   PackedAttnArgs d{};
   d.q = device_heads(a->q); d.k = device_heads(a->k); d.v = device_heads(a->v); d.out = device_heads(a->out);
-  d.qs = {a->q_offsets, static_cast<int>(nq), a->n_seqs, static_cast<int>(nq / a->n_seqs), p.tile, p.q_per};
-  d.ks = {a->k_offsets, static_cast<int>(nk), a->n_seqs, static_cast<int>(nk / a->n_seqs), p.chunk, p.k_per};
+  d.qs = {a->q_offsets, static_cast<int>(nq), a->n_seqs, static_cast<int>(nq / a->n_seqs), p.tile, p.q_per, 0};
+  d.ks = {a->k_offsets, static_cast<int>(nk), a->n_seqs, static_cast<int>(nk / a->n_seqs), p.chunk, p.k_per, p.firsts};
   d.q_pieces = p.q_pieces; d.k_pieces = p.k_pieces;
   d.lse = a->lse;
   d.part_ml = static_cast<float2*>(a->workspace);

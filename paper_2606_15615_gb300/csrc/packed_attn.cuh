@@ -5,7 +5,8 @@
 // key axis is cut into chunks, each chunk's kernel leaves its normalised result,
 // its maximum and its sum in the workspace, and a last kernel joins
 // the chunks of a row in their order.  (Maximum and sum apart: in a logarithm of
-// the sum that holds both, a score of 2^20 leaves the sum three bits.)
+// the sum that holds both, a score of 2^20 leaves the sum three bits.)  A sequence
+// whose keys are one chunk goes to its place at once.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -26,6 +27,7 @@ struct Seqs {
   int total, n, each;
   int unit;
   int per;  // pieces of each sequence, or 0: sequence b's begin at off[b] / unit + b
+  int firsts;  // how chunks are numbered, see below (with per 0)
 
   __device__ __forceinline__ int start(int b) const { return off ? min(max(off[b], 0), total) : b * each; }
   __device__ __forceinline__ int length(int b) const { return off ? max(start(b + 1) - start(b), 0) : each; }
@@ -51,6 +53,25 @@ struct Seqs {
   __device__ __forceinline__ int find(int p) const {
     if (per) return static_cast<int>(static_cast<uint32_t>(p) / static_cast<uint32_t>(per));
     return last(p, [this](int b) { return base(b); });
+  }
+  // The number of sequence b's chunk c: as pieces, or with `firsts` every sequence's first chunk, then the others, so
+  // that where most sequences have one the blocks of these start at once and those without a chunk come last.
+  // Sequence b's second is then n + off[b] / unit: floor((len - 1) / unit) others fit before the next sequence's.
+  __device__ __forceinline__ int chunk(int b, int c) const {
+    if (!firsts) return base(b) + c;
+    return c == 0 ? b : n + second(b) + c - 1;
+  }
+  __device__ __forceinline__ int second(int b) const { return static_cast<int>(static_cast<uint32_t>(start(b)) / static_cast<uint32_t>(unit)); }
+  // The sequence and its chunk (below 0: none) of number p.
+  __device__ __forceinline__ int find_chunk(int p, int* c) const {
+    if (!firsts || p < n) {
+      const int b = firsts ? p : find(p);
+      *c = firsts ? 0 : p - base(b);
+      return b;
+    }
+    const int b = last(p - n, [this](int b) { return second(b); }), more = p - n - second(b);
+    *c = more < 0 ? -1 : more + 1;
+    return b;
   }
   // The sequence of a token.
   __device__ __forceinline__ int owner(int t) const {
@@ -93,14 +114,14 @@ struct AttnWork {
 // index: the tile (no chunks), or chunk x tiles + tile.  All lanes of a warp.
 __device__ __forceinline__ AttnWork attn_work(const PackedAttnArgs& a, int index) {
   AttnWork w;
-  int b, tile;
+  int b, tile, chunk = 0;
   if (a.ks.unit == 0) {
     b = a.qs.find(index);
     tile = index - a.qs.base(b);
     w.piece = 0;
   } else {
     w.piece = static_cast<int>(static_cast<uint32_t>(index) / static_cast<uint32_t>(a.tiles));
-    b = a.ks.find(w.piece);
+    b = a.ks.find_chunk(w.piece, &chunk);
     tile = index - w.piece * a.tiles;
   }
   w.q0 = a.qs.start(b);
@@ -113,7 +134,7 @@ __device__ __forceinline__ AttnWork attn_work(const PackedAttnArgs& a, int index
   w.key_lo = 0;
   w.key_hi = w.nk;
   if (a.ks.unit) {
-    const int64_t lo = static_cast<int64_t>(w.piece - a.ks.base(b)) * a.ks.unit;
+    const int64_t lo = static_cast<int64_t>(chunk) * a.ks.unit;
     w.any = w.any && lo >= 0 && lo < w.nk;
     w.key_lo = w.any ? static_cast<int>(lo) : 0;
     w.key_hi = w.any ? min(w.key_lo + a.ks.unit, w.nk) : 0;
@@ -154,9 +175,8 @@ __device__ __noinline__ void clear_tokens(const PackedAttnArgs& a, int index, in
     tile = index - a.qs.base(b);
   } else {
     const int piece = static_cast<int>(static_cast<uint32_t>(index) / static_cast<uint32_t>(a.tiles));
-    b = a.ks.find(piece);
+    b = a.ks.find_chunk(piece, &chunk);
     tile = index - piece * a.tiles;
-    chunk = piece - a.ks.base(b);
     chunks = max((a.ks.length(b) - 1) / a.ks.unit + 1, 1);  // a sequence without keys still has its first chunk's block
   }
   if (tile < 0 || tile >= a.tiles || chunk < 0 || chunk >= chunks) return;

@@ -220,7 +220,7 @@ __global__ void __launch_bounds__(kRowsThreads, DK <= 4 ? 4 : 2) attn_rows_kerne
     for (int j = 0; j < 8; ++j) f[j] *= inv;
     const int q_i = r / G, head = kvh * G + r - q_i * G;
     const float lse2 = sum == 0.f ? -INFINITY : top * a.scale_log2 + log2f(sum);
-    if (a.ks.unit) {
+    if (a.ks.unit && w.nk > a.ks.unit) {
       const int64_t part = (static_cast<int64_t>(w.piece) * a.max_q + q_i) * a.q.heads + head;
       if (c == 0) a.part_ml[part] = make_float2(top, sum);
       store_vec(a.part_o + part * a.dim + c, f);

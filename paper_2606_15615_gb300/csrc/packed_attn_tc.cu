@@ -462,7 +462,7 @@ __global__ void __launch_bounds__(64 + 128 * NT, NT == 1 ? 2 : 1)
       const float l = (l2[0].x + l2[0].y) + (l2[1].x + l2[1].y);
       const float inv = l == 0.f ? 0.f : 1.f / l;
       const float lse2 = l == 0.f ? -INFINITY : m * sc + log2f(l);
-      const bool cut = a.ks.unit != 0;
+      const bool cut = a.ks.unit && w.nk > a.ks.unit;
       const int64_t part = (static_cast<int64_t>(w.piece) * a.max_q + query) * a.q.heads + head;
       __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out.data) + static_cast<int64_t>(w.q0 + query) * a.out.token_stride + head * a.out.head_stride;
       float* part_o = a.part_o + part * a.dim;

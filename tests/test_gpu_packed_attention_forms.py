@@ -152,3 +152,40 @@ def test_two_tiles_a_block_with_foreign_values(M, d):
     k[bad_k], v[bad_k] = float("inf"), float("nan")
     out = M.attention(q, k, v, **args)
     assert torch.equal(out[~bad_q], want[~bad_q]) and bool(out[bad_q].isnan().all())
+
+
+# Sequences of very different lengths, of which only those far above the mean are cut: the long ones first, last, among
+# others, two of them; sequences without keys or queries.
+UNEVEN = [[12000] + [100] * 38 + [4200], [9, 0] * 15 + [18000] + [150, 40, 0] * 3, [0] * 39 + [20000], [2100, 0, 4100, 6200, 1] * 2 + [13] * 30]
+
+
+@pytest.mark.parametrize("k_len", UNEVEN, ids=range(len(UNEVEN)))
+@pytest.mark.parametrize("first", [(0, 0), (3, 2500)])
+@pytest.mark.parametrize("d,H,Hk,causal", [(64, 2, 2, True), (72, 6, 2, False), (128, 2, 1, True)])
+def test_uneven_lengths(M, k_len, first, d, H, Hk, causal):
+    q_len = [20, 0, 7, 33] * 10
+    q, k, v = qkv(d, sum(q_len) + first[0] + 5, sum(k_len) + first[1] + 40, H, Hk, d)
+    got, chunk = form(M, q, k, v, q_len, k_len, max(q_len))
+    assert got == M.MOECA_ATTENTION_FORM_TILE and max(k_len) > chunk > 1536
+    q[:first[0]], k[:first[1]], v[:first[1]] = float("nan"), float("inf"), float("nan")
+    against_64_bits(M, q, k, v, q_len, k_len, causal, first=first, max_q=max(q_len))
+    args = dict(q_offsets=offsets(q_len) + first[0], k_offsets=offsets(k_len) + first[1], causal=causal, max_q=max(q_len))
+    again = M.attention(q, k, v, **args, lse=True)
+    assert all(torch.equal(x, y) for x, y in zip(again, M.attention(q, k, v, **args, lse=True)))
+
+
+@pytest.mark.parametrize("bad", [[-5, 12000, 100, 20000], [0, 25000, 3, 9000], [15000, 0, 0, 15000], [-2 ** 31, 2 ** 31 - 1, 0, 5],
+                                 [19999, 20000, 19000, 20001]])
+def test_wrong_offsets_of_uneven_lengths_stay_inside(M, bad):
+    """Offsets out of range or order: clamped, and nothing outside the tensors is touched."""
+    n = 40
+    q, k, v = qkv(3, 20 * n, 20_000, 2, 2, 64)
+    rng = np.random.default_rng(1)
+    off = torch.tensor(np.concatenate([bad, rng.integers(-100, 20_100, n + 1 - len(bad))]), dtype=torch.int32, device="cuda")
+    buf = torch.full((20 * n + 20, 2, 64), 5.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.zeros(20 * n, 2, device="cuda")
+    for q_off in (offsets([20] * n), off):
+        M.attention(q, k, v, q_offsets=q_off, k_offsets=off, max_q=20, out=buf[10:-10], lse=lse)
+        M.attention(q, k, v, q_offsets=q_off, k_offsets=off, max_q=20, lse=True)
+    torch.cuda.synchronize()
+    assert bool((buf[:10] == 5).all()) and bool((buf[-10:] == 5).all()) and not bool(buf.isnan().any())

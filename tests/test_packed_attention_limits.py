@@ -63,7 +63,8 @@ def test_what_the_norm_may_clear(M, clear):
 FORMS = [((1, 300, 1, 4, 2, 64, 0), "ROWS", False), ((1, 65536, 1, 4, 4, 128, 0), "ROWS", True), ((16, 300, 1, 2, 2, 64, 0), "ROWS", False),
          ((17, 300, 1, 2, 2, 64, 0), "TILE", False), ((128, 128, 1, 1, 1, 72, 0), "TILE", False), ((64, 32768, 1, 8, 8, 128, 0), "TILE", True),
          ((4096, 4096, 16, 16, 16, 72, 256), "TILES", False), ((16384, 16384, 5, 32, 8, 128, 6000), "TILES", False),
-         ((300, 9001, 1, 2, 2, 64, 0), "TILES", True), ((300, 300, 1, 2, 2, 130, 0), "CORES", True), ((40, 40, 1, 2, 2, 36, 0), "CORES", False)]
+         ((512, 40448, 16, 32, 2, 64, 32), "TILE", True), ((400, 4096, 4, 20, 20, 128, 200), "TILE", False),
+         ((800, 20000, 40, 2, 2, 64, 20), "TILE", True), ((300, 9001, 1, 2, 2, 64, 0), "TILES", True), ((300, 300, 1, 2, 2, 130, 0), "CORES", True), ((40, 40, 1, 2, 2, 36, 0), "CORES", False)]
 
 
 @pytest.mark.parametrize("size,form,cut", FORMS, ids=str)
