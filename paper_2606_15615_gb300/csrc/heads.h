@@ -1,6 +1,8 @@
 // Heads of packed tokens (moeca_heads): what the kernels take, and the checks of the calls.
 #pragma once
 
+#include <numeric>
+
 #include "calls.h"
 #include "moeca_attention.h"
 
@@ -44,8 +46,8 @@ inline bool same_heads(const moeca_heads& a, const moeca_heads& b) {
 }
 
 // Whether two sets of heads (an, bn tokens of dim values) share a value.  Parts
-// of one fused buffer do not, although their ranges do: within the common
-// token or head stride they lie side by side.
+// of one fused buffer do not, although their ranges do: within the common token or head
+// stride, or the largest step that all strides are multiples of, they lie side by side.
 inline bool heads_overlap(const moeca_heads& a, int64_t an, const moeca_heads& b, int64_t bn, int dim, int64_t es) {
   if (!overlap(heads_range(a, an, dim, es), heads_range(b, bn, dim, es))) return false;
   const auto apart = [&](int64_t stride, int64_t ea, int64_t eb) {
@@ -59,11 +61,19 @@ inline bool heads_overlap(const moeca_heads& a, int64_t an, const moeca_heads& b
   if (a.token_stride == b.token_stride &&
       apart(a.token_stride, (a.heads - 1) * a.head_stride + dim, (b.heads - 1) * b.head_stride + dim))
     return false;
-  const int64_t hs = a.heads > 1 ? a.head_stride : b.head_stride;
-  if (hs > 0 && (a.heads == 1 || a.head_stride == hs) && (b.heads == 1 || b.head_stride == hs) &&
-      (an == 1 || a.token_stride % hs == 0) && (bn == 1 || b.token_stride % hs == 0) && apart(hs, dim, dim))
+  if (a.heads > 1 && a.head_stride == b.head_stride && b.heads > 1 &&
+      apart(a.head_stride, (an - 1) * a.token_stride + dim, (bn - 1) * b.token_stride + dim))
     return false;
-  return true;
+  // Heads start at multiples of what divides all strides.
+  int64_t step = 0;
+  const auto meet = [&](int64_t stride, int64_t n) {
+    if (n > 1) step = std::gcd(step, stride);
+  };
+  meet(a.token_stride, an);
+  meet(b.token_stride, bn);
+  meet(a.head_stride, a.heads);
+  meet(b.head_stride, b.heads);
+  return !apart(step, dim, dim);
 }
 inline bool heads_overlap(const moeca_heads& a, int64_t an, const Range& r, int dim, int64_t es) {
   return overlap(heads_range(a, an, dim, es), r);

@@ -189,3 +189,18 @@ def test_wrong_offsets_of_uneven_lengths_stay_inside(M, bad):
         M.attention(q, k, v, q_offsets=q_off, k_offsets=off, max_q=20, lse=True)
     torch.cuda.synchronize()
     assert bool((buf[:10] == 5).all()) and bool((buf[-10:] == 5).all()) and not bool(buf.isnan().any())
+
+
+@pytest.mark.parametrize("d", [64, 72, 33])
+def test_parts_of_a_buffer_with_heads_first(M, d):
+    """[heads, tokens, 3, d]: the norm in place of queries and keys, attention in place of the queries."""
+    H, T = 3, 150
+    g = torch.Generator().manual_seed(d)
+    buf = torch.randn(H, T, 3, d, generator=g).bfloat16().cuda()
+    q, k, v = (buf[:, :, i].permute(1, 0, 2) for i in range(3))
+    nq, nk = M.qk_norm_rope(q.contiguous(), k.contiguous())
+    want, values = M.attention(nq, nk, v.contiguous()), v.clone()
+    M.qk_norm_rope(q, k, q_out=q, k_out=k)
+    assert torch.equal(q, nq) and torch.equal(k, nk)
+    M.attention(q, k, v, out=q)
+    assert torch.equal(q, want) and torch.equal(k, nk) and torch.equal(v, values)

@@ -81,3 +81,30 @@ def test_form_refusals(M):
     for bad in (args(M), args(M, 1, d=257), args(M, 1, scale=-1.0), args(M, (1 << 30) + 1)):
         with pytest.raises(M.MoecaError):
             M.moeca_probe_attention_form(bad)
+
+
+def parts(M, layout, H, T, d, parts=3):
+    """q, k, v of one fused buffer: which strides a token and a head have, and how far apart the parts are."""
+    token, head, part = {"token, part, head": (parts * H * d, d, H * d), "token, head, part": (parts * H * d, parts * d, d),
+                         "head, token, part": (parts * d, parts * T * d, d), "head, part, token": (d, parts * T * d, T * d),
+                         "part, token, head": (H * d, d, T * H * d)}[layout]
+    return [M.moeca_heads(A + 2 * p * part, token, head, H) for p in range(parts)]
+
+
+@pytest.mark.parametrize("layout", ["token, part, head", "token, head, part", "head, token, part", "head, part, token", "part, token, head"])
+@pytest.mark.parametrize("H,d", [(4, 64), (5, 72), (4, 33)])
+def test_parts_of_a_fused_buffer_do_not_overlap(M, layout, H, d):
+    """Results over the queries of a fused buffer in any order of its axes: refused for its size alone, which is
+    looked at last; a value too far, and it meets its neighbour."""
+    T = 1 << 29
+    q, k, v = parts(M, layout, H, T, d)
+    a = args(M, T, T, H=H, Hk=H, d=d)
+    a.q, a.k, a.v, a.out, a.workspace = q, k, v, q, None
+    with pytest.raises(M.MoecaError) as e:
+        M.moeca_attention(a)
+    assert e.value.status == M.MOECA_ERR_UNSUPPORTED
+    for near in (k, v):
+        a.out = M.moeca_heads(near.data - 2, q.token_stride, q.head_stride, H)
+        with pytest.raises(M.MoecaError, match="overlaps") as e:
+            M.moeca_attention(a)
+        assert e.value.status == M.MOECA_ERR_INVALID_ARG
