@@ -107,7 +107,8 @@ typedef struct {
 } moeca_attention_args;
 moeca_status moeca_attention(const moeca_attention_args* args, void* stream);
 /* Bytes that moeca_attention with these arguments works in (device pointers are
- * not looked at but for their alignment); -1 where they would be refused. */
+ * not looked at but for their alignment); -1 where sizes, types or strides would be
+ * refused, or the tokens are too many. */
 int64_t moeca_attention_workspace(const moeca_attention_args* args);
 
 #ifdef __cplusplus

@@ -1075,7 +1075,7 @@ def _plan_count(plan, dev: int) -> int:
 def expert_rows(x, plan: ExpertPlan, out=None, stream: int = 0):
     """The rows of ``x`` [T, D] (fp32 or bf16) in the plan's order: row place[t, p] is x[t].  A new result has T k rows,
     zeros behind the plan's last; rows of a given ``out`` behind it keep what they hold.  ``stream``: as for q8_read.
-    Its gradient is expert_rows_grad."""
+    Its gradient is expert_rows_grad (autograd does not see the call)."""
     dev = x.get_device()
     address, n_x, x_stride, width, code = _value_fields(x, "x", dev)
     place, T, k = _branches(plan, dev)
@@ -1092,7 +1092,7 @@ def expert_rows(x, plan: ExpertPlan, out=None, stream: int = 0):
 def expert_combine(rows, plan: ExpertPlan, weights=None, x=None, out=None, stream: int = 0):
     """x + sum_p weights[:, p] rows[place[:, p]]: ``rows`` [n, D] fp32 or bf16 in the plan's order, ``weights`` [T, k] fp32
     (None: 1), ``x`` [T, D] of rows' dtype (None: 0); a branch without a row adds nothing.  ``out`` may be x.
-    ``stream``: as for q8_read.  Its gradients are expert_combine_grad's."""
+    ``stream``: as for q8_read.  Its gradients are expert_combine_grad's (autograd does not see the call)."""
     dev = rows.get_device()
     address, n, stride, width, code = _value_fields(rows, "rows", dev)
     place, T, k = _branches(plan, dev)
@@ -1116,7 +1116,8 @@ def expert_rows_grad(drows, plan: ExpertPlan, out=None, stream: int = 0):
 def expert_combine_grad(dout, rows, plan: ExpertPlan, weights=None, drows=None, dweights=True, stream: int = 0):
     """The gradients of expert_combine's rows and weights for the gradient ``dout`` [T, D] of its result (x's is dout
     itself).  ``drows``: rows to write to (those behind the plan's last keep what they hold), by default new ones
-    (zeros there).  ``dweights``: True, False or a [T, k] fp32 tensor.  Returns (drows, dweights or None)."""
+    (zeros there), or False: not wanted.  ``dweights``: True, False or a [T, k] fp32 tensor.  Returns (drows or None,
+    dweights or None)."""
     dev = dout.get_device()
     address, n_d, d_stride, width, code = _value_fields(dout, "dout", dev)
     r_address, n, r_stride, r_width, r_code = _value_fields(rows, "rows", dev)
@@ -1125,7 +1126,10 @@ def expert_combine_grad(dout, rows, plan: ExpertPlan, weights=None, drows=None, 
         raise ValueError(f"dout must be [{T}, {r_width}] of rows' dtype")
     w = _list(weights, "f32", (T, k), "weights", dev)
     count = _plan_count(plan, dev) if drows is None else 0
-    drows, g_address, g_stride = _row_result(drows, n, width, rows, "drows", dev, stream)
+    if drows is False:
+        drows, g_address, g_stride = None, 0, 0
+    else:
+        drows, g_address, g_stride = _row_result(drows, n, width, rows, "drows", dev, stream)
     if dweights is True:
         torch = _TYPES["torch"]
         dweights = _on(stream, dev, lambda: torch.empty((T, k), dtype=torch.float32, device=rows.device))
@@ -1176,8 +1180,8 @@ def qk_norm_rope(q, k, table=None, q_weight=None, k_weight=None, pos=None, eps: 
     ``table`` [positions, P, 2] fp32 (cosines and sines, see rope_table; None: no rotation).  Pair i is (i, i + P), or
     (2 i, 2 i + 1) with ``pairs``.  ``pos`` [T] int32: the tokens' rows of the table (None: their numbers); a token whose
     position is outside it is left out: a new result is 0 there, a given one keeps what it holds.  ``q_out`` and ``k_out`` may
-    be q and k.  ``stream``: as for q8_read.  Returns
-    (q_out, k_out)."""
+    be q and k.  ``stream``: as for q8_read.  Returns (q_out, k_out).
+    No gradients: the results have no graph, whatever the inputs ask for."""
     dev = q.get_device()
     fq, T, dim, code = _head_fields(q, "q", dev)
     torch = _TYPES["torch"]
@@ -1223,7 +1227,7 @@ def attention(q, k, v, q_offsets=None, k_offsets=None, n_seqs: int = None, causa
     sees no key is 0 with lse = -inf.  ``out`` may be q; query tokens that are not computed (before the first and behind the
     last sequence, and behind a sequence's first max_q) keep what a given ``out`` holds and are 0 with a new one; their lse
     is -inf, and kept where both tensors are given.  ``status``: as for q8_matmul; ``stream``: as for q8_read.  Returns out, or
-    (out, lse)."""
+    (out, lse).  No gradients: the results have no graph, whatever the inputs ask for."""
     dev = q.get_device()
     fq, n_q, dim, code = _head_fields(q, "q", dev)
     fk, n_k, k_dim, k_code = _head_fields(k, "k", dev)
