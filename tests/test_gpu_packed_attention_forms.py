@@ -204,3 +204,27 @@ def test_parts_of_a_buffer_with_heads_first(M, d):
     assert torch.equal(q, nq) and torch.equal(k, nk)
     M.attention(q, k, v, out=q)
     assert torch.equal(q, want) and torch.equal(k, nk) and torch.equal(v, values)
+
+
+@pytest.mark.parametrize("d", [8, 16, 24, 48, 56, 88, 104, 112, 120])
+@pytest.mark.parametrize("causal", [False, True])
+def test_head_sizes_between_the_kernels_steps(M, d, causal):
+    for q_len, k_len, H, Hk, name in (([1, 3], [300, 77], 4, 2, "ROWS"), ([40, 90], [133, 500], 2, 2, "TILE"),
+                                      ([129 + i for i in range(20)], [129 + 9 * i for i in range(20)], 8, 8, "TILES")):
+        q, k, v = qkv(d, sum(q_len), sum(k_len), H, Hk, d)
+        assert form(M, q, k, v, q_len, k_len, max(q_len))[0] == getattr(M, "MOECA_ATTENTION_FORM_" + name)
+        against_64_bits(M, q, k, v, q_len, k_len, causal, max_q=max(q_len))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_as_many_sequences_as_there_may_be(M, dtype):
+    """A million sequences of one token and one key: the result is the value."""
+    n = 1 << 20
+    q, k, v = qkv(1, n, n, 1, 1, 8, dtype)
+    off = torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    for args in (dict(n_seqs=n), dict(q_offsets=off, k_offsets=off), dict(q_offsets=off, k_offsets=off, max_q=1)):
+        assert torch.equal(M.attention(q, k, v, causal=True, **args), v)
+    two = torch.arange(0, n + 1, 2, dtype=torch.int32, device="cuda")  # two queries and keys each: the first sees one key
+    assert torch.equal(M.attention(q, k, v, q_offsets=two, k_offsets=two, causal=True)[::2], v[::2])
+    with pytest.raises(M.MoecaError):
+        M.attention(q, k, v, n_seqs=n + 1)
