@@ -73,11 +73,12 @@ moeca_status moeca_qk_norm_rope(const moeca_qk_norm_rope_args* args, void* strea
  * otherwise: those of no sequence (before q_offsets[0], from q_offsets[n_seqs]
  * on), and a sequence's behind its first max_q.
  *
- * Scores, softmax statistics and sums are fp32 (the exponential's argument in
- * base 2; a row's highest score gives 0 within 2^-17, whatever its size); with bf16 values p is rounded to bf16 before it meets v, the sum of p
- * is not.  Keys and values behind a sequence's end are never looked at, whatever they
- * hold; a value that is not finite may reach, by 0 x infinity, rows of its own
- * sequence that `causal` hides it from.
+ * Scores, softmax statistics and sums are fp32, the exponential in base 2; its
+ * argument's error does not grow with the scores' size.  With bf16 values p is
+ * rounded to bf16 before it meets v, the sum of p is not.  Keys and values behind a
+ * sequence's end are never looked at, whatever they hold, nor do other sequences'
+ * queries change a result; a value that is not finite may reach, by 0 x infinity,
+ * rows of its own sequence that `causal` hides it from.
  * Splits of the key axis are joined in a fixed order.
  * UNSUPPORTED: above 2^30 tokens, or tiles beyond a grid's 2^31 - 1. */
 typedef struct {

@@ -22,7 +22,7 @@ namespace {
 // the compiler would make a fused multiply-add, whose exponent at s = m is the rounding of
 // m c, a power of two of its own for scores of 2^31.  Bound by FFMA and the shared-memory reads beside it (24.3 ms for
 // prompts of 16384 tokens, 32 heads of 128, bf16: 24 TFLOP/s); four texts of 16 to 121 tokens,
-// 12 heads of 64 in fp32, take 27 us, the latency of four blocks of keys.
+// 12 heads of 64 in fp32, take 22 us, the latency of four blocks of keys.
 // ---------------------------------------------------------------------------
 constexpr int kSimtThreads = 256, kSimtKeys = 32;
 constexpr int kSimtPitch = kSimtKeys + 4;  // floats from row to row of p
@@ -352,6 +352,8 @@ bool fits_tc(const moeca_heads& h, int64_t tokens) {
   return tokens == 0 || (addr(h.data) % 16 == 0 && stride(h.token_stride, tokens) && stride(h.head_stride, h.heads));
 }
 
+// A GB300's, not the current device's: the plan follows from the arguments alone, so that a workspace asked for with
+// another device current is the one that the call needs.
 constexpr int kSms = 152;
 constexpr int64_t kLongKeys = 4096, kKeysSaved = 1536, kKeysUneven = 8192;
 
@@ -373,7 +375,7 @@ Plan plan_attention(const moeca_attention_args& a) {
     } else {
       const int each = 128 / group;
       // One tile a block where all blocks then run at once, two an SM, and keys are too few to be cut (2 x 1024
-      // tokens, 8 heads of 64: 13.2 us, with two tiles 14.4; 2048 tokens, 8 heads of 128: 26.3 and 28.4).
+      // tokens, 8 heads of 64: 12.9 us, with two tiles 14.2; 2048 tokens, 8 heads of 128: 26.7 and 28.7).
       int per;
       const bool at_once = pieces(a.q_offsets, a.n_queries, a.n_seqs, each, p.max_q, &per) * heads <= 2 * kSms;
       p.rows = p.max_q <= each || (at_once && a.n_keys < a.n_seqs * kLongKeys) ? 1 : 2;
@@ -392,9 +394,9 @@ Plan plan_attention(const moeca_attention_args& a) {
   p.blocks = p.q_pieces * heads;
   // Few blocks with many keys each: the key axis is cut so that the chunks' blocks fill the GPU once.
   // For few rows, whose blocks are small, it is cut wherever a chunk is shorter than a sequence may be: into
-  // two blocks an SM (as many as run at once; four sequences of 131072 keys, 8 x 128, take 93 us, with six
-  // blocks an SM 98), and six of up to 64 channels (four run at once, and sequences of different lengths share
-  // the GPU more evenly: 64 sequences of 131072 keys, 8 x 64, take 54 us, with two 60).
+  // two blocks an SM (as many as run at once; four sequences of 131072 keys in all, 8 x 128, take 94 us so and with six
+  // blocks an SM), and six of up to 64 channels (four run at once, and sequences of different lengths share
+  // the GPU more evenly: 64 sequences of 131072 keys in all, 8 x 64, take 51 us, with two 57).
   if (p.blocks > 0 && (p.rows < 0 || 2 * p.blocks <= fill)) {
     const int64_t mean = a.n_keys / a.n_seqs;
     int64_t chunk;
@@ -408,7 +410,7 @@ Plan plan_attention(const moeca_attention_args& a) {
     const int64_t longest = a.k_offsets ? a.n_keys : mean;
     bool uneven = false;
     // Writing and joining the tiles' partial results costs what some 1500 keys do: 2048 tokens, 8 heads of 128, cut
-    // in two 29.5 us, whole 28.4; 4096 tokens, 4 heads, 40.6 and 50.9.
+    // in two 34.5 us, whole 26.7; 4096 tokens, 4 heads, 41.6 and 50.9.
     if (p.rows > 0 && mean - chunk < kKeysSaved) {
       // Where one sequence may hold most of the keys, those far above the mean are cut all the same, the others being
       // one chunk each: 32 queries of 32 heads on 2 (64 channels) in each of 16 sequences, one of 32768 keys among ones of

@@ -12,9 +12,10 @@
 // from the scores' fragment into the product with V (the difference first: 1 at s = m,
 // however large the scores).  The four warps' results meet in shared
 // memory at the end.
-// Four tokens over 131072 keys in all, 32 heads of 128 on 8 (537 MB): 91 us with the
-// join, 5.9 TB/s, 0.87 of the measured copy rate; one over 65536 keys on 4 key heads (134
-// MB) 32 us, a fifth of it the join's launch and its dependent loads; one over 300 keys 5.7 us.
+// Four tokens over 131072 keys in all, 32 heads of 128 on 8 (537 MB): 92 us with the
+// join, 5.8 TB/s, 0.86 of the measured copy rate; one over 65536 keys on 4 key heads (134
+// MB) 30 us, a fifth of it the join's launch and its dependent loads; one over 300 keys 6 us.
+// The exponential is ex2.approx (2 ulp), far below the bf16 rounding of P.
 #include <algorithm>
 
 #include "attn_tc.cuh"

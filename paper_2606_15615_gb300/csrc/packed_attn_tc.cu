@@ -11,8 +11,8 @@
 //               S_i = Q_i K_j^T (128 x 128, fp32), then O_i += P_i V_j
 //   warps 2 ..  softmax: four warps per tile, a row per thread.  A thread takes its
 //               row of S from TMEM, keeps the running maximum m and sum l, and
-//               writes P = 2^(s - m) in bf16 over S, where the second product
-//               reads it as its A operand.
+//               writes P = 2^((s - m) c), c = scale log2(e), in bf16 over S, where the
+//               second product reads it as its A operand.
 // With two tiles the tensor core works on one tile while the other's softmax
 // runs; S, and O beside it, take 256 TMEM columns a tile.  V is taken as it lies in
 // memory (keys x channels): the product reads it as an MN-major operand.
@@ -24,12 +24,12 @@
 // Keys behind the sequence's end are masked; value rows there are zeroed in shared
 // memory before the product, as they belong to another sequence and may hold
 // infinities or NaN.
-// 4 x 4096 tokens, 16 heads of 128: 365 us, 1.50 PFLOP/s (0.78 of the measured burst
-// rate, 0.88 of the sustained one); of 64: 307 us, 0.89 PFLOP/s: a tile's chain from
-// its scores through its softmax (1500 clocks a block) and the hand-over to the next scores
-// is longer there than the products of both tiles (1024). Causal, 8192 tokens, 32 heads
-// of 128 on 8: 356 us, 1.54 PFLOP/s. Short sequences are bound by a CTA's start and end
-// (index, TMEM and first copies some 3 us): 16 of 256, 16 heads of 72, 17 us.
+// 4 x 4096 tokens, 16 heads of 128: 366 us, 1.50 PFLOP/s (0.78 of the measured burst
+// rate, 0.88 of the sustained one); of 64: 291 us (308 in some processes), 0.94 PFLOP/s: a
+// tile's chain from its scores through its softmax and the hand-over to the next scores
+// is longer there than the products of both tiles (1024 clocks a block). Causal, 8192
+// tokens, 32 heads of 128 on 8: 357 us, 1.54 PFLOP/s. Short sequences are bound by a CTA's
+// start and end (index, TMEM and first copies some 3 us): 16 of 256, 16 heads of 72, 17 us.
 // Every wait is bounded (about one second); a wait that runs out records
 // MOECA_ERR_TIMEOUT, raises the CTA's abort flag, lets what was issued finish,
 // frees TMEM and returns.
@@ -266,9 +266,8 @@ __global__ void __launch_bounds__(64 + 128 * NT, NT == 1 ? 2 : 1)
     clear_rest<__nv_bfloat16>(a, w, index, kvh, a.k.heads, lane, 32);
   } else if (warp == 1) {
     // All lanes run the loop and one issues; what the loop turns on is read from
-    // lane 0, so that the compiler knows it to be the same in all and keeps the
-    // MMAs' operands in uniform registers (else each is moved there anew: the loop
-    // alone took 3300 clocks for a block of two tiles of 64 channels, 2500 so).
+    // lane 0, and so known to be the same in all (a block of two tiles of 64 channels
+    // then took 2500 clocks; 3300 with each lane's own).
     const auto uniform = [](auto x) { return static_cast<decltype(x)>(__shfl_sync(0xffffffffu, x, 0)); };
     uint32_t issue;
     asm volatile("{\n .reg .pred e;\n elect.sync _|e, 0xffffffff;\n selp.u32 %0, 1, 0, e;\n}" : "=r"(issue));
