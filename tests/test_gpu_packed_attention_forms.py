@@ -101,7 +101,7 @@ def form(M, q, k, v, q_len, k_len, max_q=0):
 PAIRS = [
     ([129 + 11 * i % 72 for i in range(20)], [129 + 11 * i % 72 for i in range(20)], 8, 8, False),
     ([200 - 3 * i for i in range(20)], [150 + 17 * i for i in range(20)], 16, 8, False),
-    ([513, 700, 0, 300], [513, 700, 9, 300], 24, 24, False),
+    ([385, 130, 0, 260] * 3, [385, 130, 9, 260] * 3, 11, 11, False),
     ([300, 17, 260, 1], [4100, 4500, 4097, 5003], 2, 2, True),
     ([300], [9001], 2, 2, True),
     ([150, 290], [9000, 5007], 4, 2, True),

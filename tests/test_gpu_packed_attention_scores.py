@@ -42,7 +42,7 @@ def check(M, q_len, k_len, H, Hk, d, dtype, power, sign, order, by, causal, drif
     v = torch.randn(sum(k_len), Hk, d, generator=g) + drift * torch.linspace(-1, 1, sum(k_len))[:, None, None]
     v = v.to(TYPES[dtype]).cuda()
     out, lse = M.attention(q, k, v, q_offsets=offsets(q_len), k_offsets=offsets(k_len), causal=causal, scale=scale, lse=True)
-    got, got_lse, v6 = out.double().cpu().numpy(), lse.double().cpu().numpy(), v.double().cpu().numpy()
+    got, got_lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
     key = k[:, 0, 0].double().cpu().numpy()
     i = j = 0
     for m, n in zip(q_len, k_len):
@@ -52,9 +52,9 @@ def check(M, q_len, k_len, H, Hk, d, dtype, power, sign, order, by, causal, drif
         top = x.max(-1, keepdims=True)
         p = (x == top) & see
         count = p.sum(-1)
-        vv = np.repeat(v6[j:j + n], H // Hk, 1)
-        o = np.einsum("ij,jhd->ihd", p / np.maximum(count, 1)[:, None], vv)
-        mag = np.einsum("ij,jhd->ihd", p / np.maximum(count, 1)[:, None], np.abs(vv))
+        share = torch.from_numpy(p / np.maximum(count, 1)[:, None]).cuda()
+        vv = v[j:j + n].double().repeat_interleave(H // Hk, 1)
+        o, mag = (torch.einsum("ij,jhd->ihd", share, x).cpu().numpy() for x in (vv, vv.abs()))
         slack = (n * 2.0 ** -22 + 16 * 2.0 ** -24) * mag
         live = count > 0
         err = np.abs(got[i:i + m] - o) - slack - HALF[dtype] * (np.abs(o) + slack)
@@ -71,7 +71,7 @@ WHOLE = [([1], [250], 4, 2), ([40], [250], 4, 2), ([250], [255], 2, 2), ([200] *
 
 @pytest.mark.parametrize("q_len,k_len,H,Hk", WHOLE, ids=["few", "tile", "tiles", "pairs"])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("d", [64, 72, 96, 128])
+@pytest.mark.parametrize("d", [64, 96, 128])
 @pytest.mark.parametrize("power,sign,order,by,causal", [
     (10, 1, (1, 2, 3), "values", False), (9, -1, (3, 2, 1), "scale", True), (20, 1, (1, 3, 2), "values", True),
     (31, 1, (1,), "values", False), (31, -1, (2, 1), "scale", False), (32, 1, (1, 2, 3), "values", True),
@@ -87,7 +87,7 @@ CUT = [([1], [5000], 4, 2), ([3, 1], [2600, 9001], 4, 1), ([40], [5000], 4, 2), 
 
 @pytest.mark.parametrize("q_len,k_len,H,Hk", CUT, ids=["one", "few", "tile", "tiles", "uneven"])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("d", [64, 72, 128])
+@pytest.mark.parametrize("d", [72, 128])
 @pytest.mark.parametrize("power,sign,order,by,causal", [
     (10, 1, (1,), "values", False), (16, -1, (1,), "scale", True), (20, 1, (1, 3, 2), "values", True), (24, -1, (1,), "values", False),
     (31, 1, (1,), "scale", True), (34, 1, (1, 2), "values", False), (40, -1, (2, 1), "scale", True), (100, 1, (1,), "scale", False)])
